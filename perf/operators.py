@@ -194,7 +194,7 @@ def _prepare(case, seed, library):
     if library:
         from paper_2412_04757_b200 import binding
 
-        s.cache = binding.LtriPaged(s.k, s.v, n_q_heads=case["hq"], dtype=dtype, max_rows=rows, max_pages=table.shape[1],
+        s.cache = binding.LtriPaged(s.k, s.v, n_q_heads=case["hq"], dtype=dtype, max_rows=rows,
                                     k_scale=s.k_scale, v_scale=s.v_scale, weights=s.weights, positions=s.positions)
     return s
 
