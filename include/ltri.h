@@ -361,6 +361,122 @@ int ltri_debug_wait_timeout(ltri_ctx* ctx, int64_t limit_cycles, int64_t* waited
 int ltri_segment_map_static(const int32_t* Mq, int m, int64_t theta_q, int max_spans, int32_t* pairs, int cap_pairs,
                             int32_t* n_out, void* cuda_stream);
 
+/* ---- caller-owned paged K/V cache ----
+ *
+ * Attention of single tokens over a K/V cache that belongs to the caller and is held in pages, the writing of rows into
+ * it, and the eviction of rows by the attention they have accumulated.  It stands beside the streaming context above:
+ * a context keeps every token of its own cache and retrieves; a paged cache is attended over as a whole, and bounded by
+ * eviction.  It serves short conversations, layers without retrieval, and caches that other programs allocate.
+ *
+ * State, all of it the caller's DEVICE memory:
+ *   K and V pages   rows of head_dim elements, each row contiguous.  The row of (layer, page, KV head, place) begins at
+ *                   layer * layer_stride + page * page_stride + head * head_stride + place * token_stride elements; the
+ *                   strides of K and V are the same.  Any order of the axes will do, rows must not overlap.
+ *   table           int32 [n_rows][table_pages], row stride table_stride: the pages of every row of the batch, in order.
+ *                   Slot j of a row is place j % page_tokens of page table[row][j / page_tokens].  Entries behind a
+ *                   row's last page are not read.
+ *   lens            int32 [n_rows]: slots in use.  0 is an empty row (a padded batch): nothing of it is read or written,
+ *                   its outputs are 0 and its lse is -infinity.
+ *   weights, positions  float and int32 [n_layers][n_pages][n_kv_heads][page_tokens], dense: the attention a slot has
+ *                   accumulated, and the token's position in its text.  Both or neither.
+ * Device memory that these calls read is not looked at on the host, so they can be captured into a CUDA graph and
+ * replayed with other contents.  A length outside [0, table_pages * page_tokens] makes its row empty, a page outside
+ * [0, n_pages) its slots absent; both are recorded as LTRI_EDEVICE for ltri_paged_sync_status, and nothing outside the
+ * caller's buffers is touched.  Rows of a batch may name the same page (a shared prompt) as long as no call writes to it:
+ * appended slots, accumulated weights and evicted rows need pages of their row's own, or their values are undefined.
+ *
+ * The calls of one handle must use one stream or be ordered by the caller, replays of graphs that captured them included:
+ * they share its workspace.  Handles are independent of each other, also over the same pages.  Every call runs on the
+ * device that was current when its handle was created, whichever device is current later.  Outputs are the same bits for
+ * the same inputs. */
+typedef struct ltri_paged ltri_paged; /* opaque host-side handle */
+
+enum {
+  LTRI_TYPE_BF16 = 0,
+  LTRI_TYPE_FP16 = 1,
+  LTRI_TYPE_E4M3 = 2 /* cached rows only: 8 bits an element, value = element * scale of its KV head */
+};
+
+typedef struct {
+  int32_t n_layers;
+  int32_t n_q_heads, n_kv_heads; /* n_q_heads % n_kv_heads == 0, at most 64 query heads per KV head */
+  int32_t head_dim;              /* 64, 128 or 256 */
+  int32_t type;                  /* of q, k, v and out: LTRI_TYPE_BF16 or LTRI_TYPE_FP16 */
+  int32_t cache_type;            /* of the pages: `type` or LTRI_TYPE_E4M3 */
+  int32_t page_tokens;           /* 1..65536 */
+  int32_t max_rows;              /* rows of a call, 1..65535 */
+  int64_t n_pages;               /* 1..2^31-1; n_pages * page_tokens slots at most 2^40 */
+  int64_t layer_stride, page_stride, head_stride, token_stride; /* elements, multiples of 16 bytes */
+  float softmax_scale;           /* 0 -> 1/sqrt(head_dim) */
+  float weight_decay;            /* accumulated weights are multiplied by this in every decode call, 0..1 */
+  void *k_pages, *v_pages;       /* DEVICE, 16-byte aligned */
+  const float *k_scale, *v_scale; /* DEVICE [n_kv_heads], LTRI_TYPE_E4M3 only; read by every call */
+  float* weights;                /* DEVICE or NULL */
+  int32_t* positions;            /* DEVICE or NULL */
+  void* workspace;               /* DEVICE, caller-owned, 256-byte aligned */
+  size_t workspace_bytes;        /* >= ltri_paged_workspace_bytes(params) */
+} ltri_paged_params;
+
+/* Bytes of device memory that `workspace` must provide (host only; pointers are ignored, except that weights == NULL
+ * needs less).  0 if the parameters are invalid. */
+size_t ltri_paged_workspace_bytes(const ltri_paged_params* p);
+
+/* Create a handle and initialise its workspace on `cuda_stream` (synchronises that stream once).  The pages, weights
+ * and positions are left as they are. */
+int ltri_paged_create(const ltri_paged_params* p, void* cuda_stream, ltri_paged** out);
+
+/* Free the host handle.  Device memory stays with the caller. */
+int ltri_paged_destroy(ltri_paged* cache);
+
+/* Write the K/V rows of n_rows ragged prompts (or parts of prompts) into the pages of `layer`.
+ *   starts   DEVICE int32 [n_rows + 1], ascending: tokens [starts[r], starts[r + 1]) of k and v belong to row r (there may
+ *            be none).  They take the row's last slots: lens[r] counts them already.  Tokens in front of starts[0] and
+ *            from starts[n_rows] on are ignored.
+ *   k, v     [n_tokens][n_kv_heads][head_dim], token stride kv_stride elements (0: dense)
+ *   row_pos  DEVICE int32 [n_rows]: position of each row's first new token (NULL: the slot's number)
+ *   weights  DEVICE float [n_tokens][n_kv_heads]: what the slots have accumulated already (NULL: 0)
+ * row_pos and weights are used only if the cache has weights and positions.  8-bit pages get the nearest value to
+ * element / scale, ties to even, clamped to +-448.  Tokens that a row has no slot for (more than lens[r] of them) are left
+ * out and recorded as LTRI_EDEVICE. */
+int ltri_paged_append(ltri_paged* cache, int layer, const int32_t* table, int table_pages, int64_t table_stride,
+                      const int32_t* lens, int n_rows, const int32_t* starts, int64_t n_tokens, const void* k,
+                      const void* v, int64_t kv_stride, const int32_t* row_pos, const float* weights, void* cuda_stream);
+
+/* Attention of one new token per row over the row's slots, in `layer`.
+ *   q    [n_rows][n_q_heads ][head_dim], row stride q_stride elements (0: dense)
+ *   k,v  [n_rows][n_kv_heads][head_dim], row stride kv_stride (0: dense): written into slot lens[r] - 1 (the length
+ *        counts the new token) before the attention.  Both NULL: the cache is attended over as it is.
+ *   row_pos DEVICE int32 [n_rows]: position of each row's new token (NULL: the slot's number); used only if the cache
+ *        has positions and k is given
+ *   out  [n_rows][n_q_heads ][head_dim], dense (may be q itself)
+ *   lse  float [n_rows][n_q_heads] or NULL: log of the sum of exp(logit), to merge with attention over other tokens
+ * With weights, every slot's weight becomes weight_decay * weight + the probabilities that the query heads of its KV head
+ * give it; a slot that this call writes starts from 0.
+ * Logits and sums are fp32; the probabilities enter the product with V as two terms of `type` (16 bits together, 22 in
+ * fp16), so that the outputs carry the rounding of `type` once. */
+int ltri_paged_decode(ltri_paged* cache, int layer, const int32_t* table, int table_pages, int64_t table_stride,
+                      const int32_t* lens, int n_rows, const void* q, int64_t q_stride, const void* k, const void* v,
+                      int64_t kv_stride, const int32_t* row_pos, void* out, float* lse, void* cuda_stream);
+
+/* Cut every row of more than `budget` slots to `budget`, per layer of [layer_begin, layer_begin + layer_count) and KV head.
+ * Kept are the slots of the first n_sink positions and of the newest `recent` positions (counted from the largest position
+ * in the row), n_sink + recent <= budget, and of the others those of the largest weights (NaN counts as -infinity; of equal
+ * ones, the lower slot).  The kept slots from `budget` on move, in ascending order, into the slots below it that are not
+ * kept, in ascending order, with their weights and positions; no other row is touched.  (Attention does not depend on
+ * the order of slots, so nothing else has to move: one row for a token appended to a full budget.)
+ *   new_lens DEVICE int32 [n_rows]: min(lens, budget); may be lens itself
+ * The cache needs weights and positions. */
+int ltri_paged_evict(ltri_paged* cache, int layer_begin, int layer_count, const int32_t* table, int table_pages,
+                     int64_t table_stride, const int32_t* lens, int32_t* new_lens, int n_rows, int budget, int n_sink,
+                     int recent, void* cuda_stream);
+
+/* First device-side error recorded since the last call of this function (then cleared).  Synchronises. */
+int ltri_paged_sync_status(ltri_paged* cache, void* cuda_stream);
+/* cudaError_t of the last failed runtime call (0 if none). */
+int ltri_paged_last_cuda_error(const ltri_paged* cache);
+/* Kernels launched through this handle since it was created (host counter). */
+int64_t ltri_paged_launch_count(const ltri_paged* cache);
+
 #ifdef __cplusplus
 }
 #endif

@@ -31,6 +31,8 @@ EXPORTS = [
     "ltri_debug_segment_map", "ltri_launch_count", "ltri_profile_enable", "ltri_profile_read",
     "ltri_segment_map_static", "ltri_prefill_chunk_host", "ltri_host_outputs_ready", "ltri_host_kv_bytes",
     "ltri_debug_load_index", "ltri_debug_wait_timeout",
+    "ltri_paged_workspace_bytes", "ltri_paged_create", "ltri_paged_destroy", "ltri_paged_append", "ltri_paged_decode",
+    "ltri_paged_evict", "ltri_paged_sync_status", "ltri_paged_last_cuda_error", "ltri_paged_launch_count",
 ]
 KERNEL_CLASSES = ["append", "evict_index", "attn_local", "map_pass", "segment", "score_topk", "attn_retrieved",
                   "decode_retrieve", "decode_attn", "pager_pull"]
@@ -50,6 +52,21 @@ class LtriParams(C.Structure):
         ("layer_rep_lambda", C.POINTER(C.c_float)),
         ("host_kv", C.c_void_p), ("host_kv_bytes", C.c_size_t), ("cache_units", C.c_int32), ("score_decay", C.c_float),
         ("arena", C.c_void_p), ("arena_bytes", C.c_size_t),
+    ]
+
+
+TYPE_BF16, TYPE_FP16, TYPE_E4M3 = 0, 1, 2
+
+
+class LtriPagedParams(C.Structure):
+    _fields_ = [
+        ("n_layers", C.c_int32), ("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+        ("type", C.c_int32), ("cache_type", C.c_int32), ("page_tokens", C.c_int32), ("max_rows", C.c_int32),
+        ("n_pages", C.c_int64),
+        ("layer_stride", C.c_int64), ("page_stride", C.c_int64), ("head_stride", C.c_int64), ("token_stride", C.c_int64),
+        ("softmax_scale", C.c_float), ("weight_decay", C.c_float),
+        ("k_pages", C.c_void_p), ("v_pages", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+        ("weights", C.c_void_p), ("positions", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t),
     ]
 
 
@@ -107,6 +124,18 @@ def load():
         L.ltri_segment_map_static.argtypes = [vp, ip, C.c_int64, ip, vp, ip, vp, vp]
         L.ltri_debug_load_index.argtypes = [vp, ip, ip, C.c_int64, vp, ip, vp, vp]
         L.ltri_debug_wait_timeout.argtypes = [vp, C.c_int64, vp, vp]
+        i64 = C.c_int64
+        L.ltri_paged_workspace_bytes.restype = C.c_size_t
+        L.ltri_paged_workspace_bytes.argtypes = [C.POINTER(LtriPagedParams)]
+        L.ltri_paged_create.argtypes = [C.POINTER(LtriPagedParams), vp, C.POINTER(vp)]
+        L.ltri_paged_destroy.argtypes = [vp]
+        L.ltri_paged_append.argtypes = [vp, ip, vp, ip, i64, vp, ip, vp, i64, vp, vp, i64, vp, vp, vp]
+        L.ltri_paged_decode.argtypes = [vp, ip, vp, ip, i64, vp, ip, vp, i64, vp, vp, i64, vp, vp, vp, vp]
+        L.ltri_paged_evict.argtypes = [vp, ip, ip, vp, ip, i64, vp, vp, ip, ip, ip, ip, vp]
+        L.ltri_paged_sync_status.argtypes = [vp, vp]
+        L.ltri_paged_last_cuda_error.argtypes = [vp]
+        L.ltri_paged_launch_count.restype = i64
+        L.ltri_paged_launch_count.argtypes = [vp]
         _lib = L
     return _lib
 
@@ -397,3 +426,171 @@ class Ltri:
                                              self._stream(stream))
         _check(rc, "ltri_debug_segment_map")
         return out[: n.value].copy()
+
+
+class LtriPaged:
+    """A paged K/V cache of the caller's: single-token attention, appending and eviction.  Methods mirror the C entry points.
+
+    k_pages, v_pages: [layers][pages][Hkv][page tokens][head_dim] CUDA tensors with the same strides (a permuted view of
+    token-major pages, or the halves of one tensor, will do), of ``dtype`` or float8_e4m3fn with k_scale, v_scale (float32
+    [Hkv]).  weights (float32) and positions (int32), both or neither: [layers][pages][Hkv][page tokens], contiguous.  The
+    tensors stay the caller's; the handle keeps references to them.
+    """
+
+    def __init__(self, k_pages, v_pages, n_q_heads, dtype=None, max_rows=1, k_scale=None, v_scale=None, weights=None,
+                 positions=None, softmax_scale=0.0, weight_decay=1.0, stream=None):
+        import torch
+
+        self.torch = torch
+        self.lib = load()
+        self._h = C.c_void_p()
+        types = {torch.bfloat16: TYPE_BF16, torch.float16: TYPE_FP16}
+        dtype = dtype if dtype is not None else k_pages.dtype
+        if dtype not in types:
+            raise ValueError("dtype of the queries is bfloat16 or float16 (to be named beside 8-bit pages)")
+        if k_pages.dim() != 5 or k_pages.shape != v_pages.shape or k_pages.stride() != v_pages.stride():
+            raise ValueError("k_pages and v_pages are [layers][pages][Hkv][page tokens][head_dim] of the same strides")
+        if k_pages.stride(4) != 1 or k_pages.dtype != v_pages.dtype or k_pages.dtype not in (dtype, torch.float8_e4m3fn):
+            raise ValueError("rows are contiguous, of dtype or float8_e4m3fn")
+        L, pages, hkv, P, D = k_pages.shape
+        self.device = k_pages.device
+        if self.device.type != "cuda":
+            raise ValueError("the ltri library runs on CUDA devices only")
+        scaled = k_pages.dtype == torch.float8_e4m3fn
+        if scaled != (k_scale is not None) or scaled != (v_scale is not None) or (weights is None) != (positions is None):
+            raise ValueError("8-bit pages, and only they, have k_scale and v_scale; weights and positions go together")
+        for t, want, shape in ((k_scale, torch.float32, (hkv,)), (v_scale, torch.float32, (hkv,)),
+                               (weights, torch.float32, (L, pages, hkv, P)), (positions, torch.int32, (L, pages, hkv, P))):
+            if t is not None and (t.dtype != want or t.shape != shape or not t.is_contiguous() or t.device != self.device):
+                raise ValueError(f"scales are float32 [{hkv}], weights float32 and positions int32 {(L, pages, hkv, P)}, contiguous")
+        if v_pages.device != self.device:
+            raise ValueError("k_pages and v_pages are on one device")
+        s = k_pages.stride()
+        ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+        self.params = LtriPagedParams(L, n_q_heads, hkv, D, types[dtype], TYPE_E4M3 if scaled else types[dtype], P, max_rows,
+                                      pages, s[0], s[1], s[2], s[3], softmax_scale, weight_decay, ptr(k_pages), ptr(v_pages),
+                                      ptr(k_scale), ptr(v_scale), ptr(weights), ptr(positions), None, 0)
+        nbytes = int(self.lib.ltri_paged_workspace_bytes(C.byref(self.params)))
+        if nbytes == 0:
+            raise LtriError(LTRI_EINVAL, "ltri_paged_workspace_bytes")
+        with torch.cuda.device(self.device):
+            self.workspace = torch.empty(nbytes + 256, dtype=torch.uint8, device=self.device)
+            self.params.workspace = (self.workspace.data_ptr() + 255) // 256 * 256
+            self.params.workspace_bytes = nbytes
+            self._keep = (k_pages, v_pages, k_scale, v_scale, weights, positions)
+            self.dtype, self._q_shape, self._kv_shape = dtype, (n_q_heads, D), (hkv, D)
+            self._raw_stream = torch._C._cuda_getCurrentRawStream
+            self._index = self.device.index
+            _check(self.lib.ltri_paged_create(C.byref(self.params), self._stream(stream), C.byref(self._h)),
+                   "ltri_paged_create")
+
+    def _stream(self, stream):
+        return self._raw_stream(self._index) if stream is None else stream.cuda_stream
+
+    def close(self):
+        if getattr(self, "_h", None) is not None and self._h.value:
+            self.lib.ltri_paged_destroy(self._h)
+            self._h = C.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _rows(self, table, lens):
+        """(rows, table columns, table row stride) of a call, checked."""
+        i32 = self.torch.int32
+        if table.dtype is not i32 or table.dim() != 2 or table.device != self.device or (table.shape[1] > 1 and table.stride(1) != 1):
+            raise ValueError("table is int32 [rows][pages of a row] on the cache's device, its rows contiguous")
+        n, cols = table.shape
+        self._vector(lens, n, i32, "lens")
+        return n, cols, table.stride(0) if n > 1 else cols
+
+    def _vector(self, t, n, dtype, name):
+        if t.dtype is not dtype or t.shape != (n,) or t.device != self.device or not t.is_contiguous():
+            raise ValueError(f"{name} is {dtype} [{n}], contiguous, on the cache's device")
+
+    def _heads(self, t, n, heads, name):
+        """Row stride of t [n][heads][head_dim], whose rows are dense."""
+        if t.dtype is not self.dtype or t.shape != (n, *heads) or t.device != self.device:
+            raise ValueError(f"{name} is {self.dtype} {(n, *heads)} on the cache's device")
+        row, head, one = t.stride()
+        dense = heads[0] * heads[1]
+        if (one != 1 and heads[1] > 1) or (head != heads[1] and heads[0] > 1) or (n > 1 and row < dense):
+            raise ValueError(f"{name}: a row's heads are dense")
+        return row if n > 1 else dense
+
+    def _done(self, rc, where):
+        if rc == LTRI_ECUDA:
+            raise LtriError(rc, f"{where} (cudaError {self.lib.ltri_paged_last_cuda_error(self._h)})")
+        if rc != LTRI_OK:
+            raise LtriError(rc, where)
+
+    def ltri_paged_append(self, layer, table, lens, starts, k, v, row_pos=None, weights=None, stream=None):
+        """k, v [tokens][Hkv][head_dim] into the last slots of their rows; starts int32 [rows + 1] on the device, row_pos int32
+        [rows], weights float32 [tokens][Hkv].  lens counts the tokens already."""
+        n, cols, ts = self._rows(table, lens)
+        self._vector(starts, n + 1, self.torch.int32, "starts")
+        tokens = k.shape[0]
+        stride = self._heads(k, tokens, self._kv_shape, "k")
+        if self._heads(v, tokens, self._kv_shape, "v") != stride:
+            raise ValueError("k and v have the same strides")
+        if row_pos is not None:
+            self._vector(row_pos, n, self.torch.int32, "row_pos")
+        if weights is not None and (weights.dtype is not self.torch.float32 or weights.shape != (tokens, self._kv_shape[0])
+                                    or weights.device != self.device or not weights.is_contiguous()):
+            raise ValueError(f"weights is float32 {(tokens, self._kv_shape[0])}, contiguous, on the cache's device")
+        if tokens == 0:
+            return
+        self._done(self.lib.ltri_paged_append(self._h, layer, table.data_ptr(), cols, ts, lens.data_ptr(), n, starts.data_ptr(),
+                                              tokens, k.data_ptr(), v.data_ptr(), stride,
+                                              None if row_pos is None else row_pos.data_ptr(),
+                                              None if weights is None else weights.data_ptr(), self._stream(stream)),
+                   "ltri_paged_append")
+
+    def ltri_paged_decode(self, layer, table, lens, q, k=None, v=None, row_pos=None, out=None, lse=None, stream=None):
+        """q [rows][Hq][head_dim]; k, v [rows][Hkv][head_dim], the new tokens' rows, which lens counts already (None: attend over
+        the cache as it is).  lse: float32 [rows][Hq], filled if given.  Returns out."""
+        n, cols, ts = self._rows(table, lens)
+        qs = self._heads(q, n, self._q_shape, "q")
+        kvs = kp = vp = 0
+        if k is not None or v is not None:
+            if k is None or v is None:
+                raise ValueError("k and v go together")
+            kvs = self._heads(k, n, self._kv_shape, "k")
+            if self._heads(v, n, self._kv_shape, "v") != kvs:
+                raise ValueError("k and v have the same strides")
+            kp, vp = k.data_ptr(), v.data_ptr()
+        if row_pos is not None:
+            self._vector(row_pos, n, self.torch.int32, "row_pos")
+        if out is None:
+            if stream is None:
+                out = self.torch.empty((n, *self._q_shape), dtype=self.dtype, device=self.device)
+            else:
+                with self.torch.cuda.stream(stream):
+                    out = self.torch.empty((n, *self._q_shape), dtype=self.dtype, device=self.device)
+        elif out.dtype is not self.dtype or out.shape != (n, *self._q_shape) or out.device != self.device or not out.is_contiguous():
+            raise ValueError(f"out is {self.dtype} {(n, *self._q_shape)}, contiguous, on the cache's device")
+        if lse is not None and (lse.dtype is not self.torch.float32 or lse.shape != (n, self._q_shape[0])
+                                or lse.device != self.device or not lse.is_contiguous()):
+            raise ValueError(f"lse is float32 {(n, self._q_shape[0])}, contiguous, on the cache's device")
+        self._done(self.lib.ltri_paged_decode(self._h, layer, table.data_ptr(), cols, ts, lens.data_ptr(), n, q.data_ptr(), qs, kp,
+                                              vp, kvs, None if row_pos is None else row_pos.data_ptr(), out.data_ptr(),
+                                              None if lse is None else lse.data_ptr(), self._stream(stream)),
+                   "ltri_paged_decode")
+        return out
+
+    def ltri_paged_evict(self, layer_begin, layer_count, table, lens, new_lens, budget, n_sink, recent, stream=None):
+        """Cuts rows of more than ``budget`` slots; new_lens int32 [rows] (may be lens) gets their lengths."""
+        n, cols, ts = self._rows(table, lens)
+        self._vector(new_lens, n, self.torch.int32, "new_lens")
+        self._done(self.lib.ltri_paged_evict(self._h, layer_begin, layer_count, table.data_ptr(), cols, ts, lens.data_ptr(),
+                                             new_lens.data_ptr(), n, budget, n_sink, recent, self._stream(stream)),
+                   "ltri_paged_evict")
+
+    def ltri_paged_sync_status(self, stream=None) -> int:
+        return int(self.lib.ltri_paged_sync_status(self._h, self._stream(stream)))
+
+    def ltri_paged_launch_count(self) -> int:
+        return int(self.lib.ltri_paged_launch_count(self._h))

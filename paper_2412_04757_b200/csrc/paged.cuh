@@ -1,0 +1,122 @@
+// Shared declarations of the caller-owned paged K/V cache: the device-side view of a handle and the launch wrappers of its
+// kernel files (kernels_paged_*.cu).
+#pragma once
+
+#include <cuda_fp16.h>
+#include <cuda_fp8.h>
+
+#include "../../include/ltri.h"
+#include "common.cuh"
+
+namespace ltri {
+
+// Device-side view of one handle.  Passed to kernels by value.
+struct PagedCache {
+  int Hq, Hkv, G, D, P;
+  int type, cache_type;
+  int row_bytes;                // bytes of a cached row
+  long long n_pages;
+  long long ls, ps, hs, ts;     // layer, page, head and place strides of the pages, bytes
+  float scale;                  // softmax_scale * log2(e)
+  float decay;
+  unsigned char *k, *v;
+  const float *ks, *vs;         // per KV head, or null
+  float* w;                     // [L][n_pages][Hkv][P], or null
+  int* pos;
+  int* status;                  // [4]
+  int* list;                    // [L][n_pages][Hkv][P]: an eviction's moves, in the words of the unit's own slots
+  int sms;
+};
+
+// One call's rows.
+struct PagedRows {
+  const int* table;
+  long long table_stride;
+  int table_pages;
+  const int* lens;
+  int n;
+};
+
+struct PagedAppend {
+  const int* starts;
+  long long n_tokens;
+  const unsigned char *k, *v;
+  long long stride;             // bytes between tokens
+  const int* row_pos;
+  const float* weights;
+};
+
+struct PagedStep {
+  const unsigned char *q, *k, *v;
+  long long q_stride, kv_stride;  // bytes between rows
+  const int* row_pos;
+  unsigned char* out;
+  float* lse;
+};
+
+cudaError_t prepare_paged(const PagedCache& c);
+cudaError_t launch_paged_append(const PagedCache& c, const PagedRows& r, int layer, const PagedAppend& a, cudaStream_t s);
+cudaError_t launch_paged_decode(const PagedCache& c, const PagedRows& r, int layer, const PagedStep& a, cudaStream_t s);
+cudaError_t launch_paged_evict(const PagedCache& c, const PagedRows& r, int layer_begin, int layer_count, int* new_lens,
+                               int budget, int n_sink, int recent, cudaStream_t s);
+
+#ifdef __CUDACC__
+__device__ __forceinline__ void paged_status(const PagedCache& c, int detail) {
+  if (atomicCAS(&c.status[0], 0, (int)LTRI_EDEVICE) == 0) c.status[1] = detail;
+}
+
+// Slots of row r: 0 (and the status word) where the length says more than the table can hold.
+__device__ __forceinline__ int paged_len(const PagedCache& c, const PagedRows& r, int row) {
+  const int n = r.lens[row];
+  if (n >= 0 && n <= (long long)r.table_pages * c.P) return n;
+  paged_status(c, row);
+  return 0;
+}
+
+// Page of place `slot / P` of a row, or -1 (and the status word) where the table names none.
+__device__ __forceinline__ int paged_page(const PagedCache& c, const PagedRows& r, int row, int nth) {
+  const int page = r.table[row * r.table_stride + nth];
+  if (page >= 0 && page < c.n_pages) return page;
+  paged_status(c, row);
+  return -1;
+}
+
+// Index of a slot's word in weights, positions and lists.
+__device__ __forceinline__ size_t paged_word(const PagedCache& c, int layer, int page, int head, int place) {
+  return (((size_t)layer * c.n_pages + page) * c.Hkv + head) * c.P + place;
+}
+
+__device__ __forceinline__ size_t paged_row(const PagedCache& c, int layer, int page, int head, int place) {
+  return layer * c.ls + page * c.ps + head * c.hs + place * c.ts;
+}
+
+// Two fp32 values as elements of `type`, the first in the lower half.
+__device__ __forceinline__ uint32_t paged_pack(int type, float a, float b) {
+  if (type == LTRI_TYPE_BF16) {
+    const __nv_bfloat162 x = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&x);
+  }
+  const __half2 x = __floats2half2_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&x);
+}
+__device__ __forceinline__ float2 paged_unpack(int type, uint32_t x) {
+  if (type == LTRI_TYPE_BF16) return __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&x));
+  return __half22float2(*reinterpret_cast<const __half2*>(&x));
+}
+
+// Eight elements of `type` as e4m3: the nearest value to element / scale, ties to even, clamped to the largest.
+__device__ __forceinline__ uint2 paged_quantise(int type, const uint4& x, float scale) {
+  const uint32_t in[4] = {x.x, x.y, x.z, x.w};
+  uint32_t out[2] = {0u, 0u};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float2 f = paged_unpack(type, in[i]);
+    f.x = __fdiv_rn(f.x, scale);
+    f.y = __fdiv_rn(f.y, scale);
+    out[i >> 1] |= (uint32_t)__nv_cvt_float2_to_fp8x2(f, __NV_SATFINITE, __NV_E4M3) << (16 * (i & 1));
+  }
+  return make_uint2(out[0], out[1]);
+}
+#endif
+
+}  // namespace ltri
