@@ -25,6 +25,10 @@ struct PagedCache {
   int* pos;
   int* status;                  // [4]
   int* list;                    // [L][n_pages][Hkv][P]: an eviction's moves, in the words of the unit's own slots
+  float* part;                  // [sms][2][paged_part_floats]: partial sums of units that several CTAs share
+  int* count;                   // [max_rows][Hkv][blocks of heads]: CTAs of the unit that have finished; zero between calls
+  float* logits;                // [n_pages][Hkv][P][blocks of heads], with weights: a decode call's logits
+  float* lse2;                  // [max_rows][Hq], with weights: their sums, log2
   int sms;
 };
 
@@ -54,7 +58,15 @@ struct PagedStep {
   float* lse;
 };
 
-cudaError_t prepare_paged(const PagedCache& c);
+// Query heads of a KV head in blocks that the attention kernel takes at a time.
+struct PagedBlocks {
+  int heads, count;
+};
+PagedBlocks paged_blocks(int group);
+size_t paged_part_floats(int head_dim);
+int paged_decode_kernels(const PagedCache& c);  // launches of a decode call
+
+cudaError_t prepare_paged();
 cudaError_t launch_paged_append(const PagedCache& c, const PagedRows& r, int layer, const PagedAppend& a, cudaStream_t s);
 cudaError_t launch_paged_decode(const PagedCache& c, const PagedRows& r, int layer, const PagedStep& a, cudaStream_t s);
 cudaError_t launch_paged_evict(const PagedCache& c, const PagedRows& r, int layer_begin, int layer_count, int* new_lens,

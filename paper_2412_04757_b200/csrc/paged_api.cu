@@ -16,6 +16,8 @@ struct ltri_paged {
 
 namespace {
 
+constexpr int kPagedMaxSms = 256;  // CTAs that a decode call can have partial sums of
+
 bool aligned(const void* p, uintptr_t a) { return p && (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
 bool validate(const ltri_paged_params* p) {
@@ -40,19 +42,33 @@ bool validate(const ltri_paged_params* p) {
   return true;
 }
 
-// Carves the workspace; returns its size.
-size_t layout(const ltri_paged_params& p, PagedCache* c, unsigned char* base) {
+// Carves the workspace; returns its size.  The status word and the counts come first and start at zero.
+size_t layout(const ltri_paged_params& p, int sms, PagedCache* c, unsigned char* base, size_t* zeroed) {
   size_t off = 0;
   auto take = [&](size_t bytes) {
     unsigned char* at = base ? base + off : nullptr;
     off += (bytes + 255) / 256 * 256;
     return at;
   };
+  const PagedBlocks b = paged_blocks(p.n_q_heads / p.n_kv_heads);
+  const size_t slots = (size_t)p.n_pages * p.n_kv_heads * p.page_tokens;
   unsigned char* status = take(256);
-  unsigned char* list = p.weights ? take((size_t)p.n_layers * p.n_pages * p.n_kv_heads * p.page_tokens * sizeof(int)) : nullptr;
+  unsigned char* count = take((size_t)p.max_rows * p.n_kv_heads * b.count * sizeof(int));
+  if (zeroed) *zeroed = off;
+  unsigned char* part = take((size_t)sms * 2 * paged_part_floats(p.head_dim) * sizeof(float));
+  unsigned char *list = nullptr, *logits = nullptr, *lse2 = nullptr;
+  if (p.weights) {
+    list = take(p.n_layers * slots * sizeof(int));
+    logits = take(slots * b.count * b.heads * sizeof(float));
+    lse2 = take((size_t)p.max_rows * p.n_q_heads * sizeof(float));
+  }
   if (c) {
     c->status = reinterpret_cast<int*>(status);
+    c->count = reinterpret_cast<int*>(count);
+    c->part = reinterpret_cast<float*>(part);
     c->list = reinterpret_cast<int*>(list);
+    c->logits = reinterpret_cast<float*>(logits);
+    c->lse2 = reinterpret_cast<float*>(lse2);
   }
   return off;
 }
@@ -106,7 +122,9 @@ long long row_stride(const ltri_paged* c, int64_t stride, int heads) {
 
 extern "C" {
 
-size_t ltri_paged_workspace_bytes(const ltri_paged_params* p) { return validate(p) ? layout(*p, nullptr, nullptr) : 0; }
+size_t ltri_paged_workspace_bytes(const ltri_paged_params* p) {
+  return validate(p) ? layout(*p, kPagedMaxSms, nullptr, nullptr, nullptr) : 0;
+}
 
 int ltri_paged_create(const ltri_paged_params* p, void* cuda_stream, ltri_paged** out) {
   if (!out) return LTRI_EINVAL;
@@ -117,13 +135,14 @@ int ltri_paged_create(const ltri_paged_params* p, void* cuda_stream, ltri_paged*
   if (scaled ? !aligned(p->k_scale, 4) || !aligned(p->v_scale, 4) : p->k_scale || p->v_scale) return LTRI_EINVAL;
   if (!p->weights != !p->positions) return LTRI_EINVAL;
   if (p->weights && (!aligned(p->weights, 4) || !aligned(p->positions, 4))) return LTRI_EINVAL;
-  if (p->workspace_bytes < layout(*p, nullptr, nullptr)) return LTRI_ECAPACITY;
+  if (p->workspace_bytes < ltri_paged_workspace_bytes(p)) return LTRI_ECAPACITY;
   ltri_paged* c = new (std::nothrow) ltri_paged();
   if (!c) return LTRI_ECAPACITY;
   c->p = *p;
   PagedCache& d = c->c;
   d = PagedCache{};
-  layout(*p, &d, static_cast<unsigned char*>(p->workspace));
+  size_t zeroed = 0;
+  layout(*p, kPagedMaxSms, &d, static_cast<unsigned char*>(p->workspace), &zeroed);
   const long long es = scaled ? 1 : 2;
   d.Hq = p->n_q_heads;
   d.Hkv = p->n_kv_heads;
@@ -149,8 +168,9 @@ int ltri_paged_create(const ltri_paged_params* p, void* cuda_stream, ltri_paged*
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   cudaError_t e = cudaGetDevice(&c->device);
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&d.sms, cudaDevAttrMultiProcessorCount, c->device);
-  if (e == cudaSuccess) e = prepare_paged(d);
-  if (e == cudaSuccess) e = cudaMemsetAsync(d.status, 0, 256, s);
+  if (d.sms > kPagedMaxSms) d.sms = kPagedMaxSms;
+  if (e == cudaSuccess) e = prepare_paged();
+  if (e == cudaSuccess) e = cudaMemsetAsync(p->workspace, 0, zeroed, s);
   if (e == cudaSuccess) e = cudaStreamSynchronize(s);
   if (e != cudaSuccess) {
     cudaGetLastError();
@@ -199,7 +219,8 @@ int ltri_paged_decode(ltri_paged* cache, int layer, const int32_t* table, int ta
   if (!on.ok) return done(cache, cudaErrorInvalidDevice, 0);
   const PagedStep a{static_cast<const unsigned char*>(q), static_cast<const unsigned char*>(k), static_cast<const unsigned char*>(v),
                     qs, kvs, row_pos, static_cast<unsigned char*>(out), lse};
-  return done(cache, launch_paged_decode(cache->c, r, layer, a, static_cast<cudaStream_t>(cuda_stream)), 1);
+  return done(cache, launch_paged_decode(cache->c, r, layer, a, static_cast<cudaStream_t>(cuda_stream)),
+              paged_decode_kernels(cache->c));
 }
 
 int ltri_paged_evict(ltri_paged* cache, int layer_begin, int layer_count, const int32_t* table, int table_pages,
