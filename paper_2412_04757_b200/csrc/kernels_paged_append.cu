@@ -30,7 +30,7 @@ __global__ void __launch_bounds__(kAppThreads) k_paged_append(PagedCache c, Page
       paged_status(c, row);
       continue;
     }
-    const int page = paged_page(c, r, row, (int)(slot / c.P)), place = (int)(slot % c.P);
+    const int in_row = paged_nth(c, (int)slot), page = paged_page(c, r, row, in_row), place = (int)slot - in_row * c.P;
     if (page < 0) continue;
     const uint4 kx = *reinterpret_cast<const uint4*>(a.k + tok * a.stride + in * 16);
     const uint4 vx = *reinterpret_cast<const uint4*>(a.v + tok * a.stride + in * 16);

@@ -4,15 +4,16 @@
 // reference m, sums of 2^(x_j - m) and of 2^(x_j - m) V_j, which parts of a row join by rescaling to the larger m.
 //
 // Bound: HBM (a KV head's rows are read once for all of its query heads: 2 G flop a byte in 16 bits).  So the work is the rows'
-// tiles, and it is dealt evenly: the tiles of all (row, KV head) units stand in one line, of which every CTA (one per SM) takes an
-// equal run, across units if need be.  Ragged batches and single long rows fill the GPU alike, and no count of splits has to
-// be chosen.  A unit within one run is written by its CTA; of a unit that several CTAs share, the last one to finish joins the
-// partial sums, in the order of the runs.
+// tiles, and it is dealt evenly: the tiles of all (row, KV head) units stand in one line, of which every warp takes an equal
+// run, across units if need be, and a CTA (one per SM) its warps' runs.  Ragged batches and single long rows fill the GPU
+// alike, and no count of splits has to be chosen.  A unit within one warp's run is written by the warp; of a unit that several
+// warps share, the sums are joined when their CTA has finished its run, and of one that several CTAs share, the last CTA to
+// finish joins the others' sums, always in the order of the line.
 //
-// A warp has 16 slots of a tile and a ring of its own that cp.async fills several tiles ahead, across units; warps meet
-// only at the end of a unit.  Both products run on mma.sync with the slots (or head_dim) as the 16 rows and the heads of
-// the KV group as the 8 columns: S^T = K Q^T, O^T = V^T P^T, so that up to eight heads fill the instruction exactly.  (tcgen05 takes
-// 64 rows at least, and its operands come through descriptors of whole tiles, which pages of any size are not.)
+// A warp has a ring of its own that cp.async fills several tiles ahead, across units.  Both products run on mma.sync with the
+// slots (or head_dim) as the 16 rows and the heads of the KV group as the 8 columns: S^T = K Q^T, O^T = V^T P^T, so that up to
+// eight heads fill the instruction exactly.  (tcgen05 takes 64 rows at least, and its operands come through descriptors of
+// whole tiles, which pages of any size are not.)
 #include "mma_util.cuh"
 #include "paged.cuh"
 
@@ -25,21 +26,26 @@ struct PdShape {
   static constexpr int kRow = KIND == kPdE4m3 ? D : 2 * D;      // bytes of a cached row
   static constexpr int kChunks = kRow / 16;
   static constexpr int kWarps = D == 256 ? 4 : 8;
-  static constexpr int kTile = kWarps * 16;                     // slots of a CTA's tile
-  static constexpr int kRaw = 32 * kRow;                        // a stage: 16 K rows, 16 V rows, the new token's
-  static constexpr int kStage = kRaw + 4 * D + 64;              // K and V rows as they come, 16 page numbers
-  static constexpr int kMerge = kWarps / 2 * 8 * D * 4;         // half the warps' sums of eight heads
-  static constexpr int kFit = (232448 - 1024 - kMerge - 2048) / (kWarps * kStage);
+  static constexpr int kMt = kRow >= 256 ? 1 : 256 / kRow;      // blocks of 16 slots in a tile: 8 KB of K and V rows or more
+  static constexpr int kTile = 16 * kMt;                        // slots
+  static constexpr int kRaw = 2 * kTile * kRow;                 // a stage: K rows, V rows, and
+  static constexpr int kStage = kRaw + 4 * D;                   // the new token's K and V rows as they come
+  static constexpr int kFit = (232448 - 2048) / (kWarps * (kStage + 8 * kTile));
   static constexpr int kStages = kFit > 8 ? 8 : kFit;
-  static constexpr int kSmem = kWarps * kStages * kStage + kMerge;
+  static constexpr int kAhead = kStages - 1;                    // tiles that rows are on their way of
+  static constexpr int kPages = 2 * kStages;                    // tiles whose page numbers are known or on their way
+  static constexpr int kRing = kStages * kStage;                // of a warp
+  static constexpr int kWarpSmem = kRing + kPages * kTile * 4;
+  static constexpr int kSmem = kWarps * kWarpSmem;
   static_assert(kStages >= 3, "two tiles on their way and one in use");
 };
 
 struct PdWork {
   int heads;            // of a block: 8 or 16
   int blocks;           // of a KV head's query heads
-  float* part;          // [CTAs][2] partial sums: 16 references, 16 sums, then the accumulators
-  int part_stride;      // floats
+  float* part;          // [CTAs][2] partial sums of CTAs
+  float* lead;          // [CTAs][warps] partial sums of warps whose run begins inside a unit and outlasts it
+  int stride;           // floats of one: 16 references, 16 sums, then the accumulators
   int* count;           // [rows * Hkv * blocks]: CTAs that have written their part
   float* logits;        // [n_pages][Hkv][P][blocks * heads], with weights
   float* lse2;          // [rows][Hq], with weights
@@ -66,10 +72,15 @@ __device__ __forceinline__ void pd_mma(float (&c)[4], const uint32_t (&a)[4], ui
   if (KIND == kPdBf16) mma_bf16(c, a, b0, b1);
   else mma_fp16(c, a, b0, b1);
 }
-// Two e4m3 values in the lower half of x as two halves.
-__device__ __forceinline__ uint32_t pd_halves(uint32_t x) {
+// Two e4m3 values, the lower or the upper ones of x, as two halves.
+__device__ __forceinline__ uint32_t pd_halves_lo(uint32_t x) {
   uint32_t y;
   asm("{\n.reg .b16 l, h;\nmov.b32 {l, h}, %1;\ncvt.rn.f16x2.e4m3x2 %0, l;\n}\n" : "=r"(y) : "r"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t pd_halves_hi(uint32_t x) {
+  uint32_t y;
+  asm("{\n.reg .b16 l, h;\nmov.b32 {l, h}, %1;\ncvt.rn.f16x2.e4m3x2 %0, h;\n}\n" : "=r"(y) : "r"(x));
   return y;
 }
 
@@ -99,162 +110,241 @@ __device__ __forceinline__ void pd_advance(PdCursor& u, const PagedCache& c, con
   } while (u.tiles == 0);
 }
 
-// All lanes of a warp: tiles of the whole call, and the cursor of tile CTA * per where per is every CTA's run.  Returns per.
+// All lanes of a warp: the tiles of the whole call, and the cursor of tile `runs_before` * per, where per is every run's length
+// (returned) when `runs` of them cover the line.
 template <int TILE>
-__device__ __forceinline__ long long pd_deal(PdCursor& u, long long& total, const PagedCache& c, const PagedRows& r, int blocks) {
-  const int lane = threadIdx.x & 31;
-  const long long per_row = (long long)c.Hkv * blocks;
-  total = 0;
-  long long first = 0;  // of the first 32 rows, kept
-  for (int base = 0; base < r.n; base += 32) {
-    const int row = base + lane;
-    long long t = row < r.n ? (paged_len(c, r, row) + TILE - 1) / TILE * per_row : 0;
-    if (base == 0) first = t;
-#pragma unroll
-    for (int d = 16; d; d >>= 1) t += shfl_xor_ll(t, d);
-    total += t;
-  }
-  const long long per = (total + gridDim.x - 1) / gridDim.x;
-  long long left = blockIdx.x * per;
-  if (left >= total) return per;
-  for (int base = 0; base < r.n; base += 32) {
-    const int row = base + lane;
-    const long long t = base == 0 ? first : row < r.n ? (paged_len(c, r, row) + TILE - 1) / TILE * per_row : 0;
-    long long inc = t;
+__device__ __forceinline__ int pd_deal(PdCursor& u, int& total, int runs, int runs_before, const PagedCache& c,
+                                       const PagedRows& r, int blocks) {
+  const int lane = threadIdx.x & 31, per_row = c.Hkv * blocks;
+  auto scan = [&](int x) {
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
-      const long long y = shfl_up_ll(inc, d);
-      if (lane >= d) inc += y;
+      const int y = __shfl_up_sync(0xffffffffu, x, d);
+      if (lane >= d) x += y;
     }
+    return x;
+  };
+  // the first 32 rows are kept
+  const int n0 = lane < r.n ? paged_len(c, r, lane) : 0, inc0 = scan((n0 + TILE - 1) / TILE * per_row);
+  total = __shfl_sync(0xffffffffu, inc0, 31);
+  for (int base = 32; base < r.n; base += 32) {
+    const int row = base + lane;
+    total += __reduce_add_sync(0xffffffffu, row < r.n ? (paged_len(c, r, row) + TILE - 1) / TILE * per_row : 0);
+  }
+  const int per = (int)((unsigned)(total + runs - 1) / (unsigned)runs);
+  int left = runs_before * per;
+  if (left >= total) return per;
+  for (int base = 0;; base += 32) {
+    const int row = base + lane;
+    const int n = base == 0 ? n0 : row < r.n ? paged_len(c, r, row) : 0;
+    const int inc = base == 0 ? inc0 : scan((n + TILE - 1) / TILE * per_row);
     const unsigned in = __ballot_sync(0xffffffffu, left < inc);
     if (in) {
       const int at = __ffs(in) - 1;
-      const long long begin = shfl_ll(inc - t, at);
       u.row = base + at;
-      u.n = paged_len(c, r, u.row);
+      u.n = __shfl_sync(0xffffffffu, n, at);
       u.tiles = (u.n + TILE - 1) / TILE;
-      left -= begin;
-      const long long unit = left / u.tiles;
-      u.tile = (int)(left - unit * u.tiles);
-      u.head = (int)(unit / blocks);
-      u.block = (int)(unit - (long long)u.head * blocks);
+      left -= __shfl_sync(0xffffffffu, inc, at) - u.tiles * per_row;
+      const int unit = (int)((unsigned)left / (unsigned)u.tiles);
+      u.tile = left - unit * u.tiles;
+      u.head = blocks == 1 ? unit : unit / blocks;
+      u.block = unit - u.head * blocks;
       return per;
     }
-    left -= shfl_ll(inc, 31);
+    left -= __shfl_sync(0xffffffffu, inc, 31);
   }
-  return per;
 }
+
+// A unit that a warp's run leaves unfinished, or (the last entry) that ends in the CTA's first run but began in another CTA.
+struct PdOpen {
+  int begin;                    // in the line
+  int row, head, block, tiles;  // tiles 0: none
+};
 
 template <int KIND, int D, int NT>
 __global__ void __launch_bounds__(PdShape<KIND, D>::kWarps * 32, 1)
     k_paged_decode(PagedCache c, PagedRows r, int layer, PagedStep a, PdWork wk) {
   using Sh = PdShape<KIND, D>;
-  constexpr int W = Sh::kWarps, TILE = Sh::kTile, S = Sh::kStages, RC = Sh::kChunks, DT = D / 16, H = 8 * NT;
-  constexpr int kSlices = NT * DT / W > 0 ? NT * DT / W : 1;  // 16-row slices of the sums that a warp finishes
+  constexpr int W = Sh::kWarps, TILE = Sh::kTile, MT = Sh::kMt, S = Sh::kStages, RC = Sh::kChunks, DT = D / 16, H = 8 * NT;
+  constexpr int kSlices = NT * DT / W > 0 ? NT * DT / W : 1;  // 16-row slices of the sums that a warp joins
   // Probabilities carry a factor 2^kOff that cancels in out and lse.  A half has 2^-24 as its smallest step: with the largest
   // probability at 2^10 a slot's contribution is still seen 2^-35 below it, so that 2^20 of them cannot lose 2^-14 of a sum.
   // The reference moves only when a logit exceeds it by kGrow, which bounds the probabilities by 2^(kOff + kGrow).
   constexpr float kOff = KIND == kPdBf16 ? 0.f : 10.f, kGrow = 4.f;
   extern __shared__ __align__(1024) unsigned char dsm[];
-  __shared__ float s_ref[W][16], s_sum[W][16];
-  __shared__ int s_last;
-  float4* s_merge = reinterpret_cast<float4*>(dsm + W * S * Sh::kStage);
+  __shared__ PdOpen s_open[W + 1];
+  __shared__ PdOpen s_part[2];
+  __shared__ int s_last[2];
   chain_wait();
+  if (c.w) chain_release();  // the weights kernel may take its place beside this one; it waits for this one's end
   const int warp = threadIdx.x / 32, lane = threadIdx.x & 31, g = lane >> 2, q4 = lane & 3;
-  unsigned char* ring = dsm + warp * S * Sh::kStage;
-  const uint32_t ring_s = smem_u32(ring);
+  unsigned char* ring = dsm + warp * Sh::kWarpSmem;
+  int* s_pages = reinterpret_cast<int*>(ring + Sh::kRing);
+  const uint32_t ring_s = smem_u32(ring), pages_s = smem_u32(s_pages);
+  const bool one_page = c.P % 16 == 0;  // of 16 slots
 
   PdCursor cu;
-  long long total;
-  const long long per = pd_deal<TILE>(cu, total, c, r, wk.blocks), t0 = blockIdx.x * per;
-  const int mine = t0 >= total ? 0 : (int)(t0 + per <= total ? per : total - t0);
-  PdCursor ci = cu;
-  int issued = 0;
+  int total;
+  const int per = pd_deal<TILE>(cu, total, gridDim.x * W, blockIdx.x * W + warp, c, r, wk.blocks);
+  const int c0 = blockIdx.x * W * per, c1 = min(c0 + W * per, total);  // the CTA's run
+  const int t0 = c0 + warp * per, mine = max(0, min(per, total - t0));
+  if (lane == 0) {
+    s_open[warp].tiles = 0;
+    if (warp == 0) s_open[W].tiles = 0;
+  }
 
-  auto page_of = [&](const PdCursor& u) -> int {  // of this lane's slot: -1 where there is none
-    const int slot = u.tile * TILE + warp * 16 + (lane & 15);
-    return slot < u.n ? paged_page(c, r, u.row, slot / c.P) : -1;
+  // Page numbers of a tile's slots on their way into entry `st` (-1 behind the row's end).
+  auto request_pages = [&](const PdCursor& u, int st) {
+#pragma unroll
+    for (int j = lane; j < TILE; j += 32) {
+      const int slot = u.tile * TILE + j;
+      if (slot < u.n) cp_async4(pages_s + (st * TILE + j) * 4, r.table + u.row * r.table_stride + paged_nth(c, slot));
+      else s_pages[st * TILE + j] = -1;
+    }
   };
-  int pg = mine > 0 ? page_of(ci) : -1;  // of the tile that is issued next
-  auto issue = [&]() {
-    if (issued < mine) {
-      const int slot0 = ci.tile * TILE + warp * 16, st = issued % S;
-      if (slot0 < ci.n) {
-        const int slot = slot0 + (lane & 15);
-        const long long off = pg < 0 ? -1 : (long long)paged_row(c, layer, pg, ci.head, slot % c.P);
-        int* s_page = reinterpret_cast<int*>(ring + st * Sh::kStage + Sh::kRaw + 4 * D);
-        if (lane < 16) s_page[lane] = pg;
-        const uint32_t sk = ring_s + st * Sh::kStage, sv = sk + 16 * Sh::kRow;
-        const int fresh = a.k && ci.n - 1 - slot0 < 16 ? ci.n - 1 - slot0 : -1;  // the new token's row comes from the caller
+  const int in = lane % RC, lane_row = lane / RC;  // this lane's chunk, of rows lane_row, lane_row + 32 / RC, ...
+  const size_t lane_at = lane_row * c.ts + in * 16, step = (32 / RC) * c.ts;
+  auto issue = [&](const PdCursor& u, const int* s_page, uint32_t stage) {
+    const int slot0 = u.tile * TILE;
+    const int last = a.k ? u.n - 1 : -1;  // the new token's slot: its row comes from the caller
+#pragma unroll 1
+    for (int m = 0; m < MT; ++m) {
+      const int base = slot0 + m * 16;
+      int pg = s_page[m * 16 + (lane & 15)];
+      if ((unsigned)pg >= (unsigned)c.n_pages) {
+        if (base + (lane & 15) < u.n) paged_status(c, u.row);
+        pg = -1;
+      }
+      const uint32_t sk = stage + m * 16 * Sh::kRow, sv = sk + TILE * Sh::kRow;
+      if (one_page) {
+        const int page = __shfl_sync(0xffffffffu, pg, 0);  // (slot `base` has one, or the whole block has none)
+        const size_t from = page < 0 ? 0 : paged_row(c, layer, page, u.head, base - paged_nth(c, base) * c.P) + lane_at;
+        const int end = page < 0 ? 0 : u.n - base, not_this = last - base;
 #pragma unroll
         for (int i = 0; i < RC / 2; ++i) {
-          const int row = i * (32 / RC) + lane / RC, ch = lane % RC;
+          const int row = i * (32 / RC) + lane_row;
+          const bool ok = row < end && row != not_this;
+          const size_t at = ok ? from + i * step : 0;
+          cp_async16(sk + pd_at<RC>(row, in), c.k + at, ok ? 16 : 0);
+          cp_async16(sv + pd_at<RC>(row, in), c.v + at, ok ? 16 : 0);
+        }
+      } else {
+        const int slot = base + (lane & 15), place = slot - paged_nth(c, slot) * c.P;
+        const long long off = pg < 0 ? -1 : (long long)paged_row(c, layer, pg, u.head, place);
+#pragma unroll
+        for (int i = 0; i < RC / 2; ++i) {
+          const int row = i * (32 / RC) + lane_row;
           const long long o = shfl_ll(off, row);
-          const bool in = o >= 0 && row != fresh;
-          const size_t at = in ? (size_t)o + ch * 16 : 0;
-          cp_async16(sk + pd_at<RC>(row, ch), c.k + at, in ? 16 : 0);
-          cp_async16(sv + pd_at<RC>(row, ch), c.v + at, in ? 16 : 0);
+          const bool ok = o >= 0 && base + row != last;
+          const size_t at = ok ? (size_t)o + in * 16 : 0;
+          cp_async16(sk + pd_at<RC>(row, in), c.k + at, ok ? 16 : 0);
+          cp_async16(sv + pd_at<RC>(row, in), c.v + at, ok ? 16 : 0);
         }
-        if (fresh >= 0 && lane < D / 8) {
-          const size_t at = ci.row * a.kv_stride + ((size_t)ci.head * D + lane * 8) * 2;
-          cp_async16(ring_s + st * Sh::kStage + Sh::kRaw + lane * 16, a.k + at, 16);
-          cp_async16(ring_s + st * Sh::kStage + Sh::kRaw + 2 * D + lane * 16, a.v + at, 16);
-        }
-      }
-      if (++issued < mine) {
-        pd_advance<TILE>(ci, c, r, wk.blocks);
-        pg = page_of(ci);
       }
     }
-    cp_async_commit();
+    if (last >= slot0 && last < slot0 + TILE && lane < D / 8) {
+      const size_t at = u.row * a.kv_stride + ((size_t)u.head * D + lane * 8) * 2;
+      cp_async16(stage + Sh::kRaw + lane * 16, a.k + at, 16);
+      cp_async16(stage + Sh::kRaw + 2 * D + lane * 16, a.v + at, 16);
+    }
   };
-#pragma unroll 1
-  for (int i = 0; i < S - 1; ++i) issue();
-
+  // The queries of a unit as the products' columns (head g of each block), and the logits' factors.
   uint32_t qb[NT][DT][2];
-  float sc[NT][2];      // logits' factor of this lane's heads
-  float O[NT][DT][4], ref[NT][2], sum[NT][2];
-  bool whole = false;   // the unit has begun in this CTA
-  for (int at = 0; at < mine; ++at) {
-    if (at == 0 || cu.tile == 0) {  // a unit begins: its queries
-      whole = cu.tile == 0;
-      const float ks = c.ks ? c.ks[cu.head] : 1.f;
+  float sc[NT][2];
+  auto load_queries = [&](const PdCursor& u) {
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        const int in_group = cu.block * H + nt * 8 + g;
-        const unsigned char* qr = a.q + cu.row * a.q_stride + ((size_t)cu.head * c.G + in_group) * D * 2;
+    for (int nt = 0; nt < NT; ++nt) {
+      const int in_group = u.block * H + nt * 8 + g;
+      const unsigned char* qr = a.q + u.row * a.q_stride + ((size_t)u.head * c.G + in_group) * D * 2;
+#pragma unroll
+      for (int i = 0; i < DT; ++i) {
+        // (8-bit rows: a 16-byte chunk is one step of 16, of which a lane holds four neighbours)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const int el = KIND == kPdE4m3 ? i * 16 + q4 * 4 + 2 * j : i * 16 + q4 * 2 + 8 * j;
+          qb[nt][i][j] = in_group < c.G ? *reinterpret_cast<const uint32_t*>(qr + el * 2) : 0u;
+        }
+      }
+    }
+  };
+  auto scale_queries = [&](const PdCursor& u) {
+    const float ks = c.ks ? c.ks[u.head] : 1.f;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      float back = 1.f;
+      if (KIND == kPdE4m3 && c.type == LTRI_TYPE_BF16) {
+        // bf16 queries as halves: a power of two brings the row's largest element to [2^14, 2^15); what then falls below
+        // the halves' range is 2^-39 of it
         uint32_t most = 0;
 #pragma unroll
-        for (int i = 0; i < DT; ++i) {
-          // (8-bit rows: a 16-byte chunk is one step of 16, of which a lane holds four neighbours)
-          const int e = KIND == kPdE4m3 ? i * 16 + q4 * 4 : i * 16 + q4 * 2;
+        for (int i = 0; i < DT; ++i)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) most = max(most, max(qb[nt][i][j] & 0x7fffu, (qb[nt][i][j] >> 16) & 0x7fffu));
+        most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
+        most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
+        const int ex = (int)(most >> 7);  // biased exponent
+        const int up = ex == 0 || ex == 255 ? 0 : 127 + 14 - ex;
+        // (2^up may lie outside fp32's range: two factors)
+        const float u0 = ldexpf(1.f, up / 2), u1 = ldexpf(1.f, up - up / 2);
+#pragma unroll
+        for (int i = 0; i < DT; ++i)
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
-            const int el = KIND == kPdE4m3 ? e + 2 * j : e + 8 * j;
-            qb[nt][i][j] = in_group < c.G ? *reinterpret_cast<const uint32_t*>(qr + el * 2) : 0u;
-            most = max(most, max(qb[nt][i][j] & 0x7fffu, (qb[nt][i][j] >> 16) & 0x7fffu));
+            const float2 f = paged_unpack(LTRI_TYPE_BF16, qb[nt][i][j]);
+            qb[nt][i][j] = paged_pack(LTRI_TYPE_FP16, f.x * u0 * u1, f.y * u0 * u1);
           }
-        }
-        float back = 1.f;
-        if (KIND == kPdE4m3 && c.type == LTRI_TYPE_BF16) {
-          // bf16 queries as halves: a power of two brings the row's largest element to [2^14, 2^15); what then falls below
-          // the halves' range is 2^-39 of it
-          most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
-          most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
-          const int ex = (int)(most >> 7);  // biased exponent
-          const int up = ex == 0 || ex == 255 ? 0 : 127 + 14 - ex;
+        back = ldexpf(1.f, -up);
+      }
+      // (the queries lie with head g, the logits with heads 2 q4 and 2 q4 + 1)
 #pragma unroll
-          for (int i = 0; i < DT; ++i)
+      for (int e = 0; e < 2; ++e) sc[nt][e] = c.scale * ks * __shfl_sync(0xffffffffu, back, (2 * q4 + e) * 4);
+    }
+  };
+  // A slice of 16 elements of the eight heads of block nt, normalised, to the output.
+  auto put_slice = [&](const PdCursor& u, int nt, int i, const float (&z)[4]) {
+    const uint32_t y0 = pd_transpose(paged_pack(c.type, z[0], z[1])), y1 = pd_transpose(paged_pack(c.type, z[2], z[3]));
+    const int in_group = u.block * H + nt * 8 + g;
+    if (in_group >= c.G) return;
+    unsigned char* to = a.out + (((size_t)u.row * c.Hq + (size_t)u.head * c.G + in_group) * D + i * 16) * 2;
+    if (KIND == kPdE4m3) {  // elements 4 q4, + 2 and 4 q4 + 1, + 3
+      *reinterpret_cast<uint2*>(to + q4 * 8) = make_uint2(__byte_perm(y0, y1, 0x5410), __byte_perm(y0, y1, 0x7632));
+    } else {
+      *reinterpret_cast<uint32_t*>(to + q4 * 4) = y0;
+      *reinterpret_cast<uint32_t*>(to + 16 + q4 * 4) = y1;
+    }
+  };
+  // The log-sum of head 2 q4 + e of block nt.
+  auto put_lse = [&](const PdCursor& u, int nt, int e, float top, float sum) {
+    const int in_group = u.block * H + nt * 8 + 2 * q4 + e;
+    if (g != 0 || in_group >= c.G) return;
+    const size_t at = (size_t)u.row * c.Hq + (size_t)u.head * c.G + in_group;
+    const float l2 = sum == 0.f ? -INFINITY : top + log2f(sum);
+    if (a.lse) a.lse[at] = l2 * 0.69314718055994531f;
+    if (c.w) wk.lse2[at] = l2;
+  };
+  auto scale_of = [&](const PdCursor& u, float sum) { return sum == 0.f ? 0.f : (c.vs ? c.vs[u.head] : 1.f) / sum; };
+
+  float O[NT][DT][4], ref[NT][2], sum[NT][2];
+  bool whole = false;   // the unit has begun in this run
+  // Rounds: in round `at` tile `at` is used, the rows of tile at + kAhead are requested and the page numbers of tile
+  // at + 2 kAhead.  A round's requests are one group, complete when the round kAhead later begins; only the first tiles' page
+  // numbers are waited for at once, with the first queries on their way.
+  PdCursor ci = cu, cp = cu;
+  int stage_at = 0, page_at = 0;            // of tile `at`
+  int stage_in = 0, page_in = 0, page_rq = 0;  // of the tiles that are requested
+  auto next = [](int x, int n) { return x + 1 == n ? 0 : x + 1; };
+#pragma unroll 1
+  for (int at = mine > 0 ? -2 * Sh::kAhead : 0; at < mine; ++at) {
+    if (at == -Sh::kAhead) {
+      cp_async_wait<0>();
+      __syncwarp();
+    }
+    if (at >= 0) {
+    if (at == 0 || cu.tile == 0) {  // a unit begins
+      whole = cu.tile == 0;
+      scale_queries(cu);
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-              const float2 f = paged_unpack(LTRI_TYPE_BF16, qb[nt][i][j]);
-              qb[nt][i][j] = paged_pack(LTRI_TYPE_FP16, ldexpf(f.x, up), ldexpf(f.y, up));
-            }
-          back = ldexpf(1.f, -up);
-        }
-        // (the queries lie with head g, the logits with heads 2 q4 and 2 q4 + 1)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) sc[nt][e] = c.scale * ks * __shfl_sync(0xffffffffu, back, (2 * q4 + e) * 4);
+      for (int nt = 0; nt < NT; ++nt) {
         ref[nt][0] = ref[nt][1] = -INFINITY;
         sum[nt][0] = sum[nt][1] = 0.f;
 #pragma unroll
@@ -263,118 +353,128 @@ __global__ void __launch_bounds__(PdShape<KIND, D>::kWarps * 32, 1)
     }
     cp_async_wait<S - 2>();
     __syncwarp();
-    const int slot0 = cu.tile * TILE + warp * 16, st = at % S;
-    if (slot0 < cu.n) {
-      unsigned char* stage = ring + st * Sh::kStage;
-      const uint32_t sk = ring_s + st * Sh::kStage, sv = sk + 16 * Sh::kRow;
-      const int* s_page = reinterpret_cast<const int*>(stage + Sh::kRaw + 4 * D);
-      const int fresh = a.k && cu.n - 1 - slot0 < 16 ? cu.n - 1 - slot0 : -1;
-      if (fresh >= 0 && s_page[fresh] >= 0) {  // the new token's row into the tile and into its page
-        const int page = s_page[fresh], place = (cu.n - 1) % c.P;
-        if (lane < D / 8) {
-          const uint4 kx = *reinterpret_cast<const uint4*>(stage + Sh::kRaw + lane * 16);
-          const uint4 vx = *reinterpret_cast<const uint4*>(stage + Sh::kRaw + 2 * D + lane * 16);
-          const size_t to = paged_row(c, layer, page, cu.head, place);
-          if (KIND == kPdE4m3) {
-            const uint2 ky = paged_quantise(c.type, kx, c.ks[cu.head]), vy = paged_quantise(c.type, vx, c.vs[cu.head]);
-            const uint32_t in = pd_at<RC>(fresh, lane / 2) + (lane & 1) * 8;
-            *reinterpret_cast<uint2*>(stage + in) = ky;
-            *reinterpret_cast<uint2*>(stage + 16 * Sh::kRow + in) = vy;
-            if (cu.block == 0) {
-              *reinterpret_cast<uint2*>(c.k + to + lane * 8) = ky;
-              *reinterpret_cast<uint2*>(c.v + to + lane * 8) = vy;
-            }
-          } else {
-            const uint32_t in = pd_at<RC>(fresh, lane);
-            *reinterpret_cast<uint4*>(stage + in) = kx;
-            *reinterpret_cast<uint4*>(stage + 16 * Sh::kRow + in) = vx;
-            if (cu.block == 0) {
-              *reinterpret_cast<uint4*>(c.k + to + lane * 16) = kx;
-              *reinterpret_cast<uint4*>(c.v + to + lane * 16) = vx;
-            }
+    const int slot0 = cu.tile * TILE;
+    unsigned char* stage = ring + stage_at * Sh::kStage;
+    const uint32_t sk = ring_s + stage_at * Sh::kStage, sv = sk + TILE * Sh::kRow;
+    const int* s_page = s_pages + page_at * TILE;
+    const int fresh = a.k && cu.n - 1 - slot0 < TILE ? cu.n - 1 - slot0 : -1;
+    if (fresh >= 0 && (unsigned)s_page[fresh] < (unsigned)c.n_pages) {  // the new token's row into the tile and into its page
+      const int page = s_page[fresh], place = cu.n - 1 - paged_nth(c, cu.n - 1) * c.P;
+      if (lane < D / 8) {
+        const uint4 kx = *reinterpret_cast<const uint4*>(stage + Sh::kRaw + lane * 16);
+        const uint4 vx = *reinterpret_cast<const uint4*>(stage + Sh::kRaw + 2 * D + lane * 16);
+        const size_t to = paged_row(c, layer, page, cu.head, place);
+        if (KIND == kPdE4m3) {
+          const uint2 ky = paged_quantise(c.type, kx, c.ks[cu.head]), vy = paged_quantise(c.type, vx, c.vs[cu.head]);
+          const uint32_t in = pd_at<RC>(fresh, lane / 2) + (lane & 1) * 8;
+          *reinterpret_cast<uint2*>(stage + in) = ky;
+          *reinterpret_cast<uint2*>(stage + TILE * Sh::kRow + in) = vy;
+          if (cu.block == 0) {
+            *reinterpret_cast<uint2*>(c.k + to + lane * 8) = ky;
+            *reinterpret_cast<uint2*>(c.v + to + lane * 8) = vy;
+          }
+        } else {
+          const uint32_t in = pd_at<RC>(fresh, lane);
+          *reinterpret_cast<uint4*>(stage + in) = kx;
+          *reinterpret_cast<uint4*>(stage + TILE * Sh::kRow + in) = vx;
+          if (cu.block == 0) {
+            *reinterpret_cast<uint4*>(c.k + to + lane * 16) = kx;
+            *reinterpret_cast<uint4*>(c.v + to + lane * 16) = vx;
           }
         }
-        if (c.w && cu.block == 0 && lane == 0) {
-          const size_t word = paged_word(c, layer, page, cu.head, place);
-          c.w[word] = 0.f;
-          c.pos[word] = a.row_pos ? a.row_pos[cu.row] : cu.n - 1;
-        }
-        __syncwarp();
       }
-      float x[NT][4];
+      if (c.w && cu.block == 0 && lane == 0) {
+        const size_t word = paged_word(c, layer, page, cu.head, place);
+        c.w[word] = 0.f;
+        c.pos[word] = a.row_pos ? a.row_pos[cu.row] : cu.n - 1;
+      }
+      __syncwarp();
+    }
+    float x[MT][NT][4];
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) x[nt][0] = x[nt][1] = x[nt][2] = x[nt][3] = 0.f;
+    for (int m = 0; m < MT; ++m) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) x[m][nt][0] = x[m][nt][1] = x[m][nt][2] = x[m][nt][3] = 0.f;
       if (KIND == kPdE4m3) {
 #pragma unroll
         for (int i = 0; i < DT; i += 2) {
           uint32_t b[4];
-          ldsm_x4(b, sk + pd_at<RC>(lane & 15, i + (lane >> 4)));
+          ldsm_x4(b, sk + pd_at<RC>(m * 16 + (lane & 15), i + (lane >> 4)));
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
-            const uint32_t f[4] = {pd_halves(b[2 * j]), pd_halves(b[2 * j + 1]), pd_halves(b[2 * j] >> 16),
-                                   pd_halves(b[2 * j + 1] >> 16)};
+            const uint32_t f[4] = {pd_halves_lo(b[2 * j]), pd_halves_lo(b[2 * j + 1]), pd_halves_hi(b[2 * j]),
+                                   pd_halves_hi(b[2 * j + 1])};
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) pd_mma<KIND>(x[nt], f, qb[nt][i + j][0], qb[nt][i + j][1]);
+            for (int nt = 0; nt < NT; ++nt) pd_mma<KIND>(x[m][nt], f, qb[nt][i + j][0], qb[nt][i + j][1]);
           }
         }
       } else {
 #pragma unroll
         for (int i = 0; i < DT; ++i) {
           uint32_t f[4];
-          ldsm_x4(f, sk + pd_at<RC>(lane & 15, 2 * i + (lane >> 4)));
+          ldsm_x4(f, sk + pd_at<RC>(m * 16 + (lane & 15), 2 * i + (lane >> 4)));
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt) pd_mma<KIND>(x[nt], f, qb[nt][i][0], qb[nt][i][1]);
+          for (int nt = 0; nt < NT; ++nt) pd_mma<KIND>(x[m][nt], f, qb[nt][i][0], qb[nt][i][1]);
         }
       }
-      // lane: slots slot0 + g and + 8 (x[0..1], x[2..3]), heads 2 q4 and 2 q4 + 1
-      const int p0 = s_page[g], p1 = s_page[g + 8];
-      bool grow = false;
+    }
+    // lane: slots g and g + 8 of a block (x[..][0..1], x[..][2..3]), heads 2 q4 and 2 q4 + 1
+    bool grow = false;
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+      const int p0 = s_page[m * 16 + g], p1 = s_page[m * 16 + g + 8];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          x[nt][e] = (e < 2 ? p0 : p1) >= 0 ? x[nt][e] * sc[nt][e & 1] : -INFINITY;
-          grow |= x[nt][e] > ref[nt][e & 1] + (kOff + kGrow);
+          x[m][nt][e] = (unsigned)(e < 2 ? p0 : p1) < (unsigned)c.n_pages ? x[m][nt][e] * sc[nt][e & 1] : -INFINITY;
+          grow |= x[m][nt][e] > ref[nt][e & 1] + (kOff + kGrow);
         }
       if (c.w) {
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           const int page = e ? p1 : p0;
-          if (page < 0) continue;
-          const size_t word = ((size_t)page * c.Hkv + cu.head) * c.P + (slot0 + g + 8 * e) % c.P;
+          if ((unsigned)page >= (unsigned)c.n_pages) continue;
+          const int slot = slot0 + m * 16 + g + 8 * e, place = slot - paged_nth(c, slot) * c.P;
+          const size_t word = ((size_t)page * c.Hkv + cu.head) * c.P + place;
           float2* to = reinterpret_cast<float2*>(wk.logits + word * (wk.blocks * H) + cu.block * H);
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt) to[nt * 4 + q4] = make_float2(x[nt][2 * e], x[nt][2 * e + 1]);
+          for (int nt = 0; nt < NT; ++nt) to[nt * 4 + q4] = make_float2(x[m][nt][2 * e], x[m][nt][2 * e + 1]);
         }
       }
-      if (__any_sync(0xffffffffu, grow)) {
+    }
+    if (__any_sync(0xffffffffu, grow)) {
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+      for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            float top = fmaxf(x[nt][e], x[nt][e + 2]);
+        for (int e = 0; e < 2; ++e) {
+          float top = fmaxf(x[0][nt][e], x[0][nt][e + 2]);
 #pragma unroll
-            for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-            const float to = fmaxf(ref[nt][e], top - kOff);
-            const float by = to == -INFINITY ? 1.f : pd_exp2(ref[nt][e] - to);
-            ref[nt][e] = to;
-            sum[nt][e] *= by;
+          for (int m = 1; m < MT; ++m) top = fmaxf(top, fmaxf(x[m][nt][e], x[m][nt][e + 2]));
 #pragma unroll
-            for (int i = 0; i < DT; ++i) {
-              O[nt][i][e] *= by;
-              O[nt][i][e + 2] *= by;
-            }
+          for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+          const float to = fmaxf(ref[nt][e], top - kOff);
+          const float by = to == -INFINITY ? 1.f : pd_exp2(ref[nt][e] - to);
+          ref[nt][e] = to;
+          sum[nt][e] *= by;
+#pragma unroll
+          for (int i = 0; i < DT; ++i) {
+            O[nt][i][e] *= by;
+            O[nt][i][e + 2] *= by;
           }
-      }
-      // probabilities as two terms of the products' type, as V^T P^T takes them
-      uint32_t hi[NT][2], lo[NT][2];
+        }
+    }
+    // probabilities as two terms of the products' type, as V^T P^T takes them
+    uint32_t hi[MT][NT][2], lo[MT][NT][2];
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         float p[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const float m = ref[nt][e & 1];
-          p[e] = pd_exp2(x[nt][e] - (m == -INFINITY ? 0.f : m));
+          const float to = ref[nt][e & 1];
+          p[e] = pd_exp2(x[m][nt][e] - (to == -INFINITY ? 0.f : to));
           sum[nt][e & 1] += p[e];
         }
         constexpr int T = KIND == kPdBf16 ? LTRI_TYPE_BF16 : LTRI_TYPE_FP16;
@@ -382,221 +482,247 @@ __global__ void __launch_bounds__(PdShape<KIND, D>::kWarps * 32, 1)
         for (int e = 0; e < 2; ++e) {
           const uint32_t h = paged_pack(T, p[2 * e], p[2 * e + 1]);
           const float2 back = paged_unpack(T, h);
-          hi[nt][e] = pd_transpose(h);
-          lo[nt][e] = pd_transpose(paged_pack(T, p[2 * e] - back.x, p[2 * e + 1] - back.y));
+          hi[m][nt][e] = pd_transpose(h);
+          lo[m][nt][e] = pd_transpose(paged_pack(T, p[2 * e] - back.x, p[2 * e + 1] - back.y));
         }
       }
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
 #pragma unroll
       for (int i = 0; i < DT; i += KIND == kPdE4m3 ? 2 : 1) {
         uint32_t b[4];
         if (KIND == kPdE4m3) {
           // a 16-byte chunk's 8 pairs of neighbours are the 8 rows of a transposed matrix: row g has elements 2g and 2g + 1
-          ldsm_x4_t(b, sv + pd_at<RC>(lane & 15, i + (lane >> 4)));
+          ldsm_x4_t(b, sv + pd_at<RC>(m * 16 + (lane & 15), i + (lane >> 4)));
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
             uint32_t f[4];
 #pragma unroll
             for (int e = 0; e < 2; ++e) {  // slots 2 q4, 2 q4 + 1 and, with e, 8 further
-              const uint32_t l = pd_halves(b[2 * j + e]), h = pd_halves(b[2 * j + e] >> 16);
+              const uint32_t l = pd_halves_lo(b[2 * j + e]), h = pd_halves_hi(b[2 * j + e]);
               f[2 * e] = __byte_perm(l, h, 0x5410);
               f[2 * e + 1] = __byte_perm(l, h, 0x7632);
             }
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-              pd_mma<KIND>(O[nt][i + j], f, hi[nt][0], hi[nt][1]);
-              pd_mma<KIND>(O[nt][i + j], f, lo[nt][0], lo[nt][1]);
+              pd_mma<KIND>(O[nt][i + j], f, hi[m][nt][0], hi[m][nt][1]);
+              pd_mma<KIND>(O[nt][i + j], f, lo[m][nt][0], lo[m][nt][1]);
             }
           }
         } else {
-          ldsm_x4_t(b, sv + pd_at<RC>((lane & 7) + (lane >> 4) * 8, 2 * i + ((lane >> 3) & 1)));
+          ldsm_x4_t(b, sv + pd_at<RC>(m * 16 + (lane & 7) + (lane >> 4) * 8, 2 * i + ((lane >> 3) & 1)));
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) {
-            pd_mma<KIND>(O[nt][i], b, hi[nt][0], hi[nt][1]);
-            pd_mma<KIND>(O[nt][i], b, lo[nt][0], lo[nt][1]);
+            pd_mma<KIND>(O[nt][i], b, hi[m][nt][0], hi[m][nt][1]);
+            pd_mma<KIND>(O[nt][i], b, lo[m][nt][0], lo[m][nt][1]);
           }
         }
       }
     }
     __syncwarp();
-    issue();
+    stage_at = next(stage_at, S);
+    page_at = next(page_at, Sh::kPages);
     const bool ends = cu.tile + 1 == cu.tiles;
     if (ends || at + 1 == mine) {
-      // ---- the warps' sums, brought to one reference ----
-      float top[NT][2], tot[NT][2];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
+        for (int e = 0; e < 2; ++e)
 #pragma unroll
           for (int d = 4; d < 32; d <<= 1) sum[nt][e] += __shfl_xor_sync(0xffffffffu, sum[nt][e], d);
-          if (g == 0) {
-            s_ref[warp][nt * 8 + 2 * q4 + e] = ref[nt][e];
-            s_sum[warp][nt * 8 + 2 * q4 + e] = sum[nt][e];
-          }
-        }
-      __syncthreads();
+      if (whole && ends) {
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const int h = nt * 8 + 2 * q4 + e;
-          float m = -INFINITY, t = 0.f;
-#pragma unroll
-          for (int w = 0; w < W; ++w) m = fmaxf(m, s_ref[w][h]);
-          const float mu = m == -INFINITY ? 0.f : m;
-#pragma unroll
-          for (int w = 0; w < W; ++w) t += s_sum[w][h] * pd_exp2(s_ref[w][h] - mu);
-          top[nt][e] = m;
-          tot[nt][e] = t;
-          const float by = pd_exp2(ref[nt][e] - mu);
+        for (int nt = 0; nt < NT; ++nt) {
+          const float by[2] = {scale_of(cu, sum[nt][0]), scale_of(cu, sum[nt][1])};
 #pragma unroll
           for (int i = 0; i < DT; ++i) {
-            O[nt][i][e] *= by;
-            O[nt][i][e + 2] *= by;
+            const float z[4] = {O[nt][i][0] * by[0], O[nt][i][1] * by[1], O[nt][i][2] * by[0], O[nt][i][3] * by[1]};
+            put_slice(cu, nt, i, z);
           }
+          put_lse(cu, nt, 0, ref[nt][0], sum[nt][0]);
+          put_lse(cu, nt, 1, ref[nt][1], sum[nt][1]);
         }
-      // the upper half of the warps hands its accumulators to the lower, then every warp adds up slices of the lower's
-      float4 got[kSlices];
+      } else {
+        // set aside: in the ring, which is empty at the end of the run, or, where the run goes on, in the workspace
+        float* to = ends ? wk.lead + ((size_t)blockIdx.x * W + warp) * wk.stride : reinterpret_cast<float*>(ring);
+        if (!ends || (warp == 0 && !whole)) {
+          if (lane == 0) s_open[ends ? W : warp] = PdOpen{t0 + at - cu.tile, cu.row, cu.head, cu.block, cu.tiles};
+        }
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        if (warp >= W / 2) {
+        for (int nt = 0; nt < NT; ++nt) {
+          if (g == 0) {
+            *reinterpret_cast<float2*>(to + nt * 8 + 2 * q4) = make_float2(ref[nt][0], ref[nt][1]);
+            *reinterpret_cast<float2*>(to + 16 + nt * 8 + 2 * q4) = make_float2(sum[nt][0], sum[nt][1]);
+          }
 #pragma unroll
           for (int i = 0; i < DT; ++i)
-            s_merge[((warp - W / 2) * DT + i) * 32 + lane] = make_float4(O[nt][i][0], O[nt][i][1], O[nt][i][2], O[nt][i][3]);
-        }
-        __syncthreads();
-        if (warp < W / 2) {
-#pragma unroll
-          for (int i = 0; i < DT; ++i) {
-            float4& z = s_merge[(warp * DT + i) * 32 + lane];
-            z.x += O[nt][i][0];
-            z.y += O[nt][i][1];
-            z.z += O[nt][i][2];
-            z.w += O[nt][i][3];
-          }
-        }
-        __syncthreads();
-#pragma unroll
-        for (int k = 0; k < kSlices; ++k) {
-          const int sl = k * W + warp - nt * DT;  // slice of this block of eight heads
-          if (sl >= 0 && sl < DT) {
-            float4 z = s_merge[sl * 32 + lane];
-#pragma unroll
-            for (int w = 1; w < W / 2; ++w) {
-              const float4 y = s_merge[(w * DT + sl) * 32 + lane];
-              z.x += y.x;
-              z.y += y.y;
-              z.z += y.z;
-              z.w += y.w;
-            }
-            got[k] = z;
-          }
-        }
-        __syncthreads();
-      }
-      // ---- one CTA has all of the unit, or the last of its CTAs joins the parts ----
-      bool write = whole && ends;
-      if (!write) {
-        const long long begin = t0 + at - cu.tile;  // of the unit, in the line
-        const int first = (int)(begin / per), pieces = (int)((begin + cu.tiles - 1) / per) - first + 1;
-        float* part = wk.part + (size_t)(2 * blockIdx.x + (whole ? 1 : 0)) * wk.part_stride;
-        if (warp == 0 && g == 0)
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              __stcg(part + nt * 8 + 2 * q4 + e, top[nt][e]);
-              __stcg(part + 16 + nt * 8 + 2 * q4 + e, tot[nt][e]);
-            }
-#pragma unroll
-        for (int k = 0; k < kSlices; ++k)
-          if (k * W + warp < NT * DT) __stcg(reinterpret_cast<float4*>(part + 32) + (k * W + warp) * 32 + lane, got[k]);
-        __threadfence();
-        __syncthreads();
-        int* count = wk.count + ((size_t)cu.row * c.Hkv + cu.head) * wk.blocks + cu.block;
-        if (threadIdx.x == 0) {
-          s_last = atomicAdd(count, 1) == pieces - 1;
-          if (s_last) *count = 0;
-        }
-        __syncthreads();
-        write = s_last;
-        if (write) {
-          __threadfence();
-          auto piece = [&](int i) { return wk.part + (size_t)(2 * (first + i) + (i == 0 ? 1 : 0)) * wk.part_stride; };
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              float m = -INFINITY;
-              for (int i = g; i < pieces; i += 8) m = fmaxf(m, __ldcg(piece(i) + nt * 8 + 2 * q4 + e));
-#pragma unroll
-              for (int d = 4; d < 32; d <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-              top[nt][e] = m;
-              tot[nt][e] = 0.f;
-            }
-#pragma unroll
-          for (int k = 0; k < kSlices; ++k) got[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-          for (int i = 0; i < pieces; ++i) {
-            const float* from = piece(i);
-            float by[NT][2];
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-              const float2 m = __ldcg(reinterpret_cast<const float2*>(from + nt * 8) + q4);
-              const float2 s = __ldcg(reinterpret_cast<const float2*>(from + 16 + nt * 8) + q4);
-              by[nt][0] = pd_exp2(m.x - (top[nt][0] == -INFINITY ? 0.f : top[nt][0]));
-              by[nt][1] = pd_exp2(m.y - (top[nt][1] == -INFINITY ? 0.f : top[nt][1]));
-              tot[nt][0] += s.x * by[nt][0];
-              tot[nt][1] += s.y * by[nt][1];
-            }
-#pragma unroll
-            for (int k = 0; k < kSlices; ++k) {
-              if (k * W + warp >= NT * DT) continue;
-              const int nt = (k * W + warp) / DT;
-              const float4 z = __ldcg(reinterpret_cast<const float4*>(from + 32) + (k * W + warp) * 32 + lane);
-              const float b0 = NT == 1 || nt == 0 ? by[0][0] : by[NT - 1][0], b1 = NT == 1 || nt == 0 ? by[0][1] : by[NT - 1][1];
-              got[k].x += z.x * b0;
-              got[k].y += z.y * b1;
-              got[k].z += z.z * b0;
-              got[k].w += z.w * b1;
-            }
-          }
-        }
-      }
-      if (write) {
-        const float vs = c.vs ? c.vs[cu.head] : 1.f;
-        const size_t head0 = (size_t)cu.row * c.Hq + (size_t)cu.head * c.G + cu.block * H;
-        const int heads = min(H, c.G - cu.block * H);
-#pragma unroll
-        for (int k = 0; k < kSlices; ++k) {
-          if (k * W + warp >= NT * DT) continue;
-          const int nt = (k * W + warp) / DT, i = (k * W + warp) % DT;
-          const float z[4] = {got[k].x, got[k].y, got[k].z, got[k].w};
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int h = nt * 8 + 2 * q4 + (e & 1);
-            if (h >= heads) continue;
-            const float t = NT == 1 || nt == 0 ? tot[0][e & 1] : tot[NT - 1][e & 1];
-            const int d = KIND == kPdE4m3 ? i * 16 + 2 * g + (e >> 1) : i * 16 + g + 8 * (e >> 1);
-            const uint32_t y = paged_pack(c.type, t == 0.f ? 0.f : z[e] / t * vs, 0.f);
-            reinterpret_cast<uint16_t*>(a.out)[(head0 + h) * D + d] = (uint16_t)y;
-          }
-        }
-        if (warp == 0 && g == 0) {
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const int h = nt * 8 + 2 * q4 + e;
-              if (h >= heads) continue;
-              const float l2 = tot[nt][e] == 0.f ? -INFINITY : top[nt][e] + log2f(tot[nt][e]);
-              if (a.lse) a.lse[head0 + h] = l2 * 0.69314718055994531f;
-              if (c.w) wk.lse2[head0 + h] = l2;
-            }
+            reinterpret_cast<float4*>(to + 32)[(nt * DT + i) * 32 + lane] =
+                make_float4(O[nt][i][0], O[nt][i][1], O[nt][i][2], O[nt][i][3]);
         }
       }
     }
     pd_advance<TILE>(cu, c, r, wk.blocks);
+    }
+    if (at >= -Sh::kAhead && at + Sh::kAhead < mine) {
+      issue(ci, s_pages + page_in * TILE, ring_s + stage_in * Sh::kStage);
+      stage_in = next(stage_in, S);
+      page_in = next(page_in, Sh::kPages);
+      pd_advance<TILE>(ci, c, r, wk.blocks);
+    }
+    if (at + 2 * Sh::kAhead < mine) {
+      request_pages(cp, page_rq);
+      page_rq = next(page_rq, Sh::kPages);
+      pd_advance<TILE>(cp, c, r, wk.blocks);
+    }
+    cp_async_commit();
+    if (at == -Sh::kAhead - 1 || (at >= 0 && at + 1 < mine && cu.tile == 0)) load_queries(cu);
+  }
+
+  // ---- units that the CTA's warps share, and its parts of units that it shares with other CTAs ----
+  __syncthreads();
+  // the CTA's unfinished units, each at its first piece in this CTA
+  unsigned todo;
+  {
+    const int w = min(lane, W);
+    todo = __ballot_sync(0xffffffffu, lane <= W && s_open[w].tiles != 0 && (w == 0 || w == W || s_open[w].begin >= c0 + w * per));
+  }
+  const unsigned cta_run = max(1, W * per);
+  int parts = 0;          // bits: the CTA has a part of a unit that reaches back to another CTA, or on to one
+  bool others = false;    // first the pieces of this CTA's warps, then the parts of other CTAs
+#pragma unroll 1
+  while (true) {
+    if (todo == 0) {
+      if (others || !parts) break;
+      // the parts are written: whoever comes last to a unit joins them
+      others = true;
+      __syncthreads();
+      if (threadIdx.x < 2 && (parts >> threadIdx.x & 1)) {
+        const PdOpen o = s_part[threadIdx.x];
+        const int ctas = (unsigned)(o.begin + o.tiles - 1) / cta_run - (unsigned)o.begin / cta_run + 1;
+        int* count = wk.count + ((size_t)o.row * c.Hkv + o.head) * wk.blocks + o.block;
+        __threadfence();  // (the other threads' stores are ordered in front of it by the barrier)
+        s_last[threadIdx.x] = atomicAdd(count, 1) == ctas - 1;
+        if (s_last[threadIdx.x]) *count = 0;
+        __threadfence();
+      }
+      __syncthreads();
+      todo = (parts & 1 && s_last[0] ? 1 : 0) | (parts & 2 && s_last[1] ? 2 : 0);
+      continue;
+    }
+    const int w = __ffs(todo) - 1;
+    todo &= todo - 1;
+    const PdOpen o = others ? s_part[w] : s_open[w];
+    const int end = o.begin + o.tiles;
+    const bool begins = o.begin >= c0, ends = end <= c1;
+    // piece 0, pieces 1 to n - 2 at equal distances behind `base`, piece n - 1
+    const float *p0, *base, *pn;
+    size_t stride;
+    int pieces;
+    if (others) {
+      const int first = (unsigned)o.begin / cta_run;
+      pieces = (unsigned)(end - 1) / cta_run - first + 1;
+      stride = 2 * wk.stride;
+      base = wk.part + first * stride;
+      p0 = base + wk.stride;
+      pn = base + (pieces - 1) * stride;
+    } else {
+      const int from = w == W ? 0 : w, to = w == W ? 0 : (int)((unsigned)(min(end, c1) - 1 - c0) / (unsigned)per);
+      pieces = to - from + 1;
+      stride = Sh::kWarpSmem / 4;
+      p0 = base = reinterpret_cast<const float*>(dsm + from * Sh::kWarpSmem);
+      pn = ends ? wk.lead + ((size_t)blockIdx.x * W + to) * wk.stride : base + (pieces - 1) * stride;
+    }
+    // their sums, brought to the largest reference: the heads' in top and tot, the warp's slices' in got
+    float top[NT][2], tot[NT][2];
+    float4 got[kSlices];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) top[nt][0] = top[nt][1] = -INFINITY, tot[nt][0] = tot[nt][1] = 0.f;
+#pragma unroll
+    for (int k = 0; k < kSlices; ++k) got[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+    constexpr int kBatch = kSlices > 2 ? 2 : 4;
+#pragma unroll 1
+    for (int i0 = 0; i0 < pieces; i0 += kBatch) {
+      float2 m[kBatch][NT], s[kBatch][NT];
+      float4 z[kBatch][kSlices];
+#pragma unroll
+      for (int b = 0; b < kBatch; ++b) {
+        const int i = i0 + b;
+        const float* p = i >= pieces - 1 ? pn : i == 0 ? p0 : base + i * stride;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          m[b][nt] = *reinterpret_cast<const float2*>(p + nt * 8 + 2 * q4);
+          s[b][nt] = *reinterpret_cast<const float2*>(p + 16 + nt * 8 + 2 * q4);
+          if (i >= pieces) m[b][nt] = make_float2(-INFINITY, -INFINITY), s[b][nt] = make_float2(0.f, 0.f);
+        }
+#pragma unroll
+        for (int k = 0; k < kSlices; ++k) z[b][k] = reinterpret_cast<const float4*>(p + 32)[min(k * W + warp, NT * DT - 1) * 32 + lane];
+      }
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          float to = top[nt][e];
+#pragma unroll
+          for (int b = 0; b < kBatch; ++b) to = fmaxf(to, e ? m[b][nt].y : m[b][nt].x);
+          const float at = to == -INFINITY ? 0.f : to, by = pd_exp2(top[nt][e] - at);
+          top[nt][e] = to;
+          tot[nt][e] *= by;
+          float f[kBatch];
+#pragma unroll
+          for (int b = 0; b < kBatch; ++b) {
+            f[b] = pd_exp2((e ? m[b][nt].y : m[b][nt].x) - at);
+            tot[nt][e] += f[b] * (e ? s[b][nt].y : s[b][nt].x);
+          }
+#pragma unroll
+          for (int k = 0; k < kSlices; ++k) {
+            if ((k * W + warp) / DT != nt) continue;
+            float& g0 = e ? got[k].y : got[k].x;
+            float& g1 = e ? got[k].w : got[k].z;
+            g0 *= by;
+            g1 *= by;
+#pragma unroll
+            for (int b = 0; b < kBatch; ++b) {
+              if (i0 + b >= pieces) continue;  // (a repeated piece's sums may be infinite)
+              g0 += f[b] * (e ? z[b][k].y : z[b][k].x);
+              g1 += f[b] * (e ? z[b][k].w : z[b][k].z);
+            }
+          }
+        }
+      }
+    }
+    if (others || (begins && ends)) {
+      PdCursor u;
+      u.row = o.row;
+      u.head = o.head;
+      u.block = o.block;
+#pragma unroll
+      for (int k = 0; k < kSlices; ++k) {
+        if (k * W + warp >= NT * DT) continue;
+        const bool upper = NT == 2 && (k * W + warp) / DT == 1;
+        const float b0 = scale_of(u, upper ? tot[NT - 1][0] : tot[0][0]), b1 = scale_of(u, upper ? tot[NT - 1][1] : tot[0][1]);
+        const float z[4] = {got[k].x * b0, got[k].y * b1, got[k].z * b0, got[k].w * b1};
+        put_slice(u, upper ? 1 : 0, (k * W + warp) % DT, z);
+      }
+      if (warp == 0)
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          put_lse(u, nt, 0, top[nt][0], tot[nt][0]);
+          put_lse(u, nt, 1, top[nt][1], tot[nt][1]);
+        }
+      continue;
+    }
+    parts |= begins ? 2 : 1;
+    if (threadIdx.x == 0) s_part[begins ? 1 : 0] = o;
+    float* part = wk.part + (size_t)(2 * blockIdx.x + (begins ? 1 : 0)) * wk.stride;
+    if (warp == 0 && g == 0)
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        *reinterpret_cast<float2*>(part + nt * 8 + 2 * q4) = make_float2(top[nt][0], top[nt][1]);
+        *reinterpret_cast<float2*>(part + 16 + nt * 8 + 2 * q4) = make_float2(tot[nt][0], tot[nt][1]);
+      }
+#pragma unroll
+    for (int k = 0; k < kSlices; ++k)
+      if (k * W + warp < NT * DT) reinterpret_cast<float4*>(part + 32)[(k * W + warp) * 32 + lane] = got[k];
   }
   // empty rows
   for (int row = blockIdx.x; row < r.n; row += gridDim.x) {
@@ -611,16 +737,17 @@ __global__ void __launch_bounds__(PdShape<KIND, D>::kWarps * 32, 1)
 // weights[j] = decay * weights[j] + sum over the group's heads of 2^(x_j - L), from the logits that the attention left.
 constexpr int kPwThreads = 256;
 __global__ void __launch_bounds__(kPwThreads) k_paged_weights(PagedCache c, PagedRows r, int layer, PdWork wk) {
-  chain_wait();
+  // (the lengths are older than the attention kernel, which has waited for its predecessor before it released this one)
   PdCursor u;
-  long long total;
-  const long long per = pd_deal<kPwThreads>(u, total, c, r, 1), t0 = blockIdx.x * per;
+  int total;
+  const int per = pd_deal<kPwThreads>(u, total, gridDim.x, blockIdx.x, c, r, 1), t0 = blockIdx.x * per;
   const int row = wk.blocks * wk.heads;
-  for (long long t = t0; t < t0 + per && t < total; ++t) {
+  chain_wait();
+  for (int t = t0; t < min(t0 + per, total); ++t) {
     const int slot = u.tile * kPwThreads + threadIdx.x;
-    const int page = slot < u.n ? paged_page(c, r, u.row, slot / c.P) : -1;
+    const int nth = paged_nth(c, slot), page = slot < u.n ? paged_page(c, r, u.row, nth) : -1;
     if (page >= 0) {
-      const size_t word = ((size_t)page * c.Hkv + u.head) * c.P + slot % c.P;
+      const size_t word = ((size_t)page * c.Hkv + u.head) * c.P + (slot - nth * c.P);
       const float* x = wk.logits + word * row;
       const float* l2 = wk.lse2 + (size_t)u.row * c.Hq + (size_t)u.head * c.G;
       float p = 0.f;
@@ -673,13 +800,13 @@ PagedBlocks paged_blocks(int group) {
   b.count = (group + b.heads - 1) / b.heads;
   return b;
 }
-size_t paged_part_floats(int head_dim) { return 32 + (size_t)16 * head_dim; }
+size_t paged_part_floats(int group, int head_dim) { return 32 + (size_t)paged_blocks(group).heads * head_dim; }
 
 int paged_decode_kernels(const PagedCache& c) { return c.w ? 2 : 1; }
 
 cudaError_t launch_paged_decode(const PagedCache& c, const PagedRows& r, int layer, const PagedStep& a, cudaStream_t s) {
   const PagedBlocks b = paged_blocks(c.G);
-  const PdWork w{b.heads, b.count, c.part, (int)paged_part_floats(c.D), c.count, c.logits, c.lse2};
+  const PdWork w{b.heads, b.count, c.part, c.lead, (int)paged_part_floats(c.G, c.D), c.count, c.logits, c.lse2};
   cudaError_t e;
   if (c.cache_type == LTRI_TYPE_E4M3) e = launch_kind<kPdE4m3>(c, r, layer, a, w, c.sms, s);
   else if (c.type == LTRI_TYPE_BF16) e = launch_kind<kPdBf16>(c, r, layer, a, w, c.sms, s);

@@ -55,7 +55,7 @@ __global__ void __launch_bounds__(kEvThreads) k_paged_evict(PagedCache c, PagedR
   if (n <= budget) return;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid / 32;
   auto word = [&](int slot) -> long long {  // -1: no page
-    const int page = paged_page(c, r, row, slot / c.P);
+    const int page = paged_page(c, r, row, paged_nth(c, slot));
     return page < 0 ? -1 : (long long)paged_word(c, layer, page, head, slot % c.P);
   };
   if (tid == 0) s_newest = INT_MIN, s_prefix = 0, s_need = budget;
@@ -124,7 +124,7 @@ __global__ void __launch_bounds__(kEvThreads) k_paged_evict(PagedCache c, PagedR
     const long long a0 = word(i), a1 = word(budget + i);
     if (a0 < 0 || a1 < 0) continue;
     const int src = c.list[a0], dst = c.list[a1];
-    const int sp = paged_page(c, r, row, src / c.P), dp = paged_page(c, r, row, dst / c.P);
+    const int sp = paged_page(c, r, row, paged_nth(c, src)), dp = paged_page(c, r, row, paged_nth(c, dst));
     if (sp < 0 || dp < 0) continue;
     const size_t from = paged_row(c, layer, sp, head, src % c.P), to = paged_row(c, layer, dp, head, dst % c.P);
     for (int b = lane * 16; b < 2 * c.row_bytes; b += 512) {

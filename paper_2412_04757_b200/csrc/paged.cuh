@@ -13,9 +13,11 @@ namespace ltri {
 // Device-side view of one handle.  Passed to kernels by value.
 struct PagedCache {
   int Hq, Hkv, G, D, P;
+  unsigned p_mul;               // slot / P = slot * p_mul >> p_shift for slots below 2^31: p_mul = floor(2^p_shift / P) + 1 with
+  int p_shift;                  // p_shift = 31 + ceil(log2 P), so that slot * (p_mul * P - 2^p_shift) < 2^p_shift
   int type, cache_type;
   int row_bytes;                // bytes of a cached row
-  long long n_pages;
+  int n_pages;
   long long ls, ps, hs, ts;     // layer, page, head and place strides of the pages, bytes
   float scale;                  // softmax_scale * log2(e)
   float decay;
@@ -26,6 +28,7 @@ struct PagedCache {
   int* status;                  // [4]
   int* list;                    // [L][n_pages][Hkv][P]: an eviction's moves, in the words of the unit's own slots
   float* part;                  // [sms][2][paged_part_floats]: partial sums of units that several CTAs share
+  float* lead;                  // [sms][kPagedWarps][paged_part_floats]: of units that several warps share
   int* count;                   // [max_rows][Hkv][blocks of heads]: CTAs of the unit that have finished; zero between calls
   float* logits;                // [n_pages][Hkv][P][blocks of heads], with weights: a decode call's logits
   float* lse2;                  // [max_rows][Hq], with weights: their sums, log2
@@ -36,7 +39,7 @@ struct PagedCache {
 struct PagedRows {
   const int* table;
   long long table_stride;
-  int table_pages;
+  int cap;                      // slots that the table has columns for
   const int* lens;
   int n;
 };
@@ -63,7 +66,8 @@ struct PagedBlocks {
   int heads, count;
 };
 PagedBlocks paged_blocks(int group);
-size_t paged_part_floats(int head_dim);
+size_t paged_part_floats(int group, int head_dim);  // partial sums of one block
+constexpr int kPagedWarps = 8;                      // of an attention CTA, at most
 int paged_decode_kernels(const PagedCache& c);  // launches of a decode call
 
 cudaError_t prepare_paged();
@@ -73,22 +77,28 @@ cudaError_t launch_paged_evict(const PagedCache& c, const PagedRows& r, int laye
                                int budget, int n_sink, int recent, cudaStream_t s);
 
 #ifdef __CUDACC__
-__device__ __forceinline__ void paged_status(const PagedCache& c, int detail) {
+// (out of line: the checks are everywhere, and never taken)
+static __device__ __noinline__ void paged_status(const PagedCache& c, int detail) {
   if (atomicCAS(&c.status[0], 0, (int)LTRI_EDEVICE) == 0) c.status[1] = detail;
 }
 
 // Slots of row r: 0 (and the status word) where the length says more than the table can hold.
 __device__ __forceinline__ int paged_len(const PagedCache& c, const PagedRows& r, int row) {
   const int n = r.lens[row];
-  if (n >= 0 && n <= (long long)r.table_pages * c.P) return n;
+  if ((unsigned)n <= (unsigned)r.cap) return n;
   paged_status(c, row);
   return 0;
 }
 
-// Page of place `slot / P` of a row, or -1 (and the status word) where the table names none.
+// Which of its row's pages a slot lies in.
+__device__ __forceinline__ int paged_nth(const PagedCache& c, int slot) {
+  return (int)(((unsigned long long)(unsigned)slot * c.p_mul) >> c.p_shift);
+}
+
+// The nth page of a row, or -1 (and the status word) where the table names none.
 __device__ __forceinline__ int paged_page(const PagedCache& c, const PagedRows& r, int row, int nth) {
   const int page = r.table[row * r.table_stride + nth];
-  if (page >= 0 && page < c.n_pages) return page;
+  if ((unsigned)page < (unsigned)c.n_pages) return page;
   paged_status(c, row);
   return -1;
 }
@@ -99,7 +109,7 @@ __device__ __forceinline__ size_t paged_word(const PagedCache& c, int layer, int
 }
 
 __device__ __forceinline__ size_t paged_row(const PagedCache& c, int layer, int page, int head, int place) {
-  return layer * c.ls + page * c.ps + head * c.hs + place * c.ts;
+  return layer * c.ls + page * c.ps + head * c.hs + place * c.ts;  // (the strides are 64-bit)
 }
 
 // Two fp32 values as elements of `type`, the first in the lower half.

@@ -10,6 +10,7 @@ struct ltri_paged {
   ltri_paged_params p;
   PagedCache c;
   int device = 0;
+  int blocks = 1;  // of a KV head's query heads
   int last_cuda = 0;
   int64_t launches = 0;
 };
@@ -55,7 +56,8 @@ size_t layout(const ltri_paged_params& p, int sms, PagedCache* c, unsigned char*
   unsigned char* status = take(256);
   unsigned char* count = take((size_t)p.max_rows * p.n_kv_heads * b.count * sizeof(int));
   if (zeroed) *zeroed = off;
-  unsigned char* part = take((size_t)sms * 2 * paged_part_floats(p.head_dim) * sizeof(float));
+  const size_t part_bytes = paged_part_floats(p.n_q_heads / p.n_kv_heads, p.head_dim) * sizeof(float);
+  unsigned char *part = take(sms * 2 * part_bytes), *lead = take(sms * kPagedWarps * part_bytes);
   unsigned char *list = nullptr, *logits = nullptr, *lse2 = nullptr;
   if (p.weights) {
     list = take(p.n_layers * slots * sizeof(int));
@@ -66,6 +68,7 @@ size_t layout(const ltri_paged_params& p, int sms, PagedCache* c, unsigned char*
     c->status = reinterpret_cast<int*>(status);
     c->count = reinterpret_cast<int*>(count);
     c->part = reinterpret_cast<float*>(part);
+    c->lead = reinterpret_cast<float*>(lead);
     c->list = reinterpret_cast<int*>(list);
     c->logits = reinterpret_cast<float*>(logits);
     c->lse2 = reinterpret_cast<float*>(lse2);
@@ -106,7 +109,10 @@ int check_rows(const ltri_paged* c, const int32_t* table, int table_pages, int64
   if (!aligned(table, 4) || !aligned(lens, 4) || n_rows < 1 || table_pages < 1) return LTRI_EINVAL;
   if (table_stride < 0 || (n_rows > 1 && table_stride < table_pages)) return LTRI_EINVAL;
   if (n_rows > c->p.max_rows) return LTRI_ECAPACITY;
-  *r = PagedRows{table, table_stride, table_pages, lens, n_rows};
+  // the kernels count the 16-slot tiles of all rows in 32 bits
+  const int64_t cap = (int64_t)table_pages * c->p.page_tokens;
+  if (cap > 0x7fffffffll || (cap / 16 + 1) * n_rows > (1ll << 30) / ((int64_t)c->p.n_kv_heads * c->blocks)) return LTRI_ECAPACITY;
+  *r = PagedRows{table, table_stride, (int)cap, lens, n_rows};
   return LTRI_OK;
 }
 
@@ -139,6 +145,7 @@ int ltri_paged_create(const ltri_paged_params* p, void* cuda_stream, ltri_paged*
   ltri_paged* c = new (std::nothrow) ltri_paged();
   if (!c) return LTRI_ECAPACITY;
   c->p = *p;
+  c->blocks = paged_blocks(p->n_q_heads / p->n_kv_heads).count;
   PagedCache& d = c->c;
   d = PagedCache{};
   size_t zeroed = 0;
@@ -152,7 +159,11 @@ int ltri_paged_create(const ltri_paged_params* p, void* cuda_stream, ltri_paged*
   d.type = p->type;
   d.cache_type = p->cache_type;
   d.row_bytes = (int)(d.D * es);
-  d.n_pages = p->n_pages;
+  d.n_pages = (int)p->n_pages;
+  int log = 0;
+  while ((1 << log) < d.P) ++log;
+  d.p_shift = 31 + log;
+  d.p_mul = (unsigned)((1ull << d.p_shift) / d.P + 1);
   d.ls = p->layer_stride * es;
   d.ps = p->page_stride * es;
   d.hs = p->head_stride * es;
