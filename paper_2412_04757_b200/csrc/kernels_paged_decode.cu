@@ -10,7 +10,10 @@
 // warps share, the sums are joined when their CTA has finished its run, and of one that several CTAs share, the last CTA to
 // finish joins the others' sums, always in the order of the line.
 //
-// A warp has a ring of its own that cp.async fills several tiles ahead, across units.  Both products run on mma.sync with the
+// A warp has a ring of its own that cp.async fills several tiles of 16 slots ahead, across units.  (One bulk copy a row instead:
+// 341 us for 16 rows of 24576 slots, 254 so; a row's copy costs the copy unit some 15 cycles however short it is.)  A row's
+// 16-byte chunks are permuted by its number, so that eight rows' equal chunks fall into different banks.  (Rows 16 bytes further
+// apart than they are long, which needs no permutation: 279 us, the writes then straddle lines.)  Both products run on mma.sync with the
 // slots (or head_dim) as the 16 rows and the heads of the KV group as the 8 columns: S^T = K Q^T, O^T = V^T P^T, so that up to
 // eight heads fill the instruction exactly.  (tcgen05 takes 64 rows at least, and its operands come through descriptors of
 // whole tiles, which pages of any size are not.)
@@ -21,24 +24,26 @@ namespace ltri {
 
 enum { kPdBf16 = 0, kPdFp16 = 1, kPdE4m3 = 2 };  // what the pages hold
 
-template <int KIND, int D>
+template <int KIND, int D, int NT>
 struct PdShape {
   static constexpr int kRow = KIND == kPdE4m3 ? D : 2 * D;      // bytes of a cached row
-  static constexpr int kChunks = kRow / 16;
-  static constexpr int kWarps = D == 256 ? 4 : 8;
-  static constexpr int kMt = kRow >= 256 ? 1 : 256 / kRow;      // blocks of 16 slots in a tile: 8 KB of K and V rows or more
+  // Blocks of 16 slots in a tile: 8 KB of rows or more, since what a tile costs besides its rows (cursors, page numbers, the
+  // reference) took 8-bit rows in tiles of 16 slots to 1.4 times the instructions.
+  static constexpr int kMt = kRow >= 256 ? 1 : 256 / kRow;
   static constexpr int kTile = 16 * kMt;                        // slots
-  static constexpr int kRaw = 2 * kTile * kRow;                 // a stage: K rows, V rows, and
-  static constexpr int kStage = kRaw + 4 * D;                   // the new token's K and V rows as they come
+  static constexpr int kStage = 2 * kTile * kRow;               // K rows, V rows
+  static constexpr int kWarps = kRow == 512 ? 4 : 8;            // of a CTA, one CTA an SM
   static constexpr int kFit = (232448 - 2048) / (kWarps * (kStage + 8 * kTile));
   static constexpr int kStages = kFit > 8 ? 8 : kFit;
   static constexpr int kAhead = kStages - 1;                    // tiles that rows are on their way of
   static constexpr int kPages = 2 * kStages;                    // tiles whose page numbers are known or on their way
   static constexpr int kRing = kStages * kStage;                // of a warp
-  static constexpr int kWarpSmem = kRing + kPages * kTile * 4;
-  static constexpr int kSmem = kWarps * kWarpSmem;
+  static constexpr int kSmem = kWarps * (kRing + kPages * kTile * 4);
   static_assert(kStages >= 3, "two tiles on their way and one in use");
 };
+
+// Reference of sums that nothing has entered yet: below every logit, and finite.
+constexpr float kPdNone = -3.0e38f;
 
 struct PdWork {
   int heads;            // of a block: 8 or 16
@@ -84,11 +89,10 @@ __device__ __forceinline__ uint32_t pd_halves_hi(uint32_t x) {
   return y;
 }
 
-// Byte of 16-byte chunk `ch` of row `row` in a tile of rows of CHUNKS chunks: eight rows' equal chunks lie in different banks.
+// What a row's number does to the number of a chunk in it, for rows of CHUNKS chunks.
 template <int CHUNKS>
-__device__ __forceinline__ uint32_t pd_at(int row, int ch) {
-  const int x = CHUNKS >= 8 ? row & 7 : (row >> 1) & 3;
-  return row * (CHUNKS * 16) + ((ch ^ x) << 4);
+__device__ __forceinline__ constexpr int pd_swizzle(int row) {
+  return CHUNKS >= 8 ? row & 7 : (row >> 1) & 3;
 }
 
 // A place in the line of tiles.
@@ -162,10 +166,10 @@ struct PdOpen {
 };
 
 template <int KIND, int D, int NT>
-__global__ void __launch_bounds__(PdShape<KIND, D>::kWarps * 32, 1)
+__global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
     k_paged_decode(PagedCache c, PagedRows r, int layer, PagedStep a, PdWork wk) {
-  using Sh = PdShape<KIND, D>;
-  constexpr int W = Sh::kWarps, TILE = Sh::kTile, MT = Sh::kMt, S = Sh::kStages, RC = Sh::kChunks, DT = D / 16, H = 8 * NT;
+  using Sh = PdShape<KIND, D, NT>;
+  constexpr int W = Sh::kWarps, TILE = Sh::kTile, MT = Sh::kMt, S = Sh::kStages, DT = D / 16, H = 8 * NT;
   constexpr int kSlices = NT * DT / W > 0 ? NT * DT / W : 1;  // 16-row slices of the sums that a warp joins
   // Probabilities carry a factor 2^kOff that cancels in out and lse.  A half has 2^-24 as its smallest step: with the largest
   // probability at 2^10 a slot's contribution is still seen 2^-35 below it, so that 2^20 of them cannot lose 2^-14 of a sum.
@@ -178,10 +182,10 @@ __global__ void __launch_bounds__(PdShape<KIND, D>::kWarps * 32, 1)
   chain_wait();
   if (c.w) chain_release();  // the weights kernel may take its place beside this one; it waits for this one's end
   const int warp = threadIdx.x / 32, lane = threadIdx.x & 31, g = lane >> 2, q4 = lane & 3;
-  unsigned char* ring = dsm + warp * Sh::kWarpSmem;
-  int* s_pages = reinterpret_cast<int*>(ring + Sh::kRing);
+  unsigned char* ring = dsm + warp * Sh::kRing;
+  int* s_pages = reinterpret_cast<int*>(dsm + W * Sh::kRing) + warp * Sh::kPages * TILE;
   const uint32_t ring_s = smem_u32(ring), pages_s = smem_u32(s_pages);
-  const bool one_page = c.P % 16 == 0;  // of 16 slots
+  const bool one_page = c.P % 16 == 0;  // of a block of 16 slots
 
   PdCursor cu;
   int total;
@@ -202,50 +206,50 @@ __global__ void __launch_bounds__(PdShape<KIND, D>::kWarps * 32, 1)
       else s_pages[st * TILE + j] = -1;
     }
   };
-  const int in = lane % RC, lane_row = lane / RC;  // this lane's chunk, of rows lane_row, lane_row + 32 / RC, ...
-  const size_t lane_at = lane_row * c.ts + in * 16, step = (32 / RC) * c.ts;
-  auto issue = [&](const PdCursor& u, const int* s_page, uint32_t stage) {
-    const int slot0 = u.tile * TILE;
-    const int last = a.k ? u.n - 1 : -1;  // the new token's slot: its row comes from the caller
-#pragma unroll 1
+  // Rows of a tile on their way: this lane takes chunk `in` of rows lane_row, lane_row + kStep, ...
+  constexpr int RC = Sh::kRow / 16, kStep = 32 / RC;
+  const int in = lane % RC, lane_row = lane / RC;
+  const size_t lane_at = lane_row * c.ts + in * 16, step = kStep * c.ts;
+  const uint32_t lane_s = ring_s + lane_row * Sh::kRow + ((in ^ pd_swizzle<RC>(lane_row)) << 4);
+  const long long vk = c.v - c.k;
+  auto issue = [&](const PdCursor& u, const int* s_page, int st) {
+    // the new token's row comes from the caller (in 8 bits: later, when the tile is used), rows without a slot are zeros:
+    // their probability of zero meets their values
+    const int fresh = a.k && u.n - 1 - u.tile * TILE < TILE ? u.n - 1 - u.tile * TILE : -1;
+#pragma unroll
     for (int m = 0; m < MT; ++m) {
-      const int base = slot0 + m * 16;
-      int pg = s_page[m * 16 + (lane & 15)];
-      if ((unsigned)pg >= (unsigned)c.n_pages) {
-        if (base + (lane & 15) < u.n) paged_status(c, u.row);
-        pg = -1;
-      }
-      const uint32_t sk = stage + m * 16 * Sh::kRow, sv = sk + TILE * Sh::kRow;
-      if (one_page) {
-        const int page = __shfl_sync(0xffffffffu, pg, 0);  // (slot `base` has one, or the whole block has none)
-        const size_t from = page < 0 ? 0 : paged_row(c, layer, page, u.head, base - paged_nth(c, base) * c.P) + lane_at;
-        const int end = page < 0 ? 0 : u.n - base, not_this = last - base;
+      const int base = u.tile * TILE + m * 16, slot = base + (lane & 15);
+      const int page = s_page[m * 16 + (lane & 15)];
+      const bool in_page = (unsigned)page < (unsigned)c.n_pages;
+      const uint32_t sk = lane_s + st * Sh::kStage + m * 16 * Sh::kRow;
+      // (kStep is a power of two above lane_row: their bits, and their swizzles, combine by xor)
+      auto to = [&](int i) { return (sk ^ (pd_swizzle<RC>(i * kStep) << 4)) + i * (kStep * Sh::kRow); };
+      if (one_page && base + 16 <= u.n && (unsigned)(fresh - m * 16) >= 16u && __all_sync(0xffffffffu, in_page)) {
+        const unsigned char* from = c.k + paged_row(c, layer, page, u.head, base - paged_nth(c, base) * c.P) + lane_at;
 #pragma unroll
         for (int i = 0; i < RC / 2; ++i) {
-          const int row = i * (32 / RC) + lane_row;
-          const bool ok = row < end && row != not_this;
-          const size_t at = ok ? from + i * step : 0;
-          cp_async16(sk + pd_at<RC>(row, in), c.k + at, ok ? 16 : 0);
-          cp_async16(sv + pd_at<RC>(row, in), c.v + at, ok ? 16 : 0);
+          cp_async16(to(i), from, 16);
+          cp_async16(to(i) + TILE * Sh::kRow, from + vk, 16);
+          from += step;
         }
       } else {
-        const int slot = base + (lane & 15), place = slot - paged_nth(c, slot) * c.P;
-        const long long off = pg < 0 ? -1 : (long long)paged_row(c, layer, pg, u.head, place);
+        if (!in_page && slot < u.n) paged_status(c, u.row);
+        const long long off = in_page ? (long long)paged_row(c, layer, page, u.head, slot - paged_nth(c, slot) * c.P) : -1;
 #pragma unroll
         for (int i = 0; i < RC / 2; ++i) {
-          const int row = i * (32 / RC) + lane_row;
-          const long long o = shfl_ll(off, row);
-          const bool ok = o >= 0 && base + row != last;
-          const size_t at = ok ? (size_t)o + in * 16 : 0;
-          cp_async16(sk + pd_at<RC>(row, in), c.k + at, ok ? 16 : 0);
-          cp_async16(sv + pd_at<RC>(row, in), c.v + at, ok ? 16 : 0);
+          const long long o = shfl_ll(off, i * kStep + lane_row);
+          if (m * 16 + i * kStep + lane_row == fresh) continue;
+          const unsigned char* from = c.k + (o < 0 ? 0 : o + in * 16);
+          cp_async16(to(i), from, o < 0 ? 0 : 16);
+          cp_async16(to(i) + TILE * Sh::kRow, from + vk, o < 0 ? 0 : 16);
         }
       }
     }
-    if (last >= slot0 && last < slot0 + TILE && lane < D / 8) {
-      const size_t at = u.row * a.kv_stride + ((size_t)u.head * D + lane * 8) * 2;
-      cp_async16(stage + Sh::kRaw + lane * 16, a.k + at, 16);
-      cp_async16(stage + Sh::kRaw + 2 * D + lane * 16, a.v + at, 16);
+    if (KIND != kPdE4m3 && fresh >= 0 && lane < RC) {
+      const size_t at = u.row * a.kv_stride + (size_t)u.head * (2 * D) + lane * 16;
+      const uint32_t to = ring_s + st * Sh::kStage + fresh * Sh::kRow + ((lane ^ pd_swizzle<RC>(fresh)) << 4);
+      cp_async16(to, a.k + at, 16);
+      cp_async16(to + TILE * Sh::kRow, a.v + at, 16);
     }
   };
   // The queries of a unit as the products' columns (head g of each block), and the logits' factors.
@@ -345,42 +349,44 @@ __global__ void __launch_bounds__(PdShape<KIND, D>::kWarps * 32, 1)
       scale_queries(cu);
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
-        ref[nt][0] = ref[nt][1] = -INFINITY;
+        ref[nt][0] = ref[nt][1] = kPdNone;
         sum[nt][0] = sum[nt][1] = 0.f;
 #pragma unroll
         for (int i = 0; i < DT; ++i) O[nt][i][0] = O[nt][i][1] = O[nt][i][2] = O[nt][i][3] = 0.f;
       }
     }
+    const int slot0 = cu.tile * TILE;
+    const int fresh = a.k && cu.n - 1 - slot0 < TILE ? cu.n - 1 - slot0 : -1;
+    uint4 kx = make_uint4(0u, 0u, 0u, 0u), vx = kx;
+    if (KIND == kPdE4m3 && fresh >= 0 && lane < D / 8) {
+      const size_t at_new = cu.row * a.kv_stride + ((size_t)cu.head * D + lane * 8) * 2;
+      kx = *reinterpret_cast<const uint4*>(a.k + at_new);
+      vx = *reinterpret_cast<const uint4*>(a.v + at_new);
+    }
     cp_async_wait<S - 2>();
     __syncwarp();
-    const int slot0 = cu.tile * TILE;
     unsigned char* stage = ring + stage_at * Sh::kStage;
     const uint32_t sk = ring_s + stage_at * Sh::kStage, sv = sk + TILE * Sh::kRow;
     const int* s_page = s_pages + page_at * TILE;
-    const int fresh = a.k && cu.n - 1 - slot0 < TILE ? cu.n - 1 - slot0 : -1;
-    if (fresh >= 0 && (unsigned)s_page[fresh] < (unsigned)c.n_pages) {  // the new token's row into the tile and into its page
+    if (fresh >= 0 && (unsigned)s_page[fresh] < (unsigned)c.n_pages) {  // the new token's row into its page
       const int page = s_page[fresh], place = cu.n - 1 - paged_nth(c, cu.n - 1) * c.P;
+      const size_t to = paged_row(c, layer, page, cu.head, place);
+      unsigned char* in = stage + fresh * Sh::kRow;
+      const int sw = pd_swizzle<RC>(fresh);
       if (lane < D / 8) {
-        const uint4 kx = *reinterpret_cast<const uint4*>(stage + Sh::kRaw + lane * 16);
-        const uint4 vx = *reinterpret_cast<const uint4*>(stage + Sh::kRaw + 2 * D + lane * 16);
-        const size_t to = paged_row(c, layer, page, cu.head, place);
-        if (KIND == kPdE4m3) {
+        if (KIND == kPdE4m3) {  // and into the tile
           const uint2 ky = paged_quantise(c.type, kx, c.ks[cu.head]), vy = paged_quantise(c.type, vx, c.vs[cu.head]);
-          const uint32_t in = pd_at<RC>(fresh, lane / 2) + (lane & 1) * 8;
-          *reinterpret_cast<uint2*>(stage + in) = ky;
-          *reinterpret_cast<uint2*>(stage + TILE * Sh::kRow + in) = vy;
+          in += ((lane / 2 ^ sw) << 4) + (lane & 1) * 8;
+          *reinterpret_cast<uint2*>(in) = ky;
+          *reinterpret_cast<uint2*>(in + TILE * Sh::kRow) = vy;
           if (cu.block == 0) {
             *reinterpret_cast<uint2*>(c.k + to + lane * 8) = ky;
             *reinterpret_cast<uint2*>(c.v + to + lane * 8) = vy;
           }
-        } else {
-          const uint32_t in = pd_at<RC>(fresh, lane);
-          *reinterpret_cast<uint4*>(stage + in) = kx;
-          *reinterpret_cast<uint4*>(stage + TILE * Sh::kRow + in) = vx;
-          if (cu.block == 0) {
-            *reinterpret_cast<uint4*>(c.k + to + lane * 16) = kx;
-            *reinterpret_cast<uint4*>(c.v + to + lane * 16) = vx;
-          }
+        } else if (cu.block == 0) {
+          in += (lane ^ sw) << 4;
+          *reinterpret_cast<uint4*>(c.k + to + lane * 16) = *reinterpret_cast<const uint4*>(in);
+          *reinterpret_cast<uint4*>(c.v + to + lane * 16) = *reinterpret_cast<const uint4*>(in + TILE * Sh::kRow);
         }
       }
       if (c.w && cu.block == 0 && lane == 0) {
@@ -391,6 +397,8 @@ __global__ void __launch_bounds__(PdShape<KIND, D>::kWarps * 32, 1)
       __syncwarp();
     }
     float x[MT][NT][4];
+    // (a tile lies on a multiple of its rows' length: the chunk's bits of an address can be set by xor)
+    const uint32_t k_at = sk + (lane & 15) * Sh::kRow + ((lane >> 4 ^ pd_swizzle<RC>(lane & 15)) << 4);
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
 #pragma unroll
@@ -399,7 +407,7 @@ __global__ void __launch_bounds__(PdShape<KIND, D>::kWarps * 32, 1)
 #pragma unroll
         for (int i = 0; i < DT; i += 2) {
           uint32_t b[4];
-          ldsm_x4(b, sk + pd_at<RC>(m * 16 + (lane & 15), i + (lane >> 4)));
+          ldsm_x4(b, (k_at ^ (i << 4)) + m * 16 * Sh::kRow);
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
             const uint32_t f[4] = {pd_halves_lo(b[2 * j]), pd_halves_lo(b[2 * j + 1]), pd_halves_hi(b[2 * j]),
@@ -412,49 +420,63 @@ __global__ void __launch_bounds__(PdShape<KIND, D>::kWarps * 32, 1)
 #pragma unroll
         for (int i = 0; i < DT; ++i) {
           uint32_t f[4];
-          ldsm_x4(f, sk + pd_at<RC>(m * 16 + (lane & 15), 2 * i + (lane >> 4)));
+          ldsm_x4(f, (k_at ^ (i << 5)) + m * 16 * Sh::kRow);
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) pd_mma<KIND>(x[m][nt], f, qb[nt][i][0], qb[nt][i][1]);
         }
       }
     }
-    // lane: slots g and g + 8 of a block (x[..][0..1], x[..][2..3]), heads 2 q4 and 2 q4 + 1
-    bool grow = false;
+    // lane: slots g and g + 8 of a block (x[..][..][0..1], x[..][..][2..3]), heads 2 q4 and 2 q4 + 1
+    bool every = true;  // slot of the tile is there
 #pragma unroll
-    for (int m = 0; m < MT; ++m) {
-      const int p0 = s_page[m * 16 + g], p1 = s_page[m * 16 + g + 8];
+    for (int j = lane; j < TILE; j += 32) every &= (unsigned)s_page[j] < (unsigned)c.n_pages;
+    if (!__all_sync(0xffffffffu, every)) {
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          x[m][nt][e] = (unsigned)(e < 2 ? p0 : p1) < (unsigned)c.n_pages ? x[m][nt][e] * sc[nt][e & 1] : -INFINITY;
-          grow |= x[m][nt][e] > ref[nt][e & 1] + (kOff + kGrow);
-        }
-      if (c.w) {
+      for (int m = 0; m < MT; ++m)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          const int page = e ? p1 : p0;
+          const bool there = (unsigned)s_page[m * 16 + g + 8 * e] < (unsigned)c.n_pages;
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            // (the factors are positive; an infinite logit of a slot that is not there stays below every reference)
+            if (!there) x[m][nt][2 * e] = x[m][nt][2 * e + 1] = -INFINITY;
+          }
+        }
+    }
+    if (c.w) {
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int page = s_page[m * 16 + g + 8 * e];
           if ((unsigned)page >= (unsigned)c.n_pages) continue;
           const int slot = slot0 + m * 16 + g + 8 * e, place = slot - paged_nth(c, slot) * c.P;
           const size_t word = ((size_t)page * c.Hkv + cu.head) * c.P + place;
           float2* to = reinterpret_cast<float2*>(wk.logits + word * (wk.blocks * H) + cu.block * H);
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt) to[nt * 4 + q4] = make_float2(x[m][nt][2 * e], x[m][nt][2 * e + 1]);
+          for (int nt = 0; nt < NT; ++nt) to[nt * 4 + q4] = make_float2(x[m][nt][2 * e] * sc[nt][0], x[m][nt][2 * e + 1] * sc[nt][1]);
         }
-      }
     }
+    bool grow = false;
+    float top[NT][2];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        float most = fmaxf(x[0][nt][e], x[0][nt][e + 2]);
+#pragma unroll
+        for (int m = 1; m < MT; ++m) most = fmaxf(most, fmaxf(x[m][nt][e], x[m][nt][e + 2]));
+        top[nt][e] = most * sc[nt][e];
+        grow |= top[nt][e] > ref[nt][e] + (kOff + kGrow);
+      }
     if (__any_sync(0xffffffffu, grow)) {
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          float top = fmaxf(x[0][nt][e], x[0][nt][e + 2]);
 #pragma unroll
-          for (int m = 1; m < MT; ++m) top = fmaxf(top, fmaxf(x[m][nt][e], x[m][nt][e + 2]));
-#pragma unroll
-          for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-          const float to = fmaxf(ref[nt][e], top - kOff);
-          const float by = to == -INFINITY ? 1.f : pd_exp2(ref[nt][e] - to);
+          for (int d = 4; d < 32; d <<= 1) top[nt][e] = fmaxf(top[nt][e], __shfl_xor_sync(0xffffffffu, top[nt][e], d));
+          const float to = fmaxf(ref[nt][e], top[nt][e] - kOff), by = pd_exp2(ref[nt][e] - to);
           ref[nt][e] = to;
           sum[nt][e] *= by;
 #pragma unroll
@@ -473,8 +495,7 @@ __global__ void __launch_bounds__(PdShape<KIND, D>::kWarps * 32, 1)
         float p[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const float to = ref[nt][e & 1];
-          p[e] = pd_exp2(x[m][nt][e] - (to == -INFINITY ? 0.f : to));
+          p[e] = pd_exp2(fmaf(x[m][nt][e], sc[nt][e & 1], -ref[nt][e & 1]));
           sum[nt][e & 1] += p[e];
         }
         constexpr int T = KIND == kPdBf16 ? LTRI_TYPE_BF16 : LTRI_TYPE_FP16;
@@ -486,22 +507,25 @@ __global__ void __launch_bounds__(PdShape<KIND, D>::kWarps * 32, 1)
           lo[m][nt][e] = pd_transpose(paged_pack(T, p[2 * e] - back.x, p[2 * e + 1] - back.y));
         }
       }
+    const int v_row = KIND == kPdE4m3 ? lane & 15 : (lane & 7) + (lane >> 4) * 8, v_ch = KIND == kPdE4m3 ? lane >> 4 : (lane >> 3) & 1;
+    const uint32_t v_at = sv + v_row * Sh::kRow + ((v_ch ^ pd_swizzle<RC>(v_row)) << 4);
 #pragma unroll
-    for (int m = 0; m < MT; ++m) {
+    for (int m = 0; m < MT; ++m)
 #pragma unroll
       for (int i = 0; i < DT; i += KIND == kPdE4m3 ? 2 : 1) {
         uint32_t b[4];
         if (KIND == kPdE4m3) {
-          // a 16-byte chunk's 8 pairs of neighbours are the 8 rows of a transposed matrix: row g has elements 2g and 2g + 1
-          ldsm_x4_t(b, sv + pd_at<RC>(m * 16 + (lane & 15), i + (lane >> 4)));
+          // a 16-byte chunk's 8 pairs of neighbours are the 8 rows of a transposed matrix: row g has elements 2g and 2g + 1 of
+          // slots 2 q4 and 2 q4 + 1
+          ldsm_x4_t(b, (v_at ^ (i << 4)) + m * 16 * Sh::kRow);
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
             uint32_t f[4];
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {  // slots 2 q4, 2 q4 + 1 and, with e, 8 further
-              const uint32_t l = pd_halves_lo(b[2 * j + e]), h = pd_halves_hi(b[2 * j + e]);
-              f[2 * e] = __byte_perm(l, h, 0x5410);
-              f[2 * e + 1] = __byte_perm(l, h, 0x7632);
+            for (int e = 0; e < 2; ++e) {  // (with e, 8 slots further)
+              const uint32_t y = __byte_perm(b[2 * j + e], 0u, 0x3120);
+              f[2 * e] = pd_halves_lo(y);
+              f[2 * e + 1] = pd_halves_hi(y);
             }
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
@@ -510,7 +534,7 @@ __global__ void __launch_bounds__(PdShape<KIND, D>::kWarps * 32, 1)
             }
           }
         } else {
-          ldsm_x4_t(b, sv + pd_at<RC>(m * 16 + (lane & 7) + (lane >> 4) * 8, 2 * i + ((lane >> 3) & 1)));
+          ldsm_x4_t(b, (v_at ^ (i << 5)) + m * 16 * Sh::kRow);
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) {
             pd_mma<KIND>(O[nt][i], b, hi[m][nt][0], hi[m][nt][1]);
@@ -518,7 +542,6 @@ __global__ void __launch_bounds__(PdShape<KIND, D>::kWarps * 32, 1)
           }
         }
       }
-    }
     __syncwarp();
     stage_at = next(stage_at, S);
     page_at = next(page_at, Sh::kPages);
@@ -564,7 +587,7 @@ __global__ void __launch_bounds__(PdShape<KIND, D>::kWarps * 32, 1)
     pd_advance<TILE>(cu, c, r, wk.blocks);
     }
     if (at >= -Sh::kAhead && at + Sh::kAhead < mine) {
-      issue(ci, s_pages + page_in * TILE, ring_s + stage_in * Sh::kStage);
+      issue(ci, s_pages + page_in * TILE, stage_in);
       stage_in = next(stage_in, S);
       page_in = next(page_in, Sh::kPages);
       pd_advance<TILE>(ci, c, r, wk.blocks);
@@ -628,15 +651,15 @@ __global__ void __launch_bounds__(PdShape<KIND, D>::kWarps * 32, 1)
     } else {
       const int from = w == W ? 0 : w, to = w == W ? 0 : (int)((unsigned)(min(end, c1) - 1 - c0) / (unsigned)per);
       pieces = to - from + 1;
-      stride = Sh::kWarpSmem / 4;
-      p0 = base = reinterpret_cast<const float*>(dsm + from * Sh::kWarpSmem);
+      stride = Sh::kRing / 4;
+      p0 = base = reinterpret_cast<const float*>(dsm + from * Sh::kRing);
       pn = ends ? wk.lead + ((size_t)blockIdx.x * W + to) * wk.stride : base + (pieces - 1) * stride;
     }
     // their sums, brought to the largest reference: the heads' in top and tot, the warp's slices' in got
     float top[NT][2], tot[NT][2];
     float4 got[kSlices];
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) top[nt][0] = top[nt][1] = -INFINITY, tot[nt][0] = tot[nt][1] = 0.f;
+    for (int nt = 0; nt < NT; ++nt) top[nt][0] = top[nt][1] = kPdNone, tot[nt][0] = tot[nt][1] = 0.f;
 #pragma unroll
     for (int k = 0; k < kSlices; ++k) got[k] = make_float4(0.f, 0.f, 0.f, 0.f);
     constexpr int kBatch = kSlices > 2 ? 2 : 4;
@@ -652,7 +675,7 @@ __global__ void __launch_bounds__(PdShape<KIND, D>::kWarps * 32, 1)
         for (int nt = 0; nt < NT; ++nt) {
           m[b][nt] = *reinterpret_cast<const float2*>(p + nt * 8 + 2 * q4);
           s[b][nt] = *reinterpret_cast<const float2*>(p + 16 + nt * 8 + 2 * q4);
-          if (i >= pieces) m[b][nt] = make_float2(-INFINITY, -INFINITY), s[b][nt] = make_float2(0.f, 0.f);
+          if (i >= pieces) m[b][nt] = make_float2(kPdNone, kPdNone), s[b][nt] = make_float2(0.f, 0.f);
         }
 #pragma unroll
         for (int k = 0; k < kSlices; ++k) z[b][k] = reinterpret_cast<const float4*>(p + 32)[min(k * W + warp, NT * DT - 1) * 32 + lane];
@@ -664,13 +687,13 @@ __global__ void __launch_bounds__(PdShape<KIND, D>::kWarps * 32, 1)
           float to = top[nt][e];
 #pragma unroll
           for (int b = 0; b < kBatch; ++b) to = fmaxf(to, e ? m[b][nt].y : m[b][nt].x);
-          const float at = to == -INFINITY ? 0.f : to, by = pd_exp2(top[nt][e] - at);
+          const float by = pd_exp2(top[nt][e] - to);
           top[nt][e] = to;
           tot[nt][e] *= by;
           float f[kBatch];
 #pragma unroll
           for (int b = 0; b < kBatch; ++b) {
-            f[b] = pd_exp2((e ? m[b][nt].y : m[b][nt].x) - at);
+            f[b] = pd_exp2((e ? m[b][nt].y : m[b][nt].x) - to);
             tot[nt][e] += f[b] * (e ? s[b][nt].y : s[b][nt].x);
           }
 #pragma unroll
@@ -763,7 +786,7 @@ namespace {
 
 template <int KIND, int D, int NT>
 cudaError_t prepare_one() {
-  return allow_smem(k_paged_decode<KIND, D, NT>, PdShape<KIND, D>::kSmem);
+  return allow_smem(k_paged_decode<KIND, D, NT>, PdShape<KIND, D, NT>::kSmem);
 }
 template <int KIND, int D>
 cudaError_t prepare_dim() {
@@ -774,18 +797,21 @@ cudaError_t prepare_kind() {
   return first_error(prepare_dim<KIND, 64>(), first_error(prepare_dim<KIND, 128>(), prepare_dim<KIND, 256>()));
 }
 
+template <int KIND, int D, int NT>
+cudaError_t launch_one(const PagedCache& c, const PagedRows& r, int layer, const PagedStep& a, const PdWork& w, cudaStream_t s) {
+  using Sh = PdShape<KIND, D, NT>;
+  static_assert(Sh::kWarps <= kPagedWarps, "the workspace has partial sums of that many warps");
+  return launch_chained(k_paged_decode<KIND, D, NT>, dim3(c.sms), dim3(Sh::kWarps * 32), Sh::kSmem, s, c, r, layer, a, w);
+}
 template <int KIND, int D>
-cudaError_t launch_dim(const PagedCache& c, const PagedRows& r, int layer, const PagedStep& a, const PdWork& w, int grid, cudaStream_t s) {
-  using Sh = PdShape<KIND, D>;
-  if (w.heads == 8)
-    return launch_chained(k_paged_decode<KIND, D, 1>, dim3(grid), dim3(Sh::kWarps * 32), Sh::kSmem, s, c, r, layer, a, w);
-  return launch_chained(k_paged_decode<KIND, D, 2>, dim3(grid), dim3(Sh::kWarps * 32), Sh::kSmem, s, c, r, layer, a, w);
+cudaError_t launch_dim(const PagedCache& c, const PagedRows& r, int layer, const PagedStep& a, const PdWork& w, cudaStream_t s) {
+  return w.heads == 8 ? launch_one<KIND, D, 1>(c, r, layer, a, w, s) : launch_one<KIND, D, 2>(c, r, layer, a, w, s);
 }
 template <int KIND>
-cudaError_t launch_kind(const PagedCache& c, const PagedRows& r, int layer, const PagedStep& a, const PdWork& w, int grid, cudaStream_t s) {
-  if (c.D == 64) return launch_dim<KIND, 64>(c, r, layer, a, w, grid, s);
-  if (c.D == 128) return launch_dim<KIND, 128>(c, r, layer, a, w, grid, s);
-  return launch_dim<KIND, 256>(c, r, layer, a, w, grid, s);
+cudaError_t launch_kind(const PagedCache& c, const PagedRows& r, int layer, const PagedStep& a, const PdWork& w, cudaStream_t s) {
+  if (c.D == 64) return launch_dim<KIND, 64>(c, r, layer, a, w, s);
+  if (c.D == 128) return launch_dim<KIND, 128>(c, r, layer, a, w, s);
+  return launch_dim<KIND, 256>(c, r, layer, a, w, s);
 }
 
 }  // namespace
@@ -808,9 +834,9 @@ cudaError_t launch_paged_decode(const PagedCache& c, const PagedRows& r, int lay
   const PagedBlocks b = paged_blocks(c.G);
   const PdWork w{b.heads, b.count, c.part, c.lead, (int)paged_part_floats(c.G, c.D), c.count, c.logits, c.lse2};
   cudaError_t e;
-  if (c.cache_type == LTRI_TYPE_E4M3) e = launch_kind<kPdE4m3>(c, r, layer, a, w, c.sms, s);
-  else if (c.type == LTRI_TYPE_BF16) e = launch_kind<kPdBf16>(c, r, layer, a, w, c.sms, s);
-  else e = launch_kind<kPdFp16>(c, r, layer, a, w, c.sms, s);
+  if (c.cache_type == LTRI_TYPE_E4M3) e = launch_kind<kPdE4m3>(c, r, layer, a, w, s);
+  else if (c.type == LTRI_TYPE_BF16) e = launch_kind<kPdBf16>(c, r, layer, a, w, s);
+  else e = launch_kind<kPdFp16>(c, r, layer, a, w, s);
   if (e != cudaSuccess || !c.w) return e;
   return launch_chained(k_paged_weights, dim3(c.sms * 4), dim3(kPwThreads), 0, s, c, r, layer, w);
 }

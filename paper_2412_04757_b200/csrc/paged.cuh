@@ -67,7 +67,7 @@ struct PagedBlocks {
 };
 PagedBlocks paged_blocks(int group);
 size_t paged_part_floats(int group, int head_dim);  // partial sums of one block
-constexpr int kPagedWarps = 8;                      // of an attention CTA, at most
+constexpr int kPagedWarps = 16;                     // of an attention CTA, at most
 int paged_decode_kernels(const PagedCache& c);  // launches of a decode call
 
 cudaError_t prepare_paged();
