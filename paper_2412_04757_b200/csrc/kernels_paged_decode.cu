@@ -72,6 +72,13 @@ __device__ __forceinline__ void mma_fp16(float (&c)[4], const uint32_t (&a)[4], 
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+// Adds one; what this thread has seen or written is visible to whoever finds it added.  (With __threadfence on either side, which
+// orders more than that, the step took 3000 cycles.)
+__device__ __forceinline__ int pd_arrive(int* count) {
+  int before;
+  asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(before) : "l"(count) : "memory");
+  return before;
+}
 template <int KIND>
 __device__ __forceinline__ void pd_mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
   if (KIND == kPdBf16) mma_bf16(c, a, b0, b1);
@@ -159,7 +166,7 @@ __device__ __forceinline__ int pd_deal(PdCursor& u, int& total, int runs, int ru
   }
 }
 
-// A unit that a warp's run leaves unfinished, or (the last entry) that ends in the CTA's first run but began in another CTA.
+// A unit that a warp's run, or a CTA's, leaves unfinished.
 struct PdOpen {
   int begin;                    // in the line
   int row, head, block, tiles;  // tiles 0: none
@@ -176,7 +183,7 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
   // The reference moves only when a logit exceeds it by kGrow, which bounds the probabilities by 2^(kOff + kGrow).
   constexpr float kOff = KIND == kPdBf16 ? 0.f : 10.f, kGrow = 4.f;
   extern __shared__ __align__(1024) unsigned char dsm[];
-  __shared__ PdOpen s_open[W + 1];
+  __shared__ PdOpen s_open[W];
   __shared__ PdOpen s_part[2];
   __shared__ int s_last[2];
   chain_wait();
@@ -194,7 +201,7 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
   const int t0 = c0 + warp * per, mine = max(0, min(per, total - t0));
   if (lane == 0) {
     s_open[warp].tiles = 0;
-    if (warp == 0) s_open[W].tiles = 0;
+    if (warp == 0) s_part[0].tiles = s_part[1].tiles = 0;
   }
 
   // Page numbers of a tile's slots on their way into entry `st` (-1 behind the row's end).
@@ -252,10 +259,19 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
       cp_async16(to + TILE * Sh::kRow, a.v + at, 16);
     }
   };
-  // The queries of a unit as the products' columns (head g of each block), and the logits' factors.
-  uint32_t qb[NT][DT][2];
-  float sc[NT][2];
-  auto load_queries = [&](const PdCursor& u) {
+  // The queries of a unit as the products' columns (head g of each block), and the scales of its KV head.  Behind the requests of
+  // rows that fill the memory's queues a load takes 3000 cycles, so where there are registers the next unit's are asked for when
+  // the first of its rows are.
+  constexpr bool kEarly = NT * D <= 128;
+  struct Queries {
+    uint32_t b[NT][DT][2];
+    float ks, vs;
+  };
+  Queries q, q_next;
+  int next_at = -(1 << 30);  // the tile of the run that q_next's unit begins with
+  auto load_queries = [&](Queries& x, const PdCursor& u) {
+    x.ks = c.ks ? c.ks[u.head] : 1.f;
+    x.vs = c.vs ? c.vs[u.head] : 1.f;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       const int in_group = u.block * H + nt * 8 + g;
@@ -266,13 +282,13 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           const int el = KIND == kPdE4m3 ? i * 16 + q4 * 4 + 2 * j : i * 16 + q4 * 2 + 8 * j;
-          qb[nt][i][j] = in_group < c.G ? *reinterpret_cast<const uint32_t*>(qr + el * 2) : 0u;
+          x.b[nt][i][j] = in_group < c.G ? *reinterpret_cast<const uint32_t*>(qr + el * 2) : 0u;
         }
       }
     }
   };
-  auto scale_queries = [&](const PdCursor& u) {
-    const float ks = c.ks ? c.ks[u.head] : 1.f;
+  float sc[NT][2];  // logits' factors of this lane's heads
+  auto scale_queries = [&]() {
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       float back = 1.f;
@@ -283,25 +299,25 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
 #pragma unroll
         for (int i = 0; i < DT; ++i)
 #pragma unroll
-          for (int j = 0; j < 2; ++j) most = max(most, max(qb[nt][i][j] & 0x7fffu, (qb[nt][i][j] >> 16) & 0x7fffu));
+          for (int j = 0; j < 2; ++j) most = max(most, max(q.b[nt][i][j] & 0x7fffu, (q.b[nt][i][j] >> 16) & 0x7fffu));
         most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
         most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
         const int ex = (int)(most >> 7);  // biased exponent
         const int up = ex == 0 || ex == 255 ? 0 : 127 + 14 - ex;
         // (2^up may lie outside fp32's range: two factors)
-        const float u0 = ldexpf(1.f, up / 2), u1 = ldexpf(1.f, up - up / 2);
+        const float u0 = __int_as_float((127 + up / 2) << 23), u1 = __int_as_float((127 + up - up / 2) << 23);
 #pragma unroll
         for (int i = 0; i < DT; ++i)
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
-            const float2 f = paged_unpack(LTRI_TYPE_BF16, qb[nt][i][j]);
-            qb[nt][i][j] = paged_pack(LTRI_TYPE_FP16, f.x * u0 * u1, f.y * u0 * u1);
+            const float2 f = paged_unpack(LTRI_TYPE_BF16, q.b[nt][i][j]);
+            q.b[nt][i][j] = paged_pack(LTRI_TYPE_FP16, f.x * u0 * u1, f.y * u0 * u1);
           }
-        back = ldexpf(1.f, -up);
+        back = __int_as_float((127 - up / 2) << 23) * __int_as_float((127 - up + up / 2) << 23);
       }
       // (the queries lie with head g, the logits with heads 2 q4 and 2 q4 + 1)
 #pragma unroll
-      for (int e = 0; e < 2; ++e) sc[nt][e] = c.scale * ks * __shfl_sync(0xffffffffu, back, (2 * q4 + e) * 4);
+      for (int e = 0; e < 2; ++e) sc[nt][e] = c.scale * q.ks * __shfl_sync(0xffffffffu, back, (2 * q4 + e) * 4);
     }
   };
   // A slice of 16 elements of the eight heads of block nt, normalised, to the output.
@@ -326,9 +342,37 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
     if (a.lse) a.lse[at] = l2 * 0.69314718055994531f;
     if (c.w) wk.lse2[at] = l2;
   };
-  auto scale_of = [&](const PdCursor& u, float sum) { return sum == 0.f ? 0.f : (c.vs ? c.vs[u.head] : 1.f) / sum; };
+  auto scale_of = [](float vs, float sum) { return sum == 0.f ? 0.f : vs / sum; };
 
   float O[NT][DT][4], ref[NT][2], sum[NT][2];
+  // A unit's heads, all of whose sums this warp has.
+  auto put_unit = [&](const PdCursor& u) {
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const float by[2] = {scale_of(q.vs, sum[nt][0]), scale_of(q.vs, sum[nt][1])};
+#pragma unroll
+      for (int i = 0; i < DT; ++i) {
+        const float z[4] = {O[nt][i][0] * by[0], O[nt][i][1] * by[1], O[nt][i][2] * by[0], O[nt][i][3] * by[1]};
+        put_slice(u, nt, i, z);
+      }
+      put_lse(u, nt, 0, ref[nt][0], sum[nt][0]);
+      put_lse(u, nt, 1, ref[nt][1], sum[nt][1]);
+    }
+  };
+  // This warp's sums to memory.
+  auto set_aside = [&](float* to) {
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      if (g == 0) {
+        *reinterpret_cast<float2*>(to + nt * 8 + 2 * q4) = make_float2(ref[nt][0], ref[nt][1]);
+        *reinterpret_cast<float2*>(to + 16 + nt * 8 + 2 * q4) = make_float2(sum[nt][0], sum[nt][1]);
+      }
+#pragma unroll
+      for (int i = 0; i < DT; ++i)
+        reinterpret_cast<float4*>(to + 32)[(nt * DT + i) * 32 + lane] =
+            make_float4(O[nt][i][0], O[nt][i][1], O[nt][i][2], O[nt][i][3]);
+    }
+  };
   bool whole = false;   // the unit has begun in this run
   // Rounds: in round `at` tile `at` is used, the rows of tile at + kAhead are requested and the page numbers of tile
   // at + 2 kAhead.  A round's requests are one group, complete when the round kAhead later begins; only the first tiles' page
@@ -346,7 +390,8 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
     if (at >= 0) {
     if (at == 0 || cu.tile == 0) {  // a unit begins
       whole = cu.tile == 0;
-      scale_queries(cu);
+      if (kEarly && at > 0 && next_at == at) q = q_next;
+      scale_queries();
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         ref[nt][0] = ref[nt][1] = kPdNone;
@@ -413,7 +458,7 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
             const uint32_t f[4] = {pd_halves_lo(b[2 * j]), pd_halves_lo(b[2 * j + 1]), pd_halves_hi(b[2 * j]),
                                    pd_halves_hi(b[2 * j + 1])};
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) pd_mma<KIND>(x[m][nt], f, qb[nt][i + j][0], qb[nt][i + j][1]);
+            for (int nt = 0; nt < NT; ++nt) pd_mma<KIND>(x[m][nt], f, q.b[nt][i + j][0], q.b[nt][i + j][1]);
           }
         }
       } else {
@@ -422,7 +467,7 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
           uint32_t f[4];
           ldsm_x4(f, (k_at ^ (i << 5)) + m * 16 * Sh::kRow);
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt) pd_mma<KIND>(x[m][nt], f, qb[nt][i][0], qb[nt][i][1]);
+          for (int nt = 0; nt < NT; ++nt) pd_mma<KIND>(x[m][nt], f, q.b[nt][i][0], q.b[nt][i][1]);
         }
       }
     }
@@ -554,39 +599,29 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
 #pragma unroll
           for (int d = 4; d < 32; d <<= 1) sum[nt][e] += __shfl_xor_sync(0xffffffffu, sum[nt][e], d);
       if (whole && ends) {
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          const float by[2] = {scale_of(cu, sum[nt][0]), scale_of(cu, sum[nt][1])};
-#pragma unroll
-          for (int i = 0; i < DT; ++i) {
-            const float z[4] = {O[nt][i][0] * by[0], O[nt][i][1] * by[1], O[nt][i][2] * by[0], O[nt][i][3] * by[1]};
-            put_slice(cu, nt, i, z);
-          }
-          put_lse(cu, nt, 0, ref[nt][0], sum[nt][0]);
-          put_lse(cu, nt, 1, ref[nt][1], sum[nt][1]);
-        }
+        put_unit(cu);
       } else {
-        // set aside: in the ring, which is empty at the end of the run, or, where the run goes on, in the workspace
-        float* to = ends ? wk.lead + ((size_t)blockIdx.x * W + warp) * wk.stride : reinterpret_cast<float*>(ring);
-        if (!ends || (warp == 0 && !whole)) {
-          if (lane == 0) s_open[ends ? W : warp] = PdOpen{t0 + at - cu.tile, cu.row, cu.head, cu.block, cu.tiles};
+        // Set aside.  A unit that reaches back behind the run and ends here: in the workspace, as the CTA's part of it if this is
+        // the CTA's first run, for the warp that has its first piece otherwise.  One that outlasts the run: in the ring, which is
+        // empty then, and in the registers.
+        float* to = !ends       ? reinterpret_cast<float*>(ring)
+                    : warp == 0 ? wk.part + (size_t)(2 * blockIdx.x) * wk.stride
+                                : wk.lead + ((size_t)blockIdx.x * W + warp) * wk.stride;
+        if (lane == 0) {
+          const PdOpen o{t0 + at - cu.tile, cu.row, cu.head, cu.block, cu.tiles};
+          if (!ends) s_open[warp] = o;
+          else if (warp == 0) s_part[0] = o;
         }
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          if (g == 0) {
-            *reinterpret_cast<float2*>(to + nt * 8 + 2 * q4) = make_float2(ref[nt][0], ref[nt][1]);
-            *reinterpret_cast<float2*>(to + 16 + nt * 8 + 2 * q4) = make_float2(sum[nt][0], sum[nt][1]);
-          }
-#pragma unroll
-          for (int i = 0; i < DT; ++i)
-            reinterpret_cast<float4*>(to + 32)[(nt * DT + i) * 32 + lane] =
-                make_float4(O[nt][i][0], O[nt][i][1], O[nt][i][2], O[nt][i][3]);
-        }
+        set_aside(to);
       }
     }
     pd_advance<TILE>(cu, c, r, wk.blocks);
     }
     if (at >= -Sh::kAhead && at + Sh::kAhead < mine) {
+      if (kEarly && ci.tile == 0 && at > -Sh::kAhead && next_at <= at) {
+        next_at = at + Sh::kAhead;
+        load_queries(q_next, ci);
+      }
       issue(ci, s_pages + page_in * TILE, stage_in);
       stage_in = next(stage_in, S);
       page_in = next(page_in, Sh::kPages);
@@ -598,63 +633,77 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
       pd_advance<TILE>(cp, c, r, wk.blocks);
     }
     cp_async_commit();
-    if (at == -Sh::kAhead - 1 || (at >= 0 && at + 1 < mine && cu.tile == 0)) load_queries(cu);
+    if (at == -Sh::kAhead - 1 || (at >= 0 && at + 1 < mine && cu.tile == 0 && !(kEarly && next_at == at + 1))) load_queries(q, cu);
   }
 
-  // ---- units that the CTA's warps share, and its parts of units that it shares with other CTAs ----
+  // ---- units that the CTA's warps share: the warp that has a unit's first piece in this CTA adds the others to its own ----
   __syncthreads();
-  // the CTA's unfinished units, each at its first piece in this CTA
-  unsigned todo;
-  {
-    const int w = min(lane, W);
-    todo = __ballot_sync(0xffffffffu, lane <= W && s_open[w].tiles != 0 && (w == 0 || w == W || s_open[w].begin >= c0 + w * per));
-  }
   const unsigned cta_run = max(1, W * per);
-  int parts = 0;          // bits: the CTA has a part of a unit that reaches back to another CTA, or on to one
-  bool others = false;    // first the pieces of this CTA's warps, then the parts of other CTAs
+  {
+    const PdOpen o = s_open[warp];
+    if (o.tiles != 0 && (warp == 0 || o.begin >= t0)) {
+      const int end = o.begin + o.tiles;
+      const bool begins = o.begin >= c0, ends = end <= c1;
+      const int last = (int)((unsigned)(min(end, c1) - 1 - c0) / (unsigned)per);  // warp
 #pragma unroll 1
-  while (true) {
-    if (todo == 0) {
-      if (others || !parts) break;
-      // the parts are written: whoever comes last to a unit joins them
-      others = true;
-      __syncthreads();
-      if (threadIdx.x < 2 && (parts >> threadIdx.x & 1)) {
-        const PdOpen o = s_part[threadIdx.x];
-        const int ctas = (unsigned)(o.begin + o.tiles - 1) / cta_run - (unsigned)o.begin / cta_run + 1;
-        int* count = wk.count + ((size_t)o.row * c.Hkv + o.head) * wk.blocks + o.block;
-        __threadfence();  // (the other threads' stores are ordered in front of it by the barrier)
-        s_last[threadIdx.x] = atomicAdd(count, 1) == ctas - 1;
-        if (s_last[threadIdx.x]) *count = 0;
-        __threadfence();
+      for (int w = warp + 1; w <= last; ++w) {
+        const float* from = ends && w == last ? wk.lead + ((size_t)blockIdx.x * W + w) * wk.stride
+                                              : reinterpret_cast<const float*>(dsm + w * Sh::kRing);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          const float2 m = *reinterpret_cast<const float2*>(from + nt * 8 + 2 * q4);
+          const float2 s = *reinterpret_cast<const float2*>(from + 16 + nt * 8 + 2 * q4);
+          const float t0 = fmaxf(ref[nt][0], m.x), t1 = fmaxf(ref[nt][1], m.y);
+          const float a0 = pd_exp2(ref[nt][0] - t0), a1 = pd_exp2(ref[nt][1] - t1), b0 = pd_exp2(m.x - t0), b1 = pd_exp2(m.y - t1);
+          ref[nt][0] = t0;
+          ref[nt][1] = t1;
+          sum[nt][0] = sum[nt][0] * a0 + s.x * b0;
+          sum[nt][1] = sum[nt][1] * a1 + s.y * b1;
+#pragma unroll
+          for (int i = 0; i < DT; ++i) {
+            const float4 z = reinterpret_cast<const float4*>(from + 32)[(nt * DT + i) * 32 + lane];
+            O[nt][i][0] = O[nt][i][0] * a0 + z.x * b0;
+            O[nt][i][1] = O[nt][i][1] * a1 + z.y * b1;
+            O[nt][i][2] = O[nt][i][2] * a0 + z.z * b0;
+            O[nt][i][3] = O[nt][i][3] * a1 + z.w * b1;
+          }
+        }
       }
-      __syncthreads();
-      todo = (parts & 1 && s_last[0] ? 1 : 0) | (parts & 2 && s_last[1] ? 2 : 0);
-      continue;
+      if (begins && ends) {
+        PdCursor u;
+        u.row = o.row;
+        u.head = o.head;
+        u.block = o.block;
+        put_unit(u);
+      } else {
+        if (lane == 0) s_part[begins ? 1 : 0] = o;
+        set_aside(wk.part + (size_t)(2 * blockIdx.x + (begins ? 1 : 0)) * wk.stride);
+      }
     }
-    const int w = __ffs(todo) - 1;
-    todo &= todo - 1;
-    const PdOpen o = others ? s_part[w] : s_open[w];
-    const int end = o.begin + o.tiles;
-    const bool begins = o.begin >= c0, ends = end <= c1;
-    // piece 0, pieces 1 to n - 2 at equal distances behind `base`, piece n - 1
-    const float *p0, *base, *pn;
-    size_t stride;
-    int pieces;
-    if (others) {
-      const int first = (unsigned)o.begin / cta_run;
-      pieces = (unsigned)(end - 1) / cta_run - first + 1;
-      stride = 2 * wk.stride;
-      base = wk.part + first * stride;
-      p0 = base + wk.stride;
-      pn = base + (pieces - 1) * stride;
-    } else {
-      const int from = w == W ? 0 : w, to = w == W ? 0 : (int)((unsigned)(min(end, c1) - 1 - c0) / (unsigned)per);
-      pieces = to - from + 1;
-      stride = Sh::kRing / 4;
-      p0 = base = reinterpret_cast<const float*>(dsm + from * Sh::kRing);
-      pn = ends ? wk.lead + ((size_t)blockIdx.x * W + to) * wk.stride : base + (pieces - 1) * stride;
+  }
+  // ---- units that CTAs share: whoever comes last to one joins its parts, a slice a warp ----
+  __syncthreads();
+  if (threadIdx.x < 2) {
+    const PdOpen o = s_part[threadIdx.x];
+    int last = 0;
+    if (o.tiles != 0) {
+      const int ctas = (unsigned)(o.begin + o.tiles - 1) / cta_run - (unsigned)o.begin / cta_run + 1;
+      int* count = wk.count + ((size_t)o.row * c.Hkv + o.head) * wk.blocks + o.block;
+      last = pd_arrive(count) == ctas - 1;  // (the other threads' stores are ordered in front of it by the barrier)
+      if (last) *count = 0;
     }
+    s_last[threadIdx.x] = last;
+  }
+  __syncthreads();
+#pragma unroll 1
+  for (int w = 0; w < 2; ++w) {
+    if (!s_last[w]) continue;
+    const PdOpen o = s_part[w];
+    // part 0, and parts 1 to n - 1 at equal distances
+    const unsigned first = (unsigned)o.begin / cta_run;
+    const int pieces = (unsigned)(o.begin + o.tiles - 1) / cta_run - first + 1;
+    const size_t stride = 2 * wk.stride;
+    const float *base = wk.part + first * stride, *p0 = base + wk.stride;
     // their sums, brought to the largest reference: the heads' in top and tot, the warp's slices' in got
     float top[NT][2], tot[NT][2];
     float4 got[kSlices];
@@ -662,7 +711,7 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
     for (int nt = 0; nt < NT; ++nt) top[nt][0] = top[nt][1] = kPdNone, tot[nt][0] = tot[nt][1] = 0.f;
 #pragma unroll
     for (int k = 0; k < kSlices; ++k) got[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-    constexpr int kBatch = kSlices > 2 ? 2 : 4;
+    constexpr int kBatch = kSlices == 1 ? 8 : kSlices == 2 ? 4 : 2;
 #pragma unroll 1
     for (int i0 = 0; i0 < pieces; i0 += kBatch) {
       float2 m[kBatch][NT], s[kBatch][NT];
@@ -670,7 +719,7 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
 #pragma unroll
       for (int b = 0; b < kBatch; ++b) {
         const int i = i0 + b;
-        const float* p = i >= pieces - 1 ? pn : i == 0 ? p0 : base + i * stride;
+        const float* p = i == 0 ? p0 : base + min(i, pieces - 1) * stride;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
           m[b][nt] = *reinterpret_cast<const float2*>(p + nt * 8 + 2 * q4);
@@ -713,39 +762,25 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
         }
       }
     }
-    if (others || (begins && ends)) {
-      PdCursor u;
-      u.row = o.row;
-      u.head = o.head;
-      u.block = o.block;
+    PdCursor u;
+    u.row = o.row;
+    u.head = o.head;
+    u.block = o.block;
+    const float vs = c.vs ? c.vs[o.head] : 1.f;
 #pragma unroll
-      for (int k = 0; k < kSlices; ++k) {
-        if (k * W + warp >= NT * DT) continue;
-        const bool upper = NT == 2 && (k * W + warp) / DT == 1;
-        const float b0 = scale_of(u, upper ? tot[NT - 1][0] : tot[0][0]), b1 = scale_of(u, upper ? tot[NT - 1][1] : tot[0][1]);
-        const float z[4] = {got[k].x * b0, got[k].y * b1, got[k].z * b0, got[k].w * b1};
-        put_slice(u, upper ? 1 : 0, (k * W + warp) % DT, z);
-      }
-      if (warp == 0)
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          put_lse(u, nt, 0, top[nt][0], tot[nt][0]);
-          put_lse(u, nt, 1, top[nt][1], tot[nt][1]);
-        }
-      continue;
+    for (int k = 0; k < kSlices; ++k) {
+      if (k * W + warp >= NT * DT) continue;
+      const bool upper = NT == 2 && (k * W + warp) / DT == 1;
+      const float b0 = scale_of(vs, upper ? tot[NT - 1][0] : tot[0][0]), b1 = scale_of(vs, upper ? tot[NT - 1][1] : tot[0][1]);
+      const float z[4] = {got[k].x * b0, got[k].y * b1, got[k].z * b0, got[k].w * b1};
+      put_slice(u, upper ? 1 : 0, (k * W + warp) % DT, z);
     }
-    parts |= begins ? 2 : 1;
-    if (threadIdx.x == 0) s_part[begins ? 1 : 0] = o;
-    float* part = wk.part + (size_t)(2 * blockIdx.x + (begins ? 1 : 0)) * wk.stride;
-    if (warp == 0 && g == 0)
+    if (warp == 0)
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
-        *reinterpret_cast<float2*>(part + nt * 8 + 2 * q4) = make_float2(top[nt][0], top[nt][1]);
-        *reinterpret_cast<float2*>(part + 16 + nt * 8 + 2 * q4) = make_float2(tot[nt][0], tot[nt][1]);
+        put_lse(u, nt, 0, top[nt][0], tot[nt][0]);
+        put_lse(u, nt, 1, top[nt][1], tot[nt][1]);
       }
-#pragma unroll
-    for (int k = 0; k < kSlices; ++k)
-      if (k * W + warp < NT * DT) reinterpret_cast<float4*>(part + 32)[(k * W + warp) * 32 + lane] = got[k];
   }
   // empty rows
   for (int row = blockIdx.x; row < r.n; row += gridDim.x) {
