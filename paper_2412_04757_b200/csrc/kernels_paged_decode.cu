@@ -72,13 +72,6 @@ __device__ __forceinline__ void mma_fp16(float (&c)[4], const uint32_t (&a)[4], 
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-// Adds one; what this thread has seen or written is visible to whoever finds it added.  (With __threadfence on either side, which
-// orders more than that, the step took 3000 cycles.)
-__device__ __forceinline__ int pd_arrive(int* count) {
-  int before;
-  asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(before) : "l"(count) : "memory");
-  return before;
-}
 template <int KIND>
 __device__ __forceinline__ void pd_mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
   if (KIND == kPdBf16) mma_bf16(c, a, b0, b1);
@@ -689,7 +682,8 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
     if (o.tiles != 0) {
       const int ctas = (unsigned)(o.begin + o.tiles - 1) / cta_run - (unsigned)o.begin / cta_run + 1;
       int* count = wk.count + ((size_t)o.row * c.Hkv + o.head) * wk.blocks + o.block;
-      last = pd_arrive(count) == ctas - 1;  // (the other threads' stores are ordered in front of it by the barrier)
+      // (the other threads' stores are ordered in front of it by the barrier; with __threadfence on either side 3000 cycles)
+      last = paged_arrive(count) == ctas - 1;
       if (last) *count = 0;
     }
     s_last[threadIdx.x] = last;

@@ -32,7 +32,8 @@ struct PagedCache {
   int* count;                   // [max_rows][Hkv][blocks of heads]: CTAs of the unit that have finished; zero between calls
   float* logits;                // [n_pages][Hkv][P][blocks of heads], with weights: a decode call's logits
   float* lse2;                  // [max_rows][Hq], with weights: their sums, log2
-  int sms;
+  int* seen;                    // [max_rows]: CTAs of an eviction that have read the row's length; zero between calls
+  int sms, evict_cluster;
 };
 
 // One call's rows.
@@ -71,6 +72,8 @@ constexpr int kPagedWarps = 16;                     // of an attention CTA, at m
 int paged_decode_kernels(const PagedCache& c);  // launches of a decode call
 
 cudaError_t prepare_paged();
+cudaError_t prepare_paged_evict();
+int paged_evict_cluster();
 cudaError_t launch_paged_append(const PagedCache& c, const PagedRows& r, int layer, const PagedAppend& a, cudaStream_t s);
 cudaError_t launch_paged_decode(const PagedCache& c, const PagedRows& r, int layer, const PagedStep& a, cudaStream_t s);
 cudaError_t launch_paged_evict(const PagedCache& c, const PagedRows& r, int layer_begin, int layer_count, int* new_lens,
@@ -80,6 +83,13 @@ cudaError_t launch_paged_evict(const PagedCache& c, const PagedRows& r, int laye
 // (out of line: the checks are everywhere, and never taken)
 static __device__ __noinline__ void paged_status(const PagedCache& c, int detail) {
   if (atomicCAS(&c.status[0], 0, (int)LTRI_EDEVICE) == 0) c.status[1] = detail;
+}
+
+// Adds one; what this thread has seen or written is visible to whoever finds it added.
+__device__ __forceinline__ int paged_arrive(int* count) {
+  int before;
+  asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(before) : "l"(count) : "memory");
+  return before;
 }
 
 // Slots of row r: 0 (and the status word) where the length says more than the table can hold.

@@ -55,6 +55,7 @@ size_t layout(const ltri_paged_params& p, int sms, PagedCache* c, unsigned char*
   const size_t slots = (size_t)p.n_pages * p.n_kv_heads * p.page_tokens;
   unsigned char* status = take(256);
   unsigned char* count = take((size_t)p.max_rows * p.n_kv_heads * b.count * sizeof(int));
+  unsigned char* seen = take((size_t)p.max_rows * sizeof(int));
   if (zeroed) *zeroed = off;
   const size_t part_bytes = paged_part_floats(p.n_q_heads / p.n_kv_heads, p.head_dim) * sizeof(float);
   unsigned char *part = take(sms * 2 * part_bytes), *lead = take(sms * kPagedWarps * part_bytes);
@@ -67,6 +68,7 @@ size_t layout(const ltri_paged_params& p, int sms, PagedCache* c, unsigned char*
   if (c) {
     c->status = reinterpret_cast<int*>(status);
     c->count = reinterpret_cast<int*>(count);
+    c->seen = reinterpret_cast<int*>(seen);
     c->part = reinterpret_cast<float*>(part);
     c->lead = reinterpret_cast<float*>(lead);
     c->list = reinterpret_cast<int*>(list);
@@ -180,7 +182,8 @@ int ltri_paged_create(const ltri_paged_params* p, void* cuda_stream, ltri_paged*
   cudaError_t e = cudaGetDevice(&c->device);
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&d.sms, cudaDevAttrMultiProcessorCount, c->device);
   if (d.sms > kPagedMaxSms) d.sms = kPagedMaxSms;
-  if (e == cudaSuccess) e = prepare_paged();
+  if (e == cudaSuccess) e = first_error(prepare_paged(), prepare_paged_evict());
+  if (e == cudaSuccess) d.evict_cluster = paged_evict_cluster();
   if (e == cudaSuccess) e = cudaMemsetAsync(p->workspace, 0, zeroed, s);
   if (e == cudaSuccess) e = cudaStreamSynchronize(s);
   if (e != cudaSuccess) {
@@ -242,10 +245,12 @@ int ltri_paged_evict(ltri_paged* cache, int layer_begin, int layer_count, const 
   PagedRows r;
   if (const int rc = check_rows(cache, table, table_pages, table_stride, lens, n_rows, &r)) return rc;
   if (!aligned(new_lens, 4) || budget < 1 || n_sink < 0 || recent < 0 || (int64_t)n_sink + recent > budget) return LTRI_EINVAL;
+  // (a cluster for every layer, row and KV head)
+  if ((int64_t)layer_count * n_rows > (1ll << 24) / cache->p.n_kv_heads) return LTRI_ECAPACITY;
   OnDevice on(cache->device);
   if (!on.ok) return done(cache, cudaErrorInvalidDevice, 0);
   return done(cache, launch_paged_evict(cache->c, r, layer_begin, layer_count, new_lens, budget, n_sink, recent,
-                                        static_cast<cudaStream_t>(cuda_stream)), 2);
+                                        static_cast<cudaStream_t>(cuda_stream)), 1);
 }
 
 int ltri_paged_sync_status(ltri_paged* cache, void* cuda_stream) {
