@@ -5,7 +5,8 @@
 // move if they lie behind, the i-th into the i-th hole.  Sources and destinations are disjoint, so the moves need no order, and a
 // full budget that has grown by one token costs one row, not a shifted cache.
 //
-// A cluster owns a unit; its CTAs hold a stretch of the slots each, as keys in shared memory.  A histogram of 2048 bins over the
+// A cluster owns a unit; its CTAs hold a stretch of the slots each, as keys in shared memory.  Where one slot leaves, as in a
+// step that has appended one, it is the lowest key's, and the last slot moves there.  Otherwise a histogram of 2048 bins over the
 // range that the keys really have, summed through distributed shared memory, leaves some ten keys around the cut (weights
 // of a few powers of two); they are ranked against each other.  Where many are left (equal ones above all), up to two more
 // histograms go through the bin's range instead.
@@ -23,11 +24,12 @@ namespace cg = cooperative_groups;
 constexpr int kEvThreads = 512;  // two CTAs an SM: one's rows move while another's keys are counted
 constexpr int kEvWarps = kEvThreads / 32;
 constexpr int kEvBinBits = 11, kEvBins = 1 << kEvBinBits;
-constexpr int kEvMaxCluster = 16;
-constexpr int kEvMaxSlots = 24576;  // keys that a CTA can hold (96 KB); those of longer stretches are made again for every pass
-constexpr int kEvSlots = 4096;      // of a CTA, at least, before a unit gets more CTAs
+constexpr int kEvMaxCluster = 8;    // (of sixteen CTAs too few run at once: 32 units of 32768 slots took 139 us instead of 79)
+constexpr int kEvMaxSlots = 27136;  // keys and positions that a CTA can hold (212 KB); those of longer stretches are read again
+constexpr int kEvSlots = 1024;      // of a CTA, at least, before a unit gets more CTAs
+constexpr int kEvBatch = 8;         // slots of a thread whose weights and positions are on their way
 constexpr int kEvCand = kEvThreads;       // keys around the cut that are ranked against each other
-constexpr int kEvMoves = 8;         // 16-byte chunks that a lane has on their way
+constexpr int kEvMoves = 4;         // 16-byte chunks that a lane has on their way
 
 // Order of a slot: larger is kept first.  Protected positions come before every weight, NaN counts as -infinity, and the
 // two zeros are equal.
@@ -56,12 +58,15 @@ __device__ __forceinline__ int ev_scan(int x, int* s) {
 __global__ void __launch_bounds__(kEvThreads, 2)
     k_paged_evict(PagedCache c, PagedRows r, int layer_begin, int layers, int* new_lens, int budget, int n_sink, int recent,
                   int held) {
-  extern __shared__ unsigned s_key[];  // [held]
+  extern __shared__ unsigned s_key[];  // [held], and behind them
+  int* s_pos = reinterpret_cast<int*>(s_key) + held;   // [held]: positions; then every warp's movers and holes
+  int* s_list = reinterpret_cast<int*>(s_key);         // at last the CTA's, movers from the front and holes from the back
   __shared__ __align__(16) unsigned s_hist[kEvBins];
   __shared__ unsigned s_cand[kEvCand], s_all[kEvCand];
   __shared__ int s_scan[kEvWarps], s_hole[kEvWarps], s_mover[kEvWarps];
   __shared__ int s_n, s_newest, s_stay, s_bin, s_above, s_in, s_eq, s_holes, s_movers, s_cands;
   __shared__ unsigned s_lo, s_hi, s_cut;
+  __shared__ unsigned long long s_least;
   cg::cluster_group cluster = cg::this_cluster();
   const int C = cluster.num_blocks(), rank = cluster.block_rank();
   const int unit = blockIdx.x / C, head = unit % c.Hkv, row = unit / c.Hkv % r.n, layer = layer_begin + unit / c.Hkv / r.n;
@@ -73,6 +78,7 @@ __global__ void __launch_bounds__(kEvThreads, 2)
     s_stay = s_cands = 0;
     s_lo = 0xffffffffu;
     s_hi = 0u;
+    s_least = ~0ull;
   }
   __syncthreads();
   const int n = s_n;
@@ -99,61 +105,77 @@ __global__ void __launch_bounds__(kEvThreads, 2)
   };
   // The CTA's sum, least or largest value over the cluster: lane i asks CTA i.
   auto ask = [&](int* x, int none) { return lane < C ? *cluster.map_shared_rank(x, lane) : none; };
-  // ---- keys: a thread's slots in batches whose loads are all on their way at once ----
+  // ---- keys: a thread's slots in batches whose loads are all on their way at once; the newest position is known behind them ----
+  const bool all_held = chunk <= held;
   int newest = INT_MIN;
-  for (int j0 = begin + tid; j0 < end; j0 += 8 * kEvThreads) {
-    long long at[8];
+  for (int j0 = begin + tid; j0 < end; j0 += kEvBatch * kEvThreads) {
+    long long at[kEvBatch];
 #pragma unroll
-    for (int b = 0; b < 8; ++b) at[b] = j0 + b * kEvThreads < end ? word(j0 + b * kEvThreads) : -1;
-    int pos[8];
+    for (int b = 0; b < kEvBatch; ++b) at[b] = j0 + b * kEvThreads < end ? word(j0 + b * kEvThreads) : -1;
+    int pos[kEvBatch];
+    float w[kEvBatch];
 #pragma unroll
-    for (int b = 0; b < 8; ++b) pos[b] = at[b] >= 0 ? c.pos[at[b]] : INT_MIN;
+    for (int b = 0; b < kEvBatch; ++b) {
+      pos[b] = at[b] >= 0 ? c.pos[at[b]] : INT_MIN;
+      w[b] = at[b] >= 0 ? c.w[at[b]] : 0.f;
+    }
 #pragma unroll
-    for (int b = 0; b < 8; ++b) newest = max(newest, pos[b]);
+    for (int b = 0; b < kEvBatch; ++b) {
+      const int j = j0 + b * kEvThreads;
+      newest = max(newest, pos[b]);
+      if (j < end && j - begin < held) {
+        s_key[j - begin] = at[b] < 0 ? 0u : ev_key(w[b], pos[b] < n_sink);
+        s_pos[j - begin] = pos[b];
+      }
+    }
   }
   newest = __reduce_max_sync(0xffffffffu, newest);
   if (lane == 0) atomicMax(&s_newest, newest);
   cluster.sync();
   newest = __reduce_max_sync(0xffffffffu, ask(&s_newest, INT_MIN));
   const long long first_recent = (long long)newest - recent;
-  auto key_at = [&](long long at, int pos, float w) { return at < 0 ? 0u : ev_key(w, pos < n_sink || pos > first_recent); };
   auto key = [&](int slot) {
     if (slot - begin < held) return s_key[slot - begin];
     const long long at = word(slot);
-    return at < 0 ? 0u : key_at(at, c.pos[at], c.w[at]);
+    if (at < 0) return 0u;
+    const int pos = c.pos[at];
+    return ev_key(c.w[at], pos < n_sink || pos > first_recent);
   };
   unsigned lo = 0xffffffffu, hi = 0u;
   int stay = 0;
-  for (int j0 = begin + tid; j0 < end; j0 += 4 * kEvThreads) {
-    long long at[4];
-#pragma unroll
-    for (int b = 0; b < 4; ++b) at[b] = j0 + b * kEvThreads < end ? word(j0 + b * kEvThreads) : -1;
-    int pos[4];
-    float w[4];
-#pragma unroll
-    for (int b = 0; b < 4; ++b) {
-      pos[b] = at[b] >= 0 ? c.pos[at[b]] : 0;
-      w[b] = at[b] >= 0 ? c.w[at[b]] : 0.f;
-    }
-#pragma unroll
-    for (int b = 0; b < 4; ++b) {
-      const int j = j0 + b * kEvThreads;
-      if (j >= end) break;
-      const unsigned x = key_at(at[b], pos[b], w[b]);
-      if (j - begin < held) s_key[j - begin] = x;
-      if (x == 0xffffffffu) ++stay;
-      else lo = min(lo, x), hi = max(hi, x);
-    }
+  unsigned long long least = ~0ull;  // the lowest key, and of its slots the highest
+  for (int j = begin + tid; j < end; j += kEvThreads) {
+    unsigned x = key(j);
+    // (a slot without a page has position INT_MIN here: where no position is larger, it is not protected either)
+    if (j - begin < held && s_pos[j - begin] > first_recent && s_pos[j - begin] != INT_MIN) s_key[j - begin] = x = 0xffffffffu;
+    if (x == 0xffffffffu) ++stay;
+    else lo = min(lo, x), hi = max(hi, x);
+    least = min(least, (unsigned long long)x << 32 | (unsigned)(0x7fffffff - j));
   }
   lo = __reduce_min_sync(0xffffffffu, lo);
   hi = __reduce_max_sync(0xffffffffu, hi);
   stay = __reduce_add_sync(0xffffffffu, stay);
+  const bool single = n - budget == 1;
+  if (single) {
+#pragma unroll
+    for (int d = 16; d; d >>= 1) least = min(least, __shfl_xor_sync(0xffffffffu, least, d));
+    if (lane == 0) atomicMin(&s_least, least);
+  }
   if (lane == 0) {
     atomicMin(&s_lo, lo);
     atomicMax(&s_hi, hi);
     atomicAdd(&s_stay, stay);
   }
   cluster.sync();
+  int count = 0, gap = -1;           // moves; the hole of a single one
+  int m_incl = 0, h_incl = 0;        // lane i: movers and holes up to CTA i
+  if (single) {
+    least = lane < C ? *cluster.map_shared_rank(&s_least, lane) : ~0ull;
+#pragma unroll
+    for (int d = 16; d; d >>= 1) least = min(least, __shfl_xor_sync(0xffffffffu, least, d));
+    gap = 0x7fffffff - (int)(unsigned)least;
+    count = gap < n - 1;
+  } else {
   {
     const unsigned l = lane < C ? *cluster.map_shared_rank(&s_lo, lane) : 0xffffffffu;
     const unsigned h = lane < C ? *cluster.map_shared_rank(&s_hi, lane) : 0u;
@@ -272,39 +294,39 @@ __global__ void __launch_bounds__(kEvThreads, 2)
     const int others = ask(&s_eq, 0);
     eq0 += __reduce_add_sync(0xffffffffu, lane < rank ? others : 0);
   }
+  // Lists.  In shared memory a warp's come first, movers from the front of its stretch and holes from its back, then the CTA's;
+  // of longer stretches, in a second sweep, the i-th hole goes to the word of slot budget + i, the i-th mover to that of slot i.
   int hole0 = 0, mover0 = 0;
-  // lists: the i-th hole in the word of slot budget + i, the i-th mover in the word of slot i
-  auto sweep = [&](bool emit) {
+  auto sweep = [&](bool to_words) {
     int eq = eq0;
     const unsigned before = (1u << lane) - 1;
-    for (int base = w0; base < w1; base += 4 * 32) {
-      unsigned x[4];
-#pragma unroll
-      for (int b = 0; b < 4; ++b) x[b] = base + b * 32 + lane < w1 ? key(base + b * 32 + lane) : 0u;
-      int rank_in[4];  // of a hole, or of a mover behind all holes; -1: neither
-#pragma unroll
-      for (int b = 0; b < 4; ++b) {
-        const int j = base + b * 32 + lane;
-        const bool in = j < w1;
-        const unsigned same = __ballot_sync(0xffffffffu, in && x[b] == cut);
-        const bool kept = in && (x[b] > cut || (x[b] == cut && eq + __popc(same & before) < ties));
+    for (int base = w0; base < w1; base += 32) {
+      const int j = base + lane;
+      const bool in = j < w1;
+      const unsigned x = in ? key(j) : 0u;
+      bool kept = in && x >= cut;
+      if (ties < equal) {
+        const unsigned same = __ballot_sync(0xffffffffu, in && x == cut);
+        if (x == cut && eq + __popc(same & before) >= ties) kept = false;
         eq += __popc(same);
-        const bool hole = in && j < budget && !kept, mover = j >= budget && kept;
-        const unsigned holes = __ballot_sync(0xffffffffu, hole), movers = __ballot_sync(0xffffffffu, mover);
-        rank_in[b] = hole ? budget + hole0 + __popc(holes & before) : mover ? mover0 + __popc(movers & before) : -1;
-        hole0 += __popc(holes);
-        mover0 += __popc(movers);
       }
-      if (!emit) continue;
-      long long at[4];
-#pragma unroll
-      for (int b = 0; b < 4; ++b) at[b] = rank_in[b] >= 0 ? word(rank_in[b]) : -1;
-#pragma unroll
-      for (int b = 0; b < 4; ++b)
-        if (at[b] >= 0) c.list[at[b]] = base + b * 32 + lane;
+      const bool hole = in && j < budget && !kept, mover = j >= budget && kept;
+      const unsigned holes = __ballot_sync(0xffffffffu, hole), movers = __ballot_sync(0xffffffffu, mover);
+      const int h = hole0 + __popc(holes & before), m = mover0 + __popc(movers & before);
+      if (hole || mover) {
+        if (all_held) {
+          s_pos[hole ? w1 - 1 - h - begin : w0 + m - begin] = j;
+        } else if (to_words) {
+          const long long at = word(hole ? budget + h : m);
+          if (at >= 0) c.list[at] = j;
+        }
+      }
+      hole0 += __popc(holes);
+      mover0 += __popc(movers);
     }
   };
   sweep(false);
+  const int my_holes = hole0, my_movers = mover0;
   if (lane == 0) s_hole[warp] = hole0, s_mover[warp] = mover0;
   __syncthreads();
   hole0 = __reduce_add_sync(0xffffffffu, lane < warp ? s_hole[lane] : 0);
@@ -314,69 +336,104 @@ __global__ void __launch_bounds__(kEvThreads, 2)
     const int m = __reduce_add_sync(0xffffffffu, lane < kEvWarps ? s_mover[lane] : 0);
     if (lane == 0) s_holes = h, s_movers = m;
   }
-  cluster.sync();
-  int count;
-  {
-    const int m = ask(&s_movers, 0), h = ask(&s_holes, 0);
-    count = __reduce_add_sync(0xffffffffu, m);
-    mover0 += __reduce_add_sync(0xffffffffu, lane < rank ? m : 0);
-    hole0 += __reduce_add_sync(0xffffffffu, lane < rank ? h : 0);
+  if (all_held) {
+    for (int i = lane; i < my_movers; i += 32) s_list[mover0 + i] = s_pos[w0 - begin + i];
+    for (int i = lane; i < my_holes; i += 32) s_list[held - 1 - hole0 - i] = s_pos[w1 - 1 - begin - i];
   }
-  sweep(true);
-  cluster.sync();  // the lists are complete, and no CTA's shared memory is read from here on
+  cluster.sync();
+  m_incl = ask(&s_movers, 0);
+  h_incl = ask(&s_holes, 0);
+  count = __reduce_add_sync(0xffffffffu, m_incl);
+#pragma unroll
+  for (int d = 1; d < kEvMaxCluster; d <<= 1) {
+    const int m = __shfl_up_sync(0xffffffffu, m_incl, d), h = __shfl_up_sync(0xffffffffu, h_incl, d);
+    if (lane >= d) m_incl += m, h_incl += h;
+  }
+  if (!all_held) {
+    const int m = __shfl_sync(0xffffffffu, m_incl, max(0, rank - 1)), h = __shfl_sync(0xffffffffu, h_incl, max(0, rank - 1));
+    if (rank > 0) mover0 += m, hole0 += h;
+    sweep(true);
+    cluster.sync();
+  }
+  }
   if (bad) paged_status(c, row);
+  // Entry i of the cluster's lists of movers or holes: in CTA k, the number of CTAs whose last entry lies in front of it.
+  auto entry = [&](int incl, int i, bool of_holes) {
+    int k = 0;
+    for (int q = 0; q < C - 1; ++q) k += __shfl_sync(0xffffffffu, incl, q) <= i;
+    const int before = __shfl_sync(0xffffffffu, incl, max(0, k - 1)) * (k > 0);
+    const int* list = cluster.map_shared_rank(s_list, k);
+    return i < count ? list[of_holes ? held - 1 - (i - before) : i - before] : -1;
+  };
   // ---- moves: a lane finds out about one, then the warp copies them, K and V rows as 2 * row_bytes / 16 chunks a move ----
   const int warps = kEvWarps * C, each = (count + warps - 1) / warps, m0 = (rank * kEvWarps + warp) * each;
   const int m1 = min(count, m0 + each);
-  const int chunks = c.row_bytes / 16, shift = 32 - __clz(chunks);  // 2 * chunks = 1 << shift
+  const int chunks = c.row_bytes / 16, rounds = (2 * chunks + 31) / 32;  // (row_bytes: 64, 128, 256 or 512)
+  const int together = 32 / min(32, 2 * chunks), mine = lane / min(32, 2 * chunks);  // moves that the lanes share at a time
   for (int base = m0; base < m1; base += 32) {
     const int i = base + lane;
-    long long from = -1, to = -1;
+    long long from = -1, to = -1, wt = -1;
+    float w = 0.f;
+    int pos = 0;
+    int src = n - 1, dst = gap;
+    if (!single && all_held) {
+      src = entry(m_incl, i, false);
+      dst = entry(h_incl, i, true);
+    }
     if (i < m1) {
-      const long long a0 = word(i), a1 = word(budget + i);
-      const int src = a0 < 0 ? -1 : __ldcg(&c.list[a0]), dst = a1 < 0 ? -1 : __ldcg(&c.list[a1]);
+      if (!single && !all_held) {
+        const long long a0 = word(i), a1 = word(budget + i);
+        src = a0 < 0 ? -1 : __ldcg(&c.list[a0]);
+        dst = a1 < 0 ? -1 : __ldcg(&c.list[a1]);
+      }
       if (src >= 0 && dst >= 0) {
         const int sn = paged_nth(c, src), dn = paged_nth(c, dst), sp = page_of(sn), dp = page_of(dn);
         if (sp >= 0 && dp >= 0) {
           from = (long long)paged_row(c, layer, sp, head, src - sn * c.P);
           to = (long long)paged_row(c, layer, dp, head, dst - dn * c.P);
-          const size_t wf = paged_word(c, layer, sp, head, src - sn * c.P), wt = paged_word(c, layer, dp, head, dst - dn * c.P);
-          const float w = c.w[wf];
-          const int pos = c.pos[wf];
-          c.w[wt] = w;
-          c.pos[wt] = pos;
+          const size_t wf = paged_word(c, layer, sp, head, src - sn * c.P);
+          wt = (long long)paged_word(c, layer, dp, head, dst - dn * c.P);
+          w = c.w[wf];
+          pos = c.pos[wf];
         }
       }
     }
-    const int items = min(32, m1 - base) << shift;
-    for (int t0 = 0; t0 < items; t0 += 32 * kEvMoves) {
-      uint4 x[kEvMoves];
-      unsigned char* dst[kEvMoves];
+    const int moves = min(32, m1 - base);
+    for (int round = 0; round < rounds; ++round) {
+      const int ch = (round * 32 + lane) & (2 * chunks - 1);
+      unsigned char* pages = ch >= chunks ? c.v + (ch - chunks) * 16 : c.k + ch * 16;
+      for (int m = 0; m < moves; m += kEvMoves * together) {
+        uint4 x[kEvMoves];
 #pragma unroll
-      for (int b = 0; b < kEvMoves; ++b) {
-        const int item = t0 + b * 32 + lane, mv = min(item >> shift, 31), ch = item & (2 * chunks - 1);
-        const long long f = shfl_ll(from, mv), g = shfl_ll(to, mv);
-        const bool is_v = ch >= chunks;
-        unsigned char* pages = (is_v ? c.v : c.k) + (is_v ? ch - chunks : ch) * 16;
-        dst[b] = item < items && f >= 0 ? pages + g : nullptr;
-        if (dst[b]) x[b] = __ldcs(reinterpret_cast<const uint4*>(pages + f));
+        for (int b = 0; b < kEvMoves; ++b) {
+          const int mv = m + b * together + mine;
+          const long long f = shfl_ll(from, min(31, mv));
+          if (f >= 0 && mv < moves) x[b] = __ldcs(reinterpret_cast<const uint4*>(pages + f));
+        }
+#pragma unroll
+        for (int b = 0; b < kEvMoves; ++b) {
+          const int mv = m + b * together + mine;
+          const long long g = shfl_ll(to, min(31, mv));
+          if (g >= 0 && mv < moves) __stcs(reinterpret_cast<uint4*>(pages + g), x[b]);
+        }
       }
-#pragma unroll
-      for (int b = 0; b < kEvMoves; ++b)
-        if (dst[b]) __stcs(reinterpret_cast<uint4*>(dst[b]), x[b]);
+    }
+    if (wt >= 0) {
+      c.w[wt] = w;
+      c.pos[wt] = pos;
     }
   }
+  cluster.sync();  // no CTA leaves while its shared memory is read
 }
 
 cudaError_t prepare_paged_evict() {
-  const cudaError_t e = cudaFuncSetAttribute(k_paged_evict, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-  return first_error(e, allow_smem(k_paged_evict, kEvMaxSlots * (int)sizeof(unsigned)));
+  return allow_smem(k_paged_evict, kEvMaxSlots * 8);
 }
 
 // Largest cluster size that the device runs (a power of two).
 int paged_evict_cluster() {
   for (int cl = kEvMaxCluster; cl > 1; cl >>= 1)
-    if (active_clusters(k_paged_evict, cl, kEvThreads, kEvMaxSlots * (int)sizeof(unsigned)) > 0) return cl;
+    if (active_clusters(k_paged_evict, cl, kEvThreads, kEvMaxSlots * 8) > 0) return cl;
   return 1;
 }
 
@@ -387,7 +444,7 @@ cudaError_t launch_paged_evict(const PagedCache& c, const PagedRows& r, int laye
   int cl = 1;
   while (cl < c.evict_cluster && units * cl < 2 * c.sms && (r.cap + cl - 1) / cl > kEvSlots) cl *= 2;
   const int held = min((r.cap + cl - 1) / cl, kEvMaxSlots);
-  return launch_chained_cluster(k_paged_evict, dim3((unsigned)(units * cl)), dim3(kEvThreads), cl, held * sizeof(unsigned), s, c, r,
+  return launch_chained_cluster(k_paged_evict, dim3((unsigned)(units * cl)), dim3(kEvThreads), cl, held * 8, s, c, r,
                                 layer_begin, layer_count, new_lens, budget, n_sink, recent, held);
 }
 
