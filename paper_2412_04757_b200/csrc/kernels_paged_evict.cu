@@ -26,7 +26,8 @@ constexpr int kEvWarps = kEvThreads / 32;
 constexpr int kEvBinBits = 11, kEvBins = 1 << kEvBinBits;
 constexpr int kEvMaxCluster = 8;    // (of sixteen CTAs too few run at once: 32 units of 32768 slots took 139 us instead of 79)
 constexpr int kEvMaxSlots = 27136;  // keys and positions that a CTA can hold (212 KB); those of longer stretches are read again
-constexpr int kEvSlots = 1024;      // of a CTA, at least, before a unit gets more CTAs
+constexpr int kEvSlots = 1024, kEvLong = 8192;  // slots of a CTA: above the first a unit gets more CTAs where SMs are idle,
+                                                // above the second anyway
 constexpr int kEvBatch = 8;         // slots of a thread whose weights and positions are on their way
 constexpr int kEvCand = kEvThreads;       // keys around the cut that are ranked against each other
 constexpr int kEvMoves = 4;         // 16-byte chunks that a lane has on their way
@@ -440,10 +441,12 @@ int paged_evict_cluster() {
 cudaError_t launch_paged_evict(const PagedCache& c, const PagedRows& r, int layer_begin, int layer_count, int* new_lens,
                                int budget, int n_sink, int recent, cudaStream_t s) {
   const long long units = (long long)c.Hkv * r.n * layer_count;
-  // Two CTAs for every SM and again as many, since rows within their budget leave at once; none with less than kEvSlots to do
+  // Two CTAs for every SM, none with less than kEvSlots to do, and none with more than kEvLong: rows within their budget leave
+  // at once, and a batch has few long ones (128 units, half of them of 32768 slots: 144 us in clusters of two, 112 in fours)
   int cl = 1;
-  while (cl < c.evict_cluster && units * cl < 2 * c.sms && (r.cap + cl - 1) / cl > kEvSlots) cl *= 2;
-  const int held = min((r.cap + cl - 1) / cl, kEvMaxSlots);
+  auto slots = [&] { return (r.cap + cl - 1) / cl; };
+  while (cl < c.evict_cluster && slots() > kEvSlots && (units * cl <= c.sms || slots() > kEvLong)) cl *= 2;
+  const int held = min(slots(), kEvMaxSlots);
   return launch_chained_cluster(k_paged_evict, dim3((unsigned)(units * cl)), dim3(kEvThreads), cl, held * 8, s, c, r,
                                 layer_begin, layer_count, new_lens, budget, n_sink, recent, held);
 }

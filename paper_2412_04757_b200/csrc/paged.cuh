@@ -30,7 +30,7 @@ struct PagedCache {
   float* part;                  // [sms][2][paged_part_floats]: partial sums of units that several CTAs share
   float* lead;                  // [sms][kPagedWarps][paged_part_floats]: of units that several warps share
   int* count;                   // [max_rows][Hkv][blocks of heads]: CTAs of the unit that have finished; zero between calls
-  float* logits;                // [n_pages][Hkv][P][blocks of heads], with weights: a decode call's logits
+  float* logits;                // [n_pages][Hkv][P][paged_even(G)], with weights: a decode call's logits
   float* lse2;                  // [max_rows][Hq], with weights: their sums, log2
   int* seen;                    // [max_rows]: CTAs of an eviction that have read the row's length; zero between calls
   int sms, evict_cluster;
@@ -67,6 +67,7 @@ struct PagedBlocks {
   int heads, count;
 };
 PagedBlocks paged_blocks(int group);
+__host__ __device__ constexpr int paged_even(int x) { return (x + 1) & ~1; }
 size_t paged_part_floats(int group, int head_dim);  // partial sums of one block
 constexpr int kPagedWarps = 16;                     // of an attention CTA, at most
 int paged_decode_kernels(const PagedCache& c);  // launches of a decode call

@@ -62,7 +62,7 @@ size_t layout(const ltri_paged_params& p, int sms, PagedCache* c, unsigned char*
   unsigned char *list = nullptr, *logits = nullptr, *lse2 = nullptr;
   if (p.weights) {
     list = take(p.n_layers * slots * sizeof(int));
-    logits = take(slots * b.count * b.heads * sizeof(float));
+    logits = take(slots * paged_even(p.n_q_heads / p.n_kv_heads) * sizeof(float));
     lse2 = take((size_t)p.max_rows * p.n_q_heads * sizeof(float));
   }
   if (c) {
