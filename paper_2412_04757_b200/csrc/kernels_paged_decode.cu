@@ -116,10 +116,15 @@ __device__ __forceinline__ void pd_advance(PdCursor& u, const PagedCache& c, con
 
 // All lanes of a warp: the tiles of the whole call, and the cursor of tile `runs_before` * per, where per is every run's length
 // (returned) when `runs` of them cover the line.
+// Where every unit can have a CTA of its own and a warp no more than one of its tiles, it begins with one, as if all were as
+// long as the CTAs' runs (`lone`; the cursor may then lie behind the unit's end): no two CTAs share a unit, and the join at
+// the end, two trips through L2, is spared.  (8 query heads, 2 KV heads, 100 slots: 7.1 us, 9.5 dealt evenly; with up to three
+// tiles a warp, 300 slots: 9.0 and 8.6.)
 template <int TILE>
-__device__ __forceinline__ int pd_deal(PdCursor& u, int& total, int runs, int runs_before, const PagedCache& c,
-                                       const PagedRows& r, int blocks) {
+__device__ __forceinline__ int pd_deal(PdCursor& u, int& total, bool& lone, int runs, int runs_before, int warps,
+                                       const PagedCache& c, const PagedRows& r, int blocks) {
   const int lane = threadIdx.x & 31, per_row = c.Hkv * blocks;
+  lone = false;
   auto scan = [&](int x) {
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
@@ -129,7 +134,26 @@ __device__ __forceinline__ int pd_deal(PdCursor& u, int& total, int runs, int ru
     return x;
   };
   // the first 32 rows are kept
-  const int n0 = lane < r.n ? paged_len(c, r, lane) : 0, inc0 = scan((n0 + TILE - 1) / TILE * per_row);
+  const int n0 = lane < r.n ? paged_len(c, r, lane) : 0;
+  if (r.n <= 32) {
+    const unsigned rows = __ballot_sync(0xffffffffu, n0 > 0);
+    const int units = __popc(rows) * per_row;
+    if (warps > 0 && __reduce_max_sync(0xffffffffu, n0) <= warps * TILE && units * warps <= runs) {
+      const int unit = (unsigned)runs_before / (unsigned)warps;
+      total = units * warps;
+      lone = true;
+      if (unit >= units) return 1;
+      const int nth = unit / per_row, in_row = unit - nth * per_row;
+      u.row = __fns(rows, 0, nth + 1);
+      u.n = __shfl_sync(0xffffffffu, n0, u.row);
+      u.tiles = (u.n + TILE - 1) / TILE;
+      u.tile = runs_before - unit * warps;
+      u.head = in_row / blocks;
+      u.block = in_row - u.head * blocks;
+      return 1;
+    }
+  }
+  const int inc0 = scan((n0 + TILE - 1) / TILE * per_row);
   total = __shfl_sync(0xffffffffu, inc0, 31);
   for (int base = 32; base < r.n; base += 32) {
     const int row = base + lane;
@@ -189,9 +213,11 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
 
   PdCursor cu;
   int total;
-  const int per = pd_deal<TILE>(cu, total, gridDim.x * W, blockIdx.x * W + warp, c, r, wk.blocks);
+  bool lone;  // the CTA has one unit, and all of it
+  const int per = pd_deal<TILE>(cu, total, lone, gridDim.x * W, blockIdx.x * W + warp, W, c, r, wk.blocks);
   const int c0 = blockIdx.x * W * per, c1 = min(c0 + W * per, total);  // the CTA's run
-  const int t0 = c0 + warp * per, mine = max(0, min(per, total - t0));
+  const int t0 = c0 + warp * per;
+  const int mine = t0 >= total ? 0 : max(0, min(per, lone ? cu.tiles - cu.tile : total - t0));
   if (lane == 0) {
     s_open[warp].tiles = 0;
     if (warp == 0) s_part[0].tiles = s_part[1].tiles = 0;
@@ -798,7 +824,8 @@ __global__ void __launch_bounds__(kPwThreads, kPwCtas) k_paged_weights(PagedCach
   // (the lengths and pages are older than the attention kernel, which has waited for its predecessor before it released this one)
   PdCursor u;
   int total;
-  const int per = pd_deal<kPwThreads>(u, total, gridDim.x, blockIdx.x, c, r, 1), t0 = blockIdx.x * per;
+  bool lone;
+  const int per = pd_deal<kPwThreads>(u, total, lone, gridDim.x, blockIdx.x, 0, c, r, 1), t0 = blockIdx.x * per;
   chain_wait();
   for (int t = t0; t < min(t0 + per, total); ++t) {
     const int slot = u.tile * kPwThreads + threadIdx.x;
