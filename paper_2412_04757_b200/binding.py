@@ -462,7 +462,8 @@ class LtriPaged:
         for t, want, shape in ((k_scale, torch.float32, (hkv,)), (v_scale, torch.float32, (hkv,)),
                                (weights, torch.float32, (L, pages, hkv, P)), (positions, torch.int32, (L, pages, hkv, P))):
             if t is not None and (t.dtype != want or t.shape != shape or not t.is_contiguous() or t.device != self.device):
-                raise ValueError(f"scales are float32 [{hkv}], weights float32 and positions int32 {(L, pages, hkv, P)}, contiguous")
+                raise ValueError(f"scales are float32 [{hkv}], weights float32 and positions int32 {(L, pages, hkv, P)}, "
+                                 "contiguous")
         if v_pages.device != self.device:
             raise ValueError("k_pages and v_pages are on one device")
         s = k_pages.stride()
@@ -479,6 +480,7 @@ class LtriPaged:
             self.params.workspace_bytes = nbytes
             self._keep = (k_pages, v_pages, k_scale, v_scale, weights, positions)
             self.dtype, self._q_shape, self._kv_shape = dtype, (n_q_heads, D), (hkv, D)
+            self._sizes, self._i32 = {}, torch.int32
             self._raw_stream = torch._C._cuda_getCurrentRawStream
             self._index = self.device.index
             _check(self.lib.ltri_paged_create(C.byref(self.params), self._stream(stream), C.byref(self._h)),
@@ -498,96 +500,104 @@ class LtriPaged:
         except Exception:
             pass
 
+    # Checks.  A step of a few microseconds on the GPU waits for them, so the usual case of every argument takes one expression
+    # of attributes; only what that does not settle is looked at closely.
+
+    def _sizes_of(self, n):
+        """The shapes that go with n rows: [n], [n][Hq], [n][Hq][head_dim], [n][Hkv][head_dim]."""
+        s = self._sizes.get(n)
+        if s is None:
+            size = self.torch.Size
+            s = self._sizes[n] = (size((n,)), size((n, self._q_shape[0])), size((n, *self._q_shape)), size((n, *self._kv_shape)))
+        return s
+
     def _rows(self, table, lens):
         """(rows, table columns, table row stride) of a call, checked."""
-        i32 = self.torch.int32
-        if table.dtype is not i32 or table.dim() != 2 or table.device != self.device or (table.shape[1] > 1 and table.stride(1) != 1):
+        if table.dtype is not self._i32 or table.dim() != 2 or table.get_device() != self._index or (
+                not table.is_contiguous() and table.shape[1] > 1 and table.stride(1) != 1):
             raise ValueError("table is int32 [rows][pages of a row] on the cache's device, its rows contiguous")
         n, cols = table.shape
-        self._vector(lens, n, i32, "lens")
+        self._dense(lens, self._i32, self._sizes_of(n)[0], "lens")
         return n, cols, table.stride(0) if n > 1 else cols
 
-    def _vector(self, t, n, dtype, name):
-        if t.dtype is not dtype or t.shape != (n,) or t.device != self.device or not t.is_contiguous():
-            raise ValueError(f"{name} is {dtype} [{n}], contiguous, on the cache's device")
+    def _dense(self, t, dtype, shape, name):
+        if t.dtype is dtype and t.shape == shape and t.get_device() == self._index and t.is_contiguous():
+            return t.data_ptr()
+        raise ValueError(f"{name} is {dtype} {tuple(shape)}, contiguous, on the cache's device")
 
-    def _heads(self, t, n, heads, name):
-        """Row stride of t [n][heads][head_dim], whose rows are dense."""
-        if t.dtype is not self.dtype or t.shape != (n, *heads) or t.device != self.device:
-            raise ValueError(f"{name} is {self.dtype} {(n, *heads)} on the cache's device")
-        row, head, one = t.stride()
-        dense = heads[0] * heads[1]
-        if (one != 1 and heads[1] > 1) or (head != heads[1] and heads[0] > 1) or (n > 1 and row < dense):
-            raise ValueError(f"{name}: a row's heads are dense")
-        return row if n > 1 else dense
+    def _heads(self, t, shape, name):
+        """Row stride (0: dense) of t [n][heads][head_dim], whose rows are dense."""
+        if t.dtype is self.dtype and t.shape == shape and t.get_device() == self._index:
+            if t.is_contiguous():
+                return 0
+            n, heads, dim = shape
+            row, head, one = t.stride()
+            if one == 1 and (head == dim or heads == 1) and (n == 1 or row >= heads * dim):
+                return row if n > 1 else 0
+        raise ValueError(f"{name} is {self.dtype} {tuple(shape)} on the cache's device, the heads of a row dense")
 
     def _done(self, rc, where):
         if rc == LTRI_ECUDA:
             raise LtriError(rc, f"{where} (cudaError {self.lib.ltri_paged_last_cuda_error(self._h)})")
-        if rc != LTRI_OK:
-            raise LtriError(rc, where)
+        raise LtriError(rc, where)
 
     def ltri_paged_append(self, layer, table, lens, starts, k, v, row_pos=None, weights=None, stream=None):
         """k, v [tokens][Hkv][head_dim] into the last slots of their rows; starts int32 [rows + 1] on the device, row_pos int32
         [rows], weights float32 [tokens][Hkv].  lens counts the tokens already."""
         n, cols, ts = self._rows(table, lens)
-        self._vector(starts, n + 1, self.torch.int32, "starts")
-        tokens = k.shape[0]
-        stride = self._heads(k, tokens, self._kv_shape, "k")
-        if self._heads(v, tokens, self._kv_shape, "v") != stride:
+        tokens, i32 = k.shape[0], self._i32
+        size = (tokens, *self._kv_shape)
+        sp = self._dense(starts, i32, (n + 1,), "starts")
+        stride = self._heads(k, size, "k")
+        if self._heads(v, size, "v") != stride:
             raise ValueError("k and v have the same strides")
-        if row_pos is not None:
-            self._vector(row_pos, n, self.torch.int32, "row_pos")
-        if weights is not None and (weights.dtype is not self.torch.float32 or weights.shape != (tokens, self._kv_shape[0])
-                                    or weights.device != self.device or not weights.is_contiguous()):
-            raise ValueError(f"weights is float32 {(tokens, self._kv_shape[0])}, contiguous, on the cache's device")
+        rp = None if row_pos is None else self._dense(row_pos, i32, self._sizes_of(n)[0], "row_pos")
+        wp = None if weights is None else self._dense(weights, self.torch.float32, size[:2], "weights")
         if tokens == 0:
             return
-        self._done(self.lib.ltri_paged_append(self._h, layer, table.data_ptr(), cols, ts, lens.data_ptr(), n, starts.data_ptr(),
-                                              tokens, k.data_ptr(), v.data_ptr(), stride,
-                                              None if row_pos is None else row_pos.data_ptr(),
-                                              None if weights is None else weights.data_ptr(), self._stream(stream)),
-                   "ltri_paged_append")
+        rc = self.lib.ltri_paged_append(self._h, layer, table.data_ptr(), cols, ts, lens.data_ptr(), n, sp, tokens, k.data_ptr(),
+                                        v.data_ptr(), stride, rp, wp,
+                                        self._raw_stream(self._index) if stream is None else stream.cuda_stream)
+        if rc:
+            self._done(rc, "ltri_paged_append")
 
     def ltri_paged_decode(self, layer, table, lens, q, k=None, v=None, row_pos=None, out=None, lse=None, stream=None):
-        """q [rows][Hq][head_dim]; k, v [rows][Hkv][head_dim], the new tokens' rows, which lens counts already (None: attend over
-        the cache as it is).  lse: float32 [rows][Hq], filled if given.  Returns out."""
+        """q [rows][Hq][head_dim]; k, v [rows][Hkv][head_dim], the new tokens' rows, which lens counts already (None: attend
+        over the cache as it is).  lse: float32 [rows][Hq], filled if given.  Returns out."""
         n, cols, ts = self._rows(table, lens)
-        qs = self._heads(q, n, self._q_shape, "q")
-        kvs = kp = vp = 0
+        rows, heads, q_size, kv_size = self._sizes_of(n)
+        qs = self._heads(q, q_size, "q")
+        kvs, kp, vp = 0, None, None
         if k is not None or v is not None:
             if k is None or v is None:
                 raise ValueError("k and v go together")
-            kvs = self._heads(k, n, self._kv_shape, "k")
-            if self._heads(v, n, self._kv_shape, "v") != kvs:
+            kvs = self._heads(k, kv_size, "k")
+            if self._heads(v, kv_size, "v") != kvs:
                 raise ValueError("k and v have the same strides")
             kp, vp = k.data_ptr(), v.data_ptr()
-        if row_pos is not None:
-            self._vector(row_pos, n, self.torch.int32, "row_pos")
+        rp = None if row_pos is None else self._dense(row_pos, self._i32, rows, "row_pos")
         if out is None:
             if stream is None:
-                out = self.torch.empty((n, *self._q_shape), dtype=self.dtype, device=self.device)
+                out = self.torch.empty(q_size, dtype=self.dtype, device=self.device)
             else:
                 with self.torch.cuda.stream(stream):
-                    out = self.torch.empty((n, *self._q_shape), dtype=self.dtype, device=self.device)
-        elif out.dtype is not self.dtype or out.shape != (n, *self._q_shape) or out.device != self.device or not out.is_contiguous():
-            raise ValueError(f"out is {self.dtype} {(n, *self._q_shape)}, contiguous, on the cache's device")
-        if lse is not None and (lse.dtype is not self.torch.float32 or lse.shape != (n, self._q_shape[0])
-                                or lse.device != self.device or not lse.is_contiguous()):
-            raise ValueError(f"lse is float32 {(n, self._q_shape[0])}, contiguous, on the cache's device")
-        self._done(self.lib.ltri_paged_decode(self._h, layer, table.data_ptr(), cols, ts, lens.data_ptr(), n, q.data_ptr(), qs, kp,
-                                              vp, kvs, None if row_pos is None else row_pos.data_ptr(), out.data_ptr(),
-                                              None if lse is None else lse.data_ptr(), self._stream(stream)),
-                   "ltri_paged_decode")
+                    out = self.torch.empty(q_size, dtype=self.dtype, device=self.device)
+        op = self._dense(out, self.dtype, q_size, "out")
+        lp = None if lse is None else self._dense(lse, self.torch.float32, heads, "lse")
+        rc = self.lib.ltri_paged_decode(self._h, layer, table.data_ptr(), cols, ts, lens.data_ptr(), n, q.data_ptr(), qs, kp, vp,
+                                        kvs, rp, op, lp, self._raw_stream(self._index) if stream is None else stream.cuda_stream)
+        if rc:
+            self._done(rc, "ltri_paged_decode")
         return out
 
     def ltri_paged_evict(self, layer_begin, layer_count, table, lens, new_lens, budget, n_sink, recent, stream=None):
         """Cuts rows of more than ``budget`` slots; new_lens int32 [rows] (may be lens) gets their lengths."""
         n, cols, ts = self._rows(table, lens)
-        self._vector(new_lens, n, self.torch.int32, "new_lens")
-        self._done(self.lib.ltri_paged_evict(self._h, layer_begin, layer_count, table.data_ptr(), cols, ts, lens.data_ptr(),
-                                             new_lens.data_ptr(), n, budget, n_sink, recent, self._stream(stream)),
-                   "ltri_paged_evict")
+        to = self._dense(new_lens, self._i32, self._sizes_of(n)[0], "new_lens")
+        rc = self.lib.ltri_paged_evict(self._h, layer_begin, layer_count, table.data_ptr(), cols, ts, lens.data_ptr(), to, n, budget,
+                                       n_sink, recent, self._raw_stream(self._index) if stream is None else stream.cuda_stream)
+        if rc:
+            self._done(rc, "ltri_paged_evict")
 
     def ltri_paged_sync_status(self, stream=None) -> int:
         return int(self.lib.ltri_paged_sync_status(self._h, self._stream(stream)))
