@@ -508,7 +508,8 @@ class LtriPaged:
         s = self._sizes.get(n)
         if s is None:
             size = self.torch.Size
-            s = self._sizes[n] = (size((n,)), size((n, self._q_shape[0])), size((n, *self._q_shape)), size((n, *self._kv_shape)))
+            s = (size((n,)), size((n, self._q_shape[0])), size((n, *self._q_shape)), size((n, *self._kv_shape)))
+            self._sizes[n] = s
         return s
 
     def _rows(self, table, lens):
@@ -555,9 +556,9 @@ class LtriPaged:
         wp = None if weights is None else self._dense(weights, self.torch.float32, size[:2], "weights")
         if tokens == 0:
             return
-        rc = self.lib.ltri_paged_append(self._h, layer, table.data_ptr(), cols, ts, lens.data_ptr(), n, sp, tokens, k.data_ptr(),
-                                        v.data_ptr(), stride, rp, wp,
-                                        self._raw_stream(self._index) if stream is None else stream.cuda_stream)
+        s = self._raw_stream(self._index) if stream is None else stream.cuda_stream
+        rc = self.lib.ltri_paged_append(self._h, layer, table.data_ptr(), cols, ts, lens.data_ptr(), n, sp, tokens,
+                                        k.data_ptr(), v.data_ptr(), stride, rp, wp, s)
         if rc:
             self._done(rc, "ltri_paged_append")
 
@@ -584,8 +585,9 @@ class LtriPaged:
                     out = self.torch.empty(q_size, dtype=self.dtype, device=self.device)
         op = self._dense(out, self.dtype, q_size, "out")
         lp = None if lse is None else self._dense(lse, self.torch.float32, heads, "lse")
-        rc = self.lib.ltri_paged_decode(self._h, layer, table.data_ptr(), cols, ts, lens.data_ptr(), n, q.data_ptr(), qs, kp, vp,
-                                        kvs, rp, op, lp, self._raw_stream(self._index) if stream is None else stream.cuda_stream)
+        s = self._raw_stream(self._index) if stream is None else stream.cuda_stream
+        rc = self.lib.ltri_paged_decode(self._h, layer, table.data_ptr(), cols, ts, lens.data_ptr(), n, q.data_ptr(), qs, kp,
+                                        vp, kvs, rp, op, lp, s)
         if rc:
             self._done(rc, "ltri_paged_decode")
         return out
@@ -594,8 +596,9 @@ class LtriPaged:
         """Cuts rows of more than ``budget`` slots; new_lens int32 [rows] (may be lens) gets their lengths."""
         n, cols, ts = self._rows(table, lens)
         to = self._dense(new_lens, self._i32, self._sizes_of(n)[0], "new_lens")
-        rc = self.lib.ltri_paged_evict(self._h, layer_begin, layer_count, table.data_ptr(), cols, ts, lens.data_ptr(), to, n, budget,
-                                       n_sink, recent, self._raw_stream(self._index) if stream is None else stream.cuda_stream)
+        s = self._raw_stream(self._index) if stream is None else stream.cuda_stream
+        rc = self.lib.ltri_paged_evict(self._h, layer_begin, layer_count, table.data_ptr(), cols, ts, lens.data_ptr(), to, n,
+                                       budget, n_sink, recent, s)
         if rc:
             self._done(rc, "ltri_paged_evict")
 

@@ -11,13 +11,15 @@ namespace ltri {
 constexpr int kAppThreads = 256;
 
 template <int CHUNKS>
-__global__ void __launch_bounds__(kAppThreads) k_paged_append(PagedCache c, PagedRows r, int layer, PagedAppend a, int lanes, int parts) {
+__global__ void __launch_bounds__(kAppThreads)
+    k_paged_append(PagedCache c, PagedRows r, int layer, PagedAppend a, int lanes, int parts) {
   chain_wait();
   const int chunks = c.D / 8, shift = 31 - __clz(chunks), per_token = c.Hkv * chunks;
   // `lanes` of a warp have a part of CHUNKS * lanes chunks of a token
   const int lane = threadIdx.x & 31, sub = lane / lanes, together = 32 / lanes;
   const long long items = a.n_tokens * parts, step = (long long)gridDim.x * (kAppThreads / 32) * together;
-  for (long long item = ((long long)blockIdx.x * (kAppThreads / 32) + threadIdx.x / 32) * together + sub; item < items; item += step) {
+  const long long begin = ((long long)blockIdx.x * (kAppThreads / 32) + threadIdx.x / 32) * together + sub;
+  for (long long item = begin; item < items; item += step) {
     const long long tok = parts == 1 ? item : item / parts;
     const int in0 = (int)(item - tok * parts) * (CHUNKS * lanes) + lane % lanes;
     uint4 kx[CHUNKS], vx[CHUNKS];
@@ -29,7 +31,8 @@ __global__ void __launch_bounds__(kAppThreads) k_paged_append(PagedCache c, Page
         vx[u] = __ldcs(reinterpret_cast<const uint4*>(a.v + tok * a.stride + in * 16));
       }
     }
-    // the last row that starts at or in front of the token
+    // the last row that starts at or in front of the token; the next one has been seen to start behind it, so the slot lies
+    // below the row's length even if the starts do not ascend
     int lo = 0, hi = r.n;
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1;
@@ -37,8 +40,8 @@ __global__ void __launch_bounds__(kAppThreads) k_paged_append(PagedCache c, Page
       else hi = mid - 1;
     }
     if (lo >= r.n || a.starts[lo] > tok) continue;
-    const int row = lo, nth = (int)(tok - a.starts[row]);
-    const long long slot = (long long)paged_len(c, r, row) - (a.starts[row + 1] - a.starts[row]) + nth;
+    const int row = lo;
+    const long long nth = tok - a.starts[row], slot = (long long)paged_len(c, r, row) - a.starts[row + 1] + tok;
     if (slot < 0) {
       paged_status(c, row);
       continue;
@@ -60,7 +63,7 @@ __global__ void __launch_bounds__(kAppThreads) k_paged_append(PagedCache c, Page
       if (c.w && ch == 0) {
         const size_t word = paged_word(c, layer, page, head, place);
         c.w[word] = a.weights ? a.weights[tok * c.Hkv + head] : 0.f;
-        c.pos[word] = a.row_pos ? a.row_pos[row] + nth : (int)slot;
+        c.pos[word] = a.row_pos ? a.row_pos[row] + (int)nth : (int)slot;
       }
     }
   }
@@ -74,7 +77,8 @@ cudaError_t launch_paged_append(const PagedCache& c, const PagedRows& r, int lay
   const int chunks = few ? 1 : 4, parts = (per_token + chunks * lanes - 1) / (chunks * lanes);
   const long long per_block = (kAppThreads / 32) * (32 / lanes), blocks = (a.n_tokens * parts + per_block - 1) / per_block;
   const int grid = (int)(blocks < c.sms * 16ll ? blocks : c.sms * 16ll);
-  return launch_chained(few ? k_paged_append<1> : k_paged_append<4>, dim3(grid), dim3(kAppThreads), 0, s, c, r, layer, a, lanes, parts);
+  const auto kernel = few ? k_paged_append<1> : k_paged_append<4>;
+  return launch_chained(kernel, dim3(grid), dim3(kAppThreads), 0, s, c, r, layer, a, lanes, parts);
 }
 
 }  // namespace ltri

@@ -1,7 +1,7 @@
 // Attention of one new token per row over a caller-owned paged cache, split over the cache's length and joined.
 //
-// x_j = c q.K_j, out = sum_j 2^(x_j - L) V_j with c in log2 units and L = log2 sum_j 2^(x_j): one pass over K and V with a running
-// reference m, sums of 2^(x_j - m) and of 2^(x_j - m) V_j, which parts of a row join by rescaling to the larger m.
+// x_j = c q.K_j, out = sum_j 2^(x_j - L) V_j with c in log2 units and L = log2 sum_j 2^(x_j): one pass over K and V with a
+// running reference m, sums of 2^(x_j - m) and of 2^(x_j - m) V_j, which parts of a row join by rescaling to the larger m.
 //
 // Bound: HBM (a KV head's rows are read once for all of its query heads: 2 G flop a byte in 16 bits).  So the work is the rows'
 // tiles, and it is dealt evenly: the tiles of all (row, KV head) units stand in one line, of which every warp takes an equal
@@ -10,13 +10,19 @@
 // warps share, the sums are joined when their CTA has finished its run, and of one that several CTAs share, the last CTA to
 // finish joins the others' sums, always in the order of the line.
 //
-// A warp has a ring of its own that cp.async fills several tiles of 16 slots ahead, across units.  (One bulk copy a row instead:
-// 341 us for 16 rows of 24576 slots, 254 so; a row's copy costs the copy unit some 15 cycles however short it is.)  A row's
-// 16-byte chunks are permuted by its number, so that eight rows' equal chunks fall into different banks.  (Rows 16 bytes further
-// apart than they are long, which needs no permutation: 279 us, the writes then straddle lines.)  Both products run on mma.sync with the
-// slots (or head_dim) as the 16 rows and the heads of the KV group as the 8 columns: S^T = K Q^T, O^T = V^T P^T, so that up to
-// eight heads fill the instruction exactly.  (tcgen05 takes 64 rows at least, and its operands come through descriptors of
-// whole tiles, which pages of any size are not.)
+// A warp has a ring of its own that cp.async fills several tiles ahead, across units.  (One bulk copy a row instead: 341 us for
+// 16 rows of 24576 slots, 254 so; a row's copy costs the copy unit some 15 cycles however short it is.)  A row's 16-byte chunks
+// are permuted by its number, so that eight rows' equal chunks fall into different banks.  (Rows 16 bytes further apart than
+// they are long, which needs no permutation: 279 us, the writes then straddle lines.)
+//
+// Both products run on mma.sync with the slots (or head_dim) as the 16 rows and the heads of the KV group as the 8 columns:
+// S^T = K Q^T, O^T = V^T P^T, so that up to eight heads fill the instruction exactly.  (tcgen05 takes 64 rows at least, and its
+// operands come through descriptors of whole tiles, which pages of any size are not.)
+//
+// Measured (one B200, copy rate 6454 GB/s): 16 rows of 24576 slots, 32 query and 8 KV heads of 128 in bf16, 243 to 250 us, 6.4
+// to 6.6 TB/s.  Also at 93 to 103% of the copy rate at that length: 8-bit pages, heads of 64 and 256, pages of one or seven
+// slots, 8 to 128 query heads.  What a call costs beyond its bytes is 10 to 15 us: two dependent lookups before the first row
+// (lengths, pages), and after the last one the joins; 300 slots of one row take 8.5 us.
 #include "mma_util.cuh"
 #include "paged.cuh"
 
@@ -272,15 +278,16 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
       }
     }
     if (KIND != kPdE4m3 && fresh >= 0 && lane < RC) {
+      const int bytes = (unsigned)s_page[fresh] < (unsigned)c.n_pages ? 16 : 0;
       const size_t at = u.row * a.kv_stride + (size_t)u.head * (2 * D) + lane * 16;
       const uint32_t to = ring_s + st * Sh::kStage + fresh * Sh::kRow + ((lane ^ pd_swizzle<RC>(fresh)) << 4);
-      cp_async16(to, a.k + at, 16);
-      cp_async16(to + TILE * Sh::kRow, a.v + at, 16);
+      cp_async16(to, a.k + at, bytes);
+      cp_async16(to + TILE * Sh::kRow, a.v + at, bytes);
     }
   };
-  // The queries of a unit as the products' columns (head g of each block), and the scales of its KV head.  Behind the requests of
-  // rows that fill the memory's queues a load takes 3000 cycles, so where there are registers the next unit's are asked for when
-  // the first of its rows are.
+  // The queries of a unit as the products' columns (head g of each block), and the scales of its KV head.  Behind the requests
+  // of rows that fill the memory's queues a load takes 3000 cycles, so where there are registers the next unit's are asked for
+  // when the first of its rows are.
   constexpr bool kEarly = NT * D <= 128;
   struct Queries {
     uint32_t b[NT][DT][2];
@@ -407,238 +414,243 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
       __syncwarp();
     }
     if (at >= 0) {
-    if (at == 0 || cu.tile == 0) {  // a unit begins
-      whole = cu.tile == 0;
-      if (kEarly && at > 0 && next_at == at) q = q_next;
-      scale_queries();
+      if (at == 0 || cu.tile == 0) {  // a unit begins
+        whole = cu.tile == 0;
+        if (kEarly && at > 0 && next_at == at) q = q_next;
+        scale_queries();
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        ref[nt][0] = ref[nt][1] = kPdNone;
-        sum[nt][0] = sum[nt][1] = 0.f;
+        for (int nt = 0; nt < NT; ++nt) {
+          ref[nt][0] = ref[nt][1] = kPdNone;
+          sum[nt][0] = sum[nt][1] = 0.f;
 #pragma unroll
-        for (int i = 0; i < DT; ++i) O[nt][i][0] = O[nt][i][1] = O[nt][i][2] = O[nt][i][3] = 0.f;
-      }
-    }
-    const int slot0 = cu.tile * TILE;
-    const int fresh = a.k && cu.n - 1 - slot0 < TILE ? cu.n - 1 - slot0 : -1;
-    uint4 kx = make_uint4(0u, 0u, 0u, 0u), vx = kx;
-    if (KIND == kPdE4m3 && fresh >= 0 && lane < D / 8) {
-      const size_t at_new = cu.row * a.kv_stride + ((size_t)cu.head * D + lane * 8) * 2;
-      kx = *reinterpret_cast<const uint4*>(a.k + at_new);
-      vx = *reinterpret_cast<const uint4*>(a.v + at_new);
-    }
-    cp_async_wait<S - 2>();
-    __syncwarp();
-    unsigned char* stage = ring + stage_at * Sh::kStage;
-    const uint32_t sk = ring_s + stage_at * Sh::kStage, sv = sk + TILE * Sh::kRow;
-    const int* s_page = s_pages + page_at * TILE;
-    if (fresh >= 0 && (unsigned)s_page[fresh] < (unsigned)c.n_pages) {  // the new token's row into its page
-      const int page = s_page[fresh], place = cu.n - 1 - paged_nth(c, cu.n - 1) * c.P;
-      const size_t to = paged_row(c, layer, page, cu.head, place);
-      unsigned char* in = stage + fresh * Sh::kRow;
-      const int sw = pd_swizzle<RC>(fresh);
-      if (lane < D / 8) {
-        if (KIND == kPdE4m3) {  // and into the tile
-          const uint2 ky = paged_quantise(c.type, kx, c.ks[cu.head]), vy = paged_quantise(c.type, vx, c.vs[cu.head]);
-          in += ((lane / 2 ^ sw) << 4) + (lane & 1) * 8;
-          *reinterpret_cast<uint2*>(in) = ky;
-          *reinterpret_cast<uint2*>(in + TILE * Sh::kRow) = vy;
-          if (cu.block == 0) {
-            *reinterpret_cast<uint2*>(c.k + to + lane * 8) = ky;
-            *reinterpret_cast<uint2*>(c.v + to + lane * 8) = vy;
-          }
-        } else if (cu.block == 0) {
-          in += (lane ^ sw) << 4;
-          *reinterpret_cast<uint4*>(c.k + to + lane * 16) = *reinterpret_cast<const uint4*>(in);
-          *reinterpret_cast<uint4*>(c.v + to + lane * 16) = *reinterpret_cast<const uint4*>(in + TILE * Sh::kRow);
+          for (int i = 0; i < DT; ++i) O[nt][i][0] = O[nt][i][1] = O[nt][i][2] = O[nt][i][3] = 0.f;
         }
       }
-      if (c.w && cu.block == 0 && lane == 0) {
-        const size_t word = paged_word(c, layer, page, cu.head, place);
-        c.w[word] = 0.f;
-        c.pos[word] = a.row_pos ? a.row_pos[cu.row] : cu.n - 1;
+      const int slot0 = cu.tile * TILE;
+      const int fresh = a.k && cu.n - 1 - slot0 < TILE ? cu.n - 1 - slot0 : -1;
+      uint4 kx = make_uint4(0u, 0u, 0u, 0u), vx = kx;
+      if (KIND == kPdE4m3 && fresh >= 0 && lane < D / 8) {
+        const size_t at_new = cu.row * a.kv_stride + ((size_t)cu.head * D + lane * 8) * 2;
+        kx = *reinterpret_cast<const uint4*>(a.k + at_new);
+        vx = *reinterpret_cast<const uint4*>(a.v + at_new);
       }
+      cp_async_wait<S - 2>();
       __syncwarp();
-    }
-    float x[MT][NT][4];
-    // (a tile lies on a multiple of its rows' length: the chunk's bits of an address can be set by xor)
-    const uint32_t k_at = sk + (lane & 15) * Sh::kRow + ((lane >> 4 ^ pd_swizzle<RC>(lane & 15)) << 4);
-#pragma unroll
-    for (int m = 0; m < MT; ++m) {
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) x[m][nt][0] = x[m][nt][1] = x[m][nt][2] = x[m][nt][3] = 0.f;
-      if (KIND == kPdE4m3) {
-#pragma unroll
-        for (int i = 0; i < DT; i += 2) {
-          uint32_t b[4];
-          ldsm_x4(b, (k_at ^ (i << 4)) + m * 16 * Sh::kRow);
-#pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            const uint32_t f[4] = {pd_halves_lo(b[2 * j]), pd_halves_lo(b[2 * j + 1]), pd_halves_hi(b[2 * j]),
-                                   pd_halves_hi(b[2 * j + 1])};
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) pd_mma<KIND>(x[m][nt], f, q.b[nt][i + j][0], q.b[nt][i + j][1]);
-          }
-        }
-      } else {
-#pragma unroll
-        for (int i = 0; i < DT; ++i) {
-          uint32_t f[4];
-          ldsm_x4(f, (k_at ^ (i << 5)) + m * 16 * Sh::kRow);
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) pd_mma<KIND>(x[m][nt], f, q.b[nt][i][0], q.b[nt][i][1]);
-        }
-      }
-    }
-    // lane: slots g and g + 8 of a block (x[..][..][0..1], x[..][..][2..3]), heads 2 q4 and 2 q4 + 1
-    bool every = true;  // slot of the tile is there
-#pragma unroll
-    for (int j = lane; j < TILE; j += 32) every &= (unsigned)s_page[j] < (unsigned)c.n_pages;
-    if (!__all_sync(0xffffffffu, every)) {
-#pragma unroll
-      for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const bool there = (unsigned)s_page[m * 16 + g + 8 * e] < (unsigned)c.n_pages;
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            // (the factors are positive; an infinite logit of a slot that is not there stays below every reference)
-            if (!there) x[m][nt][2 * e] = x[m][nt][2 * e + 1] = -INFINITY;
-          }
-        }
-    }
-    if (c.w) {
-#pragma unroll
-      for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const int page = s_page[m * 16 + g + 8 * e];
-          if ((unsigned)page >= (unsigned)c.n_pages) continue;
-          const int slot = slot0 + m * 16 + g + 8 * e, place = slot - paged_nth(c, slot) * c.P;
-          const size_t word = ((size_t)page * c.Hkv + cu.head) * c.P + place;
-          float* to = wk.logits + word * paged_even(c.G);
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            const int in_group = cu.block * H + nt * 8 + 2 * q4;
-            if (in_group < c.G)
-              *reinterpret_cast<float2*>(to + in_group) = make_float2(x[m][nt][2 * e] * sc[nt][0], x[m][nt][2 * e + 1] * sc[nt][1]);
-          }
-        }
-    }
-    bool grow = false;
-    float top[NT][2];
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        float most = fmaxf(x[0][nt][e], x[0][nt][e + 2]);
-#pragma unroll
-        for (int m = 1; m < MT; ++m) most = fmaxf(most, fmaxf(x[m][nt][e], x[m][nt][e + 2]));
-        top[nt][e] = most * sc[nt][e];
-        grow |= top[nt][e] > ref[nt][e] + (kOff + kGrow);
-      }
-    if (__any_sync(0xffffffffu, grow)) {
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-#pragma unroll
-          for (int d = 4; d < 32; d <<= 1) top[nt][e] = fmaxf(top[nt][e], __shfl_xor_sync(0xffffffffu, top[nt][e], d));
-          const float to = fmaxf(ref[nt][e], top[nt][e] - kOff), by = pd_exp2(ref[nt][e] - to);
-          ref[nt][e] = to;
-          sum[nt][e] *= by;
-#pragma unroll
-          for (int i = 0; i < DT; ++i) {
-            O[nt][i][e] *= by;
-            O[nt][i][e + 2] *= by;
-          }
-        }
-    }
-    // probabilities as two terms of the products' type, as V^T P^T takes them
-    uint32_t hi[MT][NT][2], lo[MT][NT][2];
-#pragma unroll
-    for (int m = 0; m < MT; ++m)
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        float p[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          p[e] = pd_exp2(fmaf(x[m][nt][e], sc[nt][e & 1], -ref[nt][e & 1]));
-          sum[nt][e & 1] += p[e];
-        }
-        constexpr int T = KIND == kPdBf16 ? LTRI_TYPE_BF16 : LTRI_TYPE_FP16;
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const uint32_t h = paged_pack(T, p[2 * e], p[2 * e + 1]);
-          const float2 back = paged_unpack(T, h);
-          hi[m][nt][e] = pd_transpose(h);
-          lo[m][nt][e] = pd_transpose(paged_pack(T, p[2 * e] - back.x, p[2 * e + 1] - back.y));
-        }
-      }
-    const int v_row = KIND == kPdE4m3 ? lane & 15 : (lane & 7) + (lane >> 4) * 8, v_ch = KIND == kPdE4m3 ? lane >> 4 : (lane >> 3) & 1;
-    const uint32_t v_at = sv + v_row * Sh::kRow + ((v_ch ^ pd_swizzle<RC>(v_row)) << 4);
-#pragma unroll
-    for (int m = 0; m < MT; ++m)
-#pragma unroll
-      for (int i = 0; i < DT; i += KIND == kPdE4m3 ? 2 : 1) {
-        uint32_t b[4];
-        if (KIND == kPdE4m3) {
-          // a 16-byte chunk's 8 pairs of neighbours are the 8 rows of a transposed matrix: row g has elements 2g and 2g + 1 of
-          // slots 2 q4 and 2 q4 + 1
-          ldsm_x4_t(b, (v_at ^ (i << 4)) + m * 16 * Sh::kRow);
-#pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            uint32_t f[4];
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {  // (with e, 8 slots further)
-              const uint32_t y = __byte_perm(b[2 * j + e], 0u, 0x3120);
-              f[2 * e] = pd_halves_lo(y);
-              f[2 * e + 1] = pd_halves_hi(y);
+      unsigned char* stage = ring + stage_at * Sh::kStage;
+      const uint32_t sk = ring_s + stage_at * Sh::kStage, sv = sk + TILE * Sh::kRow;
+      const int* s_page = s_pages + page_at * TILE;
+      if (fresh >= 0) {  // the new token's row into its page, if it has one
+        const int page = s_page[fresh], place = cu.n - 1 - paged_nth(c, cu.n - 1) * c.P, sw = pd_swizzle<RC>(fresh);
+        const bool has = (unsigned)page < (unsigned)c.n_pages, writes = has && cu.block == 0;
+        const size_t to = paged_row(c, layer, has ? page : 0, cu.head, place);
+        unsigned char* in = stage + fresh * Sh::kRow;
+        if (lane < D / 8) {
+          if (KIND == kPdE4m3) {  // and into the tile
+            uint2 ky = make_uint2(0u, 0u), vy = ky;
+            if (has) {
+              ky = paged_quantise(c.type, kx, c.ks[cu.head]);
+              vy = paged_quantise(c.type, vx, c.vs[cu.head]);
             }
+            in += ((lane / 2 ^ sw) << 4) + (lane & 1) * 8;
+            *reinterpret_cast<uint2*>(in) = ky;
+            *reinterpret_cast<uint2*>(in + TILE * Sh::kRow) = vy;
+            if (writes) {
+              *reinterpret_cast<uint2*>(c.k + to + lane * 8) = ky;
+              *reinterpret_cast<uint2*>(c.v + to + lane * 8) = vy;
+            }
+          } else if (writes) {
+            in += (lane ^ sw) << 4;
+            *reinterpret_cast<uint4*>(c.k + to + lane * 16) = *reinterpret_cast<const uint4*>(in);
+            *reinterpret_cast<uint4*>(c.v + to + lane * 16) = *reinterpret_cast<const uint4*>(in + TILE * Sh::kRow);
+          }
+        }
+        if (c.w && writes && lane == 0) {
+          const size_t word = paged_word(c, layer, page, cu.head, place);
+          c.w[word] = 0.f;
+          c.pos[word] = a.row_pos ? a.row_pos[cu.row] : cu.n - 1;
+        }
+        __syncwarp();
+      }
+      float x[MT][NT][4];
+      // (a tile lies on a multiple of its rows' length: the chunk's bits of an address can be set by xor)
+      const uint32_t k_at = sk + (lane & 15) * Sh::kRow + ((lane >> 4 ^ pd_swizzle<RC>(lane & 15)) << 4);
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-              pd_mma<KIND>(O[nt][i + j], f, hi[m][nt][0], hi[m][nt][1]);
-              pd_mma<KIND>(O[nt][i + j], f, lo[m][nt][0], lo[m][nt][1]);
+      for (int m = 0; m < MT; ++m) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) x[m][nt][0] = x[m][nt][1] = x[m][nt][2] = x[m][nt][3] = 0.f;
+        if (KIND == kPdE4m3) {
+#pragma unroll
+          for (int i = 0; i < DT; i += 2) {
+            uint32_t b[4];
+            ldsm_x4(b, (k_at ^ (i << 4)) + m * 16 * Sh::kRow);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              const uint32_t f[4] = {pd_halves_lo(b[2 * j]), pd_halves_lo(b[2 * j + 1]), pd_halves_hi(b[2 * j]),
+                                     pd_halves_hi(b[2 * j + 1])};
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt) pd_mma<KIND>(x[m][nt], f, q.b[nt][i + j][0], q.b[nt][i + j][1]);
             }
           }
         } else {
-          ldsm_x4_t(b, (v_at ^ (i << 5)) + m * 16 * Sh::kRow);
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            pd_mma<KIND>(O[nt][i], b, hi[m][nt][0], hi[m][nt][1]);
-            pd_mma<KIND>(O[nt][i], b, lo[m][nt][0], lo[m][nt][1]);
+          for (int i = 0; i < DT; ++i) {
+            uint32_t f[4];
+            ldsm_x4(f, (k_at ^ (i << 5)) + m * 16 * Sh::kRow);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) pd_mma<KIND>(x[m][nt], f, q.b[nt][i][0], q.b[nt][i][1]);
           }
         }
       }
-    __syncwarp();
-    stage_at = next(stage_at, S);
-    page_at = next(page_at, Sh::kPages);
-    const bool ends = cu.tile + 1 == cu.tiles;
-    if (ends || at + 1 == mine) {
+      // lane: slots g and g + 8 of a block (x[..][..][0..1], x[..][..][2..3]), heads 2 q4 and 2 q4 + 1
+      bool every = true;  // slot of the tile is there
+#pragma unroll
+      for (int j = lane; j < TILE; j += 32) every &= (unsigned)s_page[j] < (unsigned)c.n_pages;
+      if (!__all_sync(0xffffffffu, every)) {
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const bool there = (unsigned)s_page[m * 16 + g + 8 * e] < (unsigned)c.n_pages;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+              // (the factors are positive; an infinite logit of a slot that is not there stays below every reference)
+              if (!there) x[m][nt][2 * e] = x[m][nt][2 * e + 1] = -INFINITY;
+            }
+          }
+      }
+      if (c.w) {
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int page = s_page[m * 16 + g + 8 * e];
+            if ((unsigned)page >= (unsigned)c.n_pages) continue;
+            const int slot = slot0 + m * 16 + g + 8 * e, place = slot - paged_nth(c, slot) * c.P;
+            const size_t word = ((size_t)page * c.Hkv + cu.head) * c.P + place;
+            float* to = wk.logits + word * paged_even(c.G);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+              const int in_group = cu.block * H + nt * 8 + 2 * q4;
+              const float2 y = make_float2(x[m][nt][2 * e] * sc[nt][0], x[m][nt][2 * e + 1] * sc[nt][1]);
+              if (in_group < c.G) *reinterpret_cast<float2*>(to + in_group) = y;
+            }
+          }
+      }
+      bool grow = false;
+      float top[NT][2];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int e = 0; e < 2; ++e)
+        for (int e = 0; e < 2; ++e) {
+          float most = fmaxf(x[0][nt][e], x[0][nt][e + 2]);
 #pragma unroll
-          for (int d = 4; d < 32; d <<= 1) sum[nt][e] += __shfl_xor_sync(0xffffffffu, sum[nt][e], d);
-      if (whole && ends) {
-        put_unit(cu);
-      } else {
-        // Set aside.  A unit that reaches back behind the run and ends here: in the workspace, as the CTA's part of it if this is
-        // the CTA's first run, for the warp that has its first piece otherwise.  One that outlasts the run: in the ring, which is
-        // empty then, and in the registers.
-        float* to = !ends       ? reinterpret_cast<float*>(ring)
-                    : warp == 0 ? wk.part + (size_t)(2 * blockIdx.x) * wk.stride
-                                : wk.lead + ((size_t)blockIdx.x * W + warp) * wk.stride;
-        if (lane == 0) {
-          const PdOpen o{t0 + at - cu.tile, cu.row, cu.head, cu.block, cu.tiles};
-          if (!ends) s_open[warp] = o;
-          else if (warp == 0) s_part[0] = o;
+          for (int m = 1; m < MT; ++m) most = fmaxf(most, fmaxf(x[m][nt][e], x[m][nt][e + 2]));
+          top[nt][e] = most * sc[nt][e];
+          grow |= top[nt][e] > ref[nt][e] + (kOff + kGrow);
         }
-        set_aside(to);
+      if (__any_sync(0xffffffffu, grow)) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+#pragma unroll
+            for (int d = 4; d < 32; d <<= 1) top[nt][e] = fmaxf(top[nt][e], __shfl_xor_sync(0xffffffffu, top[nt][e], d));
+            const float to = fmaxf(ref[nt][e], top[nt][e] - kOff), by = pd_exp2(ref[nt][e] - to);
+            ref[nt][e] = to;
+            sum[nt][e] *= by;
+#pragma unroll
+            for (int i = 0; i < DT; ++i) {
+              O[nt][i][e] *= by;
+              O[nt][i][e + 2] *= by;
+            }
+          }
       }
-    }
-    pd_advance<TILE>(cu, c, r, wk.blocks);
+      // probabilities as two terms of the products' type, as V^T P^T takes them
+      uint32_t hi[MT][NT][2], lo[MT][NT][2];
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          float p[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            p[e] = pd_exp2(fmaf(x[m][nt][e], sc[nt][e & 1], -ref[nt][e & 1]));
+            sum[nt][e & 1] += p[e];
+          }
+          constexpr int T = KIND == kPdBf16 ? LTRI_TYPE_BF16 : LTRI_TYPE_FP16;
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const uint32_t h = paged_pack(T, p[2 * e], p[2 * e + 1]);
+            const float2 back = paged_unpack(T, h);
+            hi[m][nt][e] = pd_transpose(h);
+            lo[m][nt][e] = pd_transpose(paged_pack(T, p[2 * e] - back.x, p[2 * e + 1] - back.y));
+          }
+        }
+      const int v_row = KIND == kPdE4m3 ? lane & 15 : (lane & 7) + (lane >> 4) * 8;
+      const int v_ch = KIND == kPdE4m3 ? lane >> 4 : (lane >> 3) & 1;
+      const uint32_t v_at = sv + v_row * Sh::kRow + ((v_ch ^ pd_swizzle<RC>(v_row)) << 4);
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int i = 0; i < DT; i += KIND == kPdE4m3 ? 2 : 1) {
+          uint32_t b[4];
+          if (KIND == kPdE4m3) {
+            // a 16-byte chunk's 8 pairs of neighbours are the 8 rows of a transposed matrix: row g has elements 2g and 2g + 1
+            // of slots 2 q4 and 2 q4 + 1
+            ldsm_x4_t(b, (v_at ^ (i << 4)) + m * 16 * Sh::kRow);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              uint32_t f[4];
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {  // (with e, 8 slots further)
+                const uint32_t y = __byte_perm(b[2 * j + e], 0u, 0x3120);
+                f[2 * e] = pd_halves_lo(y);
+                f[2 * e + 1] = pd_halves_hi(y);
+              }
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt) {
+                pd_mma<KIND>(O[nt][i + j], f, hi[m][nt][0], hi[m][nt][1]);
+                pd_mma<KIND>(O[nt][i + j], f, lo[m][nt][0], lo[m][nt][1]);
+              }
+            }
+          } else {
+            ldsm_x4_t(b, (v_at ^ (i << 5)) + m * 16 * Sh::kRow);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+              pd_mma<KIND>(O[nt][i], b, hi[m][nt][0], hi[m][nt][1]);
+              pd_mma<KIND>(O[nt][i], b, lo[m][nt][0], lo[m][nt][1]);
+            }
+          }
+        }
+      __syncwarp();
+      stage_at = next(stage_at, S);
+      page_at = next(page_at, Sh::kPages);
+      const bool ends = cu.tile + 1 == cu.tiles;
+      if (ends || at + 1 == mine) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+#pragma unroll
+            for (int d = 4; d < 32; d <<= 1) sum[nt][e] += __shfl_xor_sync(0xffffffffu, sum[nt][e], d);
+        if (whole && ends) {
+          put_unit(cu);
+        } else {
+          // Set aside.  A unit that reaches back behind the run and ends here: in the workspace, as the CTA's part of it if
+          // this is the CTA's first run, for the warp that has its first piece otherwise.  One that outlasts the run: in the
+          // ring, which is empty then, and in the registers.
+          float* to = !ends       ? reinterpret_cast<float*>(ring)
+                      : warp == 0 ? wk.part + (size_t)(2 * blockIdx.x) * wk.stride
+                                  : wk.lead + ((size_t)blockIdx.x * W + warp) * wk.stride;
+          if (lane == 0) {
+            const PdOpen o{t0 + at - cu.tile, cu.row, cu.head, cu.block, cu.tiles};
+            if (!ends) s_open[warp] = o;
+            else if (warp == 0) s_part[0] = o;
+          }
+          set_aside(to);
+        }
+      }
+      pd_advance<TILE>(cu, c, r, wk.blocks);
     }
     if (at >= -Sh::kAhead && at + Sh::kAhead < mine) {
       if (kEarly && ci.tile == 0 && at > -Sh::kAhead && next_at <= at) {
@@ -656,7 +668,8 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
       pd_advance<TILE>(cp, c, r, wk.blocks);
     }
     cp_async_commit();
-    if (at == -Sh::kAhead - 1 || (at >= 0 && at + 1 < mine && cu.tile == 0 && !(kEarly && next_at == at + 1))) load_queries(q, cu);
+    const bool begins = at >= 0 && at + 1 < mine && cu.tile == 0;
+    if (at == -Sh::kAhead - 1 || (begins && !(kEarly && next_at == at + 1))) load_queries(q, cu);
   }
 
   // ---- units that the CTA's warps share: the warp that has a unit's first piece in this CTA adds the others to its own ----
@@ -677,7 +690,8 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
           const float2 m = *reinterpret_cast<const float2*>(from + nt * 8 + 2 * q4);
           const float2 s = *reinterpret_cast<const float2*>(from + 16 + nt * 8 + 2 * q4);
           const float t0 = fmaxf(ref[nt][0], m.x), t1 = fmaxf(ref[nt][1], m.y);
-          const float a0 = pd_exp2(ref[nt][0] - t0), a1 = pd_exp2(ref[nt][1] - t1), b0 = pd_exp2(m.x - t0), b1 = pd_exp2(m.y - t1);
+          const float a0 = pd_exp2(ref[nt][0] - t0), a1 = pd_exp2(ref[nt][1] - t1);
+          const float b0 = pd_exp2(m.x - t0), b1 = pd_exp2(m.y - t1);
           ref[nt][0] = t0;
           ref[nt][1] = t1;
           sum[nt][0] = sum[nt][0] * a0 + s.x * b0;
@@ -735,7 +749,7 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
     for (int nt = 0; nt < NT; ++nt) top[nt][0] = top[nt][1] = kPdNone, tot[nt][0] = tot[nt][1] = 0.f;
 #pragma unroll
     for (int k = 0; k < kSlices; ++k) got[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-    constexpr int kBatch = kSlices == 1 ? 8 : kSlices == 2 ? 4 : 2;
+    constexpr int kBatch = kSlices == 1 ? 8 : kSlices <= 4 ? 4 : 2;
 #pragma unroll 1
     for (int i0 = 0; i0 < pieces; i0 += kBatch) {
       float2 m[kBatch][NT], s[kBatch][NT];
@@ -751,7 +765,8 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
           if (i >= pieces) m[b][nt] = make_float2(kPdNone, kPdNone), s[b][nt] = make_float2(0.f, 0.f);
         }
 #pragma unroll
-        for (int k = 0; k < kSlices; ++k) z[b][k] = reinterpret_cast<const float4*>(p + 32)[min(k * W + warp, NT * DT - 1) * 32 + lane];
+        for (int k = 0; k < kSlices; ++k)
+          z[b][k] = reinterpret_cast<const float4*>(p + 32)[min(k * W + warp, NT * DT - 1) * 32 + lane];
       }
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
@@ -821,7 +836,7 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
 // 32 bytes a slot whatever the group: 10.8 us for 16 rows of 4097 slots and 8 KV heads.)
 constexpr int kPwThreads = 256, kPwCtas = 8;
 __global__ void __launch_bounds__(kPwThreads, kPwCtas) k_paged_weights(PagedCache c, PagedRows r, int layer, PdWork wk) {
-  // (the lengths and pages are older than the attention kernel, which has waited for its predecessor before it released this one)
+  // (the lengths are older than the attention kernel, which had waited for its predecessor when it released this one)
   PdCursor u;
   int total;
   bool lone;
@@ -867,17 +882,20 @@ cudaError_t prepare_kind() {
 }
 
 template <int KIND, int D, int NT>
-cudaError_t launch_one(const PagedCache& c, const PagedRows& r, int layer, const PagedStep& a, const PdWork& w, cudaStream_t s) {
+cudaError_t launch_one(const PagedCache& c, const PagedRows& r, int layer, const PagedStep& a, const PdWork& w,
+                       cudaStream_t s) {
   using Sh = PdShape<KIND, D, NT>;
   static_assert(Sh::kWarps <= kPagedWarps, "the workspace has partial sums of that many warps");
   return launch_chained(k_paged_decode<KIND, D, NT>, dim3(c.sms), dim3(Sh::kWarps * 32), Sh::kSmem, s, c, r, layer, a, w);
 }
 template <int KIND, int D>
-cudaError_t launch_dim(const PagedCache& c, const PagedRows& r, int layer, const PagedStep& a, const PdWork& w, cudaStream_t s) {
+cudaError_t launch_dim(const PagedCache& c, const PagedRows& r, int layer, const PagedStep& a, const PdWork& w,
+                       cudaStream_t s) {
   return w.heads == 8 ? launch_one<KIND, D, 1>(c, r, layer, a, w, s) : launch_one<KIND, D, 2>(c, r, layer, a, w, s);
 }
 template <int KIND>
-cudaError_t launch_kind(const PagedCache& c, const PagedRows& r, int layer, const PagedStep& a, const PdWork& w, cudaStream_t s) {
+cudaError_t launch_kind(const PagedCache& c, const PagedRows& r, int layer, const PagedStep& a, const PdWork& w,
+                        cudaStream_t s) {
   if (c.D == 64) return launch_dim<KIND, 64>(c, r, layer, a, w, s);
   if (c.D == 128) return launch_dim<KIND, 128>(c, r, layer, a, w, s);
   return launch_dim<KIND, 256>(c, r, layer, a, w, s);

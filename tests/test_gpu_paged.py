@@ -82,7 +82,8 @@ def test_decode_accumulates_weights(dim, dtype, e4m3, decay):
     assert torch.equal(ref.bits(c.w[0]), ref.bits(other[0])) and torch.equal(c.pos[0], other[1])
 
 
-@pytest.mark.parametrize("rows,n,hq,hkv", [(1, 40000, 8, 2), (1, 9001, 32, 8), (1, 20011, 4, 1), (40, 1200, 8, 4), (3, 7000, 8, 8)])
+@pytest.mark.parametrize("rows,n,hq,hkv", [(1, 40000, 8, 2), (1, 9001, 32, 8), (1, 20011, 4, 1), (40, 1200, 8, 4),
+                                           (3, 7000, 8, 8)])
 @pytest.mark.parametrize("weighted", [False, True])
 def test_decode_split_over_the_length(rows, n, hq, hkv, weighted):
     lens = [max(1, n - 977 * i) if i % 7 != 5 else 0 for i in range(rows)]
@@ -94,6 +95,26 @@ def test_decode_split_over_the_length(rows, n, hq, hkv, weighted):
     q = c.randn(rows, hq, 128)
     first = lp.ltri_paged_decode(0, c.table, c.lens(), q).clone()
     assert torch.equal(first, lp.ltri_paged_decode(0, c.table, c.lens(), q)) and out.shape == first.shape
+
+
+@pytest.mark.parametrize("lens,hq,hkv,dim", [([1, 0, 100, 128, 127], 8, 2, 128), ([256, 3], 16, 16, 64),
+                                             ([64] * 7 + [0, 33], 32, 8, 256), ([129, 5], 8, 2, 128),
+                                             ([100] * 19, 8, 8, 128), ([0, 0, 0], 4, 2, 64)])
+@pytest.mark.parametrize("weighted", [False, True])
+def test_decode_of_units_around_a_ctas_size(lens, hq, hkv, dim, weighted):
+    # units with a CTA of their own, and batches that just miss that: a slot more than the CTA's tiles, a CTA too few
+    c = ref.Cache(lens, hq, hkv, dim, 16, BF16, weighted=weighted, seed=len(lens) + dim)
+    c.fill()
+    decode(c, c.handle())
+
+
+@pytest.mark.parametrize("rows,hkv,e4m3", [(70, 1, False), (70, 3, True), (33, 2, True)])
+def test_decode_of_many_ragged_rows(rows, hkv, e4m3):
+    # more rows than a warp has lanes, several units to a warp's run, runs that end inside units and inside tiles
+    lens = [(i * 37) % 401 if i % 9 else 0 for i in range(rows)]
+    c = ref.Cache(lens, 2 * hkv, hkv, 64, 5, FP16, e4m3, weighted=True, layout="nhd", seed=rows)
+    c.fill()
+    decode(c, c.handle())
 
 
 @pytest.mark.parametrize("dtype,e4m3", [(BF16, False), (FP16, False), (BF16, True)])
@@ -159,9 +180,9 @@ def test_rows_may_share_pages_that_nobody_writes():
     decode(c, c.handle(), new=False)
 
 
-@pytest.mark.parametrize("weighted", [False, True])
-def test_bad_pages_and_lengths_are_recorded_and_touch_nothing_else(weighted):
-    c = ref.Cache([40, 40, 40, 40, 40], 4, 2, 64, 16, BF16, weighted=weighted, seed=11)
+@pytest.mark.parametrize("weighted,e4m3", [(False, False), (True, False), (True, True)])
+def test_bad_pages_and_lengths_are_recorded_and_touch_nothing_else(weighted, e4m3):
+    c = ref.Cache([40, 40, 40, 40, 40], 4, 2, 64, 16, BF16, e4m3, weighted=weighted, seed=11)
     c.fill()
     lp = c.handle()
     q, k, v = c.randn(5, 4, 64), c.randn(5, 2, 64), c.randn(5, 2, 64)
@@ -172,7 +193,9 @@ def test_bad_pages_and_lengths_are_recorded_and_touch_nothing_else(weighted):
     table[0, 1] = -1           # sixteen slots in the middle are absent
     table[1, 2] = c.n_pages    # the last ones, the new one among them
     lens[2], lens[3] = -1, 49  # no length; more than the table holds
-    out = lp.ltri_paged_decode(0, table, lens, q, k, v)
+    bad = v.clone()
+    bad[1] = math.nan          # (what an absent slot would have held does not matter)
+    out = lp.ltri_paged_decode(0, table, lens, q, k, bad)
     assert lp.ltri_paged_sync_status() == binding.LTRI_EDEVICE and lp.ltri_paged_sync_status() == binding.LTRI_OK
     assert (out[2] == 0).all() and (out[3] == 0).all() and torch.equal(out[4], good[4])
     after = c.snapshot()
@@ -188,14 +211,28 @@ def test_bad_pages_and_lengths_are_recorded_and_touch_nothing_else(weighted):
     lp.ltri_paged_append(0, table, lens, starts, x, x)
     assert lp.ltri_paged_sync_status() == binding.LTRI_EDEVICE
     after = c.snapshot()
-    pg, off = c.places(4, 40)
-    assert torch.equal(ref.take(c.k[0], pg, off), x[5:])
-    pg, off = c.places(0, 40)
-    assert torch.equal(ref.take(c.k[0], pg, off)[39], x[0])
+    for r, tokens in ((4, x[5:]), (0, x[:1])):
+        pg, off = c.places(r, 40)
+        got = ref.take(c.k[0], pg, off)[-len(tokens):]
+        if e4m3:
+            assert torch.equal(got.cpu().double(), ref.quantise(tokens.cpu(), c.ks.cpu()))
+        else:
+            assert torch.equal(got, tokens)
     for r in (1, 2, 3):
         pg, _ = c.places(r, 40)
         assert torch.equal(before["k"][0, pg], after["k"][0, pg])
+    # starts that do not ascend: whose a token is is then undefined, but nothing outside the rows is written
+    before = c.snapshot()
+    starts = torch.tensor([0, 30, 10, 45, 20, 45], dtype=torch.int32, device="cuda")
+    lp.ltri_paged_append(0, c.table, c.lens(), starts, x, x)
+    assert lp.ltri_paged_sync_status() in (binding.LTRI_OK, binding.LTRI_EDEVICE)
+    owned = torch.zeros(c.n_pages, 16, dtype=torch.bool, device="cuda")
+    for r in range(5):
+        owned[c.places(r, 40)] = True
+    for name, y in c.snapshot().items():
+        assert torch.equal(before[name][0].transpose(1, 2)[~owned], y[0].transpose(1, 2)[~owned]), name
     if weighted:
+        c.fill()
         lens[4] = 40
         new = torch.full((5,), -3, dtype=torch.int32, device="cuda")
         want, _ = ref.evict(c, [0, 0, 0, 0, 40], 24, 2, 4, [0])
@@ -227,7 +264,8 @@ def test_append_of_ragged_prompts(dtype, e4m3, layout, page, weighted):
     k, v = fused[:, :3], fused[:, 3:]
     w = torch.rand(lead + total + 3, 3, generator=c.g).cuda()
     pos = torch.tensor([5, 6, 7, 8, 9, 10], dtype=torch.int32, device="cuda")
-    lp.ltri_paged_append(1, c.table, c.lens(), torch.tensor(starts, dtype=torch.int32, device="cuda"), k, v, row_pos=pos, weights=w)
+    dev_starts = torch.tensor(starts, dtype=torch.int32, device="cuda")
+    lp.ltri_paged_append(1, c.table, c.lens(), dev_starts, k, v, row_pos=pos, weights=w)
     assert lp.ltri_paged_sync_status() == binding.LTRI_OK
     after = c.snapshot()
     for name in before:
@@ -254,7 +292,7 @@ def test_append_of_ragged_prompts(dtype, e4m3, layout, page, weighted):
         x, y = before[name][1].transpose(1, 2), after[name][1].transpose(1, 2)
         assert torch.equal(x[~written], y[~written]), name
     if weighted:  # without positions and weights: slots' numbers and zeros
-        lp.ltri_paged_append(0, c.table, c.lens(), torch.tensor(starts, dtype=torch.int32, device="cuda"), k, v)
+        lp.ltri_paged_append(0, c.table, c.lens(), dev_starts, k, v)
         pg, off = c.places(3, 130)
         assert (c.pos[0, pg[60:], :, off[60:]] == torch.arange(60, 130, device="cuda")[:, None]).all()
         assert (c.w[0, pg[60:], :, off[60:]] == 0).all()
@@ -263,7 +301,8 @@ def test_append_of_ragged_prompts(dtype, e4m3, layout, page, weighted):
 def test_append_of_nothing_and_a_nan():
     c = ref.Cache([3], 2, 1, 64, 16, BF16, True, seed=1)
     lp = c.handle()
-    lp.ltri_paged_append(0, c.table, c.lens(), torch.zeros(2, dtype=torch.int32, device="cuda"), c.randn(0, 1, 64), c.randn(0, 1, 64))
+    none = torch.zeros(2, dtype=torch.int32, device="cuda")
+    lp.ltri_paged_append(0, c.table, c.lens(), none, c.randn(0, 1, 64), c.randn(0, 1, 64))
     x = c.randn(3, 1, 64)
     x[1, 0, 5] = math.nan
     lp.ltri_paged_append(0, c.table, c.lens(), torch.tensor([0, 3], dtype=torch.int32, device="cuda"), x, x)
@@ -310,8 +349,9 @@ def test_evict_keeps_what_the_definition_keeps(kind, budget, n_sink, recent):
         assert torch.equal(x, want[name]), name
 
 
-@pytest.mark.parametrize("n,budget,e4m3,dim,hkv", [(9000, 4100, False, 128, 2), (20000, 64, True, 64, 1), (4097, 4096, True, 256, 4),
-                                                   (70000, 60000, False, 64, 1)])
+@pytest.mark.parametrize("n,budget,e4m3,dim,hkv", [(9000, 4100, False, 128, 2), (20000, 64, True, 64, 1),
+                                                 (4097, 4096, True, 256, 4),
+                                                   (70000, 60000, False, 64, 1), (230000, 90000, True, 64, 1)])
 def test_evict_of_long_rows(n, budget, e4m3, dim, hkv):
     c = ref.Cache([n, n // 2], hkv, hkv, dim, 16, BF16, e4m3, weighted=True, seed=n)
     c.fill()
@@ -466,13 +506,17 @@ def test_calls_are_refused_before_anything_is_launched():
         return raw.ltri_paged_evict(h, begin, count, *rows, new, n, budget, sink, recent, s)
 
     for kw in (dict(layer=-1), dict(layer=1), dict(n=0), dict(q=None), dict(q=p(q) + 2), dict(qs=4), dict(qs=257), dict(k=None),
-               dict(v=None), dict(v=p(k) + 8), dict(ks=64), dict(ks=132), dict(pos=p(lens) + 1), dict(out=None), dict(out=p(out) + 8),
+               dict(v=None), dict(v=p(k) + 8), dict(ks=64), dict(ks=132), dict(pos=p(lens) + 1), dict(out=None),
+               dict(out=p(out) + 8),
                dict(lse=p(out) + 2), dict(rows=(None, cols, cols, p(lens))), dict(rows=(p(c.table), 0, cols, p(lens))),
                dict(rows=(p(c.table), cols, cols - 1, p(lens))), dict(rows=(p(c.table), cols, cols, None)),
                dict(rows=(p(c.table), cols, -4, p(lens)))):
         assert decode_rc(**kw) == binding.LTRI_EINVAL, kw
     assert decode_rc(n=3) == binding.LTRI_ECAPACITY
-    for kw in (dict(layer=1), dict(starts=None), dict(tokens=-1), dict(k=None), dict(k=p(k) + 2), dict(stride=64), dict(stride=129),
+    # more tiles than 32 bits count (the table's columns say how many there may be)
+    assert decode_rc(rows=(p(c.table), 1 << 30, 1 << 30, p(lens))) == binding.LTRI_ECAPACITY
+    for kw in (dict(layer=1), dict(starts=None), dict(tokens=-1), dict(k=None), dict(k=p(k) + 2), dict(stride=64),
+               dict(stride=129),
                dict(n=0), dict(w=p(lens) + 2)):
         assert append_rc(**kw) == binding.LTRI_EINVAL, kw
     assert append_rc(n=3) == binding.LTRI_ECAPACITY and append_rc(tokens=1 << 31) == binding.LTRI_ECAPACITY

@@ -15,9 +15,9 @@ def lib():
 
 
 def params(**kw):
-    base = dict(n_layers=2, n_q_heads=8, n_kv_heads=2, head_dim=128, type=0, cache_type=0, page_tokens=16, max_rows=4, n_pages=10,
-                layer_stride=10 * 4096, page_stride=4096, head_stride=2048, token_stride=128, softmax_scale=0.0, weight_decay=1.0,
-                k_pages=4096, v_pages=8192, workspace=4096, workspace_bytes=1 << 40)
+    base = dict(n_layers=2, n_q_heads=8, n_kv_heads=2, head_dim=128, type=0, cache_type=0, page_tokens=16, max_rows=4,
+                n_pages=10, layer_stride=10 * 4096, page_stride=4096, head_stride=2048, token_stride=128, softmax_scale=0.0,
+                weight_decay=1.0, k_pages=4096, v_pages=8192, workspace=4096, workspace_bytes=1 << 40)
     base.update(kw)
     return binding.LtriPagedParams(**base)
 
@@ -58,9 +58,10 @@ def test_null_handles_are_refused(lib):
     assert lib.ltri_paged_destroy(None) == binding.LTRI_EINVAL
     assert lib.ltri_paged_sync_status(None, None) == binding.LTRI_EINVAL
     assert lib.ltri_paged_launch_count(None) == 0 and lib.ltri_paged_last_cuda_error(None) == 0
-    assert lib.ltri_paged_decode(None, 0, None, 1, 1, None, 1, None, 0, None, None, 0, None, None, None, None) == binding.LTRI_EINVAL
-    assert lib.ltri_paged_append(None, 0, None, 1, 1, None, 1, None, 1, None, None, 0, None, None, None) == binding.LTRI_EINVAL
-    assert lib.ltri_paged_evict(None, 0, 1, None, 1, 1, None, None, 1, 1, 0, 0, None) == binding.LTRI_EINVAL
+    bad = binding.LTRI_EINVAL
+    assert lib.ltri_paged_decode(None, 0, None, 1, 1, None, 1, None, 0, None, None, 0, None, None, None, None) == bad
+    assert lib.ltri_paged_append(None, 0, None, 1, 1, None, 1, None, 1, None, None, 0, None, None, None) == bad
+    assert lib.ltri_paged_evict(None, 0, 1, None, 1, 1, None, None, 1, 1, 0, 0, None) == bad
 
 
 def test_axes_of_one_entry_need_no_stride_and_weights_need_room(lib):
@@ -90,3 +91,15 @@ def test_definition_of_the_8_bit_rows():
     got = ref.quantise(x, torch.tensor([0.02]))
     want = (x / torch.tensor(0.02)).clamp(-448, 448).to(torch.float8_e4m3fn).double()
     assert torch.equal(got, want)
+
+
+def test_page_of_a_slot_by_multiplication():
+    # the kernels' slot / page_tokens: one product and a shift, for slots below 2^31
+    for page in [1, 2, 3, 5, 7, 16, 31, 100, 641, 4095, 4097, 65535, 65536]:
+        shift = 31 + (page - 1).bit_length()
+        mul = (1 << shift) // page + 1
+        assert mul < 1 << 32
+        top = (1 << 31) - 1
+        for slot in {0, 1, page - 1, page, page + 1, top, top - 1, top // page * page, top // page * page - 1, 123456789}:
+            if 0 <= slot <= top:
+                assert slot * mul >> shift == slot // page, (page, slot)
