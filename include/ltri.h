@@ -382,13 +382,20 @@ int ltri_segment_map_static(const int32_t* Mq, int m, int64_t theta_q, int max_s
  * Device memory that these calls read is not looked at on the host, so they can be captured into a CUDA graph and
  * replayed with other contents.  A length outside [0, table_pages * page_tokens] makes its row empty, a page outside
  * [0, n_pages) its slots absent; both are recorded as LTRI_EDEVICE for ltri_paged_sync_status, and nothing outside the
- * caller's buffers is touched.  Rows of a batch may name the same page (a shared prompt) as long as no call writes to it:
- * appended slots, accumulated weights and evicted rows need pages of their row's own, or their values are undefined.
+ * caller's buffers is touched.  What lies in slots behind a row's length is neither read nor changed, whatever it holds.
+ * Rows of a batch may name the same page (a shared prompt) as long as no call writes to it: appended slots, accumulated
+ * weights and evicted rows need pages of their row's own, or their values are undefined.
  *
  * The calls of one handle must use one stream or be ordered by the caller, replays of graphs that captured them included:
- * they share its workspace.  Handles are independent of each other, also over the same pages.  Every call runs on the
- * device that was current when its handle was created, whichever device is current later.  Outputs are the same bits for
- * the same inputs. */
+ * they share its workspace, and two that overlap leave its counters, and with them later calls, undefined.  Handles are
+ * independent of each other, also over the same pages (a workspace of its own for each).  Every call runs on the device that
+ * was current when its handle was created, whichever device is current later; its memory has to be that device's.  Outputs
+ * are the same bits for the same inputs and the same device.
+ *
+ * Arguments are checked before anything is launched: LTRI_EINVAL for null or misaligned pointers, strides that are too
+ * short or no multiple of 16 bytes, layers out of range; LTRI_ECAPACITY for more rows than max_rows, or tables so large that
+ * n_rows * (table_pages * page_tokens / 16 + 1) * n_kv_heads (times the blocks of 16 query heads of a KV head, if it has
+ * more than 8) exceeds 2^30. */
 typedef struct ltri_paged ltri_paged; /* opaque host-side handle */
 
 enum {
@@ -410,15 +417,16 @@ typedef struct {
   float softmax_scale;           /* 0 -> 1/sqrt(head_dim) */
   float weight_decay;            /* accumulated weights are multiplied by this in every decode call, 0..1 */
   void *k_pages, *v_pages;       /* DEVICE, 16-byte aligned */
-  const float *k_scale, *v_scale; /* DEVICE [n_kv_heads], LTRI_TYPE_E4M3 only; read by every call */
+  const float *k_scale, *v_scale; /* DEVICE [n_kv_heads], positive, LTRI_TYPE_E4M3 only; read by every call */
   float* weights;                /* DEVICE or NULL */
   int32_t* positions;            /* DEVICE or NULL */
-  void* workspace;               /* DEVICE, caller-owned, 256-byte aligned */
+  void* workspace;               /* DEVICE, caller-owned, 256-byte aligned, of this handle alone */
   size_t workspace_bytes;        /* >= ltri_paged_workspace_bytes(params) */
 } ltri_paged_params;
 
-/* Bytes of device memory that `workspace` must provide (host only; pointers are ignored, except that weights == NULL
- * needs less).  0 if the parameters are invalid. */
+/* Bytes of device memory that `workspace` must provide (host only; pointers are ignored, except that a cache with weights
+ * needs more: 4 bytes a slot, layer and KV head for evictions, 4 a slot and query head for one layer's logits).  0 if the
+ * parameters are invalid. */
 size_t ltri_paged_workspace_bytes(const ltri_paged_params* p);
 
 /* Create a handle and initialise its workspace on `cuda_stream` (synchronises that stream once).  The pages, weights
@@ -431,7 +439,7 @@ int ltri_paged_destroy(ltri_paged* cache);
 /* Write the K/V rows of n_rows ragged prompts (or parts of prompts) into the pages of `layer`.
  *   starts   DEVICE int32 [n_rows + 1], ascending: tokens [starts[r], starts[r + 1]) of k and v belong to row r (there may
  *            be none).  They take the row's last slots: lens[r] counts them already.  Tokens in front of starts[0] and
- *            from starts[n_rows] on are ignored.
+ *            from starts[n_rows] on are ignored.  n_tokens (0 to 2^31 - 1) is what k and v have room for.
  *   k, v     [n_tokens][n_kv_heads][head_dim], token stride kv_stride elements (0: dense)
  *   row_pos  DEVICE int32 [n_rows]: position of each row's first new token (NULL: the slot's number)
  *   weights  DEVICE float [n_tokens][n_kv_heads]: what the slots have accumulated already (NULL: 0)
@@ -452,8 +460,8 @@ int ltri_paged_append(ltri_paged* cache, int layer, const int32_t* table, int ta
  *   lse  float [n_rows][n_q_heads] or NULL: log of the sum of exp(logit), to merge with attention over other tokens
  * With weights, every slot's weight becomes weight_decay * weight + the probabilities that the query heads of its KV head
  * give it; a slot that this call writes starts from 0.
- * Logits and sums are fp32; the probabilities enter the product with V as two terms of `type` (16 bits together, 22 in
- * fp16), so that the outputs carry the rounding of `type` once. */
+ * Logits and sums are fp32; the probabilities enter the product with V as two 16-bit terms (16 bits together over bf16
+ * pages, 22 over the others), so that the outputs carry the rounding of `type` once.  Logits of any magnitude below 10^38. */
 int ltri_paged_decode(ltri_paged* cache, int layer, const int32_t* table, int table_pages, int64_t table_stride,
                       const int32_t* lens, int n_rows, const void* q, int64_t q_stride, const void* k, const void* v,
                       int64_t kv_stride, const int32_t* row_pos, void* out, float* lse, void* cuda_stream);

@@ -411,13 +411,13 @@ __global__ void __launch_bounds__(kEvThreads, 2)
         for (int b = 0; b < kEvMoves; ++b) {
           const int mv = m + b * together + mine;
           const long long f = shfl_ll(from, min(31, mv));
-          if (f >= 0 && mv < moves) x[b] = __ldcs(reinterpret_cast<const uint4*>(pages + f));
+          if (f >= 0 && mv < moves) x[b] = __ldcg(reinterpret_cast<const uint4*>(pages + f));
         }
 #pragma unroll
         for (int b = 0; b < kEvMoves; ++b) {
           const int mv = m + b * together + mine;
           const long long g = shfl_ll(to, min(31, mv));
-          if (g >= 0 && mv < moves) __stcs(reinterpret_cast<uint4*>(pages + g), x[b]);
+          if (g >= 0 && mv < moves) __stcg(reinterpret_cast<uint4*>(pages + g), x[b]);
         }
       }
     }

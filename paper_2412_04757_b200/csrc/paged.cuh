@@ -139,16 +139,32 @@ __device__ __forceinline__ float2 paged_unpack(int type, uint32_t x) {
   return __half22float2(*reinterpret_cast<const __half2*>(&x));
 }
 
-// Eight elements of `type` as e4m3: the nearest value to element / scale, ties to even, clamped to the largest.
+// Eight elements of `type` as e4m3: the nearest value to element / scale (fp32's quotient), ties to even, clamped to the
+// largest.  The quotient lies within 2^-22 of the product with 1 / scale; where 2^-21 to either side rounds to the same value,
+// as it does unless the quotient almost is a midpoint of two, no division is needed.  (Appending 22700 tokens of eight KV heads
+// of 128: 34 us, with eight divisions a chunk 44.)
 __device__ __forceinline__ uint2 paged_quantise(int type, const uint4& x, float scale) {
   const uint32_t in[4] = {x.x, x.y, x.z, x.w};
-  uint32_t out[2] = {0u, 0u};
+  uint32_t out[2] = {0u, 0u}, other[2] = {0u, 0u};
+  const float r = __fdiv_rn(1.f, scale), lo = r * (1.f - 0x1p-21f), hi = r * (1.f + 0x1p-21f);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    float2 f = paged_unpack(type, in[i]);
+    const float2 f = paged_unpack(type, in[i]);
+    const float2 a = make_float2(f.x * lo, f.y * lo), b = make_float2(f.x * hi, f.y * hi);
+    out[i >> 1] |= (uint32_t)__nv_cvt_float2_to_fp8x2(a, __NV_SATFINITE, __NV_E4M3) << (16 * (i & 1));
+    other[i >> 1] |= (uint32_t)__nv_cvt_float2_to_fp8x2(b, __NV_SATFINITE, __NV_E4M3) << (16 * (i & 1));
+  }
+  const bool normal = fabsf(lo) >= 0x1p-126f && fabsf(hi) <= 3.0e38f;
+  if (normal && out[0] == other[0] && out[1] == other[1]) return make_uint2(out[0], out[1]);
+  out[0] = out[1] = 0u;
+#pragma unroll 1
+  for (int i = 0; i < 4; ++i) {
+    float2 f = paged_unpack(type, i == 0 ? x.x : i == 1 ? x.y : i == 2 ? x.z : x.w);
     f.x = __fdiv_rn(f.x, scale);
     f.y = __fdiv_rn(f.y, scale);
-    out[i >> 1] |= (uint32_t)__nv_cvt_float2_to_fp8x2(f, __NV_SATFINITE, __NV_E4M3) << (16 * (i & 1));
+    const uint32_t y = (uint32_t)__nv_cvt_float2_to_fp8x2(f, __NV_SATFINITE, __NV_E4M3) << (16 * (i & 1));
+    if (i < 2) out[0] |= y;
+    else out[1] |= y;
   }
   return make_uint2(out[0], out[1]);
 }

@@ -311,6 +311,24 @@ def test_append_of_nothing_and_a_nan():
     assert torch.isnan(got[1, 0, 5]) and int(torch.isnan(got).sum()) == 1
 
 
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+def test_append_rounds_every_quotient_to_the_nearest_8_bit_value(dtype):
+    # every finite 16-bit value against scales that make quotients ties, near ties, tiny and huge, and reciprocals that are
+    # not normal numbers
+    bits = torch.arange(1 << 16, dtype=torch.int32).to(torch.int16).view(dtype)
+    bits = torch.where(torch.isfinite(bits.float()), bits, 1.0).view(-1, 64)
+    scales = [1.0, 0.5, 1 / 3, 0.0123, 2.0 ** -9, 17 / 16, 2.0 ** 100, 2.0 ** 127, 2.0 ** -120, 1.1754944e-38, 1e-40, 3e38]
+    n = bits.shape[0]
+    c = ref.Cache([n], len(scales), len(scales), 64, 64, dtype, True, seed=1)
+    c.ks = c.vs = torch.tensor(scales, device="cuda")
+    lp = c.handle()
+    x = bits[:, None].expand(n, len(scales), 64).contiguous().cuda()
+    lp.ltri_paged_append(0, c.table, c.lens(), torch.tensor([0, n], dtype=torch.int32, device="cuda"), x, x)
+    pg, off = c.places(0, n)
+    got = ref.take(c.k[0], pg, off).cpu().double()
+    assert torch.equal(got, ref.quantise(x.cpu(), c.ks.cpu()))
+
+
 def weights_of(kind, c, shape):
     w = torch.rand(shape, generator=c.g)
     if kind == "ties":
