@@ -433,7 +433,7 @@ size_t ltri_paged_workspace_bytes(const ltri_paged_params* p);
  * and positions are left as they are. */
 int ltri_paged_create(const ltri_paged_params* p, void* cuda_stream, ltri_paged** out);
 
-/* Free the host handle.  Device memory stays with the caller. */
+/* Free the host handle.  Device memory stays with the caller, who keeps it until the calls in flight are through. */
 int ltri_paged_destroy(ltri_paged* cache);
 
 /* Write the K/V rows of n_rows ragged prompts (or parts of prompts) into the pages of `layer`.

@@ -434,7 +434,8 @@ class LtriPaged:
     k_pages, v_pages: [layers][pages][Hkv][page tokens][head_dim] CUDA tensors with the same strides (a permuted view of
     token-major pages, or the halves of one tensor, will do), of ``dtype`` or float8_e4m3fn with k_scale, v_scale (float32
     [Hkv]).  weights (float32) and positions (int32), both or neither: [layers][pages][Hkv][page tokens], contiguous.  The
-    tensors stay the caller's; the handle keeps references to them.
+    tensors stay the caller's; the handle keeps references to them.  It allocates its workspace on the stream that is current
+    when it is made: let it go only when its calls on other streams are through.
     """
 
     def __init__(self, k_pages, v_pages, n_q_heads, dtype=None, max_rows=1, k_scale=None, v_scale=None, weights=None,

@@ -34,10 +34,13 @@ bool validate(const ltri_paged_params* p) {
   // an axis of one entry may have any stride; the others keep 16-byte chunks aligned and rows apart from each other
   const struct { long long n, stride; } axes[4] = {{p->n_layers, p->layer_stride}, {p->n_pages, p->page_stride},
                                                    {p->n_kv_heads, p->head_stride}, {p->page_tokens, p->token_stride}};
+  double extent = 0.0;  // bytes; far from where 64 bits end, as are the workspace's
   for (const auto& a : axes) {
     if (a.stride < 0 || a.stride > (1ll << 42) || a.stride * es % 16) return false;
     if (a.n > 1 && a.stride < p->head_dim) return false;
+    extent += (double)(a.n - 1) * (double)a.stride * (double)es;
   }
+  if (extent > 0x1p56 || (double)p->n_layers * (double)p->n_pages * p->page_tokens * p->n_kv_heads > 0x1p48) return false;
   if (!std::isfinite(p->softmax_scale) || p->softmax_scale < 0.f) return false;
   if (!(p->weight_decay >= 0.f && p->weight_decay <= 1.f)) return false;
   return true;

@@ -30,7 +30,8 @@ def test_struct_size_matches_header():
     dict(n_layers=0), dict(n_q_heads=7), dict(n_q_heads=0), dict(n_kv_heads=0), dict(n_q_heads=130), dict(head_dim=96),
     dict(head_dim=512), dict(type=2), dict(type=-1), dict(cache_type=1), dict(cache_type=3), dict(page_tokens=0),
     dict(page_tokens=65537), dict(max_rows=0), dict(max_rows=65536), dict(n_pages=0), dict(n_pages=1 << 31),
-    dict(n_pages=(1 << 31) - 1, page_tokens=65536), dict(token_stride=132), dict(token_stride=64), dict(page_stride=-4096),
+    dict(n_pages=(1 << 31) - 1, page_tokens=65536), dict(n_pages=(1 << 31) - 1, page_stride=1 << 40),
+    dict(n_layers=65535, n_pages=1 << 30, page_tokens=512, n_kv_heads=64, n_q_heads=64), dict(token_stride=132), dict(token_stride=64), dict(page_stride=-4096),
     dict(layer_stride=0), dict(head_stride=2044), dict(softmax_scale=-1.0), dict(softmax_scale=float("nan")),
     dict(softmax_scale=float("inf")), dict(weight_decay=1.5), dict(weight_decay=-0.1), dict(weight_decay=float("nan")),
 ])
