@@ -48,6 +48,9 @@ struct PdShape {
   static_assert(kStages >= 3, "two tiles on their way and one in use");
 };
 
+// Parts of a unit, up to which the warp that hands in the last of them joins them.
+constexpr int kPdFew = 3;
+
 // Reference of sums that nothing has entered yet: below every logit, and finite.
 constexpr float kPdNone = -3.0e38f;
 
@@ -139,8 +142,8 @@ __device__ __forceinline__ int pd_deal(PdCursor& u, int& total, bool& lone, int 
     }
     return x;
   };
-  // the first 32 rows are kept
-  const int n0 = lane < r.n ? paged_len(c, r, lane) : 0;
+  // the first 64 rows are asked for at once, and kept
+  const int n0 = lane < r.n ? paged_len(c, r, lane) : 0, n1 = lane + 32 < r.n ? paged_len(c, r, lane + 32) : 0;
   if (r.n <= 32) {
     const unsigned rows = __ballot_sync(0xffffffffu, n0 > 0);
     const int units = __popc(rows) * per_row;
@@ -161,7 +164,8 @@ __device__ __forceinline__ int pd_deal(PdCursor& u, int& total, bool& lone, int 
   }
   const int inc0 = scan((n0 + TILE - 1) / TILE * per_row);
   total = __shfl_sync(0xffffffffu, inc0, 31);
-  for (int base = 32; base < r.n; base += 32) {
+  if (r.n > 32) total += __reduce_add_sync(0xffffffffu, (n1 + TILE - 1) / TILE * per_row);
+  for (int base = 64; base < r.n; base += 32) {
     const int row = base + lane;
     total += __reduce_add_sync(0xffffffffu, row < r.n ? (paged_len(c, r, row) + TILE - 1) / TILE * per_row : 0);
   }
@@ -170,7 +174,7 @@ __device__ __forceinline__ int pd_deal(PdCursor& u, int& total, bool& lone, int 
   if (left >= total) return per;
   for (int base = 0;; base += 32) {
     const int row = base + lane;
-    const int n = base == 0 ? n0 : row < r.n ? paged_len(c, r, row) : 0;
+    const int n = base == 0 ? n0 : base == 32 ? n1 : row < r.n ? paged_len(c, r, row) : 0;
     const int inc = base == 0 ? inc0 : scan((n + TILE - 1) / TILE * per_row);
     const unsigned in = __ballot_sync(0xffffffffu, left < inc);
     if (in) {
@@ -399,6 +403,60 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
             make_float4(O[nt][i][0], O[nt][i][1], O[nt][i][2], O[nt][i][3]);
     }
   };
+  // Adds a piece of the same unit to this warp's sums.
+  auto add = [&](const float* from) {
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const float2 m = *reinterpret_cast<const float2*>(from + nt * 8 + 2 * q4);
+      const float2 s = *reinterpret_cast<const float2*>(from + 16 + nt * 8 + 2 * q4);
+      const float t0 = fmaxf(ref[nt][0], m.x), t1 = fmaxf(ref[nt][1], m.y);
+      const float a0 = pd_exp2(ref[nt][0] - t0), a1 = pd_exp2(ref[nt][1] - t1);
+      const float b0 = pd_exp2(m.x - t0), b1 = pd_exp2(m.y - t1);
+      ref[nt][0] = t0;
+      ref[nt][1] = t1;
+      sum[nt][0] = sum[nt][0] * a0 + s.x * b0;
+      sum[nt][1] = sum[nt][1] * a1 + s.y * b1;
+#pragma unroll
+      for (int i = 0; i < DT; ++i) {
+        const float4 z = reinterpret_cast<const float4*>(from + 32)[(nt * DT + i) * 32 + lane];
+        O[nt][i][0] = O[nt][i][0] * a0 + z.x * b0;
+        O[nt][i][1] = O[nt][i][1] * a1 + z.y * b1;
+        O[nt][i][2] = O[nt][i][2] * a0 + z.z * b0;
+        O[nt][i][3] = O[nt][i][3] * a1 + z.w * b1;
+      }
+    }
+  };
+  // This CTA's part of a unit that other CTAs share is complete in this warp's sums: into the workspace with it.  Of a unit of
+  // few parts the last to hand in its own adds up all of them (in their order, so that it does not matter who it is) and
+  // returns true; units of many are left to the whole CTA.
+  const unsigned cta_run = max(1, W * per);
+  auto hand_in = [&](const PdOpen& o, bool begins) {
+    const unsigned first = (unsigned)o.begin / cta_run;
+    const int parts = (unsigned)(o.begin + o.tiles - 1) / cta_run - first + 1;
+    set_aside(wk.part + (size_t)(2 * blockIdx.x + (begins ? 1 : 0)) * wk.stride);
+    if (parts > kPdFew) {
+      if (lane == 0) s_part[begins ? 1 : 0] = o;
+      return false;
+    }
+    int last = 0;
+    __syncwarp();
+    if (lane == 0) {
+      int* count = wk.count + ((size_t)o.row * c.Hkv + o.head) * wk.blocks + o.block;
+      last = paged_arrive(count) == parts - 1;
+      if (last) *count = 0;
+    }
+    if (!__shfl_sync(0xffffffffu, last, 0)) return false;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      ref[nt][0] = ref[nt][1] = kPdNone;
+      sum[nt][0] = sum[nt][1] = 0.f;
+#pragma unroll
+      for (int i = 0; i < DT; ++i) O[nt][i][0] = O[nt][i][1] = O[nt][i][2] = O[nt][i][3] = 0.f;
+    }
+#pragma unroll 1
+    for (int i = 0; i < parts; ++i) add(wk.part + (size_t)(2 * (first + i) + (i == 0 ? 1 : 0)) * wk.stride);
+    return true;
+  };
   bool whole = false;   // the unit has begun in this run
   // Rounds: in round `at` tile `at` is used, the rows of tile at + kAhead are requested and the page numbers of tile
   // at + 2 kAhead.  A round's requests are one group, complete when the round kAhead later begins; only the first tiles' page
@@ -464,11 +522,8 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
             *reinterpret_cast<uint4*>(c.v + to + lane * 16) = *reinterpret_cast<const uint4*>(in + TILE * Sh::kRow);
           }
         }
-        if (c.w && writes && lane == 0) {
-          const size_t word = paged_word(c, layer, page, cu.head, place);
-          c.w[word] = 0.f;
-          c.pos[word] = a.row_pos ? a.row_pos[cu.row] : cu.n - 1;
-        }
+        if (c.w && writes && lane == 0)
+          c.pos[paged_word(c, layer, page, cu.head, place)] = a.row_pos ? a.row_pos[cu.row] : cu.n - 1;
         __syncwarp();
       }
       float x[MT][NT][4];
@@ -633,22 +688,20 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
           for (int e = 0; e < 2; ++e)
 #pragma unroll
             for (int d = 4; d < 32; d <<= 1) sum[nt][e] += __shfl_xor_sync(0xffffffffu, sum[nt][e], d);
-        if (whole && ends) {
-          put_unit(cu);
-        } else {
-          // Set aside.  A unit that reaches back behind the run and ends here: in the workspace, as the CTA's part of it if
-          // this is the CTA's first run, for the warp that has its first piece otherwise.  One that outlasts the run: in the
-          // ring, which is empty then, and in the registers.
-          float* to = !ends       ? reinterpret_cast<float*>(ring)
-                      : warp == 0 ? wk.part + (size_t)(2 * blockIdx.x) * wk.stride
-                                  : wk.lead + ((size_t)blockIdx.x * W + warp) * wk.stride;
-          if (lane == 0) {
-            const PdOpen o{t0 + at - cu.tile, cu.row, cu.head, cu.block, cu.tiles};
-            if (!ends) s_open[warp] = o;
-            else if (warp == 0) s_part[0] = o;
-          }
-          set_aside(to);
+        // A unit that reaches back behind the run and ends here is set aside for the warp that has its first piece, or, if
+        // that is another CTA's, handed in; one that outlasts the run stays in the registers, and in the ring, which is empty
+        // then.
+        const PdOpen o{t0 + at - cu.tile, cu.row, cu.head, cu.block, cu.tiles};
+        bool complete = whole && ends;
+        if (!ends) {
+          if (lane == 0) s_open[warp] = o;
+          set_aside(reinterpret_cast<float*>(ring));
+        } else if (!whole && warp > 0) {
+          set_aside(wk.lead + ((size_t)blockIdx.x * W + warp) * wk.stride);
+        } else if (!whole) {
+          complete = hand_in(o, false);
         }
+        if (complete) put_unit(cu);
       }
       pd_advance<TILE>(cu, c, r, wk.blocks);
     }
@@ -674,7 +727,6 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
 
   // ---- units that the CTA's warps share: the warp that has a unit's first piece in this CTA adds the others to its own ----
   __syncthreads();
-  const unsigned cta_run = max(1, W * per);
   {
     const PdOpen o = s_open[warp];
     if (o.tiles != 0 && (warp == 0 || o.begin >= t0)) {
@@ -682,43 +734,17 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
       const bool begins = o.begin >= c0, ends = end <= c1;
       const int last = (int)((unsigned)(min(end, c1) - 1 - c0) / (unsigned)per);  // warp
 #pragma unroll 1
-      for (int w = warp + 1; w <= last; ++w) {
-        const float* from = ends && w == last ? wk.lead + ((size_t)blockIdx.x * W + w) * wk.stride
-                                              : reinterpret_cast<const float*>(dsm + w * Sh::kRing);
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          const float2 m = *reinterpret_cast<const float2*>(from + nt * 8 + 2 * q4);
-          const float2 s = *reinterpret_cast<const float2*>(from + 16 + nt * 8 + 2 * q4);
-          const float t0 = fmaxf(ref[nt][0], m.x), t1 = fmaxf(ref[nt][1], m.y);
-          const float a0 = pd_exp2(ref[nt][0] - t0), a1 = pd_exp2(ref[nt][1] - t1);
-          const float b0 = pd_exp2(m.x - t0), b1 = pd_exp2(m.y - t1);
-          ref[nt][0] = t0;
-          ref[nt][1] = t1;
-          sum[nt][0] = sum[nt][0] * a0 + s.x * b0;
-          sum[nt][1] = sum[nt][1] * a1 + s.y * b1;
-#pragma unroll
-          for (int i = 0; i < DT; ++i) {
-            const float4 z = reinterpret_cast<const float4*>(from + 32)[(nt * DT + i) * 32 + lane];
-            O[nt][i][0] = O[nt][i][0] * a0 + z.x * b0;
-            O[nt][i][1] = O[nt][i][1] * a1 + z.y * b1;
-            O[nt][i][2] = O[nt][i][2] * a0 + z.z * b0;
-            O[nt][i][3] = O[nt][i][3] * a1 + z.w * b1;
-          }
-        }
-      }
-      if (begins && ends) {
-        PdCursor u;
-        u.row = o.row;
-        u.head = o.head;
-        u.block = o.block;
-        put_unit(u);
-      } else {
-        if (lane == 0) s_part[begins ? 1 : 0] = o;
-        set_aside(wk.part + (size_t)(2 * blockIdx.x + (begins ? 1 : 0)) * wk.stride);
-      }
+      for (int w = warp + 1; w <= last; ++w)
+        add(ends && w == last ? wk.lead + ((size_t)blockIdx.x * W + w) * wk.stride
+                              : reinterpret_cast<const float*>(dsm + w * Sh::kRing));
+      PdCursor u;
+      u.row = o.row;
+      u.head = o.head;
+      u.block = o.block;
+      if ((begins && ends) || hand_in(o, begins)) put_unit(u);
     }
   }
-  // ---- units that CTAs share: whoever comes last to one joins its parts, a slice a warp ----
+  // ---- units of many CTAs: whoever comes last to one joins its parts, a slice a warp ----
   __syncthreads();
   if (threadIdx.x < 2) {
     const PdOpen o = s_part[threadIdx.x];
@@ -832,25 +858,36 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
 }
 
 // weights[j] = decay * weights[j] + sum over the group's heads of 2^(x_j - L), from the logits that the attention left in L2.
-// Bound: latency (page number, then logits and weight): as many threads as the GPU holds, a slot each.  (Four CTAs an SM and
-// 32 bytes a slot whatever the group: 10.8 us for 16 rows of 4097 slots and 8 KV heads.)
-constexpr int kPwThreads = 256, kPwCtas = 8;
-__global__ void __launch_bounds__(kPwThreads, kPwCtas) k_paged_weights(PagedCache c, PagedRows r, int layer, PdWork wk) {
-  // (the lengths are older than the attention kernel, which had waited for its predecessor when it released this one)
+// Bound: latency (page number, then logits and weight), so a slot's page and weight are asked for ahead of its logits, the
+// first ones before the attention kernel is through.  (32 bytes a slot whatever the group, and nothing ahead: 10.8 us for 16
+// rows of 4097 slots and 8 KV heads, 9.5 so; eight CTAs an SM instead of four: a step of two layers 3 us longer.)
+constexpr int kPwThreads = 256, kPwCtas = 4;
+__global__ void __launch_bounds__(kPwThreads, kPwCtas)
+    k_paged_weights(PagedCache c, PagedRows r, int layer, PdWork wk, bool fresh) {
+  // (the lengths are older than the attention kernel, which had waited for its predecessor when it released this one; so are
+  // the weights, but for the new token's slot, which starts from 0)
   PdCursor u;
   int total;
   bool lone;
   const int per = pd_deal<kPwThreads>(u, total, lone, gridDim.x, blockIdx.x, 0, c, r, 1), t0 = blockIdx.x * per;
+  const int t1 = min(t0 + per, total);
+  float* weights = c.w + (size_t)layer * c.n_pages * c.Hkv * c.P;
+  size_t word = 0;
+  float old = 0.f;
+  int page = -1;
+  auto ask = [&]() {
+    const int slot = u.tile * kPwThreads + threadIdx.x, nth = paged_nth(c, slot);
+    page = slot < u.n ? paged_page(c, r, u.row, nth) : -1;
+    word = ((size_t)max(page, 0) * c.Hkv + u.head) * c.P + (slot - nth * c.P);
+    old = page < 0 || (fresh && slot == u.n - 1) ? 0.f : weights[word];
+  };
+  if (t0 < t1) ask();
   chain_wait();
-  for (int t = t0; t < min(t0 + per, total); ++t) {
-    const int slot = u.tile * kPwThreads + threadIdx.x;
-    const int nth = paged_nth(c, slot), page = slot < u.n ? paged_page(c, r, u.row, nth) : -1;
+  for (int t = t0; t < t1; ++t) {
+    if (t > t0) ask();
     if (page >= 0) {
-      const size_t word = ((size_t)page * c.Hkv + u.head) * c.P + (slot - nth * c.P);
       const float2* x = reinterpret_cast<const float2*>(wk.logits + word * paged_even(c.G));
       const float* l2 = wk.lse2 + (size_t)u.row * c.Hq + (size_t)u.head * c.G;
-      float* to = c.w + (size_t)layer * c.n_pages * c.Hkv * c.P + word;
-      const float old = *to;
       float p = 0.f;
       int h = 0;
 #pragma unroll 4
@@ -860,7 +897,7 @@ __global__ void __launch_bounds__(kPwThreads, kPwCtas) k_paged_weights(PagedCach
         p += pd_exp2(y.y - l2[h + 1]);
       }
       if (h < c.G) p += pd_exp2(x[h / 2].x - l2[h]);
-      *to = old * c.decay + p;
+      weights[word] = old * c.decay + p;
     }
     pd_advance<kPwThreads>(u, c, r, 1);
   }
@@ -925,7 +962,7 @@ cudaError_t launch_paged_decode(const PagedCache& c, const PagedRows& r, int lay
   else if (c.type == LTRI_TYPE_BF16) e = launch_kind<kPdBf16>(c, r, layer, a, w, s);
   else e = launch_kind<kPdFp16>(c, r, layer, a, w, s);
   if (e != cudaSuccess || !c.w) return e;
-  return launch_chained(k_paged_weights, dim3(c.sms * kPwCtas), dim3(kPwThreads), 0, s, c, r, layer, w);
+  return launch_chained(k_paged_weights, dim3(c.sms * kPwCtas), dim3(kPwThreads), 0, s, c, r, layer, w, a.k != nullptr);
 }
 
 }  // namespace ltri

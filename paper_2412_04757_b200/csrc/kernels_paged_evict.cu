@@ -30,7 +30,7 @@ constexpr int kEvMaxCluster = 8;    // (of sixteen CTAs too few run at once: 32 
 constexpr int kEvMaxSlots = 27136;  // keys and positions that a CTA can hold (212 KB); those of longer stretches are read again
 constexpr int kEvSlots = 1024, kEvLong = 8192;  // slots of a CTA: above the first a unit gets more CTAs where SMs are idle,
                                                 // above the second anyway
-constexpr int kEvBatch = 8;         // slots of a thread whose weights and positions are on their way
+constexpr int kEvBatch = 9;         // slots of a thread whose weights and positions are on their way
 constexpr int kEvCand = kEvThreads;       // keys around the cut that are ranked against each other
 constexpr int kEvGroup = 4;         // moves that a warp takes side by side
 constexpr int kEvMoves = 2;         // 16-byte chunks that a lane has on their way
@@ -109,6 +109,28 @@ __global__ void __launch_bounds__(kEvThreads, 2)
   };
   // The CTA's sum, least or largest value over the cluster: lane i asks CTA i.
   auto ask = [&](int* x, int none) { return lane < C ? *cluster.map_shared_rank(x, lane) : none; };
+  // ---- where one slot leaves, the last one's rows are on their way to its place from the beginning ----
+  const bool single = n - budget == 1, carries = single && rank == 0 && warp == kEvWarps - 1;
+  const int chunks = c.row_bytes / 16;  // 4, 8, 16 or 32 of 16 bytes: a move is 2 * chunks
+  uint4 carried[2];
+  float carried_w = 0.f;
+  int carried_pos = 0, carried_page = -1;
+  if (carries) {
+    const int nth = paged_nth(c, n - 1), place = n - 1 - nth * c.P;
+    carried_page = page_of(nth);
+    if (carried_page >= 0) {
+      const size_t from = paged_row(c, layer, carried_page, head, place);
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const int ch = k * 32 + lane;
+        if (ch < 2 * chunks)
+          carried[k] = __ldcg(reinterpret_cast<const uint4*>((ch >= chunks ? c.v + (ch - chunks) * 16 : c.k + ch * 16) + from));
+      }
+      const size_t at = paged_word(c, layer, carried_page, head, place);
+      carried_w = c.w[at];
+      carried_pos = c.pos[at];
+    }
+  }
   // ---- keys: a thread's slots in batches whose loads are all on their way at once; the newest position comes out of them ----
   const bool all_held = chunk <= held;
   int newest = INT_MIN;
@@ -159,7 +181,6 @@ __global__ void __launch_bounds__(kEvThreads, 2)
   lo = __reduce_min_sync(0xffffffffu, lo);
   hi = __reduce_max_sync(0xffffffffu, hi);
   stay = __reduce_add_sync(0xffffffffu, stay);
-  const bool single = n - budget == 1;
   if (single) {
 #pragma unroll
     for (int d = 16; d; d >>= 1) least = min(least, __shfl_xor_sync(0xffffffffu, least, d));
@@ -171,14 +192,30 @@ __global__ void __launch_bounds__(kEvThreads, 2)
     atomicAdd(&s_stay, stay);
   }
   cluster.sync();
-  int count = 0, gap = -1;           // moves; the hole of a single one
+  int count = 0;                     // moves
   int m_incl = 0, h_incl = 0;        // lane i: movers and holes up to CTA i
   if (single) {
     least = lane < C ? *cluster.map_shared_rank(&s_least, lane) : ~0ull;
 #pragma unroll
     for (int d = 16; d; d >>= 1) least = min(least, __shfl_xor_sync(0xffffffffu, least, d));
-    gap = 0x7fffffff - (int)(unsigned)least;
-    count = gap < n - 1;
+    const int gap = 0x7fffffff - (int)(unsigned)least;
+    if (carries && carried_page >= 0 && gap < n - 1) {
+      const int nth = paged_nth(c, gap), place = gap - nth * c.P, page = page_of(nth);
+      if (page >= 0) {
+        const size_t to = paged_row(c, layer, page, head, place);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const int ch = k * 32 + lane;
+          if (ch < 2 * chunks)
+            __stcg(reinterpret_cast<uint4*>((ch >= chunks ? c.v + (ch - chunks) * 16 : c.k + ch * 16) + to), carried[k]);
+        }
+        if (lane == 0) {
+          const size_t at = paged_word(c, layer, page, head, place);
+          c.w[at] = carried_w;
+          c.pos[at] = carried_pos;
+        }
+      }
+    }
   } else {
   {
     const unsigned l = lane < C ? *cluster.map_shared_rank(&s_lo, lane) : 0xffffffffu;
@@ -371,20 +408,20 @@ __global__ void __launch_bounds__(kEvThreads, 2)
   };
   // ---- moves: a lane finds out about one, then the warp copies them, K and V rows as 2 * row_bytes / 16 chunks a move ----
   const int stride = kEvWarps * C * kEvGroup;
-  const int chunks = c.row_bytes / 16, rounds = (2 * chunks + 31) / 32;  // (row_bytes: 64, 128, 256 or 512)
+  const int rounds = (2 * chunks + 31) / 32;
   const int together = 32 / min(32, 2 * chunks), mine = lane / min(32, 2 * chunks);  // moves that the lanes share at a time
   for (int base = (rank * kEvWarps + warp) * kEvGroup; base < count; base += 32 / kEvGroup * stride) {
     const int i = base + lane / kEvGroup * stride + lane % kEvGroup;
     long long from = -1, to = -1, wt = -1;
     float w = 0.f;
     int pos = 0;
-    int src = n - 1, dst = gap;
-    if (!single && all_held) {
+    int src = -1, dst = -1;
+    if (all_held) {
       src = entry(m_incl, i, false);
       dst = entry(h_incl, i, true);
     }
     if (i < count) {
-      if (!single && !all_held) {
+      if (!all_held) {
         const long long a0 = word(i), a1 = word(budget + i);
         src = a0 < 0 ? -1 : __ldcg(&c.list[a0]);
         dst = a1 < 0 ? -1 : __ldcg(&c.list[a1]);
