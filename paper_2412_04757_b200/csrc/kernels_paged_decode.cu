@@ -775,7 +775,7 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
     for (int nt = 0; nt < NT; ++nt) top[nt][0] = top[nt][1] = kPdNone, tot[nt][0] = tot[nt][1] = 0.f;
 #pragma unroll
     for (int k = 0; k < kSlices; ++k) got[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-    constexpr int kBatch = kSlices == 1 ? 8 : kSlices <= 4 ? 4 : 2;
+    constexpr int kBatch = kSlices <= 4 ? 4 : 2;  // (more make the passage longer, which costs as much as they save)
 #pragma unroll 1
     for (int i0 = 0; i0 < pieces; i0 += kBatch) {
       float2 m[kBatch][NT], s[kBatch][NT];
