@@ -22,7 +22,7 @@
 // Measured (one B200, copy rate 6454 GB/s): 16 rows of 24576 slots, 32 query and 8 KV heads of 128 in bf16, 243 to 250 us, 6.4
 // to 6.6 TB/s.  Also at 93 to 103% of the copy rate at that length: 8-bit pages, heads of 64 and 256, pages of one or seven
 // slots, 8 to 128 query heads.  What a call costs beyond its bytes is 10 to 15 us: two dependent lookups before the first row
-// (lengths, pages), and after the last one the joins; 300 slots of one row take 8.5 us.
+// (lengths, pages), and after the last one the joins; 300 slots of one row take 8.7 us.
 #include "mma_util.cuh"
 #include "paged.cuh"
 
@@ -45,11 +45,19 @@ struct PdShape {
   static constexpr int kPages = 2 * kStages;                    // tiles whose page numbers are known or on their way
   static constexpr int kRing = kStages * kStage;                // of a warp
   static constexpr int kSmem = kWarps * (kRing + kPages * kTile * 4);
+  // Blocks of 16 slots within a page are requested from one address, stepping; others a row at a time, from addresses that the
+  // lanes exchange.  For 16-bit rows of 128 the latter takes longer to issue, and the evener flow of requests pays: replayed
+  // from a graph 16 rows of 24576 slots take 244 us, 252 by steps (launched one by one 244 either way), one row of 131072 88.6
+  // and 91, one of 300 8.65 and 8.45.  Rows of 64 are about equal; 8-bit ones (59.5 us by steps, 63.4 without) and 16-bit rows
+  // of 256 (46.1 us, 48.3) are better off with the steps.
+  static constexpr bool kSteps = KIND == kPdE4m3 || kRow > 256;
   static_assert(kStages >= 3, "two tiles on their way and one in use");
 };
 
-// Parts of a unit, up to which the warp that hands in the last of them joins them.
-constexpr int kPdFew = 3;
+// Parts of a unit, up to which the warp that hands in the last of them joins them; more of them take a whole CTA, behind a
+// barrier.  (Always the CTA: 64 ragged rows in 8 bits 61.8 us, 59.5 so.  Up to 3 parts: 10 ragged rows of 1700 slots at
+// most 10.9 us, 10.1 to 10.5 so.  Up to 12 or 24: two rows of 4000 slots 14.1 us, 12.0 so.)
+constexpr int kPdFew = 6;
 
 // Reference of sums that nothing has entered yet: below every logit, and finite.
 constexpr float kPdNone = -3.0e38f;
@@ -219,7 +227,7 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
   unsigned char* ring = dsm + warp * Sh::kRing;
   int* s_pages = reinterpret_cast<int*>(dsm + W * Sh::kRing) + warp * Sh::kPages * TILE;
   const uint32_t ring_s = smem_u32(ring), pages_s = smem_u32(s_pages);
-  const bool one_page = c.P % 16 == 0;  // of a block of 16 slots
+  const bool one_page = Sh::kSteps && c.P % 16 == 0;  // of a block of 16 slots
 
   PdCursor cu;
   int total;
