@@ -394,8 +394,8 @@ int ltri_segment_map_static(const int32_t* Mq, int m, int64_t theta_q, int max_s
  *
  * Arguments are checked before anything is launched: LTRI_EINVAL for null or misaligned pointers, strides that are too
  * short or no multiple of 16 bytes, layers out of range; LTRI_ECAPACITY for more rows than max_rows, or tables so large that
- * n_rows * (table_pages * page_tokens / 16 + 1) * n_kv_heads (times the blocks of 16 query heads of a KV head, if it has
- * more than 8) exceeds 2^30. */
+ * table_pages * page_tokens exceeds 2^31 - 2^16 or n_rows * (table_pages * page_tokens / 16 + 1) * n_kv_heads (times the
+ * blocks of 16 query heads of a KV head, if it has more than 8) exceeds 2^30. */
 typedef struct ltri_paged ltri_paged; /* opaque host-side handle */
 
 enum {

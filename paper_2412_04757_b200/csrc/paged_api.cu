@@ -114,10 +114,10 @@ int check_rows(const ltri_paged* c, const int32_t* table, int table_pages, int64
   if (!aligned(table, 4) || !aligned(lens, 4) || n_rows < 1 || table_pages < 1) return LTRI_EINVAL;
   if (table_stride < 0 || (n_rows > 1 && table_stride < table_pages)) return LTRI_EINVAL;
   if (n_rows > c->p.max_rows) return LTRI_ECAPACITY;
-  // the kernels count the 16-slot tiles of all rows in 32 bits
+  // the kernels count the 16-slot tiles of all rows in 32 bits, and a row's slots with a stride of theirs behind its end
   const int64_t cap = (int64_t)table_pages * c->p.page_tokens;
   const int64_t units = (int64_t)c->p.n_kv_heads * c->blocks;
-  if (cap > 0x7fffffffll || (cap / 16 + 1) * n_rows > (1ll << 30) / units) return LTRI_ECAPACITY;
+  if (cap > 0x7fff0000ll || (cap / 16 + 1) * n_rows > (1ll << 30) / units) return LTRI_ECAPACITY;
   *r = PagedRows{table, table_stride, (int)cap, lens, n_rows};
   return LTRI_OK;
 }

@@ -502,6 +502,33 @@ def test_offsets_beyond_32_bits():
     assert ((out[0].cpu().double() - o).abs() <= o.abs() * 2.0 ** -8 + 2 * tol).all()
 
 
+def test_the_longest_row_and_tables_for_longer_ones():
+    # 32767 times the same page of 65536 slots: the softmax is that of one page, its log-sum larger by log(32767)
+    c = ref.Cache([65536], 1, 1, 64, 65536, BF16, seed=5)
+    c.fill()
+    lp = c.handle()
+    q = c.randn(1, 1, 64)
+    one = torch.empty(1, 1, device="cuda")
+    out1 = lp.ltri_paged_decode(0, c.table, c.lens(), q, lse=one)
+    table = c.table[:, :1].repeat(1, 32767).contiguous()
+    lens = torch.full((1,), 32767 * 65536, dtype=torch.int32, device="cuda")
+    many = torch.empty(1, 1, device="cuda")
+    out = lp.ltri_paged_decode(0, table, lens, q, lse=many)
+    assert lp.ltri_paged_sync_status() == binding.LTRI_OK
+    # a warp adds up 2^27 / 1184 < 113400 tiles one after the other; a tile's sum may lose 2^-23 of what is there, its two
+    # products with V as much each, and the output is the quotient, rounded
+    slack, most = 113400 * 2.0 ** -23, float(c.v[0, int(c.table_cpu[0, 0])].float().abs().max())
+    assert abs(float(many) - float(one) - math.log(32767)) < slack
+    assert float((out.float() - out1.float()).abs().max()) < (3 * slack + 2.0 ** -8) * most
+    # a table that could hold one slot more, and one of the largest row that 31 bits count, whatever the lengths are
+    for cols, page in ((32768, 65536), (2 ** 31 - 2 ** 16 + 1, 1), (2 ** 31 - 1, 1)):
+        d = ref.Cache([1], 1, 1, 64, page, BF16, seed=5)
+        h, n = d.handle(), d.lens()
+        rc = binding.load().ltri_paged_decode(h._h, 0, d.table.data_ptr(), cols, cols, n.data_ptr(), 1, q.data_ptr(), 0, None,
+                                              None, 0, None, out.data_ptr(), None, None)
+        assert rc == binding.LTRI_ECAPACITY and h.ltri_paged_launch_count() == 0
+
+
 def test_calls_are_refused_before_anything_is_launched():
     c = ref.Cache([20, 30], 4, 2, 64, 16, BF16, weighted=True, seed=1)
     c.fill()
