@@ -461,8 +461,8 @@ int ltri_paged_append(ltri_paged* cache, int layer, const int32_t* table, int ta
  * With weights, every slot's weight becomes weight_decay * weight + the probabilities that the query heads of its KV head
  * give it; a slot that this call writes starts from 0.
  * Logits and sums are fp32; the probabilities enter the product with V as two 16-bit terms (16 bits together over bf16
- * pages, 22 over the others), so that the outputs carry the rounding of `type` once.  Logits and products q.K of any magnitude below
- * 10^38. */
+ * pages, 22 over the others), so that the outputs carry the rounding of `type` once.  Logits and products q.K of any
+ * magnitude below 10^38. */
 int ltri_paged_decode(ltri_paged* cache, int layer, const int32_t* table, int table_pages, int64_t table_stride,
                       const int32_t* lens, int n_rows, const void* q, int64_t q_stride, const void* k, const void* v,
                       int64_t kv_stride, const int32_t* row_pos, void* out, float* lse, void* cuda_stream);
