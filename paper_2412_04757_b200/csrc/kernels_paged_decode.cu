@@ -454,6 +454,7 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
       if (last) *count = 0;
     }
     if (!__shfl_sync(0xffffffffu, last, 0)) return false;
+    __syncwarp();  // (what lane 0 has acquired, for the others: the shuffle orders no memory)
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       ref[nt][0] = ref[nt][1] = kPdNone;
