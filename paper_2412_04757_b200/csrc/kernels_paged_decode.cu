@@ -25,6 +25,7 @@
 // (lengths, pages), and after the last one the joins; 300 slots of one row take 8.7 us.
 #include "mma_util.cuh"
 #include "paged.cuh"
+#include "paged_deal.cuh"
 
 namespace ltri {
 
@@ -110,95 +111,6 @@ __device__ __forceinline__ uint32_t pd_halves_hi(uint32_t x) {
 template <int CHUNKS>
 __device__ __forceinline__ constexpr int pd_swizzle(int row) {
   return CHUNKS >= 8 ? row & 7 : (row >> 1) & 3;
-}
-
-// A place in the line of tiles.
-struct PdCursor {
-  int row, head, block, tile, tiles, n;
-};
-
-template <int TILE>
-__device__ __forceinline__ void pd_advance(PdCursor& u, const PagedCache& c, const PagedRows& r, int blocks) {
-  if (++u.tile < u.tiles) return;
-  u.tile = 0;
-  if (++u.block < blocks) return;
-  u.block = 0;
-  if (++u.head < c.Hkv) return;
-  u.head = 0;
-  do {
-    u.n = ++u.row < r.n ? paged_len(c, r, u.row) : 1;
-    u.tiles = (u.n + TILE - 1) / TILE;
-  } while (u.tiles == 0);
-}
-
-// All lanes of a warp: the tiles of the whole call, and the cursor of tile `runs_before` * per, where per is every run's length
-// (returned) when `runs` of them cover the line.
-// Where every unit can have a CTA of its own and a warp no more than one of its tiles, it begins with one, as if all were as
-// long as the CTAs' runs (`lone`; the cursor may then lie behind the unit's end): no two CTAs share a unit, and the join at
-// the end, two trips through L2, is spared.  (8 query heads, 2 KV heads, 100 slots: 7.1 us, 9.5 dealt evenly; with up to three
-// tiles a warp, 300 slots: 9.0 and 8.6.)
-template <int TILE>
-__device__ __forceinline__ int pd_deal(PdCursor& u, int& total, bool& lone, int runs, int runs_before, int warps,
-                                       const PagedCache& c, const PagedRows& r, int blocks) {
-  const int lane = threadIdx.x & 31, per_row = c.Hkv * blocks;
-  lone = false;
-  auto scan = [&](int x) {
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-      const int y = __shfl_up_sync(0xffffffffu, x, d);
-      if (lane >= d) x += y;
-    }
-    return x;
-  };
-  // the first 64 rows are asked for at once, and kept
-  const int n0 = lane < r.n ? paged_len(c, r, lane) : 0, n1 = lane + 32 < r.n ? paged_len(c, r, lane + 32) : 0;
-  if (r.n <= 32) {
-    const unsigned rows = __ballot_sync(0xffffffffu, n0 > 0);
-    const int units = __popc(rows) * per_row;
-    if (warps > 0 && __reduce_max_sync(0xffffffffu, n0) <= warps * TILE && units * warps <= runs) {
-      const int unit = (unsigned)runs_before / (unsigned)warps;
-      total = units * warps;
-      lone = true;
-      if (unit >= units) return 1;
-      const int nth = unit / per_row, in_row = unit - nth * per_row;
-      u.row = __fns(rows, 0, nth + 1);
-      u.n = __shfl_sync(0xffffffffu, n0, u.row);
-      u.tiles = (u.n + TILE - 1) / TILE;
-      u.tile = runs_before - unit * warps;
-      u.head = in_row / blocks;
-      u.block = in_row - u.head * blocks;
-      return 1;
-    }
-  }
-  const int inc0 = scan((n0 + TILE - 1) / TILE * per_row);
-  total = __shfl_sync(0xffffffffu, inc0, 31);
-  if (r.n > 32) total += __reduce_add_sync(0xffffffffu, (n1 + TILE - 1) / TILE * per_row);
-  for (int base = 64; base < r.n; base += 32) {
-    const int row = base + lane;
-    total += __reduce_add_sync(0xffffffffu, row < r.n ? (paged_len(c, r, row) + TILE - 1) / TILE * per_row : 0);
-  }
-  const int per = (int)((unsigned)(total + runs - 1) / (unsigned)runs);
-  int left = runs_before * per;
-  if (left >= total) return per;
-  for (int base = 0;; base += 32) {
-    const int row = base + lane;
-    const int n = base == 0 ? n0 : base == 32 ? n1 : row < r.n ? paged_len(c, r, row) : 0;
-    const int inc = base == 0 ? inc0 : scan((n + TILE - 1) / TILE * per_row);
-    const unsigned in = __ballot_sync(0xffffffffu, left < inc);
-    if (in) {
-      const int at = __ffs(in) - 1;
-      u.row = base + at;
-      u.n = __shfl_sync(0xffffffffu, n, at);
-      u.tiles = (u.n + TILE - 1) / TILE;
-      left -= __shfl_sync(0xffffffffu, inc, at) - u.tiles * per_row;
-      const int unit = (int)((unsigned)left / (unsigned)u.tiles);
-      u.tile = left - unit * u.tiles;
-      u.head = blocks == 1 ? unit : unit / blocks;
-      u.block = unit - u.head * blocks;
-      return per;
-    }
-    left -= __shfl_sync(0xffffffffu, inc, 31);
-  }
 }
 
 // A unit that a warp's run, or a CTA's, leaves unfinished.
@@ -438,9 +350,12 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
   // few parts the last to hand in its own adds up all of them (in their order, so that it does not matter who it is) and
   // returns true; units of many are left to the whole CTA.
   const unsigned cta_run = max(1, W * per);
+  auto parts_of = [&](const PdOpen& o) {  // (never behind the grid's, whatever the lengths have become meanwhile)
+    return (int)(min((unsigned)(o.begin + o.tiles - 1) / cta_run, gridDim.x - 1) - (unsigned)o.begin / cta_run) + 1;
+  };
   auto hand_in = [&](const PdOpen& o, bool begins) {
     const unsigned first = (unsigned)o.begin / cta_run;
-    const int parts = (unsigned)(o.begin + o.tiles - 1) / cta_run - first + 1;
+    const int parts = parts_of(o);
     set_aside(wk.part + (size_t)(2 * blockIdx.x + (begins ? 1 : 0)) * wk.stride);
     if (parts > kPdFew) {
       if (lane == 0) s_part[begins ? 1 : 0] = o;
@@ -759,7 +674,7 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
     const PdOpen o = s_part[threadIdx.x];
     int last = 0;
     if (o.tiles != 0) {
-      const int ctas = (unsigned)(o.begin + o.tiles - 1) / cta_run - (unsigned)o.begin / cta_run + 1;
+      const int ctas = parts_of(o);
       int* count = wk.count + ((size_t)o.row * c.Hkv + o.head) * wk.blocks + o.block;
       // (the other threads' stores are ordered in front of it by the barrier; with __threadfence on either side 3000 cycles)
       last = paged_arrive(count) == ctas - 1;
@@ -774,7 +689,7 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
     const PdOpen o = s_part[w];
     // part 0, and parts 1 to n - 1 at equal distances
     const unsigned first = (unsigned)o.begin / cta_run;
-    const int pieces = (unsigned)(o.begin + o.tiles - 1) / cta_run - first + 1;
+    const int pieces = parts_of(o);
     const size_t stride = 2 * wk.stride;
     const float *base = wk.part + first * stride, *p0 = base + wk.stride;
     // their sums, brought to the largest reference: the heads' in top and tot, the warp's slices' in got
