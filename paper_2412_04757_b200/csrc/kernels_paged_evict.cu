@@ -11,6 +11,10 @@
 // of a few powers of two); they are ranked against each other.  Where many are left (equal ones above all), up to two more
 // histograms go through the bin's range instead.
 //
+// Keys that shared memory does not hold are read again by every sweep.  Where rows share pages that are evicted, or somebody
+// else writes to them, the sweeps then differ: which slots stay is undefined, but bins, candidates and lists are bounded, and
+// every CTA of a cluster takes the same way through the barriers.
+//
 // Bound: latency where few slots leave, HBM where many rows move (read once, written once).  Measured: one slot of each of 256
 // units of 4097 slots, 16 us; 64 units of 29369 to 32768 slots cut to 5120, 100 us, 33 of them for the keys and lists, the rest
 // for 5000 moves a unit at 4.5 TB/s (read and written), which neither more rows on the way nor rows side by side raise.
@@ -263,10 +267,11 @@ __global__ void __launch_bounds__(kEvThreads, 2)
       }
       const int to = ev_scan(sum[0] + sum[1] + sum[2] + sum[3], s_scan);
       int from = to - sum[0] - sum[1] - sum[2] - sum[3];
-      if (from < need && need <= to) {
+      const bool lowest = tid == kEvThreads - 1;  // (has what no bin holds)
+      if (from < need && (need <= to || lowest)) {
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
-          if (from < need && need <= from + sum[b]) {
+          if ((from < need && need <= from + sum[b]) || (lowest && b == 3)) {
             s_bin = kEvBins - 1 - 4 * tid - b;
             s_above = from;
             s_in = sum[b];
@@ -287,13 +292,19 @@ __global__ void __launch_bounds__(kEvThreads, 2)
       // few keys left: every CTA gets all of them (in whatever order) and ranks them
       for (int j = begin + tid; j < end; j += kEvThreads) {
         const unsigned x = key(j);
-        if (x >= lo && x <= hi && x != 0xffffffffu) s_cand[atomicAdd(&s_cands, 1)] = x;
+        if (x >= lo && x <= hi && x != 0xffffffffu) {
+          const int at = atomicAdd(&s_cands, 1);
+          if (at < kEvCand) s_cand[at] = x;
+        }
       }
+      static_assert(kEvCand == kEvThreads, "a thread has a candidate");
+      s_all[tid] = 0u;
       cluster.sync();
+      if (tid == 0) s_cut = lo, s_above = 0, s_in = equal;
       if (warp < C) {
-        const int count = ask(&s_cands, 0), before = __reduce_add_sync(0xffffffffu, lane < warp ? count : 0);
+        const int count = min(ask(&s_cands, 0), kEvCand), before = __reduce_add_sync(0xffffffffu, lane < warp ? count : 0);
         const unsigned* from = cluster.map_shared_rank(s_cand, warp);
-        const int theirs = __shfl_sync(0xffffffffu, count, warp);
+        const int theirs = min(__shfl_sync(0xffffffffu, count, warp), kEvCand - before);
         for (int i = lane; i < theirs; i += 32) s_all[before + i] = from[i];
       }
       __syncthreads();
@@ -358,7 +369,7 @@ __global__ void __launch_bounds__(kEvThreads, 2)
         if (all_held) {
           s_pos[hole ? w1 - 1 - h - begin : w0 + m - begin] = j;
         } else if (to_words) {
-          const long long at = word(hole ? budget + h : m);
+          const long long at = !hole ? word(m) : h < n - budget ? word(budget + h) : -1;
           if (at >= 0) c.list[at] = j;
         }
       }
@@ -426,7 +437,7 @@ __global__ void __launch_bounds__(kEvThreads, 2)
         src = a0 < 0 ? -1 : __ldcg(&c.list[a0]);
         dst = a1 < 0 ? -1 : __ldcg(&c.list[a1]);
       }
-      if (src >= 0 && dst >= 0) {
+      if ((unsigned)src < (unsigned)n && (unsigned)dst < (unsigned)n) {
         const int sn = paged_nth(c, src), dn = paged_nth(c, dst), sp = page_of(sn), dp = page_of(dn);
         if (sp >= 0 && dp >= 0) {
           from = (long long)paged_row(c, layer, sp, head, src - sn * c.P);

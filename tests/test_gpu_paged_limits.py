@@ -1,0 +1,38 @@
+"""The paged cache's operators where the first tests of them do not reach: calls at the borders of what the header allows."""
+import math
+
+import pytest
+import torch
+
+from paper_2412_04757_b200 import binding
+from tests import paged_reference as ref
+
+pytestmark = pytest.mark.gpu
+
+BF16, FP16 = torch.bfloat16, torch.float16
+
+
+@pytest.mark.parametrize("n,budget", [(300, 100), (230000, 90000)])
+def test_rows_that_share_evicted_pages_are_undefined_but_in_bounds(n, budget):
+    # shared memory holds the shorter rows' keys, the longer ones' are read again while the other row moves its slots
+    c = ref.Cache([n, n - 11, 50], 1, 1, 64, 16, BF16, True, weighted=True, seed=n)
+    c.fill()
+    shared = c.table_cpu[0].clone()
+    own = torch.zeros(c.n_pages, dtype=torch.bool)
+    own[shared.long()[:-(-n // 16)]] = True
+    table = torch.stack([shared, shared, c.table_cpu[2]]).cuda()
+    lp, before = c.handle(), c.snapshot()
+    for _ in range(3):
+        got = torch.zeros(3, dtype=torch.int32, device="cuda")
+        lp.ltri_paged_evict(0, 1, table, c.lens(), got, budget, 16, 20)
+        assert lp.ltri_paged_sync_status() == binding.LTRI_OK
+        assert got.tolist() == [budget, budget, 50]
+    for name, x in c.snapshot().items():
+        assert torch.equal(x[0][~own.cuda()], before[name][0][~own.cuda()]), name
+    # and the handle is as it was: rows of their own afterwards are cut as the definition says
+    c.fill()
+    want, new = ref.evict(c, c.lens_cpu, budget, 16, 20, [0])
+    lp.ltri_paged_evict(0, 1, c.table, c.lens(), got, budget, 16, 20)
+    assert lp.ltri_paged_sync_status() == binding.LTRI_OK and got.tolist() == new
+    for name, x in c.snapshot().items():
+        assert torch.equal(x, want[name]), name

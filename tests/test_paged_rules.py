@@ -19,3 +19,22 @@ def test_what_an_arrival_has_acquired_is_ordered_for_the_threads_that_read_it():
         rest = text[at:]
         read = re.search(r"wk\.part \+", rest).start()
         assert re.search(r"__sync(warp|threads)\(\)", rest[:read]), rest[:200]
+
+
+def test_what_an_eviction_has_read_again_is_bounded_before_it_is_an_index():
+    # the keys of long rows are read several times, and rows that share pages change them in between: the candidates, the words
+    # of the lists and the slots that they name are compared with their arrays' sizes
+    text = re.sub(r"\s+", " ", source("kernels_paged_evict.cu"))
+    assert not re.search(r"s_cand\[\s*atomicAdd", text) and re.search(r"if \((\w+) < kEvCand\) s_cand\[\1\]", text)
+    assert re.search(r"min\(__shfl_sync\(0xffffffffu, count, warp\), kEvCand - before\)", text)
+    assert "h < n - budget ? word(budget + h) : -1" in text
+    moves = text[text.index("__ldcg(&c.list["):]
+    assert moves.index("(unsigned)src < (unsigned)n") < moves.index("paged_nth(c, src)")
+    assert moves.index("(unsigned)dst < (unsigned)n") < moves.index("paged_nth(c, dst)")
+
+
+def test_an_eviction_takes_a_bin_whatever_the_histogram_holds():
+    # s_bin, s_above and s_in are set in every round, by the thread of the lowest bins if no bin reaches the sum
+    text = re.sub(r"\s+", " ", source("kernels_paged_evict.cu"))
+    assert "const bool lowest = tid == kEvThreads - 1;" in text and "(need <= to || lowest)" in text
+    assert "(lowest && b == 3)" in text
