@@ -473,7 +473,7 @@ int ltri_paged_decode(ltri_paged* cache, int layer, const int32_t* table, int ta
  * ones, the lower slot).  The kept slots from `budget` on move, in ascending order, into the slots below it that are not
  * kept, in ascending order, with their weights and positions; no other row is touched.  (Attention does not depend on
  * the order of slots, so nothing else has to move: one row for a token appended to a full budget.)
- *   new_lens DEVICE int32 [n_rows]: min(lens, budget); may be lens itself
+ *   new_lens DEVICE int32 [n_rows]: min(lens, budget); may be lens itself (LTRI_EINVAL if it overlaps it otherwise)
  * The cache needs weights and positions. */
 int ltri_paged_evict(ltri_paged* cache, int layer_begin, int layer_count, const int32_t* table, int table_pages,
                      int64_t table_stride, const int32_t* lens, int32_t* new_lens, int n_rows, int budget, int n_sink,

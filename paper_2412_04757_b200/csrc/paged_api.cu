@@ -249,6 +249,9 @@ int ltri_paged_evict(ltri_paged* cache, int layer_begin, int layer_count, const 
   PagedRows r;
   if (const int rc = check_rows(cache, table, table_pages, table_stride, lens, n_rows, &r)) return rc;
   if (!aligned(new_lens, 4) || budget < 1 || n_sink < 0 || recent < 0 || (int64_t)n_sink + recent > budget) return LTRI_EINVAL;
+  // the same lengths or others: where one row's new length replaced another's old one, its CTAs would disagree about it
+  const uintptr_t l0 = reinterpret_cast<uintptr_t>(lens), l1 = reinterpret_cast<uintptr_t>(new_lens);
+  if (l0 != l1 && (l0 < l1 ? l1 - l0 : l0 - l1) < (uintptr_t)n_rows * sizeof(int32_t)) return LTRI_EINVAL;
   // (a cluster for every layer, row and KV head)
   if ((int64_t)layer_count * n_rows > (1ll << 24) / cache->p.n_kv_heads) return LTRI_ECAPACITY;
   OnDevice on(cache->device);

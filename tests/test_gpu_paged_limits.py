@@ -36,3 +36,23 @@ def test_rows_that_share_evicted_pages_are_undefined_but_in_bounds(n, budget):
     assert lp.ltri_paged_sync_status() == binding.LTRI_OK and got.tolist() == new
     for name, x in c.snapshot().items():
         assert torch.equal(x, want[name]), name
+
+
+def test_new_lengths_over_other_rows_lengths_are_refused():
+    c = ref.Cache([40, 30, 20], 2, 1, 64, 16, FP16, weighted=True, room=4, seed=2)
+    c.fill()
+    lp, before = c.handle(), c.snapshot()
+    both = torch.tensor([40, 30, 20, 7, 7, 7, 7], dtype=torch.int32, device="cuda")
+    for lens, new in ((both[:3], both[1:4]), (both[:3], both[2:5]), (both[1:4], both[:3]), (both[2:5], both[:3])):
+        with pytest.raises(binding.LtriError) as e:
+            lp.ltri_paged_evict(0, 1, c.table, lens, new, 8, 1, 1)
+        assert e.value.code == binding.LTRI_EINVAL
+    torch.cuda.synchronize()
+    assert lp.ltri_paged_launch_count() == 0 and both.tolist() == [40, 30, 20, 7, 7, 7, 7]
+    for name, x in c.snapshot().items():
+        assert torch.equal(x, before[name]), name
+    want, _ = ref.evict(c, [40, 30, 20], 8, 1, 1, [0])
+    lp.ltri_paged_evict(0, 1, c.table, both[:3], both[3:6], 8, 1, 1)  # side by side
+    assert lp.ltri_paged_sync_status() == binding.LTRI_OK and both.tolist() == [40, 30, 20, 8, 8, 8, 7]
+    for name, x in c.snapshot().items():
+        assert torch.equal(x, want[name]), name
