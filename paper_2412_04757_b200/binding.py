@@ -434,8 +434,8 @@ class LtriPaged:
     k_pages, v_pages: [layers][pages][Hkv][page tokens][head_dim] CUDA tensors with the same strides (a permuted view of
     token-major pages, or the halves of one tensor, will do), of ``dtype`` or float8_e4m3fn with k_scale, v_scale (float32
     [Hkv]).  weights (float32) and positions (int32), both or neither: [layers][pages][Hkv][page tokens], contiguous.  The
-    tensors stay the caller's; the handle keeps references to them.  It allocates its workspace on the stream that is current
-    when it is made: let it go only when its calls on other streams are through.
+    tensors stay the caller's; the handle keeps references to them.  It allocates its workspace on ``stream`` (None: the one
+    that is current when it is made): let it go only when its calls on other streams are through.
     """
 
     def __init__(self, k_pages, v_pages, n_q_heads, dtype=None, max_rows=1, k_scale=None, v_scale=None, weights=None,
@@ -476,7 +476,9 @@ class LtriPaged:
         if nbytes == 0:
             raise LtriError(LTRI_EINVAL, "ltri_paged_workspace_bytes")
         with torch.cuda.device(self.device):
-            self.workspace = torch.empty(nbytes + 256, dtype=torch.uint8, device=self.device)
+            # (on the stream that zeroes it: work of other streams on a block freed there is not ordered with that)
+            with torch.cuda.stream(stream):
+                self.workspace = torch.empty(nbytes + 256, dtype=torch.uint8, device=self.device)
             self.params.workspace = (self.workspace.data_ptr() + 255) // 256 * 256
             self.params.workspace_bytes = nbytes
             self._keep = (k_pages, v_pages, k_scale, v_scale, weights, positions)

@@ -56,3 +56,30 @@ def test_new_lengths_over_other_rows_lengths_are_refused():
     assert lp.ltri_paged_sync_status() == binding.LTRI_OK and both.tolist() == [40, 30, 20, 8, 8, 8, 7]
     for name, x in c.snapshot().items():
         assert torch.equal(x, want[name]), name
+
+
+def test_a_handle_made_on_another_stream_while_the_current_one_is_busy():
+    c = ref.Cache([3000, 500, 70], 8, 2, 128, 16, BF16, weighted=True, seed=3)
+    c.fill()
+    q, start, lens = c.randn(3, 8, 128), c.w.clone(), c.lens()
+    lp = c.handle()
+    want = lp.ltri_paged_decode(0, c.table, lens, q).clone()
+    nbytes = lp.workspace.numel()
+    weights = c.w.clone()
+    c.w.copy_(start)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    del lp
+    # a block of the workspace's size, freed while its stream still has writes to it before it
+    block = torch.empty(nbytes, dtype=torch.uint8, device="cuda")
+    torch.cuda._sleep(200_000_000)
+    block.fill_(1)
+    del block
+    lp = c.handle(stream=side)
+    torch.cuda.synchronize()
+    got = lp.ltri_paged_decode(0, c.table, lens, q)
+    assert lp.ltri_paged_sync_status() == binding.LTRI_OK
+    assert torch.equal(got, want) and torch.equal(ref.bits(c.w), ref.bits(weights))
+    new = torch.zeros_like(lens)
+    lp.ltri_paged_evict(0, 1, c.table, lens, new, 100, 4, 10)
+    assert lp.ltri_paged_sync_status() == binding.LTRI_OK and new.tolist() == [100, 100, 70]
