@@ -267,7 +267,15 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
       }
       // (the queries lie with head g, the logits with heads 2 q4 and 2 q4 + 1)
 #pragma unroll
-      for (int e = 0; e < 2; ++e) sc[nt][e] = c.scale * q.ks * __shfl_sync(0xffffffffu, back, (2 * q4 + e) * 4);
+      for (int e = 0; e < 2; ++e) {
+        const float b = __shfl_sync(0xffffffffu, back, (2 * q4 + e) * 4);
+        sc[nt][e] = c.scale;
+        if (KIND != kPdE4m3) continue;
+        // The three factors' product may lie in fp32's range where that of two does not.  Never zero: the logits of slots that
+        // are not there are -infinity times this, and at the smallest normal number products q.K, here below 2^36, are nothing.
+        const float f = (float)((double)c.scale * q.ks * b);
+        sc[nt][e] = f < 0x1p-126f ? 0x1p-126f : f;
+      }
     }
   };
   // A slice of 16 elements of the eight heads of block nt, normalised, to the output.

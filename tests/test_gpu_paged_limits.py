@@ -83,3 +83,25 @@ def test_a_handle_made_on_another_stream_while_the_current_one_is_busy():
     new = torch.zeros_like(lens)
     lp.ltri_paged_evict(0, 1, c.table, lens, new, 100, 4, 10)
     assert lp.ltri_paged_sync_status() == binding.LTRI_OK and new.tolist() == [100, 100, 70]
+
+
+def check_step(c, lens, q, decay=1.0, **kw):
+    """One decode call over the cache as it is, compared with the definition."""
+    before, lse = None if c.w is None else c.w.clone(), torch.full(q.shape[:2], 7.0, device="cuda")
+    lp = c.handle(**kw)
+    out = lp.ltri_paged_decode(0, c.table, c.lens(), q, lse=lse)
+    assert lp.ltri_paged_sync_status() == binding.LTRI_OK
+    ref.check_decode(c, 0, q, out, lse, lens, before, decay)
+    return out, lse
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("k_scale,q_scale", [(1e-40, 1.0), (2.0 ** -126 / 448, 1.0), (0.02, 2.0 ** -124), (3e-39, 2.0 ** -60),
+                                             (2.0 ** 100, 2.0 ** -124), (1e-40, 2.0 ** 125)])
+def test_logits_whose_factor_lies_below_fp32s_range(dim, k_scale, q_scale):
+    # scale * k_scale * the queries' power of two: the logits are what they are, and slots behind a row's end stay outside
+    c = ref.Cache([1, 17, 40, 300, 33, 64], 4, 2, dim, 16, BF16, True, weighted=True, seed=dim)
+    c.fill()
+    c.ks = torch.full_like(c.ks, k_scale)
+    q = (torch.randn(6, 4, dim, generator=c.g).clamp(-3.5, 3.5) * q_scale).to(BF16).cuda()
+    check_step(c, c.lens_cpu, q)
