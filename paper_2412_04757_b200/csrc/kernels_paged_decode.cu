@@ -300,17 +300,20 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
     if (a.lse) a.lse[at] = l2 * 0.69314718055994531f;
     if (c.w) wk.lse2[at] = l2;
   };
-  auto scale_of = [](float vs, float sum) { return sum == 0.f ? 0.f : vs / sum; };
+  // (one after the other: the quotient of a small scale and a large sum may lie below fp32's range where the output does not)
+  auto one_over = [](float sum) { return sum == 0.f ? 0.f : 1.f / sum; };
+  auto scaled = [](float x, float by, float vs) { return KIND == kPdE4m3 ? x * by * vs : x * by; };
 
   float O[NT][DT][4], ref[NT][2], sum[NT][2];
   // A unit's heads, all of whose sums this warp has.
   auto put_unit = [&](const PdCursor& u) {
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      const float by[2] = {scale_of(q.vs, sum[nt][0]), scale_of(q.vs, sum[nt][1])};
+      const float by[2] = {one_over(sum[nt][0]), one_over(sum[nt][1])};
 #pragma unroll
       for (int i = 0; i < DT; ++i) {
-        const float z[4] = {O[nt][i][0] * by[0], O[nt][i][1] * by[1], O[nt][i][2] * by[0], O[nt][i][3] * by[1]};
+        const float z[4] = {scaled(O[nt][i][0], by[0], q.vs), scaled(O[nt][i][1], by[1], q.vs), scaled(O[nt][i][2], by[0], q.vs),
+                            scaled(O[nt][i][3], by[1], q.vs)};
         put_slice(u, nt, i, z);
       }
       put_lse(u, nt, 0, ref[nt][0], sum[nt][0]);
@@ -768,8 +771,8 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
     for (int k = 0; k < kSlices; ++k) {
       if (k * W + warp >= NT * DT) continue;
       const bool upper = NT == 2 && (k * W + warp) / DT == 1;
-      const float b0 = scale_of(vs, upper ? tot[NT - 1][0] : tot[0][0]), b1 = scale_of(vs, upper ? tot[NT - 1][1] : tot[0][1]);
-      const float z[4] = {got[k].x * b0, got[k].y * b1, got[k].z * b0, got[k].w * b1};
+      const float b0 = one_over(upper ? tot[NT - 1][0] : tot[0][0]), b1 = one_over(upper ? tot[NT - 1][1] : tot[0][1]);
+      const float z[4] = {scaled(got[k].x, b0, vs), scaled(got[k].y, b1, vs), scaled(got[k].z, b0, vs), scaled(got[k].w, b1, vs)};
       put_slice(u, upper ? 1 : 0, (k * W + warp) % DT, z);
     }
     if (warp == 0)

@@ -105,3 +105,17 @@ def test_logits_whose_factor_lies_below_fp32s_range(dim, k_scale, q_scale):
     c.ks = torch.full_like(c.ks, k_scale)
     q = (torch.randn(6, 4, dim, generator=c.g).clamp(-3.5, 3.5) * q_scale).to(BF16).cuda()
     check_step(c, c.lens_cpu, q)
+
+
+@pytest.mark.parametrize("v_scale", [1e-40, 2.0 ** -126 / 448, 1e-38, 2.0 ** 110])
+@pytest.mark.parametrize("n", [1, 8, 100, 5000])
+def test_values_whose_scale_is_at_the_ends_of_fp32s_range(n, v_scale):
+    # outputs that are normal numbers of their type, from scales that are not: all slots' logits are zero, V is 320 or 384, so
+    # that nothing cancels.  n = 5000: parts of several CTAs are joined.
+    c = ref.Cache([n], 2, 1, 64, 16, BF16, True, seed=n)
+    pg, off = c.places(0, n)
+    v = torch.where(torch.rand(n, 1, 64, generator=c.g) < 0.5, 320.0, 384.0)
+    ref.put(c.k[0], pg, off, torch.ones(n, 1, 64).to(ref.E4M3))
+    ref.put(c.v[0], pg, off, v.to(ref.E4M3))
+    c.vs = torch.full_like(c.vs, v_scale)
+    check_step(c, [n], torch.zeros(1, 2, 64, dtype=BF16, device="cuda"))
