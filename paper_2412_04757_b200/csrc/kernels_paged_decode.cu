@@ -298,7 +298,7 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
     const size_t at = (size_t)u.row * c.Hq + (size_t)u.head * c.G + in_group;
     const float l2 = sum == 0.f ? -INFINITY : top + log2f(sum);
     if (a.lse) a.lse[at] = l2 * 0.69314718055994531f;
-    if (c.w) wk.lse2[at] = l2;
+    if (c.w) wk.lse2[at] = sum == 0.f ? INFINITY : l2;  // (logits of -infinity alone: 2^(x - L) is to be 0)
   };
   // (one after the other: the quotient of a small scale and a large sum may lie below fp32's range where the output does not)
   auto one_over = [](float sum) { return sum == 0.f ? 0.f : 1.f / sum; };

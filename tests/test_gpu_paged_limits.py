@@ -119,3 +119,29 @@ def test_values_whose_scale_is_at_the_ends_of_fp32s_range(n, v_scale):
     ref.put(c.v[0], pg, off, v.to(ref.E4M3))
     c.vs = torch.full_like(c.vs, v_scale)
     check_step(c, [n], torch.zeros(1, 2, 64, dtype=BF16, device="cuda"))
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+@pytest.mark.parametrize("hq,hkv", [(4, 2), (3, 1)])
+def test_rows_whose_logits_are_all_minus_infinity(dtype, hq, hkv):
+    # the softmax of nothing, as of an empty row: out 0, lse -infinity, and the slots get no weight; rows beside are as they were
+    lens = [20, 3000, 40]
+    c = ref.Cache(lens, hq, hkv, 64, 16, dtype, weighted=True, seed=hq)
+    c.fill()
+    for r in (0, 1):
+        pg, off = c.places(r, lens[r])
+        k = torch.randn(lens[r], hkv, 64, generator=c.g)
+        k[..., 0] = -math.inf
+        ref.put(c.k[0], pg, off, k.to(dtype))
+    q = c.randn(3, hq, 64)
+    q[:, :, 0] = 1.0
+    before, lse = c.w.clone(), torch.zeros(3, hq, device="cuda")
+    lp = c.handle(weight_decay=0.5)
+    out = lp.ltri_paged_decode(0, c.table, c.lens(), q, lse=lse)
+    assert lp.ltri_paged_sync_status() == binding.LTRI_OK
+    for r in (0, 1):
+        pg, off = c.places(r, lens[r])
+        assert (out[r] == 0).all() and (lse[r] == -math.inf).all()
+        assert torch.equal(ref.take(c.w[0], pg, off), 0.5 * ref.take(before[0], pg, off))
+    c.lens_cpu = [0, 0, 40]
+    ref.check_decode(c, 0, torch.cat([q[:2] * 0, q[2:]]), out, lse, c.lens_cpu, before, 0.5)
