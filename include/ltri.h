@@ -460,9 +460,11 @@ int ltri_paged_append(ltri_paged* cache, int layer, const int32_t* table, int ta
  *   lse  float [n_rows][n_q_heads] or NULL: log of the sum of exp(logit), to merge with attention over other tokens
  * With weights, every slot's weight becomes weight_decay * weight + the probabilities that the query heads of its KV head
  * give it; a slot that this call writes starts from 0.
- * Logits and sums are fp32; the probabilities enter the product with V as two 16-bit terms (16 bits together over bf16
- * pages, 22 over the others), so that the outputs carry the rounding of `type` once.  Logits and products q.K of any
- * magnitude below 10^38. */
+ * Logits and sums are fp32; the probabilities enter the product with V as sums of 16-bit terms, so that the outputs carry the
+ * rounding of `type` once.  Over bf16 pages these have fp32's 24 bits.  Over fp16 and 8-bit pages they have 22 bits down to
+ * 2^-13 of the row's largest probability, and below that steps of 2^-34 of it: n slots that are all small lose at most n * 2^-35
+ * of the sum (2^-15 for 2^20 slots).  Logits and products q.K of any magnitude below 10^38; over bf16 pages the sums with V are
+ * divided at the end, so that 16 times the sum of a row's |V| has to stay below 10^38, too. */
 int ltri_paged_decode(ltri_paged* cache, int layer, const int32_t* table, int table_pages, int64_t table_stride,
                       const int32_t* lens, int n_rows, const void* q, int64_t q_stride, const void* k, const void* v,
                       int64_t kv_stride, const int32_t* row_pos, void* out, float* lse, void* cuda_stream);

@@ -129,6 +129,9 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
   // probability at 2^10 a slot's contribution is still seen 2^-35 below it, so that 2^20 of them cannot lose 2^-14 of a sum.
   // The reference moves only when a logit exceeds it by kGrow, which bounds the probabilities by 2^(kOff + kGrow).
   constexpr float kOff = KIND == kPdBf16 ? 0.f : 10.f, kGrow = 4.f;
+  // Probabilities meet V as that many terms of the products' type: fp32's 24 bits over bf16 rows, 22 over the others (with two
+  // terms over bf16 rows, 16 bits, cancelling values would show it).
+  constexpr int kTerms = KIND == kPdBf16 ? 3 : 2;
   extern __shared__ __align__(1024) unsigned char dsm[];
   __shared__ PdOpen s_open[W];
   __shared__ PdOpen s_part[2];
@@ -555,8 +558,8 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
             }
           }
       }
-      // probabilities as two terms of the products' type, as V^T P^T takes them
-      uint32_t hi[MT][NT][2], lo[MT][NT][2];
+      // probabilities as a sum of terms of the products' type, as V^T P^T takes them
+      uint32_t term[kTerms][MT][NT][2];
 #pragma unroll
       for (int m = 0; m < MT; ++m)
 #pragma unroll
@@ -570,10 +573,14 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
           constexpr int T = KIND == kPdBf16 ? LTRI_TYPE_BF16 : LTRI_TYPE_FP16;
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            const uint32_t h = paged_pack(T, p[2 * e], p[2 * e + 1]);
-            const float2 back = paged_unpack(T, h);
-            hi[m][nt][e] = pd_transpose(h);
-            lo[m][nt][e] = pd_transpose(paged_pack(T, p[2 * e] - back.x, p[2 * e + 1] - back.y));
+#pragma unroll
+            for (int t = 0; t < kTerms; ++t) {
+              const uint32_t h = paged_pack(T, p[2 * e], p[2 * e + 1]);
+              term[t][m][nt][e] = pd_transpose(h);
+              const float2 back = paged_unpack(T, h);
+              p[2 * e] -= back.x;
+              p[2 * e + 1] -= back.y;
+            }
           }
         }
       const int v_row = KIND == kPdE4m3 ? lane & 15 : (lane & 7) + (lane >> 4) * 8;
@@ -599,16 +606,16 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
               }
 #pragma unroll
               for (int nt = 0; nt < NT; ++nt) {
-                pd_mma<KIND>(O[nt][i + j], f, hi[m][nt][0], hi[m][nt][1]);
-                pd_mma<KIND>(O[nt][i + j], f, lo[m][nt][0], lo[m][nt][1]);
+#pragma unroll
+                for (int t = 0; t < kTerms; ++t) pd_mma<KIND>(O[nt][i + j], f, term[t][m][nt][0], term[t][m][nt][1]);
               }
             }
           } else {
             ldsm_x4_t(b, (v_at ^ (i << 5)) + m * 16 * Sh::kRow);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-              pd_mma<KIND>(O[nt][i], b, hi[m][nt][0], hi[m][nt][1]);
-              pd_mma<KIND>(O[nt][i], b, lo[m][nt][0], lo[m][nt][1]);
+#pragma unroll
+              for (int t = 0; t < kTerms; ++t) pd_mma<KIND>(O[nt][i], b, term[t][m][nt][0], term[t][m][nt][1]);
             }
           }
         }

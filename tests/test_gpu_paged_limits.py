@@ -145,3 +145,39 @@ def test_rows_whose_logits_are_all_minus_infinity(dtype, hq, hkv):
         assert torch.equal(ref.take(c.w[0], pg, off), 0.5 * ref.take(before[0], pg, off))
     c.lens_cpu = [0, 0, 40]
     ref.check_decode(c, 0, torch.cat([q[:2] * 0, q[2:]]), out, lse, c.lens_cpu, before, 0.5)
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("dtype,hq", [(BF16, 8), (BF16, 16), (FP16, 8)])
+def test_probabilities_meet_v_with_all_their_bits(dim, dtype, hq):
+    # Three slots: one of logit 0 and V = 0, and two of logits -a and -a - 2^-14 or so with V = 1 and -1, which leave some
+    # 2^-16 of probabilities of 0.5 to 1.  What an output may be off: two products make a logit, below 1 in log2 units, which
+    # is off by 2^-22 (their sum, scale * log2(e)) and a rounding of 2^-24 of its distance to the maximum; exp2 by 2^-22; so p by
+    # 2^-21.  A product of a term of p (up to three) with V may lose 2^-23 of what it is added to.
+    rows = 64
+    c = ref.Cache([3] * rows, hq, 1, dim, 16, dtype, seed=dim)
+    q = torch.zeros(rows, hq, dim)
+    q[..., 0] = 4.0 + 4.0 * torch.rand(rows, hq, generator=c.g)
+    q[..., 1] = 2.0 ** -12 * (1 + torch.rand(rows, hq, generator=c.g))
+    q = q.to(dtype)
+    for r in range(rows):
+        k, v = torch.zeros(3, 1, dim), torch.zeros(3, 1, dim)
+        k[1:, 0, 0] = -0.1 - 0.5 * torch.rand(1, generator=c.g)
+        k[2, 0, 1] = -4.0
+        v[1], v[2] = 1.0, -1.0
+        pg, off = c.places(r, 3)
+        ref.put(c.k[0], pg, off, k.to(dtype))
+        ref.put(c.v[0], pg, off, v.to(dtype))
+    lp = c.handle(softmax_scale=0.125)
+    out = lp.ltri_paged_decode(0, c.table, c.lens(), q.cuda()).cpu().double()
+    assert lp.ltri_paged_sync_status() == binding.LTRI_OK
+    for r in range(rows):
+        K, V = c.row(0, r, 3)
+        for h in range(hq):
+            x = K[:, 0] @ q[r, h].double() * 0.125
+            assert float(x.abs().max()) * 1.4427 < 1
+            p = torch.exp(x)
+            want, most = (p[1] - p[2]) / p.sum(), float(p[1] / p.sum())
+            # (fp16 outputs of 2^-16 are subnormal: half their spacing of 2^-24)
+            bound = 2 * most * 2.0 ** -21 + 3 * most * 2.0 ** -23 + max(abs(float(want)) * ref.HALF_STEP[dtype], 2.0 ** -25)
+            assert float((out[r, h] - want).abs().max()) <= bound, (r, h)
