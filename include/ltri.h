@@ -413,7 +413,8 @@ typedef struct {
   int32_t page_tokens;           /* 1..65536 */
   int32_t max_rows;              /* rows of a call, 1..65535 */
   int64_t n_pages;               /* 1..2^31-1; n_pages * page_tokens slots at most 2^40 */
-  int64_t layer_stride, page_stride, head_stride, token_stride; /* elements, multiples of 16 bytes */
+  int64_t layer_stride, page_stride, head_stride, token_stride; /* elements, multiples of 16 bytes; that of an axis of one
+                                                                     * entry is not looked at */
   float softmax_scale;           /* 0 -> 1/sqrt(head_dim) */
   float weight_decay;            /* accumulated weights are multiplied by this in every decode call, 0..1 */
   void *k_pages, *v_pages;       /* DEVICE, 16-byte aligned */

@@ -449,7 +449,8 @@ class LtriPaged:
         dtype = dtype if dtype is not None else k_pages.dtype
         if dtype not in types:
             raise ValueError("dtype of the queries is bfloat16 or float16 (to be named beside 8-bit pages)")
-        if k_pages.dim() != 5 or k_pages.shape != v_pages.shape or k_pages.stride() != v_pages.stride():
+        if k_pages.dim() != 5 or k_pages.shape != v_pages.shape or any(
+                a != b for n, a, b in zip(k_pages.shape, k_pages.stride(), v_pages.stride()) if n > 1):
             raise ValueError("k_pages and v_pages are [layers][pages][Hkv][page tokens][head_dim] of the same strides")
         if k_pages.stride(4) != 1 or k_pages.dtype != v_pages.dtype or k_pages.dtype not in (dtype, torch.float8_e4m3fn):
             raise ValueError("rows are contiguous, of dtype or float8_e4m3fn")

@@ -36,8 +36,8 @@ bool validate(const ltri_paged_params* p) {
                                                    {p->n_kv_heads, p->head_stride}, {p->page_tokens, p->token_stride}};
   double extent = 0.0;  // bytes; far from where 64 bits end, as are the workspace's
   for (const auto& a : axes) {
-    if (a.stride < 0 || a.stride > (1ll << 42) || a.stride * es % 16) return false;
-    if (a.n > 1 && a.stride < p->head_dim) return false;
+    if (a.n == 1) continue;
+    if (a.stride < p->head_dim || a.stride > (1ll << 42) || a.stride * es % 16) return false;
     extent += (double)(a.n - 1) * (double)a.stride * (double)es;
   }
   if (extent > 0x1p56 || (double)p->n_layers * (double)p->n_pages * p->page_tokens * p->n_kv_heads > 0x1p48) return false;
@@ -170,10 +170,10 @@ int ltri_paged_create(const ltri_paged_params* p, void* cuda_stream, ltri_paged*
   while ((1 << log) < d.P) ++log;
   d.p_shift = 31 + log;
   d.p_mul = (unsigned)((1ull << d.p_shift) / d.P + 1);
-  d.ls = p->layer_stride * es;
-  d.ps = p->page_stride * es;
-  d.hs = p->head_stride * es;
-  d.ts = p->token_stride * es;
+  d.ls = p->n_layers > 1 ? p->layer_stride * es : 0;
+  d.ps = p->n_pages > 1 ? p->page_stride * es : 0;
+  d.hs = p->n_kv_heads > 1 ? p->head_stride * es : 0;
+  d.ts = p->page_tokens > 1 ? p->token_stride * es : 0;
   d.scale = (p->softmax_scale > 0.f ? p->softmax_scale : 1.f / std::sqrt((float)d.D)) * 1.4426950408889634f;
   d.decay = p->weight_decay;
   d.k = static_cast<unsigned char*>(p->k_pages);

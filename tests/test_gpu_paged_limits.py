@@ -181,3 +181,19 @@ def test_probabilities_meet_v_with_all_their_bits(dim, dtype, hq):
             # (fp16 outputs of 2^-16 are subnormal: half their spacing of 2^-24)
             bound = 2 * most * 2.0 ** -21 + 3 * most * 2.0 ** -23 + max(abs(float(want)) * ref.HALF_STEP[dtype], 2.0 ** -25)
             assert float((out[r, h] - want).abs().max()) <= bound, (r, h)
+
+
+@pytest.mark.parametrize("page,hkv", [(1, 1), (1, 2), (16, 1)])
+def test_pages_with_axes_of_one_entry_at_any_stride(page, hkv):
+    c = ref.Cache([40, 1, 17], 2 * hkv, hkv, 64, page, BF16, seed=page + hkv)
+    c.fill()
+    new = [1, c.k.stride(1), 3 if hkv == 1 else c.k.stride(2), 5 if page == 1 else c.k.stride(3), 1]
+    c.k, c.v = c.k.as_strided(c.k.shape, new), c.v.as_strided(c.v.shape, new)
+    q = c.randn(3, 2 * hkv, 64)
+    check_step(c, c.lens_cpu, q)
+    x, starts = c.randn(3, hkv, 64), torch.tensor([0, 1, 1, 3], dtype=torch.int32, device="cuda")
+    lp = c.handle()
+    lp.ltri_paged_append(0, c.table, c.lens(), starts, x, x)
+    assert lp.ltri_paged_sync_status() == binding.LTRI_OK
+    pg, off = c.places(2, 17)
+    assert torch.equal(ref.take(c.k[0], pg[-2:], off[-2:]), x[1:]) and torch.equal(ref.take(c.v[0], pg[-2:], off[-2:]), x[1:])

@@ -74,3 +74,13 @@ def test_the_workspace_is_allocated_on_the_stream_that_zeroes_it(fake, stream):
     k, v = Tensor([2, 5, 1, 16, 64], "bf16"), Tensor([2, 5, 1, 16, 64], "bf16", ptr=1 << 16)
     binding.LtriPaged(k, v, 2, stream=None if stream is None else types.SimpleNamespace(cuda_stream=stream))
     assert fake.events == [("empty", stream or 11), ("create", stream or 11)] and fake.current == 11
+
+
+def test_strides_of_axes_of_one_entry_do_not_matter(fake):
+    shape = [1, 5, 1, 16, 64]
+    k, v = Tensor(shape, "bf16", [1, 1024, 3, 64, 1]), Tensor(shape, "bf16", [5120, 1024, 1024, 64, 1], ptr=1 << 16)
+    binding.LtriPaged(k, v, 2)
+    assert fake.events[-1][0] == "create" and fake.params.page_stride == 1024
+    for strides in ([5120, 2048, 1024, 64, 1], [5120, 1024, 1024, 128, 1]):
+        with pytest.raises(ValueError):
+            binding.LtriPaged(k, Tensor(shape, "bf16", strides, ptr=1 << 16), 2)
