@@ -197,3 +197,39 @@ def test_pages_with_axes_of_one_entry_at_any_stride(page, hkv):
     assert lp.ltri_paged_sync_status() == binding.LTRI_OK
     pg, off = c.places(2, 17)
     assert torch.equal(ref.take(c.k[0], pg[-2:], off[-2:]), x[1:]) and torch.equal(ref.take(c.v[0], pg[-2:], off[-2:]), x[1:])
+
+
+def test_every_part_of_the_longest_row_is_in_its_output():
+    # 32767 pages of 65536 slots, of four in memory that have the same keys: the first, one in the middle and the last one have
+    # V of 2^15 in 16 elements each, the others none there, and all have 1 in the rest
+    P, cols, dim = 65536, 32767, 64
+    c = ref.Cache([4 * P], 1, 1, dim, P, BF16, seed=5)
+    pages = c.table_cpu[0].long()
+    k = torch.randn(P, 1, dim, generator=c.g).to(BF16)
+    where = torch.arange(P, device="cuda")
+    for i, page in enumerate(pages):
+        v = torch.zeros(P, 1, dim)
+        v[..., 48:] = 1.0
+        if i > 0:
+            v[..., 16 * (i - 1):16 * i] = 2.0 ** 15
+        pg = torch.full((P,), int(page), device="cuda")
+        ref.put(c.k[0], pg, where, k)
+        ref.put(c.v[0], pg, where, v.to(BF16))
+    table = torch.full((1, cols), int(pages[0]), dtype=torch.int32)
+    table[0, 0], table[0, cols // 2], table[0, -1] = pages[1], pages[2], pages[3]
+    lens = torch.full((1,), cols * P, dtype=torch.int32, device="cuda")
+    q, lse = c.randn(1, 1, dim), torch.empty(1, 1, device="cuda")
+    lp = c.handle()
+    out = lp.ltri_paged_decode(0, table.cuda(), lens, q, lse=lse)[0, 0].cpu().double()
+    assert lp.ltri_paged_sync_status() == binding.LTRI_OK
+    x = k[:, 0].double() @ q[0, 0].cpu().double() * dim ** -0.5
+    d = float((k[:, 0].double().abs() @ q[0, 0].cpu().double().abs()).max()) * dim ** -0.5 * (dim + 8) * 2.0 ** -23
+    # a warp adds up 2^27 / 1184 < 113400 tiles one after the other, for the sum of the probabilities two slots of each, rounded;
+    # a product of one of three terms with V may lose 2^-23 of what it is added to, on 4096 tiles of a page or on all
+    total, page, row = 2 * 113400 * 2.0 ** -24, 3 * 4096 * 2.0 ** -23, 3 * 113400 * 2.0 ** -23
+    assert abs(float(lse) - float(torch.logsumexp(x, 0)) - math.log(cols)) < total + 2 * d
+    want = torch.full((dim,), 2.0 ** 15 / cols, dtype=torch.float64)
+    want[48:] = 1.0
+    bound = torch.full((dim,), total + page, dtype=torch.float64)
+    bound[48:] = total + row
+    assert ((out / want - 1).abs() <= bound + 2 * d + 2.0 ** -8).all(), out
