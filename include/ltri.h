@@ -457,7 +457,7 @@ int ltri_paged_append(ltri_paged* cache, int layer, const int32_t* table, int ta
  *        counts the new token) before the attention.  Both NULL: the cache is attended over as it is.
  *   row_pos DEVICE int32 [n_rows]: position of each row's new token (NULL: the slot's number); used only if the cache
  *        has positions and k is given
- *   out  [n_rows][n_q_heads ][head_dim], dense (may be q itself)
+ *   out  [n_rows][n_q_heads ][head_dim], dense (may be q itself, if that is dense; LTRI_EINVAL if it overlaps it otherwise)
  *   lse  float [n_rows][n_q_heads] or NULL: log of the sum of exp(logit), to merge with attention over other tokens
  * With weights, every slot's weight becomes weight_decay * weight + the probabilities that the query heads of its KV head
  * give it; a slot that this call writes starts from 0.

@@ -130,6 +130,13 @@ long long row_stride(const ltri_paged* c, int64_t stride, int heads) {
   return stride * 2;
 }
 
+// Whether `bytes` bytes at a meet one of n rows of `row` bytes at b, `stride` apart.
+bool meets(const void* a, long long bytes, const void* b, long long n, long long row, long long stride) {
+  const long long d = (long long)(reinterpret_cast<uintptr_t>(a) - reinterpret_cast<uintptr_t>(b));  // (addresses have 57 bits)
+  const long long first = d < row ? 0 : (d - row) / stride + 1;  // the first row that ends behind a
+  return first < n && first * stride < d + bytes;
+}
+
 }  // namespace
 
 extern "C" {
@@ -233,6 +240,9 @@ int ltri_paged_decode(ltri_paged* cache, int layer, const int32_t* table, int ta
   if (!aligned(q, 16) || !aligned(out, 16) || !qs || !kvs || !k != !v) return LTRI_EINVAL;
   if (k && (!aligned(k, 16) || !aligned(v, 16))) return LTRI_EINVAL;
   if ((row_pos && !aligned(row_pos, 4)) || (lse && !aligned(lse, 4))) return LTRI_EINVAL;
+  // outputs are written while other rows' queries are still to be read
+  const long long row = (long long)cache->p.n_q_heads * cache->p.head_dim * 2;
+  if (!(out == q && (qs == row || n_rows == 1)) && meets(out, n_rows * row, q, n_rows, row, qs)) return LTRI_EINVAL;
   OnDevice on(cache->device);
   if (!on.ok) return done(cache, cudaErrorInvalidDevice, 0);
   const PagedStep a{static_cast<const unsigned char*>(q), static_cast<const unsigned char*>(k),

@@ -233,3 +233,30 @@ def test_every_part_of_the_longest_row_is_in_its_output():
     bound = torch.full((dim,), total + page, dtype=torch.float64)
     bound[48:] = total + row
     assert ((out / want - 1).abs() <= bound + 2 * d + 2.0 ** -8).all(), out
+
+
+def test_outputs_over_other_rows_queries_are_refused():
+    c = ref.Cache([40, 30, 20], 4, 2, 64, 16, FP16, seed=2)
+    c.fill()
+    lp, lens = c.handle(), c.lens()
+    buf = c.randn(40 * 64).view(-1)
+    at = lambda first, stride: buf[first * 64:].as_strided((3, 4, 64), (stride * 64, 64, 1))  # noqa: E731  (heads)
+    want = lp.ltri_paged_decode(0, c.table, lens, at(0, 6).contiguous())
+    launches, before = lp.ltri_paged_launch_count(), buf.clone()
+    # (queries' first head and stride, outputs' first head): one over the other, over a row of it, over itself with gaps
+    for first, stride, o in ((0, 4, 1), (4, 4, 0), (0, 6, 0), (0, 6, 15), (5, 6, 0), (0, 12, 4), (12, 4, 1)):
+        with pytest.raises(binding.LtriError) as e:
+            lp.ltri_paged_decode(0, c.table, lens, at(first, stride), out=at(o, 4))
+        assert e.value.code == binding.LTRI_EINVAL
+    torch.cuda.synchronize()
+    assert lp.ltri_paged_launch_count() == launches and torch.equal(buf, before)
+    # beside them, behind them, and between two rows that are far apart
+    wide = torch.zeros(40 * 64, dtype=FP16, device="cuda")
+    for first, stride, o in ((0, 6, 16), (12, 6, 0), (0, 16, 4)):
+        x = wide[first * 64:].as_strided((3, 4, 64), (stride * 64, 64, 1))
+        x.copy_(at(0, 6))
+        got = lp.ltri_paged_decode(0, c.table, lens, x, out=wide[o * 64:].as_strided((3, 4, 64), (256, 64, 1)))
+        assert torch.equal(got, want), (first, stride, o)
+    x = at(0, 4)
+    x.copy_(at(0, 6).contiguous())
+    assert torch.equal(lp.ltri_paged_decode(0, c.table, lens, x, out=x), want)
