@@ -260,3 +260,63 @@ def test_outputs_over_other_rows_queries_are_refused():
     x = at(0, 4)
     x.copy_(at(0, 6).contiguous())
     assert torch.equal(lp.ltri_paged_decode(0, c.table, lens, x, out=x), want)
+
+
+@pytest.mark.parametrize("hq,hkv,dim,dtype,e4m3", [(64, 1, 128, BF16, False), (48, 2, 256, BF16, True), (40, 1, 64, FP16, False),
+                                                   (34, 2, 256, FP16, False)])
+@pytest.mark.parametrize("weighted", [False, True])
+def test_wide_groups_split_over_many_ctas(hq, hkv, dim, dtype, e4m3, weighted):
+    lens = [5000, 17, 0, 900]
+    c = ref.Cache(lens, hq, hkv, dim, 16, dtype, e4m3, weighted=weighted, seed=hq)
+    c.fill()
+    check_step(c, lens, c.randn(4, hq, dim))
+
+
+@pytest.mark.parametrize("rows,kind", [(1500, "short"), (300, "ragged")])
+def test_batches_of_many_rows(rows, kind):
+    g = torch.Generator().manual_seed(rows)
+    top = 20 if kind == "short" else 600
+    lens = [0 if i % 7 == 3 else int(torch.randint(1, top, (1,), generator=g)) for i in range(rows)]
+    c = ref.Cache(lens, 4, 2, 64, 16, BF16, weighted=True, seed=rows)
+    c.fill()
+    lp = c.handle()
+    q, before, lse = c.randn(rows, 4, 64), c.w.clone(), torch.zeros(rows, 4, device="cuda")
+    out = lp.ltri_paged_decode(0, c.table, c.lens(), q, lse=lse)
+    assert lp.ltri_paged_sync_status() == binding.LTRI_OK
+    ref.check_decode(c, 0, q, out, lse, lens, before)
+    want, new = ref.evict(c, lens, 10, 2, 3, [0])
+    got = c.lens()
+    lp.ltri_paged_evict(0, 1, c.table, got, got, 10, 2, 3)
+    assert lp.ltri_paged_sync_status() == binding.LTRI_OK and got.tolist() == new
+    for name, x in c.snapshot().items():
+        assert torch.equal(x, want[name]), name
+
+
+def test_a_capture_whose_steps_come_from_two_streams():
+    # a side stream prepares the new token's rows while the main one evicts; both are followed by the attention
+    c = ref.Cache([50, 33], 8, 2, 64, 16, BF16, weighted=True, room=1, seed=4)
+    c.fill()
+    lp, dev, one = c.handle(), c.lens(), torch.ones(2, dtype=torch.int32, device="cuda")
+    q, x, kv = c.randn(2, 8, 64), c.randn(2, 4, 64), torch.zeros(2, 4, 64, dtype=BF16, device="cuda")
+    out = torch.zeros_like(q)
+    graph, main, side = torch.cuda.CUDAGraph(), torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=main):
+        side.wait_stream(main)
+        with torch.cuda.stream(side):
+            kv.copy_(x)
+        lp.ltri_paged_evict(0, 1, c.table, dev, dev, 40, 4, 8)
+        dev.add_(one)
+        main.wait_stream(side)
+        lp.ltri_paged_decode(0, c.table, dev, q, kv[:, :2], kv[:, 2:], out=out)
+    for step in range(3):
+        x.copy_(c.randn(2, 4, 64))
+        want, lens = ref.evict(c, dev.tolist(), 40, 4, 8, [0])
+        w = want["w"].view(torch.float32)
+        graph.replay()
+        assert lp.ltri_paged_sync_status() == binding.LTRI_OK
+        lens = [n + 1 for n in lens]
+        assert dev.tolist() == lens
+        ref.check_decode(c, 0, q, out, None, lens, w, 1.0, True)
+        pg, off = c.places(0, lens[0])
+        assert torch.equal(ref.take(c.k[0], pg[-1:], off[-1:])[0], x[0, :2])
