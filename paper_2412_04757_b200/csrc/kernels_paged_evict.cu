@@ -95,7 +95,15 @@ __global__ void __launch_bounds__(kEvThreads, 2)
     c.seen[row] = 0;
     new_lens[row] = min(n, budget);
   }
-  if (n <= budget) return;
+  // A cluster goes on if all of it has read the same length: should somebody write to the lengths meanwhile, no CTA may be gone
+  // while another one asks for its shared memory.
+  if (n <= budget) {
+    if (C > 1) {
+      cluster.sync();
+      cluster.sync();
+    }
+    return;
+  }
 
   const int chunk = (n + C - 1) / C, begin = rank * chunk, end = min(n, begin + chunk);
   bool bad = false;  // a page that is none
@@ -162,6 +170,7 @@ __global__ void __launch_bounds__(kEvThreads, 2)
   newest = __reduce_max_sync(0xffffffffu, newest);
   if (lane == 0) atomicMax(&s_newest, newest);
   cluster.sync();
+  const bool agreed = __all_sync(0xffffffffu, ask(&s_n, n) == n);
   newest = __reduce_max_sync(0xffffffffu, ask(&s_newest, INT_MIN));
   const long long first_recent = (long long)newest - recent;
   auto key = [&](int slot) {
@@ -196,6 +205,10 @@ __global__ void __launch_bounds__(kEvThreads, 2)
     atomicAdd(&s_stay, stay);
   }
   cluster.sync();
+  if (!agreed) {
+    paged_status(c, row);
+    return;
+  }
   int count = 0;                     // moves
   int m_incl = 0, h_incl = 0;        // lane i: movers and holes up to CTA i
   if (single) {

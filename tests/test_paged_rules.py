@@ -38,3 +38,16 @@ def test_an_eviction_takes_a_bin_whatever_the_histogram_holds():
     text = re.sub(r"\s+", " ", source("kernels_paged_evict.cu"))
     assert "const bool lowest = tid == kEvThreads - 1;" in text and "(need <= to || lowest)" in text
     assert "(lowest && b == 3)" in text
+
+
+def test_no_cta_of_an_evicting_cluster_leaves_while_another_may_ask_for_its_length():
+    # lengths that change while they are read: who returns early passes the two barriers between which the others compare theirs
+    text = re.sub(r"\s+", " ", source("kernels_paged_evict.cu"))
+    early = text.index("if (n <= budget) {")
+    assert text[early:].startswith("if (n <= budget) { if (C > 1) { cluster.sync(); cluster.sync(); } return; }")
+    rest = text[early:][len("if (n <= budget) { if (C > 1) { cluster.sync(); cluster.sync(); } return; }"):]
+    first = rest.index("cluster.sync();")
+    second = rest.index("cluster.sync();", first + 1)
+    assert "map_shared_rank(x, lane)" in rest[:first] and "ask(&" not in rest[:first]
+    assert first < rest.index("ask(&s_n, n) == n") < second
+    assert rest[second:].startswith("cluster.sync(); if (!agreed) { paged_status(c, row); return; }")
