@@ -46,12 +46,6 @@ struct PdShape {
   static constexpr int kPages = 2 * kStages;                    // tiles whose page numbers are known or on their way
   static constexpr int kRing = kStages * kStage;                // of a warp
   static constexpr int kSmem = kWarps * (kRing + kPages * kTile * 4);
-  // Blocks of 16 slots within a page are requested from one address, stepping; others a row at a time, from addresses that the
-  // lanes exchange.  For 16-bit rows of 128 the latter takes longer to issue, and the evener flow of requests pays: replayed
-  // from a graph 16 rows of 24576 slots take 244 us, 252 by steps (launched one by one 244 either way), one row of 131072 88.6
-  // and 91, one of 300 8.65 and 8.45.  Rows of 64 are about equal; 8-bit ones (59.5 us by steps, 63.4 without) and 16-bit rows
-  // of 256 (46.1 us, 48.3) are better off with the steps.
-  static constexpr bool kSteps = KIND == kPdE4m3 || kRow > 256;
   static_assert(kStages >= 3, "two tiles on their way and one in use");
 };
 
@@ -142,7 +136,10 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
   unsigned char* ring = dsm + warp * Sh::kRing;
   int* s_pages = reinterpret_cast<int*>(dsm + W * Sh::kRing) + warp * Sh::kPages * TILE;
   const uint32_t ring_s = smem_u32(ring), pages_s = smem_u32(s_pages);
-  const bool one_page = Sh::kSteps && c.P % 16 == 0;  // of a block of 16 slots
+  // Blocks of 16 slots within a page are requested from one address, stepping; others a row at a time, from addresses that the
+  // lanes exchange.  (All by single rows, which some GPUs like and others do not: 16 rows of 24576 slots of 128 in bf16 took 238
+  // to 263 us on three of them, by steps 243 to 247; 64 ragged rows in 8 bits 63.4 us, by steps 59.5.)
+  const bool one_page = c.P % 16 == 0;
 
   PdCursor cu;
   int total;
