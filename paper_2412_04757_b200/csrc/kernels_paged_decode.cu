@@ -3,9 +3,10 @@
 // x_j = c q.K_j, out = sum_j 2^(x_j - L) V_j with c in log2 units and L = log2 sum_j 2^(x_j): one pass over K and V with a
 // running reference m, sums of 2^(x_j - m) and of 2^(x_j - m) V_j, which parts of a row join by rescaling to the larger m.
 //
-// Bound: HBM (a KV head's rows are read once for all of its query heads: 2 G flop a byte in 16 bits).  So the work is the rows'
-// tiles, and it is dealt evenly: the tiles of all (row, KV head) units stand in one line, of which every warp takes an equal
-// run, across units if need be, and a CTA (one per SM) its warps' runs.  Ragged batches and single long rows fill the GPU
+// Bound: HBM (a KV head's rows are read once for up to 16 of its query heads: 2 G flop a byte in 16 bits; more heads are blocks
+// of 16 with a unit each, which read the rows again).  So the work is the rows' tiles, and it is dealt evenly: the tiles of all
+// (row, KV head, block) units stand in one line, of which every warp takes an equal run, across units if need be, and a CTA (one
+// per SM) its warps' runs.  Ragged batches and single long rows fill the GPU
 // alike, and no count of splits has to be chosen.  A unit within one warp's run is written by the warp; of a unit that several
 // warps share, the sums are joined when their CTA has finished its run, and of one that several CTAs share, the last CTA to
 // finish joins the others' sums, always in the order of the line.
@@ -16,13 +17,13 @@
 // they are long, which needs no permutation: 279 us, the writes then straddle lines.)
 //
 // Both products run on mma.sync with the slots (or head_dim) as the 16 rows and the heads of the KV group as the 8 columns:
-// S^T = K Q^T, O^T = V^T P^T, so that up to eight heads fill the instruction exactly.  (tcgen05 takes 64 rows at least, and its
-// operands come through descriptors of whole tiles, which pages of any size are not.)
+// S^T = K Q^T, O^T = V^T P^T, so that up to eight heads fill the instruction exactly.  (Memory is the bound and the tensor pipe
+// 19% busy: tcgen05, with 64 rows at least and accumulators to fetch, has nothing to gain.)
 //
-// Measured (one B200, copy rate 6454 GB/s): 16 rows of 24576 slots, 32 query and 8 KV heads of 128 in bf16, 243 to 250 us, 6.4
-// to 6.6 TB/s.  Also at 93 to 103% of the copy rate at that length: 8-bit pages, heads of 64 and 256, pages of one or seven
-// slots, 8 to 128 query heads.  What a call costs beyond its bytes is 10 to 15 us: two dependent lookups before the first row
-// (lengths, pages), and after the last one the joins; 300 slots of one row take 8.7 us.
+// Measured (five B200s, copy rate 6454 GB/s): 16 rows of 24576 slots, 32 query and 8 KV heads of 128 in bf16, 243 to 247 us, 6.5
+// to 6.6 TB/s; one row of 131072, 88 to 94 us, 5.7 to 6.1 TB/s.  What a call costs beyond its bytes is 10 to 15 us: two
+// dependent lookups before the first row (lengths, pages), and after the last one the joins; 300 slots of one row take 8.7 to
+// 9.5 us.  32 query heads of one KV head, 16 rows of 24576 slots: 85 us, 64 of them 166, at a floor of 31 us.
 #include "mma_util.cuh"
 #include "paged.cuh"
 #include "paged_deal.cuh"
@@ -124,21 +125,23 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
   // The reference moves only when a logit exceeds it by kGrow, which bounds the probabilities by 2^(kOff + kGrow).
   constexpr float kOff = KIND == kPdBf16 ? 0.f : 10.f, kGrow = 4.f;
   // Probabilities meet V as that many terms of the products' type: fp32's 24 bits over bf16 rows, 22 over the others (with two
-  // terms over bf16 rows, 16 bits, cancelling values would show it).
+  // terms over bf16 rows, 16 bits, values that cancel show it).
   constexpr int kTerms = KIND == kPdBf16 ? 3 : 2;
   extern __shared__ __align__(1024) unsigned char dsm[];
   __shared__ PdOpen s_open[W];
   __shared__ PdOpen s_part[2];
   __shared__ int s_last[2];
   chain_wait();
-  if (c.w) chain_release();  // the weights kernel may take its place beside this one; it waits for this one's end
+  // The weights kernel waits for this one's end, but may start: beside this one's CTAs where they leave it registers (head_dim
+  // 64 and up to eight heads in 16 bits), else on SMs whose CTA is through.
+  if (c.w) chain_release();
   const int warp = threadIdx.x / 32, lane = threadIdx.x & 31, g = lane >> 2, q4 = lane & 3;
   unsigned char* ring = dsm + warp * Sh::kRing;
   int* s_pages = reinterpret_cast<int*>(dsm + W * Sh::kRing) + warp * Sh::kPages * TILE;
   const uint32_t ring_s = smem_u32(ring), pages_s = smem_u32(s_pages);
   // Blocks of 16 slots within a page are requested from one address, stepping; others a row at a time, from addresses that the
-  // lanes exchange.  (All by single rows, which some GPUs like and others do not: 16 rows of 24576 slots of 128 in bf16 took 238
-  // to 263 us on three of them, by steps 243 to 247; 64 ragged rows in 8 bits 63.4 us, by steps 59.5.)
+  // lanes exchange.  (All by single rows: 16 rows of 24576 slots of 128 in bf16 263 to 274 us, one row of 131072 95 to 97, by
+  // steps 242 to 248 and 89 to 91; 64 ragged rows in 8 bits 4 us more.)
   const bool one_page = c.P % 16 == 0;
 
   PdCursor cu;
@@ -580,42 +583,51 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
             }
           }
         }
+      // A tile's products are added up by themselves, a block's smallest term first, and their sum to the other tiles'.  (The
+      // tensor cores cut off what an accumulator has no bits for, always towards zero: with O as the accumulator small values
+      // beside large ones were lost, and outputs over bf16 pages differed twice as much from fp32 arithmetic's.  64 ragged rows in
+      // 8 bits 61.5 us, with O 59.8; rows of 256 in 16 bits 35.8 and 34.7; the others no slower.)
       const int v_row = KIND == kPdE4m3 ? lane & 15 : (lane & 7) + (lane >> 4) * 8;
       const int v_ch = KIND == kPdE4m3 ? lane >> 4 : (lane >> 3) & 1;
       const uint32_t v_at = sv + v_row * Sh::kRow + ((v_ch ^ pd_swizzle<RC>(v_row)) << 4);
+      constexpr int kAtOnce = KIND == kPdE4m3 ? 2 : 1;  // slices of 16 elements
 #pragma unroll
-      for (int m = 0; m < MT; ++m)
+      for (int i = 0; i < DT; i += kAtOnce) {
+        float z[kAtOnce][NT][4];
 #pragma unroll
-        for (int i = 0; i < DT; i += KIND == kPdE4m3 ? 2 : 1) {
+        for (int j = 0; j < kAtOnce; ++j)
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) z[j][nt][0] = z[j][nt][1] = z[j][nt][2] = z[j][nt][3] = 0.f;
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
           uint32_t b[4];
-          if (KIND == kPdE4m3) {
-            // a 16-byte chunk's 8 pairs of neighbours are the 8 rows of a transposed matrix: row g has elements 2g and 2g + 1
-            // of slots 2 q4 and 2 q4 + 1
-            ldsm_x4_t(b, (v_at ^ (i << 4)) + m * 16 * Sh::kRow);
+          ldsm_x4_t(b, (v_at ^ (i << (KIND == kPdE4m3 ? 4 : 5))) + m * 16 * Sh::kRow);
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-              uint32_t f[4];
+          for (int j = 0; j < kAtOnce; ++j) {
+            uint32_t f[4] = {b[0], b[1], b[2], b[3]};
+            if (KIND == kPdE4m3) {
+              // a 16-byte chunk's 8 pairs of neighbours are the 8 rows of a transposed matrix: row g has elements 2g and 2g + 1
+              // of slots 2 q4 and 2 q4 + 1
 #pragma unroll
               for (int e = 0; e < 2; ++e) {  // (with e, 8 slots further)
                 const uint32_t y = __byte_perm(b[2 * j + e], 0u, 0x3120);
                 f[2 * e] = pd_halves_lo(y);
                 f[2 * e + 1] = pd_halves_hi(y);
               }
-#pragma unroll
-              for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-                for (int t = 0; t < kTerms; ++t) pd_mma<KIND>(O[nt][i + j], f, term[t][m][nt][0], term[t][m][nt][1]);
-              }
             }
-          } else {
-            ldsm_x4_t(b, (v_at ^ (i << 5)) + m * 16 * Sh::kRow);
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
+            for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-              for (int t = 0; t < kTerms; ++t) pd_mma<KIND>(O[nt][i], b, term[t][m][nt][0], term[t][m][nt][1]);
-            }
+              for (int t = kTerms - 1; t >= 0; --t) pd_mma<KIND>(z[j][nt], f, term[t][m][nt][0], term[t][m][nt][1]);
           }
         }
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j)
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) O[nt][i + j][e] += z[j][nt][e];
+      }
       __syncwarp();
       stage_at = next(stage_at, S);
       page_at = next(page_at, Sh::kPages);

@@ -320,3 +320,26 @@ def test_a_capture_whose_steps_come_from_two_streams():
         ref.check_decode(c, 0, q, out, None, lens, w, 1.0, True)
         pg, off = c.places(0, lens[0])
         assert torch.equal(ref.take(c.k[0], pg[-1:], off[-1:])[0], x[0, :2])
+
+
+@pytest.mark.parametrize("dim,hq", [(64, 8), (128, 8), (256, 8), (64, 128), (128, 128), (256, 128)])
+@pytest.mark.parametrize("dtype,e4m3", [(BF16, False), (FP16, False), (BF16, True)])
+def test_small_values_survive_among_large_ones_that_cancel(dim, hq, dtype, e4m3):
+    # All probabilities are equal.  1024 slots of V = B, 2048 of 2^-9 and 1024 of -B: a block of 16 of the small ones, 2^-5, is
+    # exact beside the large ones' sum (1024 B < 2^19), and so are all sums of blocks, whoever adds them: what is left is
+    # 2048 * 2^-9 of 4096 slots.  As many units as the GPU has warps at work, so that runs are whole rows.
+    n, hkv, rows = 4096, 8, torch.cuda.get_device_properties(0).multi_processor_count
+    c = ref.Cache([n], hq, hkv, dim, 16, dtype, e4m3, seed=dim)
+    pg, off = c.places(0, n)
+    v = torch.full((n, hkv, dim), 2.0 ** -9)
+    v[:1024], v[3072:] = (448.0, -448.0) if e4m3 else (128.0, -128.0)
+    ref.put(c.k[0], pg, off, torch.zeros(n, hkv, dim).to(c.k.dtype))
+    ref.put(c.v[0], pg, off, v.to(c.v.dtype))
+    if e4m3:
+        c.vs = torch.ones_like(c.vs)
+    lp = c.handle(max_rows=rows)
+    q, lse = c.randn(rows, hq, dim), torch.empty(rows, hq, device="cuda")
+    lens = torch.full((rows,), n, dtype=torch.int32, device="cuda")
+    out = lp.ltri_paged_decode(0, c.table.repeat(rows, 1), lens, q, lse=lse)
+    assert lp.ltri_paged_sync_status() == binding.LTRI_OK
+    assert (out == 2.0 ** -10).all() and float((lse - 12 * math.log(2.0)).abs().max()) < 2.0 ** -20
