@@ -6,10 +6,10 @@
 // Bound: HBM (a KV head's rows are read once for up to 16 of its query heads: 2 G flop a byte in 16 bits; more heads are blocks
 // of 16 with a unit each, which read the rows again).  So the work is the rows' tiles, and it is dealt evenly: the tiles of all
 // (row, KV head, block) units stand in one line, of which every warp takes an equal run, across units if need be, and a CTA (one
-// per SM) its warps' runs.  Ragged batches and single long rows fill the GPU
-// alike, and no count of splits has to be chosen.  A unit within one warp's run is written by the warp; of a unit that several
-// warps share, the sums are joined when their CTA has finished its run, and of one that several CTAs share, the last CTA to
-// finish joins the others' sums, always in the order of the line.
+// per SM) its warps' runs.  Ragged batches and single long rows fill the GPU alike, and no count of splits has to be chosen.  A
+// unit within one warp's run is written by the warp; of a unit that several warps share, the sums are joined when their CTA has
+// finished its run, and of one that several CTAs share, the last CTA to finish joins the others' sums, always in the order of
+// the line.
 //
 // A warp has a ring of its own that cp.async fills several tiles ahead, across units.  (One bulk copy a row instead: 341 us for
 // 16 rows of 24576 slots, 254 so; a row's copy costs the copy unit some 15 cycles however short it is.)  A row's 16-byte chunks
@@ -20,10 +20,10 @@
 // S^T = K Q^T, O^T = V^T P^T, so that up to eight heads fill the instruction exactly.  (Memory is the bound and the tensor pipe
 // 19% busy: tcgen05, with 64 rows at least and accumulators to fetch, has nothing to gain.)
 //
-// Measured (five B200s, copy rate 6454 GB/s): 16 rows of 24576 slots, 32 query and 8 KV heads of 128 in bf16, 243 to 247 us, 6.5
-// to 6.6 TB/s; one row of 131072, 88 to 94 us, 5.7 to 6.1 TB/s.  What a call costs beyond its bytes is 10 to 15 us: two
-// dependent lookups before the first row (lengths, pages), and after the last one the joins; 300 slots of one row take 8.7 to
-// 9.5 us.  32 query heads of one KV head, 16 rows of 24576 slots: 85 us, 64 of them 166, at a floor of 31 us.
+// Measured (eight B200s, copy rate 6454 GB/s): 16 rows of 24576 slots, 32 query and 8 KV heads of 128 in bf16, 239 to 258 us on
+// all but one (270), 6.2 to 6.7 TB/s; one row of 131072, 88 to 94 us, 5.7 to 6.1 TB/s.  What a call costs beyond its bytes is 10
+// to 15 us: two dependent lookups before the first row (lengths, pages), and after the last one the joins; 300 slots of one row
+// take 8.6 to 9.5 us.  32 query heads of one KV head, 16 rows of 24576 slots: 76 to 83 us, 64 of them 138 to 167, at a floor of 31.
 #include "mma_util.cuh"
 #include "paged.cuh"
 #include "paged_deal.cuh"

@@ -16,8 +16,10 @@
 // every CTA of a cluster takes the same way through the barriers.
 //
 // Bound: latency where few slots leave, HBM where many rows move (read once, written once).  Measured: one slot of each of 256
-// units of 4097 slots, 16 us; 64 units of 29369 to 32768 slots cut to 5120, 100 us, 33 of them for the keys and lists, the rest
-// for 5000 moves a unit at 4.5 TB/s (read and written), which neither more rows on the way nor rows side by side raise.
+// units of 4097 slots, 8 to 14 us within a step; 64 of 128 units, of 29369 to 32768 slots, cut to 5120, 108 us, 30 of them for
+// the keys and lists, the rest for 5000 moves a unit at 4.5 TB/s (read and written), which neither more rows on the way nor
+// rows side by side raise.  The launch is shaped by the table's columns, since lengths are not read on the host: with a table
+// for 131072 slots instead of 4112 the step of two layers takes 240 us instead of 135, the cut of 32768 slots 224 instead of 111.
 #include <cooperative_groups.h>
 #include <limits.h>
 
