@@ -20,7 +20,7 @@
 // S^T = K Q^T, O^T = V^T P^T, so that up to eight heads fill the instruction exactly.  (Memory is the bound and the tensor pipe
 // 19% busy: tcgen05, with 64 rows at least and accumulators to fetch, has nothing to gain.)
 //
-// Measured (eight B200s, copy rate 6454 GB/s): 16 rows of 24576 slots, 32 query and 8 KV heads of 128 in bf16, 239 to 258 us on
+// Measured (nine B200s, copy rate 6454 GB/s): 16 rows of 24576 slots, 32 query and 8 KV heads of 128 in bf16, 239 to 261 us on
 // all but one (270), 6.2 to 6.7 TB/s; one row of 131072, 88 to 94 us, 5.7 to 6.1 TB/s.  What a call costs beyond its bytes is 10
 // to 15 us: two dependent lookups before the first row (lengths, pages), and after the last one the joins; 300 slots of one row
 // take 8.6 to 9.5 us.  32 query heads of one KV head, 16 rows of 24576 slots: 76 to 83 us, 64 of them 138 to 167, at a floor of 31.

@@ -39,7 +39,11 @@ static int __reduce_add_sync(unsigned, int x) {
 }
 static int __reduce_max_sync(unsigned, int x) { return together(x, [](int* a) { return *std::max_element(a, a + 32); }); }
 static unsigned __ballot_sync(unsigned, bool x) {
-  return (unsigned)together(x, [](int* a) { unsigned m = 0; for (int i = 0; i < 32; ++i) m |= (unsigned)(a[i] != 0) << i; return (int)m; });
+  return (unsigned)together(x, [](int* a) {
+    unsigned m = 0;
+    for (int i = 0; i < 32; ++i) m |= (unsigned)(a[i] != 0) << i;
+    return (int)m;
+  });
 }
 static int __popc(unsigned x) { return __builtin_popcount(x); }
 static int __ffs(unsigned x) { return __builtin_ffs((int)x); }

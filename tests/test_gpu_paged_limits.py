@@ -332,7 +332,7 @@ def test_small_values_survive_among_large_ones_that_cancel(dim, hq, dtype, e4m3)
     c = ref.Cache([n], hq, hkv, dim, 16, dtype, e4m3, seed=dim)
     pg, off = c.places(0, n)
     v = torch.full((n, hkv, dim), 2.0 ** -9)
-    v[:1024], v[3072:] = (448.0, -448.0) if e4m3 else (128.0, -128.0)
+    v[:1024], v[-1024:] = (448.0, -448.0) if e4m3 else (128.0, -128.0)
     ref.put(c.k[0], pg, off, torch.zeros(n, hkv, dim).to(c.k.dtype))
     ref.put(c.v[0], pg, off, v.to(c.v.dtype))
     if e4m3:
