@@ -401,7 +401,11 @@ typedef struct ltri_paged ltri_paged; /* opaque host-side handle */
 enum {
   LTRI_TYPE_BF16 = 0,
   LTRI_TYPE_FP16 = 1,
-  LTRI_TYPE_E4M3 = 2 /* cached rows only: 8 bits an element, value = element * scale of its KV head */
+  LTRI_TYPE_E4M3 = 2, /* cached rows only: 8 bits an element, value = element * scale of its KV head */
+  /* Cached rows only: 4 bits an element and 8 for every 32 of them.  value = number * scale of its block of 32 elements of the
+   * row.  A number, -7 to 7, is held as number + 8, that of the even element in the lower half of its byte; a scale as the upper
+   * half of a half-precision number without its sign (5 bits of exponent with bias 15, 3 of mantissa), up to 480 (0xBF). */
+  LTRI_TYPE_INT4 = 4
 };
 
 typedef struct {
@@ -409,7 +413,7 @@ typedef struct {
   int32_t n_q_heads, n_kv_heads; /* n_q_heads % n_kv_heads == 0, at most 64 query heads per KV head */
   int32_t head_dim;              /* 64, 128 or 256 */
   int32_t type;                  /* of q, k, v and out: LTRI_TYPE_BF16 or LTRI_TYPE_FP16 */
-  int32_t cache_type;            /* of the pages: `type` or LTRI_TYPE_E4M3 */
+  int32_t cache_type;            /* of the pages: `type`, LTRI_TYPE_E4M3 or LTRI_TYPE_INT4 */
   int32_t page_tokens;           /* 1..65536 */
   int32_t max_rows;              /* rows of a call, 1..65535 */
   int64_t n_pages;               /* 1..2^31-1; n_pages * page_tokens slots at most 2^40 */
@@ -434,6 +438,14 @@ size_t ltri_paged_workspace_bytes(const ltri_paged_params* p);
  * and positions are left as they are. */
 int ltri_paged_create(const ltri_paged_params* p, void* cuda_stream, ltri_paged** out);
 
+/* ltri_paged_create for pages of LTRI_TYPE_INT4, which ltri_paged_create refuses.
+ *   block_scales  DEVICE uint8 [n_layers][n_pages][n_kv_heads][page_tokens][2][head_dim / 32], dense, 16-byte aligned: the scales
+ *                 of every slot's K row, then of its V row
+ * Strides are counted in elements as ever (32 of them are 16 bytes); k_scale and v_scale are NULL.  All calls of the handle go on as
+ * they do over other pages: rows are quantised as ltri_paged_append and ltri_paged_decode write them, each block by itself, so
+ * that no scale has to be known beforehand, and ltri_paged_evict moves a slot's scales with its rows. */
+int ltri_paged_create_int4(const ltri_paged_params* p, uint8_t* block_scales, void* cuda_stream, ltri_paged** out);
+
 /* Free the host handle.  Device memory stays with the caller, who keeps it until the calls in flight are through. */
 int ltri_paged_destroy(ltri_paged* cache);
 
@@ -445,11 +457,25 @@ int ltri_paged_destroy(ltri_paged* cache);
  *   row_pos  DEVICE int32 [n_rows]: position of each row's first new token (NULL: the slot's number)
  *   weights  DEVICE float [n_tokens][n_kv_heads]: what the slots have accumulated already (NULL: 0)
  * row_pos and weights are used only if the cache has weights and positions.  8-bit pages get the nearest value to
- * element / scale, ties to even, clamped to +-448.  Tokens that a row has no slot for (more than lens[r] of them) are left
- * out and recorded as LTRI_EDEVICE. */
+ * element / scale, ties to even, clamped to +-448.  4-bit pages: a block's scale is the one nearest to its largest magnitude / 7,
+ * its numbers the nearest to element / scale, ties to even both, clamped to +-480 and +-7 (elements below half the smallest scale,
+ * 2^-18, are 0); a block that holds a NaN is held as NaN.  Tokens that a row has no slot for (more than lens[r] of them) are
+ * left out and recorded as LTRI_EDEVICE. */
 int ltri_paged_append(ltri_paged* cache, int layer, const int32_t* table, int table_pages, int64_t table_stride,
                       const int32_t* lens, int n_rows, const int32_t* starts, int64_t n_tokens, const void* k,
                       const void* v, int64_t kv_stride, const int32_t* row_pos, const float* weights, void* cuda_stream);
+
+/* Read rows of `layer` back: slots of n_rows ragged rows, as dense rows of `type`.
+ *   starts   DEVICE int32 [n_rows + 1], ascending: rows [starts[r], starts[r + 1]) of k and v are row r's.  Those in front of
+ *            starts[0] and from starts[n_rows] on are left as they are.  n_tokens (0 to 2^31 - 1) is what k and v have room for.
+ *   first    DEVICE int32 [n_rows]: the slots begin with this one (NULL: they are the row's last, those that ltri_paged_append
+ *            with the same starts writes).  Slots that the row does not have, or whose page is none, read as 0 and are recorded
+ *            as LTRI_EDEVICE.
+ *   k, v     [n_tokens][n_kv_heads][head_dim], token stride kv_stride elements (0: dense); one of them may be NULL
+ * Values over 8-bit pages are rounded once to `type`; the others are exact. */
+int ltri_paged_read(ltri_paged* cache, int layer, const int32_t* table, int table_pages, int64_t table_stride,
+                    const int32_t* lens, int n_rows, const int32_t* starts, const int32_t* first, int64_t n_tokens, void* k,
+                    void* v, int64_t kv_stride, void* cuda_stream);
 
 /* Attention of one new token per row over the row's slots, in `layer`.
  *   q    [n_rows][n_q_heads ][head_dim], row stride q_stride elements (0: dense)
@@ -462,7 +488,7 @@ int ltri_paged_append(ltri_paged* cache, int layer, const int32_t* table, int ta
  * With weights, every slot's weight becomes weight_decay * weight + the probabilities that the query heads of its KV head
  * give it; a slot that this call writes starts from 0.
  * Logits and sums are fp32; the probabilities enter the product with V as sums of 16-bit terms, so that the outputs carry the
- * rounding of `type` once.  Over bf16 pages these have fp32's 24 bits.  Over fp16 and 8-bit pages they have 22 bits down to
+ * rounding of `type` once.  Over bf16 pages these have fp32's 24 bits.  Over fp16, 8-bit and 4-bit pages they have 22 bits down to
  * 2^-13 of the row's largest probability, and below that steps of 2^-34 of it: n slots that are all small lose at most n * 2^-35
  * of the sum (2^-15 for 2^20 slots).  Logits and products q.K of any magnitude below 10^38; over bf16 pages the sums with V are
  * divided at the end, so that 16 times the sum of a row's |V| has to stay below 10^38, too. */

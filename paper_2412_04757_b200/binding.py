@@ -32,6 +32,7 @@ EXPORTS = [
     "ltri_segment_map_static", "ltri_prefill_chunk_host", "ltri_host_outputs_ready", "ltri_host_kv_bytes",
     "ltri_debug_load_index", "ltri_debug_wait_timeout",
     "ltri_paged_workspace_bytes", "ltri_paged_create", "ltri_paged_destroy", "ltri_paged_append", "ltri_paged_decode",
+    "ltri_paged_create_int4", "ltri_paged_read",
     "ltri_paged_evict", "ltri_paged_sync_status", "ltri_paged_last_cuda_error", "ltri_paged_launch_count",
 ]
 KERNEL_CLASSES = ["append", "evict_index", "attn_local", "map_pass", "segment", "score_topk", "attn_retrieved",
@@ -55,7 +56,8 @@ class LtriParams(C.Structure):
     ]
 
 
-TYPE_BF16, TYPE_FP16, TYPE_E4M3 = 0, 1, 2
+TYPE_BF16, TYPE_FP16, TYPE_E4M3, TYPE_INT4 = 0, 1, 2, 4
+INT4_BLOCK = 32  # elements of a 4-bit row that share a scale
 
 
 class LtriPagedParams(C.Structure):
@@ -128,8 +130,10 @@ def load():
         L.ltri_paged_workspace_bytes.restype = C.c_size_t
         L.ltri_paged_workspace_bytes.argtypes = [C.POINTER(LtriPagedParams)]
         L.ltri_paged_create.argtypes = [C.POINTER(LtriPagedParams), vp, C.POINTER(vp)]
+        L.ltri_paged_create_int4.argtypes = [C.POINTER(LtriPagedParams), vp, vp, C.POINTER(vp)]
         L.ltri_paged_destroy.argtypes = [vp]
         L.ltri_paged_append.argtypes = [vp, ip, vp, ip, i64, vp, ip, vp, i64, vp, vp, i64, vp, vp, vp]
+        L.ltri_paged_read.argtypes = [vp, ip, vp, ip, i64, vp, ip, vp, vp, i64, vp, vp, i64, vp]
         L.ltri_paged_decode.argtypes = [vp, ip, vp, ip, i64, vp, ip, vp, i64, vp, vp, i64, vp, vp, vp, vp]
         L.ltri_paged_evict.argtypes = [vp, ip, ip, vp, ip, i64, vp, vp, ip, ip, ip, ip, vp]
         L.ltri_paged_sync_status.argtypes = [vp, vp]
@@ -429,17 +433,18 @@ class Ltri:
 
 
 class LtriPaged:
-    """A paged K/V cache of the caller's: single-token attention, appending and eviction.  Methods mirror the C entry points.
+    """A paged K/V cache of the caller's: attention, appending, reading back and eviction.  Methods mirror the C entry points.
 
     k_pages, v_pages: [layers][pages][Hkv][page tokens][head_dim] CUDA tensors with the same strides (a permuted view of
     token-major pages, or the halves of one tensor, will do), of ``dtype`` or float8_e4m3fn with k_scale, v_scale (float32
-    [Hkv]).  weights (float32) and positions (int32), both or neither: [layers][pages][Hkv][page tokens], contiguous.  The
+    [Hkv]), or of 4 bits: uint8 [layers][pages][Hkv][page tokens][head_dim / 2] with block_scales (uint8
+    [layers][pages][Hkv][page tokens][2][head_dim / 32], contiguous).  weights (float32) and positions (int32), both or neither: [layers][pages][Hkv][page tokens], contiguous.  The
     tensors stay the caller's; the handle keeps references to them.  It allocates its workspace on ``stream`` (None: the one
     that is current when it is made): let it go only when its calls on other streams are through.
     """
 
     def __init__(self, k_pages, v_pages, n_q_heads, dtype=None, max_rows=1, k_scale=None, v_scale=None, weights=None,
-                 positions=None, softmax_scale=0.0, weight_decay=1.0, stream=None):
+                 positions=None, softmax_scale=0.0, weight_decay=1.0, stream=None, block_scales=None):
         import torch
 
         self.torch = torch
@@ -448,13 +453,16 @@ class LtriPaged:
         types = {torch.bfloat16: TYPE_BF16, torch.float16: TYPE_FP16}
         dtype = dtype if dtype is not None else k_pages.dtype
         if dtype not in types:
-            raise ValueError("dtype of the queries is bfloat16 or float16 (to be named beside 8-bit pages)")
+            raise ValueError("dtype of the queries is bfloat16 or float16 (to be named beside 8-bit and 4-bit pages)")
         if k_pages.dim() != 5 or k_pages.shape != v_pages.shape or any(
                 a != b for n, a, b in zip(k_pages.shape, k_pages.stride(), v_pages.stride()) if n > 1):
             raise ValueError("k_pages and v_pages are [layers][pages][Hkv][page tokens][head_dim] of the same strides")
-        if k_pages.stride(4) != 1 or k_pages.dtype != v_pages.dtype or k_pages.dtype not in (dtype, torch.float8_e4m3fn):
-            raise ValueError("rows are contiguous, of dtype or float8_e4m3fn")
+        int4 = block_scales is not None
+        if k_pages.stride(4) != 1 or k_pages.dtype != v_pages.dtype or (
+                k_pages.dtype != torch.uint8 if int4 else k_pages.dtype not in (dtype, torch.float8_e4m3fn)):
+            raise ValueError("rows are contiguous, of dtype or float8_e4m3fn, or uint8 beside block_scales")
         L, pages, hkv, P, D = k_pages.shape
+        D = 2 * D if int4 else D
         self.device = k_pages.device
         if self.device.type != "cuda":
             raise ValueError("the ltri library runs on CUDA devices only")
@@ -462,15 +470,18 @@ class LtriPaged:
         if scaled != (k_scale is not None) or scaled != (v_scale is not None) or (weights is None) != (positions is None):
             raise ValueError("8-bit pages, and only they, have k_scale and v_scale; weights and positions go together")
         for t, want, shape in ((k_scale, torch.float32, (hkv,)), (v_scale, torch.float32, (hkv,)),
-                               (weights, torch.float32, (L, pages, hkv, P)), (positions, torch.int32, (L, pages, hkv, P))):
+                               (weights, torch.float32, (L, pages, hkv, P)), (positions, torch.int32, (L, pages, hkv, P)),
+                               (block_scales, torch.uint8, (L, pages, hkv, P, 2, D // INT4_BLOCK))):
             if t is not None and (t.dtype != want or t.shape != shape or not t.is_contiguous() or t.device != self.device):
                 raise ValueError(f"scales are float32 [{hkv}], weights float32 and positions int32 {(L, pages, hkv, P)}, "
-                                 "contiguous")
+                                 f"block_scales uint8 {(L, pages, hkv, P, 2, D // INT4_BLOCK)}, contiguous")
         if v_pages.device != self.device:
             raise ValueError("k_pages and v_pages are on one device")
         s = k_pages.stride()
         ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
-        self.params = LtriPagedParams(L, n_q_heads, hkv, D, types[dtype], TYPE_E4M3 if scaled else types[dtype], P, max_rows,
+        s = [2 * x for x in s] if int4 else s  # elements
+        held = TYPE_INT4 if int4 else TYPE_E4M3 if scaled else types[dtype]
+        self.params = LtriPagedParams(L, n_q_heads, hkv, D, types[dtype], held, P, max_rows,
                                       pages, s[0], s[1], s[2], s[3], softmax_scale, weight_decay, ptr(k_pages), ptr(v_pages),
                                       ptr(k_scale), ptr(v_scale), ptr(weights), ptr(positions), None, 0)
         nbytes = int(self.lib.ltri_paged_workspace_bytes(C.byref(self.params)))
@@ -482,13 +493,17 @@ class LtriPaged:
                 self.workspace = torch.empty(nbytes + 256, dtype=torch.uint8, device=self.device)
             self.params.workspace = (self.workspace.data_ptr() + 255) // 256 * 256
             self.params.workspace_bytes = nbytes
-            self._keep = (k_pages, v_pages, k_scale, v_scale, weights, positions)
+            self._keep = (k_pages, v_pages, k_scale, v_scale, weights, positions, block_scales)
             self.dtype, self._q_shape, self._kv_shape = dtype, (n_q_heads, D), (hkv, D)
             self._sizes, self._i32 = {}, torch.int32
             self._raw_stream = torch._C._cuda_getCurrentRawStream
             self._index = self.device.index
-            _check(self.lib.ltri_paged_create(C.byref(self.params), self._stream(stream), C.byref(self._h)),
-                   "ltri_paged_create")
+            if int4:
+                _check(self.lib.ltri_paged_create_int4(C.byref(self.params), ptr(block_scales), self._stream(stream),
+                                                       C.byref(self._h)), "ltri_paged_create_int4")
+            else:
+                _check(self.lib.ltri_paged_create(C.byref(self.params), self._stream(stream), C.byref(self._h)),
+                       "ltri_paged_create")
 
     def _stream(self, stream):
         return self._raw_stream(self._index) if stream is None else stream.cuda_stream
@@ -565,6 +580,27 @@ class LtriPaged:
                                         k.data_ptr(), v.data_ptr(), stride, rp, wp, s)
         if rc:
             self._done(rc, "ltri_paged_append")
+
+    def ltri_paged_read(self, layer, table, lens, starts, k=None, v=None, first=None, stream=None):
+        """Slots of the rows into k, v [tokens][Hkv][head_dim] (either may be None), row r's into [starts[r], starts[r + 1]): those
+        from first (int32 [rows]) on, or the row's last."""
+        n, cols, ts = self._rows(table, lens)
+        if k is None and v is None:
+            raise ValueError("k, v or both")
+        tokens = (v if k is None else k).shape[0]
+        size = (tokens, *self._kv_shape)
+        sp = self._dense(starts, self._i32, (n + 1,), "starts")
+        strides = {self._heads(t, size, name) for t, name in ((k, "k"), (v, "v")) if t is not None}
+        if len(strides) != 1:
+            raise ValueError("k and v have the same strides")
+        fp = None if first is None else self._dense(first, self._i32, self._sizes_of(n)[0], "first")
+        if tokens == 0:
+            return
+        s = self._raw_stream(self._index) if stream is None else stream.cuda_stream
+        rc = self.lib.ltri_paged_read(self._h, layer, table.data_ptr(), cols, ts, lens.data_ptr(), n, sp, fp, tokens,
+                                      None if k is None else k.data_ptr(), None if v is None else v.data_ptr(), strides.pop(), s)
+        if rc:
+            self._done(rc, "ltri_paged_read")
 
     def ltri_paged_decode(self, layer, table, lens, q, k=None, v=None, row_pos=None, out=None, lse=None, stream=None):
         """q [rows][Hq][head_dim]; k, v [rows][Hkv][head_dim], the new tokens' rows, which lens counts already (None: attend

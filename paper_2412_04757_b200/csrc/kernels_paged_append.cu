@@ -4,7 +4,7 @@
 // rows and as many of its V rows before they look up the token's row, slot and page, which the loads do not depend on.
 // Consecutive lanes take consecutive chunks, so both sides move whole rows whatever the order of the axes.  (A chunk a thread,
 // behind the lookups: 38 us for 22700 tokens of eight KV heads, 33 so.)
-#include "paged.cuh"
+#include "paged_int4.cuh"
 
 namespace ltri {
 
@@ -56,6 +56,17 @@ __global__ void __launch_bounds__(kAppThreads)
       if (c.cache_type == LTRI_TYPE_E4M3) {
         *reinterpret_cast<uint2*>(c.k + at + ch * 8) = paged_quantise(c.type, kx[u], c.ks[head]);
         *reinterpret_cast<uint2*>(c.v + at + ch * 8) = paged_quantise(c.type, vx[u], c.vs[head]);
+      } else if (c.cache_type == LTRI_TYPE_INT4) {
+        // (the four lanes of a block have the same token and head, and are all here: rows are multiples of four chunks)
+        unsigned ks, vs;
+        const uint32_t kn = i4_quantise(c.type, kx[u], ks), vn = i4_quantise(c.type, vx[u], vs);
+        *reinterpret_cast<uint32_t*>(c.k + at + ch * 4) = kn;
+        *reinterpret_cast<uint32_t*>(c.v + at + ch * 4) = vn;
+        if ((ch & 3) == 0) {
+          unsigned char* to = c.sc + paged_word(c, layer, page, head, place) * (c.D / 16) + ch / 4;
+          to[0] = (unsigned char)ks;
+          to[c.D / 32] = (unsigned char)vs;
+        }
       } else {
         *reinterpret_cast<uint4*>(c.k + at + ch * 16) = kx[u];
         *reinterpret_cast<uint4*>(c.v + at + ch * 16) = vx[u];

@@ -25,21 +25,22 @@
 // to 15 us: two dependent lookups before the first row (lengths, pages), and after the last one the joins; 300 slots of one row
 // take 8.6 to 9.5 us.  32 query heads of one KV head, 16 rows of 24576 slots: 76 to 83 us, 64 of them 138 to 167, at a floor of 31.
 #include "mma_util.cuh"
-#include "paged.cuh"
 #include "paged_deal.cuh"
+#include "paged_int4.cuh"
 
 namespace ltri {
 
-enum { kPdBf16 = 0, kPdFp16 = 1, kPdE4m3 = 2 };  // what the pages hold
+enum { kPdBf16 = 0, kPdFp16 = 1, kPdE4m3 = 2, kPdInt4 = 3 };  // what the pages hold
 
 template <int KIND, int D, int NT>
 struct PdShape {
-  static constexpr int kRow = KIND == kPdE4m3 ? D : 2 * D;      // bytes of a cached row
+  static constexpr int kRow = KIND == kPdInt4 ? D / 2 : KIND == kPdE4m3 ? D : 2 * D;  // bytes of a cached row
+  static constexpr int kScales = KIND == kPdInt4 ? D / 16 : 0;  // bytes of a slot's scales, K's and V's
   // Blocks of 16 slots in a tile: 8 KB of rows or more, since what a tile costs besides its rows (cursors, page numbers, the
   // reference) took 8-bit rows in tiles of 16 slots to 1.4 times the instructions.
-  static constexpr int kMt = kRow >= 256 ? 1 : 256 / kRow;
+  static constexpr int kMt = kRow >= 256 ? 1 : kRow == 32 ? 4 : 256 / kRow;
   static constexpr int kTile = 16 * kMt;                        // slots
-  static constexpr int kStage = 2 * kTile * kRow;               // K rows, V rows
+  static constexpr int kStage = kTile * (2 * kRow + kScales);   // K rows, V rows, scales
   static constexpr int kWarps = kRow == 512 ? 4 : 8;            // of a CTA, one CTA an SM
   static constexpr int kFit = (232448 - 2048) / (kWarps * (kStage + 8 * kTile));
   static constexpr int kStages = kFit > 8 ? 8 : kFit;
@@ -105,7 +106,16 @@ __device__ __forceinline__ uint32_t pd_halves_hi(uint32_t x) {
 // What a row's number does to the number of a chunk in it, for rows of CHUNKS chunks.
 template <int CHUNKS>
 __device__ __forceinline__ constexpr int pd_swizzle(int row) {
-  return CHUNKS >= 8 ? row & 7 : (row >> 1) & 3;
+  return CHUNKS >= 8 ? row & 7 : CHUNKS == 4 ? (row >> 1) & 3 : (row >> 2) & 1;
+}
+
+// BYTES bytes on their way, or zeros.
+template <int BYTES>
+__device__ __forceinline__ void pd_request(uint32_t to, const void* from, bool there) {
+  const int n = there ? BYTES : 0;
+  if (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"(to), "l"(from), "r"(n));
+  else if (BYTES == 8) asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;\n" ::"r"(to), "l"(from), "r"(n));
+  else asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;\n" ::"r"(to), "l"(from), "r"(n));
 }
 
 // A unit that a warp's run, or a CTA's, leaves unfinished.
@@ -204,7 +214,16 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
         }
       }
     }
-    if (KIND != kPdE4m3 && fresh >= 0 && lane < RC) {
+    if constexpr (KIND == kPdInt4) {
+#pragma unroll
+      for (int j = lane; j < TILE; j += 32) {
+        const int slot = u.tile * TILE + j, page = s_page[j];
+        const bool there = (unsigned)page < (unsigned)c.n_pages && j != fresh;
+        const size_t word = there ? paged_word(c, layer, page, u.head, slot - paged_nth(c, slot) * c.P) : 0;
+        pd_request<Sh::kScales>(ring_s + st * Sh::kStage + 2 * TILE * Sh::kRow + j * Sh::kScales, c.sc + word * Sh::kScales, there);
+      }
+    }
+    if (KIND != kPdE4m3 && KIND != kPdInt4 && fresh >= 0 && lane < RC) {
       const int bytes = (unsigned)s_page[fresh] < (unsigned)c.n_pages ? 16 : 0;
       const size_t at = u.row * a.kv_stride + (size_t)u.head * (2 * D) + lane * 16;
       const uint32_t to = ring_s + st * Sh::kStage + fresh * Sh::kRow + ((lane ^ pd_swizzle<RC>(fresh)) << 4);
@@ -224,11 +243,23 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
   int next_at = -(1 << 30);  // the tile of the run that q_next's unit begins with
   auto load_queries = [&](Queries& x, const PdCursor& u) {
     x.ks = c.ks ? c.ks[u.head] : 1.f;
-    x.vs = c.vs ? c.vs[u.head] : 1.f;
+    x.vs = KIND == kPdInt4 ? kI4Back : c.vs ? c.vs[u.head] : 1.f;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       const int in_group = u.block * H + nt * 8 + g;
       const unsigned char* qr = a.q + u.row * a.q_stride + ((size_t)u.head * c.G + in_group) * D * 2;
+      if constexpr (KIND == kPdInt4) {
+        // (a lane's eight neighbours of 32 elements, as the numbers' bits lie in a word: 0 and 4, 1 and 5; 2 and 6, 3 and 7)
+#pragma unroll
+        for (int i = 0; i < DT; i += 2) {
+          const uint4 e = in_group < c.G ? *reinterpret_cast<const uint4*>(qr + (i * 16 + q4 * 8) * 2) : make_uint4(0u, 0u, 0u, 0u);
+          x.b[nt][i][0] = __byte_perm(e.x, e.z, 0x5410);
+          x.b[nt][i][1] = __byte_perm(e.x, e.z, 0x7632);
+          x.b[nt][i + 1][0] = __byte_perm(e.y, e.w, 0x5410);
+          x.b[nt][i + 1][1] = __byte_perm(e.y, e.w, 0x7632);
+        }
+        continue;
+      }
 #pragma unroll
       for (int i = 0; i < DT; ++i) {
         // (8-bit rows: a 16-byte chunk is one step of 16, of which a lane holds four neighbours)
@@ -241,10 +272,51 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
     }
   };
   float sc[NT][2];  // logits' factors of this lane's heads
+  // 4-bit rows: what 8 more in every number adds to the sums of a block's products, for this lane's heads, with its sign turned
+  float bias[NT][KIND == kPdInt4 ? D / kI4Block : 1][2];
   auto scale_queries = [&]() {
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       float back = 1.f;
+      if constexpr (KIND == kPdInt4) {
+        // As over 8-bit rows, a power of two brings the row's largest element to [2^14, 2^15), and halves do the rest.  The
+        // numbers enter as the smallest halves, n * 2^-24, and every other pair of them 2^4 larger, which is taken from its
+        // queries: what falls below the halves' range is 2^-35 of the largest.
+        float most = 0.f;
+#pragma unroll
+        for (int i = 0; i < DT; ++i)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const float2 f = paged_unpack(c.type, q.b[nt][i][j]);
+            most = fmaxf(most, fmaxf(fabsf(f.x), fabsf(f.y)));
+          }
+        most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
+        most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
+        const int ex = (int)(__float_as_uint(most) >> 23);  // biased exponent
+        const int up = ex == 0 || ex == 255 ? 0 : 127 + 14 - ex;
+        // (2^up may lie outside fp32's range: two factors)
+        const float u0 = __int_as_float((127 + up / 2) << 23), u1 = __int_as_float((127 + up - up / 2) << 23);
+#pragma unroll
+        for (int b = 0; b < D / kI4Block; ++b) {
+          float all = 0.f;
+#pragma unroll
+          for (int i = 2 * b; i < 2 * b + 2; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              const float2 f = paged_unpack(c.type, q.b[nt][i][j]);
+              const float by = j ? u1 * 0x1p-4f : u1;
+              const uint32_t h = paged_pack(LTRI_TYPE_FP16, f.x * u0 * by, f.y * u0 * by);
+              q.b[nt][i][j] = h;
+              const float2 z = paged_unpack(LTRI_TYPE_FP16, h);
+              all += (z.x + z.y) * (j ? 16.f : 1.f);
+            }
+          all += __shfl_xor_sync(0xffffffffu, all, 1);
+          all += __shfl_xor_sync(0xffffffffu, all, 2);
+#pragma unroll
+          for (int e = 0; e < 2; ++e) bias[nt][b][e] = -0x1p-21f * __shfl_sync(0xffffffffu, all, (2 * q4 + e) * 4);
+        }
+        back = 0x1p24f * __int_as_float((127 - up / 2) << 23) * __int_as_float((127 - up + up / 2) << 23);
+      }
       if (KIND == kPdE4m3 && c.type == LTRI_TYPE_BF16) {
         // bf16 queries as halves: a power of two brings the row's largest element to [2^14, 2^15); what then falls below
         // the halves' range is 2^-39 of it
@@ -273,7 +345,7 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
       for (int e = 0; e < 2; ++e) {
         const float b = __shfl_sync(0xffffffffu, back, (2 * q4 + e) * 4);
         sc[nt][e] = c.scale;
-        if (KIND != kPdE4m3) continue;
+        if (KIND != kPdE4m3 && KIND != kPdInt4) continue;
         // The three factors' product may lie in fp32's range where that of two does not.  Never zero: the logits of slots that
         // are not there are -infinity times this, and at the smallest normal number products q.K, here below 2^36, are nothing.
         const float f = (float)((double)c.scale * q.ks * b);
@@ -286,6 +358,14 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
     const uint32_t y0 = pd_transpose(paged_pack(c.type, z[0], z[1])), y1 = pd_transpose(paged_pack(c.type, z[2], z[3]));
     const int in_group = u.block * H + nt * 8 + g;
     if (in_group >= c.G) return;
+    if constexpr (KIND == kPdInt4) {  // element i % 4 of the groups of four 2 q4 and 2 q4 + 1 of 32, and of the next 32
+      unsigned char* to = a.out + (((size_t)u.row * c.Hq + (size_t)u.head * c.G + in_group) * D + i / 4 * 64 + q4 * 8 + i % 4) * 2;
+      *reinterpret_cast<unsigned short*>(to) = (unsigned short)y0;
+      *reinterpret_cast<unsigned short*>(to + 8) = (unsigned short)(y0 >> 16);
+      *reinterpret_cast<unsigned short*>(to + 64) = (unsigned short)y1;
+      *reinterpret_cast<unsigned short*>(to + 72) = (unsigned short)(y1 >> 16);
+      return;
+    }
     unsigned char* to = a.out + (((size_t)u.row * c.Hq + (size_t)u.head * c.G + in_group) * D + i * 16) * 2;
     if (KIND == kPdE4m3) {  // elements 4 q4, + 2 and 4 q4 + 1, + 3
       *reinterpret_cast<uint2*>(to + q4 * 8) = make_uint2(__byte_perm(y0, y1, 0x5410), __byte_perm(y0, y1, 0x7632));
@@ -305,7 +385,7 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
   };
   // (one after the other: the quotient of a small scale and a large sum may lie below fp32's range where the output does not)
   auto one_over = [](float sum) { return sum == 0.f ? 0.f : 1.f / sum; };
-  auto scaled = [](float x, float by, float vs) { return KIND == kPdE4m3 ? x * by * vs : x * by; };
+  auto scaled = [](float x, float by, float vs) { return KIND == kPdE4m3 || KIND == kPdInt4 ? x * by * vs : x * by; };
 
   float O[NT][DT][4], ref[NT][2], sum[NT][2];
   // A unit's heads, all of whose sums this warp has.
@@ -425,7 +505,7 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
       const int slot0 = cu.tile * TILE;
       const int fresh = a.k && cu.n - 1 - slot0 < TILE ? cu.n - 1 - slot0 : -1;
       uint4 kx = make_uint4(0u, 0u, 0u, 0u), vx = kx;
-      if (KIND == kPdE4m3 && fresh >= 0 && lane < D / 8) {
+      if ((KIND == kPdE4m3 || KIND == kPdInt4) && fresh >= 0 && lane < D / 8) {
         const size_t at_new = cu.row * a.kv_stride + ((size_t)cu.head * D + lane * 8) * 2;
         kx = *reinterpret_cast<const uint4*>(a.k + at_new);
         vx = *reinterpret_cast<const uint4*>(a.v + at_new);
@@ -441,7 +521,31 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
         const size_t to = paged_row(c, layer, has ? page : 0, cu.head, place);
         unsigned char* in = stage + fresh * Sh::kRow;
         if (lane < D / 8) {
-          if (KIND == kPdE4m3) {  // and into the tile
+          if constexpr (KIND == kPdInt4) {  // and into the tile
+            uint32_t kn = 0u, vn = 0u;
+            unsigned ks = 0u, vs = 0u;
+            if (has) {
+              kn = i4_quantise(c.type, kx, ks);
+              vn = i4_quantise(c.type, vx, vs);
+            }
+            in += ((lane / 4 ^ sw) << 4) + (lane & 3) * 4;
+            *reinterpret_cast<uint32_t*>(in) = kn;
+            *reinterpret_cast<uint32_t*>(in + TILE * Sh::kRow) = vn;
+            unsigned char* s_sc = stage + 2 * TILE * Sh::kRow + fresh * Sh::kScales;
+            if ((lane & 3) == 0) {
+              s_sc[lane / 4] = (unsigned char)ks;
+              s_sc[D / 32 + lane / 4] = (unsigned char)vs;
+            }
+            if (writes) {
+              *reinterpret_cast<uint32_t*>(c.k + to + lane * 4) = kn;
+              *reinterpret_cast<uint32_t*>(c.v + to + lane * 4) = vn;
+              unsigned char* g_sc = c.sc + paged_word(c, layer, page, cu.head, place) * Sh::kScales;
+              if ((lane & 3) == 0) {
+                g_sc[lane / 4] = (unsigned char)ks;
+                g_sc[D / 32 + lane / 4] = (unsigned char)vs;
+              }
+            }
+          } else if (KIND == kPdE4m3) {  // and into the tile
             uint2 ky = make_uint2(0u, 0u), vy = ky;
             if (has) {
               ky = paged_quantise(c.type, kx, c.ks[cu.head]);
@@ -471,7 +575,46 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
       for (int m = 0; m < MT; ++m) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) x[m][nt][0] = x[m][nt][1] = x[m][nt][2] = x[m][nt][3] = 0.f;
-        if (KIND == kPdE4m3) {
+        if constexpr (KIND == kPdInt4) {
+          // S^T = sum over the blocks of 32 elements of scale * (numbers Q^T): a product's accumulator begins with what makes up
+          // for the numbers' offset
+          const unsigned char* sc_k = stage + 2 * TILE * Sh::kRow + (m * 16 + g) * Sh::kScales;
+          float s_lo[D / kI4Block], s_hi[D / kI4Block];
+#pragma unroll
+          for (int b = 0; b < D / kI4Block; b += 2) {
+            const int at_b = b / 4 * 4, in_b = b % 4;  // (64 elements a row: two scales beside V's, in one word)
+            const float2 lo = i4_scales_f32(*reinterpret_cast<const uint32_t*>(sc_k + at_b), in_b,
+                                            *reinterpret_cast<const uint32_t*>(sc_k + at_b), in_b + 1);
+            const float2 hi = i4_scales_f32(*reinterpret_cast<const uint32_t*>(sc_k + 8 * Sh::kScales + at_b), in_b,
+                                            *reinterpret_cast<const uint32_t*>(sc_k + 8 * Sh::kScales + at_b), in_b + 1);
+            s_lo[b] = lo.x;
+            s_lo[b + 1] = lo.y;
+            s_hi[b] = hi.x;
+            s_hi[b + 1] = hi.y;
+          }
+#pragma unroll
+          for (int b2 = 0; b2 < D / kI4Block; b2 += 2) {
+            uint32_t w[4];
+            ldsm_x4(w, (k_at ^ (b2 << 4)) + m * 16 * Sh::kRow);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              const int b = b2 + j;
+              const uint32_t w0 = w[2 * j], w1 = w[2 * j + 1], u0 = w0 >> 8, u1 = w1 >> 8;
+              const uint32_t f0[4] = {w0 & 0x000f000fu, w1 & 0x000f000fu, w0 & 0x00f000f0u, w1 & 0x00f000f0u};
+              const uint32_t f1[4] = {u0 & 0x000f000fu, u1 & 0x000f000fu, u0 & 0x00f000f0u, u1 & 0x00f000f0u};
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt) {
+                float z[4] = {bias[nt][b][0], bias[nt][b][1], bias[nt][b][0], bias[nt][b][1]};
+                pd_mma<KIND>(z, f0, q.b[nt][2 * b][0], q.b[nt][2 * b][1]);
+                pd_mma<KIND>(z, f1, q.b[nt][2 * b + 1][0], q.b[nt][2 * b + 1][1]);
+                x[m][nt][0] = fmaf(s_lo[b], z[0], x[m][nt][0]);
+                x[m][nt][1] = fmaf(s_lo[b], z[1], x[m][nt][1]);
+                x[m][nt][2] = fmaf(s_hi[b], z[2], x[m][nt][2]);
+                x[m][nt][3] = fmaf(s_hi[b], z[3], x[m][nt][3]);
+              }
+            }
+          }
+        } else if (KIND == kPdE4m3) {
 #pragma unroll
           for (int i = 0; i < DT; i += 2) {
             uint32_t b[4];
@@ -587,10 +730,11 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
       // tensor cores cut off what an accumulator has no bits for, always towards zero: with O as the accumulator small values
       // beside large ones were lost, and outputs over bf16 pages differed twice as much from fp32 arithmetic's.  64 ragged rows in
       // 8 bits 61.5 us, with O 59.8; rows of 256 in 16 bits 35.8 and 34.7; the others no slower.)
-      const int v_row = KIND == kPdE4m3 ? lane & 15 : (lane & 7) + (lane >> 4) * 8;
-      const int v_ch = KIND == kPdE4m3 ? lane >> 4 : (lane >> 3) & 1;
+      constexpr bool kPacked = KIND == kPdE4m3 || KIND == kPdInt4;
+      const int v_row = kPacked ? lane & 15 : (lane & 7) + (lane >> 4) * 8;
+      const int v_ch = kPacked ? lane >> 4 : (lane >> 3) & 1;
       const uint32_t v_at = sv + v_row * Sh::kRow + ((v_ch ^ pd_swizzle<RC>(v_row)) << 4);
-      constexpr int kAtOnce = KIND == kPdE4m3 ? 2 : 1;  // slices of 16 elements
+      constexpr int kAtOnce = KIND == kPdInt4 ? 4 : KIND == kPdE4m3 ? 2 : 1;  // slices of 16 elements
 #pragma unroll
       for (int i = 0; i < DT; i += kAtOnce) {
         float z[kAtOnce][NT][4];
@@ -601,10 +745,33 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
           uint32_t b[4];
-          ldsm_x4_t(b, (v_at ^ (i << (KIND == kPdE4m3 ? 4 : 5))) + m * 16 * Sh::kRow);
+          ldsm_x4_t(b, (v_at ^ (KIND == kPdInt4 ? i << 3 : i << (KIND == kPdE4m3 ? 4 : 5))) + m * 16 * Sh::kRow);
+          uint32_t v4[4][4];
+          if constexpr (KIND == kPdInt4) {
+            // a 16-byte chunk's 8 groups of four neighbours are the 8 rows of a transposed matrix: row g has elements 4g to
+            // 4g + 3 of slots 2 q4 and 2 q4 + 1 (b[0], b[2]: of 32 elements and the next 32) or of slots 8 further (b[1], b[3])
+            const unsigned char* sc_v = stage + 2 * TILE * Sh::kRow + (m * 16 + 2 * q4) * Sh::kScales + Sh::kScales / 2;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const unsigned char* at_s = sc_v + e * 8 * Sh::kScales;
+              // (64 elements a row: V's two scales are the upper half of their word)
+              const int at_b = D == 64 ? -2 : i / 8 * 4, in_b = D == 64 ? 2 : i / 4 * 2 % 4;
+              const uint32_t s0 = *reinterpret_cast<const uint32_t*>(at_s + at_b);
+              const uint32_t s1 = *reinterpret_cast<const uint32_t*>(at_s + Sh::kScales + at_b);
+#pragma unroll
+              for (int j = 0; j < 2; ++j)
+                i4_values(v4[2 * j + e], b[2 * j + e], i4_factors(i4_scales(s0, in_b + j, s1, in_b + j)));
+            }
+          }
 #pragma unroll
           for (int j = 0; j < kAtOnce; ++j) {
             uint32_t f[4] = {b[0], b[1], b[2], b[3]};
+            if constexpr (KIND == kPdInt4) {  // rows g: an element of b[0] and b[1], rows g + 8: the same of the next 32
+              f[0] = v4[0][j];
+              f[1] = v4[2][j];
+              f[2] = v4[1][j];
+              f[3] = v4[3][j];
+            }
             if (KIND == kPdE4m3) {
               // a 16-byte chunk's 8 pairs of neighbours are the 8 rows of a transposed matrix: row g has elements 2g and 2g + 1
               // of slots 2 q4 and 2 q4 + 1
@@ -782,7 +949,7 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
     u.row = o.row;
     u.head = o.head;
     u.block = o.block;
-    const float vs = c.vs ? c.vs[o.head] : 1.f;
+    const float vs = KIND == kPdInt4 ? kI4Back : c.vs ? c.vs[o.head] : 1.f;
 #pragma unroll
     for (int k = 0; k < kSlices; ++k) {
       if (k * W + warp >= NT * DT) continue;
@@ -892,7 +1059,8 @@ cudaError_t launch_kind(const PagedCache& c, const PagedRows& r, int layer, cons
 }  // namespace
 
 cudaError_t prepare_paged() {
-  return first_error(prepare_kind<kPdBf16>(), first_error(prepare_kind<kPdFp16>(), prepare_kind<kPdE4m3>()));
+  return first_error(first_error(prepare_kind<kPdBf16>(), prepare_kind<kPdFp16>()),
+                     first_error(prepare_kind<kPdE4m3>(), prepare_kind<kPdInt4>()));
 }
 
 PagedBlocks paged_blocks(int group) {
@@ -909,7 +1077,8 @@ cudaError_t launch_paged_decode(const PagedCache& c, const PagedRows& r, int lay
   const PagedBlocks b = paged_blocks(c.G);
   const PdWork w{b.heads, b.count, c.part, c.lead, (int)paged_part_floats(c.G, c.D), c.count, c.logits, c.lse2};
   cudaError_t e;
-  if (c.cache_type == LTRI_TYPE_E4M3) e = launch_kind<kPdE4m3>(c, r, layer, a, w, s);
+  if (c.cache_type == LTRI_TYPE_INT4) e = launch_kind<kPdInt4>(c, r, layer, a, w, s);
+  else if (c.cache_type == LTRI_TYPE_E4M3) e = launch_kind<kPdE4m3>(c, r, layer, a, w, s);
   else if (c.type == LTRI_TYPE_BF16) e = launch_kind<kPdBf16>(c, r, layer, a, w, s);
   else e = launch_kind<kPdFp16>(c, r, layer, a, w, s);
   if (e != cudaSuccess || !c.w) return e;

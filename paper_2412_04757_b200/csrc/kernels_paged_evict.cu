@@ -125,8 +125,10 @@ __global__ void __launch_bounds__(kEvThreads, 2)
   auto ask = [&](int* x, int none) { return lane < C ? *cluster.map_shared_rank(x, lane) : none; };
   // ---- where one slot leaves, the last one's rows are on their way to its place from the beginning ----
   const bool single = n - budget == 1, carries = single && rank == 0 && warp == kEvWarps - 1;
-  const int chunks = c.row_bytes / 16;  // 4, 8, 16 or 32 of 16 bytes: a move is 2 * chunks
+  const int chunks = c.row_bytes / 16;  // 2, 4, 8, 16 or 32 of 16 bytes: a move is 2 * chunks
+  const int sc_words = c.sc ? c.D / 64 : 0;  // a slot's scales beside 4-bit rows, 1, 2 or 4 words of 4 bytes
   uint4 carried[2];
+  uint32_t carried_sc = 0u;
   float carried_w = 0.f;
   int carried_pos = 0, carried_page = -1;
   if (carries) {
@@ -143,6 +145,7 @@ __global__ void __launch_bounds__(kEvThreads, 2)
       const size_t at = paged_word(c, layer, carried_page, head, place);
       carried_w = c.w[at];
       carried_pos = c.pos[at];
+      if (lane < sc_words) carried_sc = reinterpret_cast<const uint32_t*>(c.sc)[at * sc_words + lane];
     }
   }
   // ---- keys: a thread's slots in batches whose loads are all on their way at once; the newest position comes out of them ----
@@ -228,8 +231,9 @@ __global__ void __launch_bounds__(kEvThreads, 2)
           if (ch < 2 * chunks)
             __stcg(reinterpret_cast<uint4*>((ch >= chunks ? c.v + (ch - chunks) * 16 : c.k + ch * 16) + to), carried[k]);
         }
+        const size_t at = paged_word(c, layer, page, head, place);
+        if (lane < sc_words) reinterpret_cast<uint32_t*>(c.sc)[at * sc_words + lane] = carried_sc;
         if (lane == 0) {
-          const size_t at = paged_word(c, layer, page, head, place);
           c.w[at] = carried_w;
           c.pos[at] = carried_pos;
         }
@@ -440,6 +444,7 @@ __global__ void __launch_bounds__(kEvThreads, 2)
     const int i = base + lane / kEvGroup * stride + lane % kEvGroup;
     long long from = -1, to = -1, wt = -1;
     float w = 0.f;
+    uint32_t sc[4];
     int pos = 0;
     int src = -1, dst = -1;
     if (all_held) {
@@ -461,6 +466,9 @@ __global__ void __launch_bounds__(kEvThreads, 2)
           wt = (long long)paged_word(c, layer, dp, head, dst - dn * c.P);
           w = c.w[wf];
           pos = c.pos[wf];
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if (k < sc_words) sc[k] = reinterpret_cast<const uint32_t*>(c.sc)[wf * sc_words + k];
         }
       }
     }
@@ -487,6 +495,9 @@ __global__ void __launch_bounds__(kEvThreads, 2)
     if (wt >= 0) {
       c.w[wt] = w;
       c.pos[wt] = pos;
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (k < sc_words) reinterpret_cast<uint32_t*>(c.sc)[wt * sc_words + k] = sc[k];
     }
   }
   cluster.sync();  // no CTA leaves while its shared memory is read

@@ -25,6 +25,7 @@ struct PagedCache {
   float decay;
   unsigned char *k, *v;
   const float *ks, *vs;         // per KV head, or null
+  unsigned char* sc;            // [L][n_pages][Hkv][P][2][D / 32], K's and V's scales of 4-bit rows, or null
   float* w;                     // [L][n_pages][Hkv][P], or null
   int* pos;
   int* status;                  // [4]
@@ -56,6 +57,13 @@ struct PagedAppend {
   const float* weights;
 };
 
+struct PagedRead {
+  const int *starts, *first;
+  long long n_tokens;
+  unsigned char *k, *v;         // either may be null
+  long long stride;             // bytes between tokens
+};
+
 struct PagedStep {
   const unsigned char *q, *k, *v;
   long long q_stride, kv_stride;  // bytes between rows
@@ -78,6 +86,7 @@ cudaError_t prepare_paged();
 cudaError_t prepare_paged_evict();
 int paged_evict_cluster();
 cudaError_t launch_paged_append(const PagedCache& c, const PagedRows& r, int layer, const PagedAppend& a, cudaStream_t s);
+cudaError_t launch_paged_read(const PagedCache& c, const PagedRows& r, int layer, const PagedRead& a, cudaStream_t s);
 cudaError_t launch_paged_decode(const PagedCache& c, const PagedRows& r, int layer, const PagedStep& a, cudaStream_t s);
 cudaError_t launch_paged_evict(const PagedCache& c, const PagedRows& r, int layer_begin, int layer_count, int* new_lens,
                                int budget, int n_sink, int recent, cudaStream_t s);

@@ -19,6 +19,8 @@ namespace {
 
 constexpr int kPagedMaxSms = 256;  // CTAs that a decode call can have partial sums of
 
+int element_bits(int type) { return type == LTRI_TYPE_INT4 ? 4 : type == LTRI_TYPE_E4M3 ? 8 : 16; }
+
 bool aligned(const void* p, uintptr_t a) { return p && (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
 bool validate(const ltri_paged_params* p) {
@@ -27,18 +29,18 @@ bool validate(const ltri_paged_params* p) {
   if (p->n_q_heads % p->n_kv_heads || p->n_q_heads / p->n_kv_heads > 64) return false;
   if (p->head_dim != 64 && p->head_dim != 128 && p->head_dim != 256) return false;
   if (p->type != LTRI_TYPE_BF16 && p->type != LTRI_TYPE_FP16) return false;
-  if (p->cache_type != p->type && p->cache_type != LTRI_TYPE_E4M3) return false;
+  if (p->cache_type != p->type && p->cache_type != LTRI_TYPE_E4M3 && p->cache_type != LTRI_TYPE_INT4) return false;
   if (p->page_tokens < 1 || p->page_tokens > 65536 || p->max_rows < 1 || p->max_rows > 65535) return false;
   if (p->n_pages < 1 || p->n_pages > 0x7fffffffll || p->n_pages * p->page_tokens > (1ll << 40)) return false;
-  const long long es = p->cache_type == LTRI_TYPE_E4M3 ? 1 : 2;
+  const long long bits = element_bits(p->cache_type);
   // an axis of one entry may have any stride; the others keep 16-byte chunks aligned and rows apart from each other
   const struct { long long n, stride; } axes[4] = {{p->n_layers, p->layer_stride}, {p->n_pages, p->page_stride},
                                                    {p->n_kv_heads, p->head_stride}, {p->page_tokens, p->token_stride}};
   double extent = 0.0;  // bytes; far from where 64 bits end, as are the workspace's
   for (const auto& a : axes) {
     if (a.n == 1) continue;
-    if (a.stride < p->head_dim || a.stride > (1ll << 42) || a.stride * es % 16) return false;
-    extent += (double)(a.n - 1) * (double)a.stride * (double)es;
+    if (a.stride < p->head_dim || a.stride > (1ll << 42) || a.stride * bits % 128) return false;
+    extent += (double)(a.n - 1) * (double)a.stride * (double)bits / 8.0;
   }
   if (extent > 0x1p56 || (double)p->n_layers * (double)p->n_pages * p->page_tokens * p->n_kv_heads > 0x1p48) return false;
   if (!std::isfinite(p->softmax_scale) || p->softmax_scale < 0.f) return false;
@@ -137,18 +139,8 @@ bool meets(const void* a, long long bytes, const void* b, long long n, long long
   return first < n && first * stride < d + bytes;
 }
 
-}  // namespace
-
-extern "C" {
-
-size_t ltri_paged_workspace_bytes(const ltri_paged_params* p) {
-  return validate(p) ? layout(*p, kPagedMaxSms, nullptr, nullptr, nullptr) : 0;
-}
-
-int ltri_paged_create(const ltri_paged_params* p, void* cuda_stream, ltri_paged** out) {
-  if (!out) return LTRI_EINVAL;
-  *out = nullptr;
-  if (!validate(p)) return LTRI_EINVAL;
+// block_scales: 4-bit pages' (not looked at beside others).
+int create(const ltri_paged_params* p, uint8_t* block_scales, cudaStream_t s, ltri_paged** out) {
   if (!aligned(p->k_pages, 16) || !aligned(p->v_pages, 16) || !aligned(p->workspace, 256)) return LTRI_EINVAL;
   const bool scaled = p->cache_type == LTRI_TYPE_E4M3;
   if (scaled ? !aligned(p->k_scale, 4) || !aligned(p->v_scale, 4) : p->k_scale || p->v_scale) return LTRI_EINVAL;
@@ -163,7 +155,8 @@ int ltri_paged_create(const ltri_paged_params* p, void* cuda_stream, ltri_paged*
   d = PagedCache{};
   size_t zeroed = 0;
   layout(*p, kPagedMaxSms, &d, static_cast<unsigned char*>(p->workspace), &zeroed);
-  const long long es = scaled ? 1 : 2;
+  const long long bits = element_bits(p->cache_type);
+  auto bytes = [bits](long long elements) { return elements / 8 * bits; };  // (strides are multiples of 16 bytes)
   d.Hq = p->n_q_heads;
   d.Hkv = p->n_kv_heads;
   d.G = d.Hq / d.Hkv;
@@ -171,25 +164,25 @@ int ltri_paged_create(const ltri_paged_params* p, void* cuda_stream, ltri_paged*
   d.P = p->page_tokens;
   d.type = p->type;
   d.cache_type = p->cache_type;
-  d.row_bytes = (int)(d.D * es);
+  d.row_bytes = (int)bytes(d.D);
   d.n_pages = (int)p->n_pages;
   int log = 0;
   while ((1 << log) < d.P) ++log;
   d.p_shift = 31 + log;
   d.p_mul = (unsigned)((1ull << d.p_shift) / d.P + 1);
-  d.ls = p->n_layers > 1 ? p->layer_stride * es : 0;
-  d.ps = p->n_pages > 1 ? p->page_stride * es : 0;
-  d.hs = p->n_kv_heads > 1 ? p->head_stride * es : 0;
-  d.ts = p->page_tokens > 1 ? p->token_stride * es : 0;
+  d.ls = p->n_layers > 1 ? bytes(p->layer_stride) : 0;
+  d.ps = p->n_pages > 1 ? bytes(p->page_stride) : 0;
+  d.hs = p->n_kv_heads > 1 ? bytes(p->head_stride) : 0;
+  d.ts = p->page_tokens > 1 ? bytes(p->token_stride) : 0;
   d.scale = (p->softmax_scale > 0.f ? p->softmax_scale : 1.f / std::sqrt((float)d.D)) * 1.4426950408889634f;
   d.decay = p->weight_decay;
   d.k = static_cast<unsigned char*>(p->k_pages);
   d.v = static_cast<unsigned char*>(p->v_pages);
   d.ks = p->k_scale;
   d.vs = p->v_scale;
+  d.sc = p->cache_type == LTRI_TYPE_INT4 ? block_scales : nullptr;
   d.w = p->weights;
   d.pos = p->positions;
-  cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   cudaError_t e = cudaGetDevice(&c->device);
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&d.sms, cudaDevAttrMultiProcessorCount, c->device);
   if (d.sms > kPagedMaxSms) d.sms = kPagedMaxSms;
@@ -204,6 +197,28 @@ int ltri_paged_create(const ltri_paged_params* p, void* cuda_stream, ltri_paged*
   }
   *out = c;
   return LTRI_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t ltri_paged_workspace_bytes(const ltri_paged_params* p) {
+  return validate(p) ? layout(*p, kPagedMaxSms, nullptr, nullptr, nullptr) : 0;
+}
+
+int ltri_paged_create(const ltri_paged_params* p, void* cuda_stream, ltri_paged** out) {
+  if (!out) return LTRI_EINVAL;
+  *out = nullptr;
+  if (!validate(p) || p->cache_type == LTRI_TYPE_INT4) return LTRI_EINVAL;
+  return create(p, nullptr, static_cast<cudaStream_t>(cuda_stream), out);
+}
+
+int ltri_paged_create_int4(const ltri_paged_params* p, uint8_t* block_scales, void* cuda_stream, ltri_paged** out) {
+  if (!out) return LTRI_EINVAL;
+  *out = nullptr;
+  if (!validate(p) || p->cache_type != LTRI_TYPE_INT4 || !aligned(block_scales, 16)) return LTRI_EINVAL;
+  return create(p, block_scales, static_cast<cudaStream_t>(cuda_stream), out);
 }
 
 int ltri_paged_destroy(ltri_paged* cache) {
@@ -228,6 +243,23 @@ int ltri_paged_append(ltri_paged* cache, int layer, const int32_t* table, int ta
   const PagedAppend a{starts, n_tokens, static_cast<const unsigned char*>(k), static_cast<const unsigned char*>(v), stride,
                       row_pos, weights};
   return done(cache, launch_paged_append(cache->c, r, layer, a, static_cast<cudaStream_t>(cuda_stream)), 1);
+}
+
+int ltri_paged_read(ltri_paged* cache, int layer, const int32_t* table, int table_pages, int64_t table_stride,
+                    const int32_t* lens, int n_rows, const int32_t* starts, const int32_t* first, int64_t n_tokens, void* k,
+                    void* v, int64_t kv_stride, void* cuda_stream) {
+  if (!cache || layer < 0 || layer >= cache->p.n_layers || !aligned(starts, 4) || n_tokens < 0) return LTRI_EINVAL;
+  PagedRows r;
+  if (const int rc = check_rows(cache, table, table_pages, table_stride, lens, n_rows, &r)) return rc;
+  if (n_tokens > 0x7fffffffll) return LTRI_ECAPACITY;
+  if (n_tokens == 0) return LTRI_OK;
+  const long long stride = row_stride(cache, kv_stride, cache->p.n_kv_heads);
+  if ((!k && !v) || (k && !aligned(k, 16)) || (v && !aligned(v, 16)) || !stride) return LTRI_EINVAL;
+  if (first && !aligned(first, 4)) return LTRI_EINVAL;
+  OnDevice on(cache->device);
+  if (!on.ok) return done(cache, cudaErrorInvalidDevice, 0);
+  const PagedRead a{starts, first, n_tokens, static_cast<unsigned char*>(k), static_cast<unsigned char*>(v), stride};
+  return done(cache, launch_paged_read(cache->c, r, layer, a, static_cast<cudaStream_t>(cuda_stream)), 1);
 }
 
 int ltri_paged_decode(ltri_paged* cache, int layer, const int32_t* table, int table_pages, int64_t table_stride,
