@@ -496,6 +496,28 @@ int ltri_paged_decode(ltri_paged* cache, int layer, const int32_t* table, int ta
                       const int32_t* lens, int n_rows, const void* q, int64_t q_stride, const void* k, const void* v,
                       int64_t kv_stride, const int32_t* row_pos, void* out, float* lse, void* cuda_stream);
 
+/* Attention of n_rows ragged parts of prompts (or whole prompts, or a few drafted tokens a row), in `layer`, whose K/V rows are in
+ * the pages already (ltri_paged_append with the same starts and lens).
+ *   starts    DEVICE int32 [n_rows + 1], ascending: queries [starts[r], starts[r + 1]) belong to row r (there may be none).  They
+ *             are the row's last tokens: of m of them, number i sees slots 0 to lens[r] - m + i.  Outputs in front of starts[0]
+ *             and from starts[n_rows] on are left as they are.  n_tokens (0 to 2^24) is what q and out have room for.
+ *   q         [n_tokens][n_q_heads][head_dim], token stride q_stride elements (0: dense)
+ *   out       [n_tokens][n_q_heads][head_dim], dense (may be q itself, if that is dense; LTRI_EINVAL if it overlaps it otherwise)
+ *   lse       float [n_tokens][n_q_heads] or NULL: log of the sum of exp(logit)
+ *   workspace DEVICE, 256-byte aligned, at least ltri_paged_attend_workspace_bytes(cache, n_tokens): scratch of this call alone
+ *             until it is through.  Nothing has to be in it.
+ * Queries without a slot (more than lens[r] of them) have outputs of 0 and an lse of -infinity, as have those of rows of bad
+ * lengths, and are recorded as LTRI_EDEVICE.  Weights are not accumulated.  V rows of the call's own tokens have to be finite:
+ * the products multiply those that a token does not see by 0.
+ * Logits and sums are fp32; the probabilities enter the product with V as two 16-bit terms: 22 bits as in ltri_paged_decode over
+ * fp16, 8-bit and 4-bit pages, 16 bits over bf16 pages.  Outputs are the same bits for the same inputs and the same device. */
+int ltri_paged_attend(ltri_paged* cache, int layer, const int32_t* table, int table_pages, int64_t table_stride,
+                      const int32_t* lens, int n_rows, const int32_t* starts, int64_t n_tokens, const void* q, int64_t q_stride,
+                      void* out, float* lse, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/* Bytes of workspace that calls of up to max_tokens (1 to 2^24) tokens need; 0 if that is out of range. */
+size_t ltri_paged_attend_workspace_bytes(const ltri_paged* cache, int64_t max_tokens);
+
 /* Cut every row of more than `budget` slots to `budget`, per layer of [layer_begin, layer_begin + layer_count) and KV head.
  * Kept are the slots of the first n_sink positions and of the newest `recent` positions (counted from the largest position
  * in the row), n_sink + recent <= budget, and of the others those of the largest weights (NaN counts as -infinity; of equal
@@ -508,7 +530,8 @@ int ltri_paged_evict(ltri_paged* cache, int layer_begin, int layer_count, const 
                      int64_t table_stride, const int32_t* lens, int32_t* new_lens, int n_rows, int budget, int n_sink,
                      int recent, void* cuda_stream);
 
-/* First device-side error recorded since the last call of this function (then cleared).  Synchronises. */
+/* First device-side error recorded since the last call of this function (then cleared): LTRI_EDEVICE, or LTRI_ETIMEOUT if a
+ * bounded wait inside ltri_paged_attend expired.  Synchronises. */
 int ltri_paged_sync_status(ltri_paged* cache, void* cuda_stream);
 /* cudaError_t of the last failed runtime call (0 if none). */
 int ltri_paged_last_cuda_error(const ltri_paged* cache);

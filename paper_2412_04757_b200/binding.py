@@ -32,7 +32,7 @@ EXPORTS = [
     "ltri_segment_map_static", "ltri_prefill_chunk_host", "ltri_host_outputs_ready", "ltri_host_kv_bytes",
     "ltri_debug_load_index", "ltri_debug_wait_timeout",
     "ltri_paged_workspace_bytes", "ltri_paged_create", "ltri_paged_destroy", "ltri_paged_append", "ltri_paged_decode",
-    "ltri_paged_create_int4", "ltri_paged_read",
+    "ltri_paged_create_int4", "ltri_paged_read", "ltri_paged_attend", "ltri_paged_attend_workspace_bytes",
     "ltri_paged_evict", "ltri_paged_sync_status", "ltri_paged_last_cuda_error", "ltri_paged_launch_count",
 ]
 KERNEL_CLASSES = ["append", "evict_index", "attn_local", "map_pass", "segment", "score_topk", "attn_retrieved",
@@ -135,6 +135,9 @@ def load():
         L.ltri_paged_append.argtypes = [vp, ip, vp, ip, i64, vp, ip, vp, i64, vp, vp, i64, vp, vp, vp]
         L.ltri_paged_read.argtypes = [vp, ip, vp, ip, i64, vp, ip, vp, vp, i64, vp, vp, i64, vp]
         L.ltri_paged_decode.argtypes = [vp, ip, vp, ip, i64, vp, ip, vp, i64, vp, vp, i64, vp, vp, vp, vp]
+        L.ltri_paged_attend.argtypes = [vp, ip, vp, ip, i64, vp, ip, vp, i64, vp, i64, vp, vp, vp, C.c_size_t, vp]
+        L.ltri_paged_attend_workspace_bytes.restype = C.c_size_t
+        L.ltri_paged_attend_workspace_bytes.argtypes = [vp, i64]
         L.ltri_paged_evict.argtypes = [vp, ip, ip, vp, ip, i64, vp, vp, ip, ip, ip, ip, vp]
         L.ltri_paged_sync_status.argtypes = [vp, vp]
         L.ltri_paged_last_cuda_error.argtypes = [vp]
@@ -440,11 +443,12 @@ class LtriPaged:
     [Hkv]), or of 4 bits: uint8 [layers][pages][Hkv][page tokens][head_dim / 2] with block_scales (uint8
     [layers][pages][Hkv][page tokens][2][head_dim / 32], contiguous).  weights (float32) and positions (int32), both or neither: [layers][pages][Hkv][page tokens], contiguous.  The
     tensors stay the caller's; the handle keeps references to them.  It allocates its workspace on ``stream`` (None: the one
-    that is current when it is made): let it go only when its calls on other streams are through.
+    that is current when it is made): let it go only when its calls on other streams are through.  max_tokens: tokens of the
+    largest ltri_paged_attend call, whose workspace it allocates too (0: none).
     """
 
     def __init__(self, k_pages, v_pages, n_q_heads, dtype=None, max_rows=1, k_scale=None, v_scale=None, weights=None,
-                 positions=None, softmax_scale=0.0, weight_decay=1.0, stream=None, block_scales=None):
+                 positions=None, softmax_scale=0.0, weight_decay=1.0, stream=None, block_scales=None, max_tokens=0):
         import torch
 
         self.torch = torch
@@ -504,6 +508,14 @@ class LtriPaged:
             else:
                 _check(self.lib.ltri_paged_create(C.byref(self.params), self._stream(stream), C.byref(self._h)),
                        "ltri_paged_create")
+            self._attend = (None, 0)
+            if max_tokens:
+                nbytes = int(self.lib.ltri_paged_attend_workspace_bytes(self._h, max_tokens))
+                if nbytes == 0:
+                    raise LtriError(LTRI_EINVAL, "ltri_paged_attend_workspace_bytes")
+                with torch.cuda.stream(stream):
+                    self.attend_workspace = torch.empty(nbytes + 256, dtype=torch.uint8, device=self.device)
+                self._attend = ((self.attend_workspace.data_ptr() + 255) // 256 * 256, nbytes)
 
     def _stream(self, stream):
         return self._raw_stream(self._index) if stream is None else stream.cuda_stream
@@ -630,6 +642,28 @@ class LtriPaged:
                                         vp, kvs, rp, op, lp, s)
         if rc:
             self._done(rc, "ltri_paged_decode")
+        return out
+
+    def ltri_paged_attend(self, layer, table, lens, starts, q, out=None, lse=None, stream=None):
+        """q [tokens][Hq][head_dim], the last tokens of their rows ([starts[r], starts[r + 1]) row r's), whose K/V rows are in the
+        pages, over the rows' slots up to their own.  lse: float32 [tokens][Hq], filled if given.  Returns out."""
+        n, cols, ts = self._rows(table, lens)
+        tokens = q.shape[0]
+        size = (tokens, *self._q_shape)
+        sp = self._dense(starts, self._i32, (n + 1,), "starts")
+        qs = self._heads(q, size, "q")
+        if out is None:
+            with self.torch.cuda.stream(stream):
+                out = self.torch.empty(size, dtype=self.dtype, device=self.device)
+        op = self._dense(out, self.dtype, size, "out")
+        lp = None if lse is None else self._dense(lse, self.torch.float32, size[:2], "lse")
+        if tokens == 0:
+            return out
+        s = self._raw_stream(self._index) if stream is None else stream.cuda_stream
+        rc = self.lib.ltri_paged_attend(self._h, layer, table.data_ptr(), cols, ts, lens.data_ptr(), n, sp, tokens, q.data_ptr(), qs,
+                                        op, lp, *self._attend, s)
+        if rc:
+            self._done(rc, "ltri_paged_attend")
         return out
 
     def ltri_paged_evict(self, layer_begin, layer_count, table, lens, new_lens, budget, n_sink, recent, stream=None):

@@ -64,6 +64,15 @@ struct PagedRead {
   long long stride;             // bytes between tokens
 };
 
+struct PagedQueries {
+  const int* starts;
+  long long n_tokens;
+  const unsigned char* q;
+  long long q_stride;           // bytes between tokens
+  unsigned char* out;
+  float* lse;
+};
+
 struct PagedStep {
   const unsigned char *q, *k, *v;
   long long q_stride, kv_stride;  // bytes between rows
@@ -84,6 +93,10 @@ int paged_decode_kernels(const PagedCache& c);  // launches of a decode call
 
 cudaError_t prepare_paged();
 cudaError_t prepare_paged_evict();
+cudaError_t prepare_paged_attend();
+size_t paged_attend_workspace(const PagedCache& c, long long n_tokens, long long n_rows);
+cudaError_t launch_paged_attend(const PagedCache& c, const PagedRows& r, int layer, const PagedQueries& a, unsigned char* workspace,
+                                cudaStream_t s);
 int paged_evict_cluster();
 cudaError_t launch_paged_append(const PagedCache& c, const PagedRows& r, int layer, const PagedAppend& a, cudaStream_t s);
 cudaError_t launch_paged_read(const PagedCache& c, const PagedRows& r, int layer, const PagedRead& a, cudaStream_t s);

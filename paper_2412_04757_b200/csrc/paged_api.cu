@@ -17,6 +17,7 @@ struct ltri_paged {
 
 namespace {
 
+constexpr int64_t kPagedMaxTokens = 1 << 24;  // of an attend call: query rows of a KV head are counted in 32 bits
 constexpr int kPagedMaxSms = 256;  // CTAs that a decode call can have partial sums of
 
 int element_bits(int type) { return type == LTRI_TYPE_INT4 ? 4 : type == LTRI_TYPE_E4M3 ? 8 : 16; }
@@ -186,7 +187,7 @@ int create(const ltri_paged_params* p, uint8_t* block_scales, cudaStream_t s, lt
   cudaError_t e = cudaGetDevice(&c->device);
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&d.sms, cudaDevAttrMultiProcessorCount, c->device);
   if (d.sms > kPagedMaxSms) d.sms = kPagedMaxSms;
-  if (e == cudaSuccess) e = first_error(prepare_paged(), prepare_paged_evict());
+  if (e == cudaSuccess) e = first_error(first_error(prepare_paged(), prepare_paged_evict()), prepare_paged_attend());
   if (e == cudaSuccess) d.evict_cluster = paged_evict_cluster();
   if (e == cudaSuccess) e = cudaMemsetAsync(p->workspace, 0, zeroed, s);
   if (e == cudaSuccess) e = cudaStreamSynchronize(s);
@@ -283,6 +284,32 @@ int ltri_paged_decode(ltri_paged* cache, int layer, const int32_t* table, int ta
               paged_decode_kernels(cache->c));
 }
 
+size_t ltri_paged_attend_workspace_bytes(const ltri_paged* cache, int64_t max_tokens) {
+  if (!cache || max_tokens < 1 || max_tokens > kPagedMaxTokens) return 0;
+  return paged_attend_workspace(cache->c, max_tokens, cache->p.max_rows);
+}
+
+int ltri_paged_attend(ltri_paged* cache, int layer, const int32_t* table, int table_pages, int64_t table_stride,
+                      const int32_t* lens, int n_rows, const int32_t* starts, int64_t n_tokens, const void* q, int64_t q_stride,
+                      void* out, float* lse, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  if (!cache || layer < 0 || layer >= cache->p.n_layers || !aligned(starts, 4) || n_tokens < 0) return LTRI_EINVAL;
+  PagedRows r;
+  if (const int rc = check_rows(cache, table, table_pages, table_stride, lens, n_rows, &r)) return rc;
+  if (n_tokens > kPagedMaxTokens) return LTRI_ECAPACITY;
+  if (n_tokens == 0) return LTRI_OK;
+  const long long qs = row_stride(cache, q_stride, cache->p.n_q_heads);
+  if (!aligned(q, 16) || !aligned(out, 16) || !qs || (lse && !aligned(lse, 4)) || !aligned(workspace, 256)) return LTRI_EINVAL;
+  if (workspace_bytes < paged_attend_workspace(cache->c, n_tokens, n_rows)) return LTRI_ECAPACITY;
+  // outputs are written while other tokens' queries are still to be read
+  const long long row = (long long)cache->p.n_q_heads * cache->p.head_dim * 2;
+  if (!(out == q && (qs == row || n_tokens == 1)) && meets(out, n_tokens * row, q, n_tokens, row, qs)) return LTRI_EINVAL;
+  OnDevice on(cache->device);
+  if (!on.ok) return done(cache, cudaErrorInvalidDevice, 0);
+  const PagedQueries a{starts, n_tokens, static_cast<const unsigned char*>(q), qs, static_cast<unsigned char*>(out), lse};
+  return done(cache, launch_paged_attend(cache->c, r, layer, a, static_cast<unsigned char*>(workspace),
+                                         static_cast<cudaStream_t>(cuda_stream)), 3);
+}
+
 int ltri_paged_evict(ltri_paged* cache, int layer_begin, int layer_count, const int32_t* table, int table_pages,
                      int64_t table_stride, const int32_t* lens, int32_t* new_lens, int n_rows, int budget, int n_sink,
                      int recent, void* cuda_stream) {
@@ -315,7 +342,7 @@ int ltri_paged_sync_status(ltri_paged* cache, void* cuda_stream) {
     if (e == cudaSuccess) e = cudaStreamSynchronize(s);
   }
   if (e != cudaSuccess) return done(cache, e, 0);
-  return w[0] == 0 ? LTRI_OK : LTRI_EDEVICE;
+  return w[0];
 }
 
 int ltri_paged_last_cuda_error(const ltri_paged* cache) { return cache ? cache->last_cuda : 0; }

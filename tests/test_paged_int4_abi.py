@@ -73,3 +73,9 @@ def test_definition_of_the_format():
     assert torch.equal(i4.values(code, scale), value)
     s = i4.scales64()[scale.long()].repeat_interleave(32, -1)
     assert ((value - y).abs() <= s / 2 * (1 + 1e-9)).all()  # (the nearest scale is at most 1/17 below the block's seventh)
+
+
+def test_null_handles_of_attend_are_refused(lib):
+    bad = binding.LTRI_EINVAL
+    assert lib.ltri_paged_attend(None, 0, None, 1, 1, None, 1, None, 1, None, 0, None, None, None, 0, None) == bad
+    assert lib.ltri_paged_attend_workspace_bytes(None, 8) == 0
