@@ -15,8 +15,8 @@
 // puts all units' tiles into one line, of which every CTA (one per SM) takes an equal run, across units if need be; the partial sums
 // of units that CTAs share are joined by a third kernel, in the order of the line.
 //
-// Roles of a CTA's 17 warps: 0-3 and 4-7 softmax of the two tiles of 128 query rows (a thread a row; it also loads the row's
-// queries and writes its outputs), 8-15 bring K and V tiles into shared memory, 16 issues the products.  TMEM: S0, S1, O0, O1 of
+// Roles of a CTA's 28 warps: 0-7 and 8-15 softmax of the two tiles of 128 query rows (two threads a row; they also load the row's
+// queries and write its outputs), 16-23 bring K and V tiles into shared memory, 24 issues the products.  TMEM: S0, S1, O0, O1 of
 // 128 columns each; P replaces S in its columns.  head_dim 256: one tile of query rows, whose O takes 256 columns, and two S of 64
 // columns in turn.
 #include "paged_int4.cuh"
@@ -41,8 +41,9 @@ struct PaShape {
   static constexpr int kSmem = kQt * kQBytes + kStages * 2 * kMat + 1024;
 };
 
-constexpr int kPaLoaders = 8;  // warps
-constexpr int kPaThreads = 32 * (8 + kPaLoaders + 1);
+constexpr int kPaSoftmax = 16, kPaLoaders = 8;  // warps
+constexpr int kPaIssuer = kPaSoftmax + kPaLoaders;  // this warp
+constexpr int kPaThreads = 32 * (kPaIssuer + 4);
 // Upper bound of any single wait, in SM cycles (about ten seconds: a CTA's longest run of tiles lies far below)
 constexpr long long kPaWaitLimit = 10 * kWaitLimitCycles;
 constexpr float kPaNone = -3.0e38f;  // reference of sums that nothing has entered yet: below every logit, and finite
@@ -74,6 +75,13 @@ __host__ __device__ constexpr size_t pa_part_floats() {
   return (size_t)PaShape<KIND, D>::kRows * (D + 2);
 }
 
+// mbar_wait with all but the first try out of line
+static __device__ __noinline__ bool pa_wait_long(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+  return mbar_wait(bar, parity, abort_flag, kPaWaitLimit);
+}
+__device__ __forceinline__ bool pa_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+  return mbar_try(bar, parity) || pa_wait_long(bar, parity, abort_flag);
+}
 __device__ __forceinline__ float pa_exp2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -177,25 +185,39 @@ __global__ void __launch_bounds__(kPlThreads)
   }
 }
 
-// A CTA's run of the line, part of a unit after the other.
-struct PaWalk {
-  PaEntry e;
-  int at, head;       // entry, KV head
-  int begin, end;     // tiles of the unit
-  long long left;     // of the run, this part's included
+// A place in a CTA's run of the line: a part of a unit after the other, and their tiles.
+struct PaPlace {
+  int at, head;           // entry, KV head
+  int row, start;         // of the batch; the row's first token in q
+  int rows, rho;          // query rows of the row, and the unit's first
+  int base, limit;        // slots in front of the row's tokens, and those that the unit's last token sees
+  int tiles, tile, end;   // of the unit; the place; behind the part
+  long long left;         // tiles of the run behind the part
 };
-__device__ __forceinline__ void pa_part(PaWalk& w) { w.end = (int)min((long long)w.e.tiles, w.begin + w.left); }
+__device__ __forceinline__ void pa_entry(PaPlace& w, const PaEntry& e, int G, int rows) {
+  w.row = e.row;
+  w.start = e.start;
+  w.rows = e.m * G;
+  w.rho = e.block * rows;
+  w.base = e.base;
+  w.limit = pa_limit(e, G, rows);
+  w.tiles = e.tiles;
+}
 // The next part; false at the run's end.
-__device__ __forceinline__ bool pa_next(PaWalk& w, const PaWork& wk, int heads) {
-  w.left -= w.end - w.begin;
+__device__ __forceinline__ bool pa_next(PaPlace& w, const PaWork& wk, int heads, int G, int rows) {
   if (w.left <= 0) return false;
-  w.begin = 0;
+  w.tile = 0;
   if (++w.head == heads) {
     w.head = 0;
-    w.e = wk.entry[++w.at];
+    pa_entry(w, wk.entry[++w.at], G, rows);
   }
-  pa_part(w);
+  w.end = (int)min((long long)w.tiles, w.left);
+  w.left -= w.end;
   return true;
+}
+// The next tile; false at the run's end.
+__device__ __forceinline__ bool pa_step(PaPlace& w, const PaWork& wk, int heads, int G, int rows) {
+  return ++w.tile < w.end || pa_next(w, wk, heads, G, rows);
 }
 // One warp: the entry of a tile (below the line's total).
 __device__ __forceinline__ int pa_find(const PaWork& wk, int entries, long long tile) {
@@ -211,11 +233,48 @@ __device__ __forceinline__ int pa_find(const PaWork& wk, int entries, long long 
   return lo;
 }
 
-// Two terms of `type` that add up to two fp32 values.
-__device__ __forceinline__ void pa_terms(int type, float a, float b, uint32_t& hi, uint32_t& lo) {
-  hi = paged_pack(type, a, b);
+// Pairs of fp32 values, one instruction for both.
+__device__ __forceinline__ unsigned long long pa_pair(float a, float b) {
+  unsigned long long x;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(x) : "f"(a), "f"(b));
+  return x;
+}
+__device__ __forceinline__ float2 pa_split(unsigned long long x) {
+  float2 y;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(y.x), "=f"(y.y) : "l"(x));
+  return y;
+}
+__device__ __forceinline__ unsigned long long pa_fma2(unsigned long long a, unsigned long long b, unsigned long long c) {
+  unsigned long long d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+__device__ __forceinline__ unsigned long long pa_add2(unsigned long long a, unsigned long long b) {
+  unsigned long long d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+// Two terms of `type` that add up to a pair of fp32 values.
+__device__ __forceinline__ void pa_terms(int type, unsigned long long p, uint32_t& hi, uint32_t& lo) {
+  const float2 f = pa_split(p);
+  hi = paged_pack(type, f.x, f.y);
   const float2 back = paged_unpack(type, hi);
-  lo = paged_pack(type, a - back.x, b - back.y);
+  const float2 rest = pa_split(pa_fma2(pa_pair(back.x, back.y), pa_pair(-1.f, -1.f), p));
+  lo = paged_pack(type, rest.x, rest.y);
+}
+// A barrier of 256 threads: whether it is so for any of them.
+__device__ __forceinline__ bool pa_any(int id, bool so) {
+  uint32_t any;
+  asm volatile(
+      "{\n.reg .pred p, r;\nsetp.ne.b32 p, %1, 0;\nbar.red.or.pred r, %2, 256, p;\nselp.u32 %0, 1, 0, r;\n}\n"
+      : "=r"(any)
+      : "r"((uint32_t)so), "r"(id)
+      : "memory");
+  return any != 0;
+}
+// A bulk of 16 bytes on its way into shared memory, or zeros.
+__device__ __forceinline__ void pa_request(uint32_t to, const void* from, bool there) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(there ? 16 : 0) : "memory");
 }
 
 // Sixteen bytes of a cached row as 16-bit elements, in the order that the products take them (see pa_element).
@@ -275,18 +334,21 @@ __global__ void __launch_bounds__(kPaThreads, 1)
   // by kGrow
   constexpr float kOff = KIND == kPaBf16 ? 0.f : 10.f, kGrow = 4.f;
   extern __shared__ unsigned char smem_raw[];
-  enum {
+  enum {  // (P is handed over in up to two parts)
     B_KFULL = 0, B_VFULL = S, B_KEMPTY = 2 * S, B_VEMPTY = 3 * S, B_QFULL = 4 * S, B_SREADY = B_QFULL + QT,
-    B_PREADY = B_SREADY + QT * SB, B_OFREE = B_PREADY + QT * SB, B_ODONE = B_OFREE + QT, B_PVDONE = B_ODONE + QT,
+    B_PREADY = B_SREADY + QT * SB, B_OFREE = B_PREADY + 2 * QT * SB, B_ODONE = B_OFREE + QT, B_PVDONE = B_ODONE + QT,
     B_DRAIN = B_PVDONE + 1, B_COUNT = B_DRAIN + 1
   };
   __shared__ __align__(8) unsigned long long bars[B_COUNT];
   __shared__ uint32_t s_tmem;
   __shared__ int s_abort;
-  __shared__ PaWalk s_walk;
+  __shared__ PaPlace s_place;
   // by tile: slots that have a page, a bit each.  (Eight tiles: when the K of tile j is written, that of j - S has met its
   // queries, and so the softmax of j - S - 1 and those in front of it have ended.)
-  __shared__ __align__(16) unsigned short s_there[8][kPaLoaders];
+  __shared__ __align__(16) uint32_t s_there[8][4];
+  // of a tile of queries: rows' largest logits of each half of the columns, and their sums
+  __shared__ float s_top[QT][2][128], s_sum[QT][2][128];
+  __shared__ int s_bad[QT];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t sbase = (smem_addr(smem_raw) + 1023u) & ~1023u, sQ = sbase, sKV = sbase + QT * Sh::kQBytes;
   auto bar = [&](int i) { return smem_addr(&bars[i]); };
@@ -300,25 +362,27 @@ __global__ void __launch_bounds__(kPaThreads, 1)
   if (tid == 0) {
     s_abort = 0;
     for (int i = 0; i < S; ++i) {
-      mbar_init(bar(B_KFULL + i), kPaLoaders);
-      mbar_init(bar(B_VFULL + i), kPaLoaders);
-      mbar_init(bar(B_KEMPTY + i), 1);
-      mbar_init(bar(B_VEMPTY + i), 1);
+      mbar_init(bar(B_KFULL + i), kPaLoaders / 2);
+      mbar_init(bar(B_VFULL + i), kPaLoaders / 2);
+      mbar_init(bar(B_KEMPTY + i), QT);
+      mbar_init(bar(B_VEMPTY + i), QT);
     }
     for (int q = 0; q < QT; ++q) {
-      mbar_init(bar(B_QFULL + q), 4);
-      mbar_init(bar(B_OFREE + q), 4);
+      s_bad[q] = 0;
+      mbar_init(bar(B_QFULL + q), 8);
+      mbar_init(bar(B_OFREE + q), 8);
       mbar_init(bar(B_ODONE + q), 1);
       for (int b = 0; b < SB; ++b) {
         mbar_init(bar(B_SREADY + q * SB + b), 1);
-        mbar_init(bar(B_PREADY + q * SB + b), 4);
+        mbar_init(bar(B_PREADY + 2 * (q * SB + b)), 8);
+        mbar_init(bar(B_PREADY + 2 * (q * SB + b) + 1), 8);
       }
     }
     mbar_init(bar(B_PVDONE), 1);
-    mbar_init(bar(B_DRAIN), 1);
+    mbar_init(bar(B_DRAIN), QT);
     fence_mbar_init();
   }
-  if (warp == 16) tmem_alloc(smem_addr(&s_tmem), 512);
+  if (warp == kPaIssuer) tmem_alloc(smem_addr(&s_tmem), 512);
   chain_wait();
   // the CTA's run
   const long long total = wk.plan->total;
@@ -327,224 +391,266 @@ __global__ void __launch_bounds__(kPaThreads, 1)
   if (warp == 0 && works) {
     const int at = pa_find(wk, wk.plan->entries, c0);
     if (lane == 0) {
-      PaWalk w;
-      w.e = wk.entry[at];
+      const PaEntry e = wk.entry[at];
+      PaPlace w;
+      pa_entry(w, e, c.G, ROWS);
       w.at = at;
-      w.head = (int)((c0 - w.e.before) / w.e.tiles);
-      w.begin = (int)((c0 - w.e.before) % w.e.tiles);
+      w.head = (int)((c0 - e.before) / e.tiles);
+      w.tile = (int)((c0 - e.before) % e.tiles);
       w.left = min(per, total - c0);
-      pa_part(w);
-      s_walk = w;
+      w.end = (int)min((long long)w.tiles, w.tile + w.left);
+      w.left -= w.end - w.tile;
+      s_place = w;
     }
   }
   fence_before_sync();
   __syncthreads();
   fence_after_sync();
   const uint32_t tmem = s_tmem;
-  // query rows of a part's unit
-  auto rows_of = [&](const PaEntry& e) { return min(ROWS, e.m * c.G - e.block * ROWS); };
+  auto next_part = [&](PaPlace& w) { return pa_next(w, wk, c.Hkv, c.G, ROWS); };
 
-  if (works && warp >= 8 && warp < 16) {
+  if (warp >= kPaSoftmax && warp < kPaIssuer) {
     // ------------------------------------------------------------------ K and V tiles
+    // Four warps bring K and four V, so that what a tile costs them (page numbers, addresses, the wait for its stage) passes twice
+    // at a time.
     constexpr int RC = Sh::kRow / 16, CL = RC < 4 ? RC : 4, SL = 32 / CL;  // lanes: SL slots, CL chunks of 16 bytes of each
-    constexpr int PASSES = TILE / kPaLoaders / SL, KC = RC / CL;           // of slots, of chunks
-    static_assert(PASSES >= 1 && PASSES * SL * kPaLoaders == TILE, "");
-    constexpr int OUT = PaChunk<KIND>::kOut;
-    const int lw = warp - 8, sub = lane % SL, ch0 = lane / SL;
-    const unsigned char* pages_k = c.k + layer * c.ls;
-    const long long vk = c.v - c.k;
-    PaWalk wp = s_walk, wd = s_walk;  // of the page numbers that are asked for, of the rows that are
-    int tp = wp.begin, td = wd.begin;
-    bool more_p = true, more_d = true;
-    auto step = [&](PaWalk& w, int& t, bool& more) {
-      if (++t >= w.end) {
-        more = pa_next(w, wk, c.Hkv);
-        t = w.begin;
-      }
+    constexpr int MINE = TILE / 4, PASSES = MINE / SL, KC = RC / CL;       // slots of a warp; passes of slots, of chunks
+    static_assert(PASSES >= 1 && PASSES * SL == MINE && SL % 8 == 0 && (MINE == 32 || MINE == 16), "a warp's slots");
+    constexpr bool kCopy = KIND == kPaBf16 || KIND == kPaFp16;  // rows go into shared memory as they are
+    const bool of_v = warp - kPaSoftmax >= 4;
+    const int lw = warp & 3, sub = lane % SL, ch0 = lane / SL, full = of_v ? B_VFULL : B_KFULL;
+    const unsigned char* pages = (of_v ? c.v : c.k) + layer * c.ls;
+    bool more_p = works, more_d = works;
+    PaPlace wd = s_place, wp = s_place;  // of the rows that are asked for, of the page numbers
+    // A lane finds out about one of the warp's slots, and the others ask it.  (Every lane about those whose rows it loads: 3000 of
+    // 9300 cycles a tile.)
+    int page, page_next;
+    auto ask_page = [&]() {
+      const int slot = wp.tile * TILE + lw * MINE + lane % MINE;
+      const int x = more_p && slot < wp.limit ? table[wp.row * table_stride + paged_nth(c, slot)] : -1;
+      if (more_p) more_p = pa_step(wp, wk, c.Hkv, c.G, ROWS);
+      return x;
     };
-    int page[PASSES], page_next[PASSES];
-    auto ask_pages = [&](int (&to)[PASSES]) {
-      const int limit = pa_limit(wp.e, c.G, ROWS);
-#pragma unroll
-      for (int p = 0; p < PASSES; ++p) {
-        const int slot = tp * TILE + lw * (TILE / kPaLoaders) + p * SL + sub;
-        to[p] = more_p && slot < limit ? table[wp.e.row * table_stride + paged_nth(c, slot)] : -1;
-      }
-      if (more_p) step(wp, tp, more_p);
-    };
-    // rows of a tile as they lie in the cache, and 4-bit rows' scales
-    uint4 raw[2][PASSES][KC];
-    unsigned scale[2][PASSES][KC];
-    long long off[PASSES];
-    int there;  // slots of the warp with a page, of the tile whose rows are on their way
-    size_t word[PASSES];
+    long long off = -1;
+    uint32_t there = 0;  // slots with a page, of the tile whose rows are asked for
+    constexpr int SW = D <= 128 ? 1 : 2;
+    uint32_t scales[SW];  // of a 4-bit row (64 elements: K's and V's in one word)
     auto locate = [&]() {
-      const int limit = pa_limit(wd.e, c.G, ROWS);
-      there = 0;
+      const int slot = wd.tile * TILE + lw * MINE + lane % MINE;
+      const bool in = more_d && slot < wd.limit, has = in && (unsigned)page < (unsigned)c.n_pages;
+      if (in && !has) paged_status(c, wd.row);
+      const int place = slot - paged_nth(c, slot) * c.P;
+      off = has ? (long long)paged_row(c, 0, page, wd.head, place) : -1;
+      if constexpr (KIND == kPaInt4) {
+        const size_t word = has ? paged_word(c, layer, page, wd.head, place) : 0;
+        const uint32_t* sc = reinterpret_cast<const uint32_t*>(c.sc) + (D == 64 ? word : (word * 2 + of_v) * SW);
 #pragma unroll
-      for (int p = 0; p < PASSES; ++p) {
-        const int slot = td * TILE + lw * (TILE / kPaLoaders) + p * SL + sub;
-        const bool in = more_d && slot < limit, has = in && (unsigned)page[p] < (unsigned)c.n_pages;
-        if (in && !has) paged_status(c, wd.e.row);
-        const int place = slot - paged_nth(c, slot) * c.P;
-        off[p] = has ? (long long)paged_row(c, 0, page[p], wd.head, place) : -1;
-        if (KIND == kPaInt4) word[p] = has ? paged_word(c, layer, page[p], wd.head, place) : 0;
-        const unsigned b = __ballot_sync(0xffffffffu, has || !in);  // (slots behind the limit are masked by their number)
-        there |= (int)(b & ((1ull << SL) - 1)) << (p * SL);
+        for (int i = 0; i < SW; ++i) scales[i] = has ? sc[i] : 0u;
+      }
+      there = __ballot_sync(0xffffffffu, has || !in);  // (slots behind the limit are masked by their number)
+    };
+    uint4 raw[kCopy ? 1 : PASSES][kCopy ? 1 : KC];
+    auto ask_rows = [&]() {
+      if constexpr (!kCopy) {
+#pragma unroll
+        for (int p = 0; p < PASSES; ++p) {
+          const long long o = shfl_ll(off, p * SL + sub);
+          const unsigned char* from = pages + o + ch0 * 16;
+#pragma unroll
+          for (int k = 0; k < KC; ++k)
+            raw[p][k] = o < 0 ? make_uint4(0u, 0u, 0u, 0u) : *reinterpret_cast<const uint4*>(from + k * CL * 16);
+        }
       }
     };
-    auto ask_rows = [&](int of_v) {
-#pragma unroll
-      for (int p = 0; p < PASSES; ++p)
-#pragma unroll
-        for (int k = 0; k < KC; ++k) {
-          raw[of_v][p][k] = make_uint4(0u, 0u, 0u, 0u);
-          scale[of_v][p][k] = 0u;
-          if (off[p] < 0) continue;
-          const int ch = ch0 + k * CL;
-          raw[of_v][p][k] = *reinterpret_cast<const uint4*>(pages_k + (of_v ? vk : 0) + off[p] + ch * 16);
-          if (KIND == kPaInt4) scale[of_v][p][k] = c.sc[(word[p] * 2 + of_v) * (D / kI4Block) + ch];
-        }
+    // where a lane's 16-byte chunk of a tile's row goes; chunks further on and rows of other passes lie at distances that all lanes
+    // share, but for the swizzle's bits
+    constexpr int OUT = PaChunk<KIND>::kOut;
+    const int row0 = lw * MINE + sub;
+    auto place_of = [&](uint32_t mat, int p, int oc) {
+      return mat + (oc >> 3) * (TILE * 128) + (row0 + p * SL) * 128 + (((oc & 7) ^ (row0 & 7)) << 4);  // (SL is a multiple of 8)
     };
-    auto write_rows = [&](int of_v, uint32_t mat) {
+    auto copy_rows = [&](uint32_t mat) {
 #pragma unroll
-      for (int p = 0; p < PASSES; ++p)
+      for (int p = 0; p < PASSES; ++p) {
+        const long long o = shfl_ll(off, p * SL + sub);
+        const unsigned char* from = pages + (o < 0 ? 0 : o + ch0 * 16);
 #pragma unroll
-        for (int k = 0; k < KC; ++k) {
-          const int row = lw * (TILE / kPaLoaders) + p * SL + sub, ch = ch0 + k * CL;
-          const uint4& x = raw[of_v][p][k];
-          const uint32_t in[4] = {x.x, x.y, x.z, x.w};
-          I4Scale f;
-          if (KIND == kPaInt4) f = i4_factors(scale[of_v][p][k] * 0x00800080u);
+        for (int k = 0; k < KC; ++k) pa_request(place_of(mat, p, ch0 + k * CL), from + (o < 0 ? 0 : k * CL * 16), o >= 0);
+      }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    auto write_rows = [&](uint32_t mat) {
+      if constexpr (!kCopy) {
 #pragma unroll
-          for (int o = 0; o < OUT; ++o) {
-            uint4 y = x;
-            if (KIND == kPaInt4) {
-              uint32_t v[4];
-              i4_values(v, in[o], f);
-              y = make_uint4(v[0], v[1], v[2], v[3]);
+        for (int p = 0; p < PASSES; ++p)
+#pragma unroll
+          for (int k = 0; k < KC; ++k) {
+            const uint4& x = raw[p][k];
+            const uint32_t in[4] = {x.x, x.y, x.z, x.w};
+            I4Scale f;
+            if constexpr (KIND == kPaInt4) {
+              const uint32_t w = __shfl_sync(0xffffffffu, scales[k * CL / 4], p * SL + sub);
+              f = i4_factors((w >> (8 * ((D == 64 && of_v ? 2 : 0) + ch0)) & 0xffu) * 0x00800080u);
             }
-            if (KIND == kPaE4m3) {
-              uint32_t v[4];
 #pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const __nv_fp8x2_storage_t two = (__nv_fp8x2_storage_t)(in[2 * o + i / 2] >> (16 * (i & 1)));
-                const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(two, __NV_E4M3);
-                v[i] = (uint32_t)h.x | (uint32_t)h.y << 16;
+            for (int o = 0; o < OUT; ++o) {
+              uint32_t v[4];
+              if constexpr (KIND == kPaInt4) {
+                i4_values(v, in[o], f);
+              } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                  const __nv_fp8x2_storage_t two = (__nv_fp8x2_storage_t)(in[(2 * o + i / 2) & 3] >> (16 * (i & 1)));
+                  const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(two, __NV_E4M3);
+                  v[i] = (uint32_t)h.x | (uint32_t)h.y << 16;
+                }
               }
-              y = make_uint4(v[0], v[1], v[2], v[3]);
+              pa_store(place_of(mat, p, (ch0 + k * CL) * OUT + o), make_uint4(v[0], v[1], v[2], v[3]));
             }
-            const int oc = ch * OUT + o;  // 16-byte chunk of the dense row
-            pa_store(mat + (oc >> 3) * (TILE * 128) + row * 128 + (((oc & 7) ^ (row & 7)) << 4), y);
           }
-        }
-      fence_async_smem();
+        fence_async_smem();
+      }
     };
-    ask_pages(page);
-    locate();
-    ask_rows(0);
-    ask_rows(1);
-    int there_now = there;
-    ask_pages(page_next);
-    bool ok = true;
-    for (int jt = 0; more_d; ++jt) {
-      const int st = jt % S;
-      const uint32_t mat = sKV + st * 2 * Sh::kMat;
-      step(wd, td, more_d);  // now of the next tile
-#pragma unroll
-      for (int p = 0; p < PASSES; ++p) page[p] = page_next[p];
-      ask_pages(page_next);
-      if (jt >= S) ok = wait(B_KEMPTY + st, jt / S - 1);
-      if (!__all_sync(0xffffffffu, ok)) break;
-      if (lane == 0) s_there[jt & 7][lw] = (unsigned short)there_now;
-      write_rows(0, mat);
-      arrive(B_KFULL + st);
+    if (works) {
+      page = ask_page();
       locate();
-      if (more_d) ask_rows(0);
-      there_now = there;
-      if (jt >= S) ok = wait(B_VEMPTY + st, jt / S - 1);
-      if (!__all_sync(0xffffffffu, ok)) break;
-      write_rows(1, mat + Sh::kMat);
-      arrive(B_VFULL + st);
-      if (more_d) ask_rows(1);
+      ask_rows();
+      page_next = ask_page();
     }
-  } else if (works && warp == 16) {
+    int jt = 0;
+    while (more_d) {
+      const int st = jt % S;
+      const uint32_t mat = sKV + st * 2 * Sh::kMat + (of_v ? Sh::kMat : 0);
+      // the stage is free again
+      const bool ok = jt < S || wait((of_v ? B_VEMPTY : B_KEMPTY) + st, jt / S - 1);
+      if (!__all_sync(0xffffffffu, ok)) break;
+      if (!of_v && lane == 0) {
+        if (MINE == 32) s_there[jt & 7][lw] = there;
+        else reinterpret_cast<unsigned short*>(s_there[jt & 7])[lw] = (unsigned short)there;
+      }
+      if (kCopy) {
+        copy_rows(mat);
+        if (jt > 0) {  // the tile before has arrived
+          asm volatile("cp.async.wait_group 1;" ::: "memory");
+          fence_async_smem();
+          arrive(full + (jt - 1) % S);
+        }
+      } else {
+        write_rows(mat);
+        arrive(full + st);
+      }
+      more_d = pa_step(wd, wk, c.Hkv, c.G, ROWS);  // now of the next tile
+      page = page_next;
+      page_next = ask_page();
+      locate();
+      if (more_d) ask_rows();
+      ++jt;
+    }
+    if (kCopy && works) {
+      asm volatile("cp.async.wait_group 0;" ::: "memory");
+      fence_async_smem();
+      if (jt > 0) arrive(full + (jt - 1) % S);
+    }
+  } else if (warp >= kPaIssuer) {
     // ------------------------------------------------------------------ products
-    if (lane == 0) {
+    // A thread for each tile of query rows: S(q) of the next tile of slots follows O(q) += P(q) V of this one, and the other
+    // tile's products run while this one's softmax does.
+    if (works && warp < kPaIssuer + QT && lane == 0) {
       constexpr uint32_t kFmt = kType == LTRI_TYPE_BF16 ? 1u : 0u;
       constexpr uint32_t kF = (1u << 4) | (kFmt << 7) | (kFmt << 10) | (8u << 24);  // fp32 sums, both operands' type, M = 128
       constexpr uint32_t idesc_qk = kF | (uint32_t)(TILE >> 3) << 17, idesc_pv = kF | 1u << 16 | (uint32_t)(D >> 3) << 17;
-      const uint64_t dQ = make_desc(sQ, 16, 1024), dK = make_desc(sKV, 16, 1024), dV = make_desc(sKV + Sh::kMat, TILE * 128, 1024);
-      constexpr uint32_t kO = 256;  // first column of O
-      auto s_col = [&](int q, int b) { return tmem + (SB == 2 ? b * TILE : q * 128); };
-      auto issue_qk = [&](int q, int b, int st) {
+      const int q = warp - kPaIssuer;
+      const uint64_t dQ = make_desc(sQ + q * Sh::kQBytes, 16, 1024), dK = make_desc(sKV, 16, 1024);
+      const uint64_t dV = make_desc(sKV + Sh::kMat, TILE * 128, 1024);
+      const uint32_t tS = tmem + q * 128, tO = tmem + 256 + q * D;
+      const uint32_t bars0 = bar(0), q_bars = bars0 + 8 * q, s_bars = bars0 + 8 * (q * SB), p_bars = bars0 + 16 * (q * SB);
+      auto issue_qk = [&](int b, int st) {
+        const uint64_t db = dK + (uint32_t)(st * (2 * Sh::kMat >> 4));
+        const uint32_t d = tS + b * TILE;
 #pragma unroll
         for (int ks = 0; ks < D / 16; ++ks) {
           const uint32_t half = ks >> 2, in = (ks & 3) * 32;
-          mma_ss(s_col(q, b), dQ + ((q * Sh::kQBytes + half * 16384 + in) >> 4),
-                 dK + ((uint32_t)(st * 2 * Sh::kMat + half * (TILE * 128) + in) >> 4), idesc_qk, ks > 0);
+          mma_ss(d, dQ + ((half * 16384 + in) >> 4), db + ((half * (TILE * 128) + in) >> 4), idesc_qk, ks > 0);
         }
-        mma_commit(bar(B_SREADY + q * SB + b));
+        mma_commit(s_bars + 8 * B_SREADY + 8 * b);
       };
-      // P of 32 slots: 16 columns of first terms, 16 of second ones
-      auto issue_pv = [&](int q, int b, int st, bool acc) {
+      // P of 16 slots: 8 columns of first terms, 8 of second ones.  A part is 32 slots of either half of the tile.
+      auto issue_pv = [&](int b, int st, int part, bool acc) {
+        const uint32_t pa = tS + b * TILE + part * 32;
+        const uint64_t db = dV + (uint32_t)(st * (2 * Sh::kMat >> 4) + part * (32 * 128 >> 4));
 #pragma unroll
-        for (int ks = 0; ks < TILE / 16; ++ks) {
-          const uint64_t db = dV + ((uint32_t)(st * 2 * Sh::kMat + ks * 2048) >> 4);
-          const uint32_t pa = s_col(q, b) + (ks >> 1) * 32 + (ks & 1) * 8;
-          mma_ts(tmem + kO + q * D, pa + 16, db, idesc_pv, acc || ks > 0);
-          mma_ts(tmem + kO + q * D, pa, db, idesc_pv, true);
+        for (int i = 0; i < 4; ++i) {
+          const int slot = (i >> 1) * (TILE / 2) + (i & 1) * 16;
+          mma_ts(tO, pa + slot + 8, db + (slot * 128 >> 4), idesc_pv, acc || i > 0);
+          mma_ts(tO, pa + slot, db + (slot * 128 >> 4), idesc_pv, true);
         }
       };
-      PaWalk w = s_walk;
-      int jt = 0, n[QT] = {}, units[QT] = {};  // tiles; of each tile of queries: tiles, parts
-      bool ok = true;
+      auto wait_at = [&](uint32_t at, uint32_t parity) { return pa_wait(at, parity, abortp); };
+      PaPlace w = s_place;
+      uint32_t st = 0, turn = 0;           // the stage and its parity
+      uint32_t s_turn = 0, unit_turn = 0;  // a bit for each S: the parity of S and P; that of the parts of units
+      int b = 0;                           // the S in turn
+      bool ok = true, had = false;         // had: a part before this one
       do {
-        const int nq = QT == 2 && rows_of(w.e) > 128 ? 2 : 1, T = w.end - w.begin;
-        for (int q = 0; ok && q < nq; ++q) ok = wait(B_QFULL + q, units[q]);
-        if (ok) ok = wait(B_KFULL + jt % S, jt / S);
+        int left = w.end - w.tile;
+        if (q == 1 && w.rows - w.rho <= 128) {
+          // none of this tile's rows: its leave to the stages alone
+          for (; ok && left > 0; --left) {
+            ok = wait_at(bars0 + 8 * B_KFULL + 8 * st, turn);
+            mbar_arrive(bars0 + 8 * B_KEMPTY + 8 * st);
+            ok = ok && wait_at(bars0 + 8 * B_VFULL + 8 * st, turn);
+            mbar_arrive(bars0 + 8 * B_VEMPTY + 8 * st);
+            if (++st == S) st = 0, turn ^= 1;
+          }
+          continue;
+        }
+        ok = wait_at(q_bars + 8 * B_QFULL, unit_turn) && wait_at(bars0 + 8 * B_KFULL + 8 * st, turn);
         if (!ok) break;
         fence_after_sync();
-#pragma unroll
-        for (int q = 0; q < QT; ++q)
-          if (q < nq) issue_qk(q, n[q] % SB, jt % S);
-        mma_commit(bar(B_KEMPTY + jt % S));
-        for (int j = 0; ok && j < T; ++j, ++jt) {
-          const int st = jt % S, nst = (jt + 1) % S;
-          const bool next = j + 1 < T;
+        issue_qk(b, st);
+        mma_commit(bars0 + 8 * B_KEMPTY + 8 * st);
+        bool first = true;
+#pragma unroll 1
+        for (; left > 0; --left) {
+          const bool next = left > 1;
+          const uint32_t nst = st + 1 == S ? 0 : st + 1, nturn = turn ^ (nst == 0);
           if (SB == 2 && next) {
-            ok = wait(B_KFULL + nst, (jt + 1) / S);
+            ok = wait_at(bars0 + 8 * B_KFULL + 8 * nst, nturn);
             if (!ok) break;
             fence_after_sync();
-            issue_qk(0, (n[0] + 1) % SB, nst);
-            mma_commit(bar(B_KEMPTY + nst));
+            issue_qk(b ^ 1, nst);
+            mma_commit(bars0 + 8 * B_KEMPTY + 8 * nst);
           }
-          ok = wait(B_VFULL + st, jt / S);
-#pragma unroll
-          for (int q = 0; q < QT; ++q) {
-            if (!ok || q >= nq) continue;
-            ok = wait(B_PREADY + q * SB + n[q] % SB, n[q] / SB);
-            // the first product of a part overwrites O: the one before it must have been read
-            if (ok && j == 0 && units[q] > 0) ok = wait(B_OFREE + q, units[q] - 1);
-            if (!ok) continue;
+          ok = wait_at(bars0 + 8 * B_VFULL + 8 * st, turn);
+#pragma unroll 1
+          for (int part = 0; part < TILE / 64; ++part) {
+            ok = ok && wait_at(p_bars + 8 * B_PREADY + 16 * b + 8 * part, s_turn >> b & 1);
+            // the first product of a part of a unit overwrites O: the one before it must have been read
+            if (part == 0 && first && had) ok = ok && wait_at(q_bars + 8 * B_OFREE, unit_turn ^ 1);
+            if (!ok) break;
             fence_after_sync();
-            issue_pv(q, n[q] % SB, st, j > 0);
-            if (SB == 2) mma_commit(bar(B_PVDONE));
-            if (SB == 1 && next) {
-              if (q == 0) ok = wait(B_KFULL + nst, (jt + 1) / S);
-              if (!ok) continue;
-              fence_after_sync();
-              issue_qk(q, 0, nst);
-            }
-            if (!next) mma_commit(bar(B_ODONE + q));
-            ++n[q];
+            issue_pv(b, st, part, !first || part > 0);
           }
           if (!ok) break;
-          mma_commit(bar(B_VEMPTY + st));
-          if (SB == 1 && next) mma_commit(bar(B_KEMPTY + nst));
+          mma_commit(bars0 + 8 * B_VEMPTY + 8 * st);
+          if (SB == 2) mma_commit(bars0 + 8 * B_PVDONE);
+          if (SB == 1 && next) {
+            ok = wait_at(bars0 + 8 * B_KFULL + 8 * nst, nturn);
+            if (!ok) break;
+            fence_after_sync();
+            issue_qk(0, nst);
+            mma_commit(bars0 + 8 * B_KEMPTY + 8 * nst);
+          }
+          if (!next) mma_commit(q_bars + 8 * B_ODONE);
+          s_turn ^= 1u << b;
+          first = false;
+          st = nst;
+          turn = nturn;
+          if (SB == 2) b ^= 1;
         }
-        for (int q = 0; q < nq; ++q) ++units[q];
-      } while (ok && pa_next(w, wk, c.Hkv));
+        unit_turn ^= 1;
+        had = true;
+      } while (ok && next_part(w));
       // nothing of this CTA's is under way when it gives its TMEM back
       mma_commit(bar(B_DRAIN));
       const long long t0 = clock64();
@@ -552,200 +658,219 @@ __global__ void __launch_bounds__(kPaThreads, 1)
       }
     }
     __syncwarp();
-  } else if (works && warp < 4 * QT) {
-    // ------------------------------------------------------------------ softmax, queries and outputs: a thread a row
-    const int q = warp >> 2, r = (warp & 3) * 32 + lane;
-    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-    const uint32_t tO = tmem + lanes + 256 + q * D;
-    PaWalk w = s_walk;
-    int n = 0, unit = 0, jt = 0;  // tiles and parts of this tile of queries; the CTA's tiles
-    bool ok = true, more = true;
-    float back = 1.f;
-    // the row's queries of part w into shared memory (free: all products with the last ones have been seen to end)
-    auto load_queries = [&]() {
-      const int rho = w.e.block * ROWS + q * 128 + r;
-      const bool in = rho < w.e.m * c.G;
-      const int tok = w.e.start + rho / c.G, h = w.head * c.G + rho % c.G;
-      const unsigned char* from = a.q + (in ? tok * a.q_stride + (size_t)h * (D * 2) : 0);
-      const uint32_t to = sQ + q * Sh::kQBytes + r * 128;
-      back = 1.f;
-      float u0 = 1.f, u1 = 1.f;
-      if (KIND >= kPaE4m3 && c.type == LTRI_TYPE_BF16) {
-        // bf16 queries as halves: a power of two brings the row's largest element to [2^14, 2^15)
-        uint32_t most = 0;
-        if (in) {
-#pragma unroll 8
-          for (int i = 0; i < D / 8; ++i) {
-            const uint4 x = *reinterpret_cast<const uint4*>(from + i * 16);
-            most = __vmaxu2(most, __vmaxu2(__vmaxu2(x.x & 0x7fff7fffu, x.y & 0x7fff7fffu),
-                                           __vmaxu2(x.z & 0x7fff7fffu, x.w & 0x7fff7fffu)));
-          }
-        }
-        most = max(most & 0xffffu, most >> 16);
-        const int ex = (int)(most >> 7);  // biased exponent
-        const int up = ex == 0 || ex == 255 ? 0 : 127 + 14 - ex;
-        // (2^up may lie outside fp32's range: two factors)
-        u0 = __int_as_float((127 + up / 2) << 23), u1 = __int_as_float((127 + up - up / 2) << 23);
-        back = __int_as_float((127 - up / 2) << 23) * __int_as_float((127 - up + up / 2) << 23);
-      }
-#pragma unroll 4
-      for (int i = 0; i < D / 8; ++i) {
-        uint4 x = in ? *reinterpret_cast<const uint4*>(from + i * 16) : make_uint4(0u, 0u, 0u, 0u);
+  } else {
+    // ------------------------------------------------------------------ softmax, queries and outputs
+    // Two threads a row, each with half of S's columns and of O's.  Every decision is one of all 256 threads of a tile of queries,
+    // so that they meet at the same barriers.
+    if (works && warp < 8 * QT) {
+      constexpr int CH = TILE / 64;  // times 32 columns a thread
+      const int q = warp >> 3, half = warp >> 2 & 1, r = (warp & 3) * 32 + lane;
+      const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+      const uint32_t tO = tmem + lanes + 256 + q * D + half * (D / 2);
+      PaPlace w = s_place;
+      int n = 0, unit = 0, jt = 0;  // tiles and parts of this tile of queries; the CTA's tiles
+      bool ok = true, more = true;
+      float back = 1.f;
+      // the row's queries of part w into shared memory (free: all products with the last ones have been seen to end)
+      auto load_queries = [&]() {
+        const int rho = w.rho + q * 128 + r;
+        const bool in = rho < w.rows;
+        const int tok = w.start + rho / c.G, h = w.head * c.G + rho % c.G;
+        const unsigned char* from = a.q + (in ? tok * a.q_stride + (size_t)h * (D * 2) : 0);
+        const uint32_t to = sQ + q * Sh::kQBytes + r * 128;
+        back = 1.f;
+        float u0 = 1.f, u1 = 1.f;
         if (KIND >= kPaE4m3 && c.type == LTRI_TYPE_BF16) {
-          auto half = [&](uint32_t y) {
-            const float2 f = paged_unpack(LTRI_TYPE_BF16, y);
-            return paged_pack(LTRI_TYPE_FP16, f.x * u0 * u1, f.y * u0 * u1);
-          };
-          x = make_uint4(half(x.x), half(x.y), half(x.z), half(x.w));
-        }
-        pa_store(to + (i >> 3) * 16384 + (((i & 7) ^ (r & 7)) << 4), pa_order<KIND>(x));
-      }
-      fence_async_smem();
-      arrive(B_QFULL + q);
-    };
-    // (a tile of queries without a row in the unit takes no part in it)
-    auto skip = [&]() {
-      while (more && rows_of(w.e) <= q * 128) {
-        jt += w.end - w.begin;
-        more = pa_next(w, wk, c.Hkv);
-      }
-    };
-    skip();
-    if (more) load_queries();
-    while (more && ok) {
-      const PaWalk now = w;
-      const int rho = now.e.block * ROWS + q * 128 + r;
-      const bool row_ok = rho < now.e.m * c.G;
-      const int own = row_ok ? now.e.base + rho / c.G + 1 : 0;  // slots that the row sees
-      float sc = c.scale;
-      if (KIND == kPaInt4) sc = (float)((double)c.scale * back * kI4Back);
-      if (KIND == kPaE4m3) sc = (float)((double)c.scale * c.ks[now.head] * back);
-      if (KIND >= kPaE4m3 && sc < 0x1p-126f) sc = 0x1p-126f;  // (as for single tokens)
-      float ref = kPaNone, sum = 0.f;
-      for (int t = now.begin; t < now.end; ++t, ++n, ++jt) {
-        const int b = n % SB;
-        const uint32_t tS = tmem + lanes + (SB == 2 ? b * TILE : q * 128);
-        ok = wait(B_SREADY + q * SB + b, n / SB);
-        if (!__all_sync(0xffffffffu, ok)) {
-          ok = false;
-          break;
-        }
-        fence_after_sync();
-        // columns that the row sees, as a number of the first ones, and where pages are missing, a bit each
-        const int lim = own - t * TILE;
-        const uint4 words = *reinterpret_cast<const uint4*>(s_there[jt & 7]);  // (16 slots a half-word, 8 where tiles are of 64)
-        const uint32_t there[4] = {TILE == 128 ? words.x : __byte_perm(words.x, words.y, 0x6420),
-                                   TILE == 128 ? words.y : __byte_perm(words.z, words.w, 0x6420), words.z, words.w};
-        bool holes = false;
-#pragma unroll
-        for (int i = 0; i < TILE / 32; ++i) holes |= there[i] != 0xffffffffu;
-        const bool masked = __any_sync(0xffffffffu, lim < TILE) || holes;
-        auto mask = [&](uint32_t (&v)[32], int i) {
-          const int l = lim - i * 32;
-          const uint32_t m = (l >= 32 ? 0xffffffffu : l <= 0 ? 0u : (1u << l) - 1u) & there[i];
-#pragma unroll
-          for (int e = 0; e < 32; ++e)
-            if (!(m >> e & 1u)) v[e] = 0xff800000u;
-        };
-        float most = -INFINITY;
-#pragma unroll
-        for (int i = 0; i < TILE / 32; ++i) {
-          uint32_t v[32];
-          tmem_ld32(tS + i * 32, v);
-          tmem_ld_wait();
-          if (masked) mask(v, i);
-          float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-          for (int e = 0; e < 32; ++e) m4[e & 3] = fmaxf(m4[e & 3], __uint_as_float(v[e]));
-          most = fmaxf(most, fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])));
-        }
-        const float top = most * sc;
-        const bool grow = top > ref + (kOff + kGrow);
-        if (__any_sync(0xffffffffu, grow)) {
-          const float to = grow ? fmaxf(ref, top - kOff) : ref, by = pa_exp2(ref - to);
-          ref = to;
-          sum *= by;
-          if (t > now.begin) {
-            if (SB == 2 && !wait(B_PVDONE, n - 1)) ok = false;
-            fence_after_sync();
-#pragma unroll 1
-            for (int i = 0; i < D / 32; ++i) {
-              uint32_t v[32];
-              tmem_ld32(tO + i * 32, v);
-              tmem_ld_wait();
-#pragma unroll
-              for (int e = 0; e < 32; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) * by);
-              tmem_st32(tO + i * 32, v);
+          // bf16 queries as halves: a power of two brings the row's largest element to [2^14, 2^15)
+          uint32_t most = 0;
+          if (in) {
+#pragma unroll 8
+            for (int i = 0; i < D / 8; ++i) {
+              const uint4 x = *reinterpret_cast<const uint4*>(from + i * 16);
+              most = __vmaxu2(most, __vmaxu2(__vmaxu2(x.x & 0x7fff7fffu, x.y & 0x7fff7fffu),
+                                             __vmaxu2(x.z & 0x7fff7fffu, x.w & 0x7fff7fffu)));
             }
-            tmem_st_wait();
           }
+          most = max(most & 0xffffu, most >> 16);
+          const int ex = (int)(most >> 7);  // biased exponent
+          const int up = ex == 0 || ex == 255 ? 0 : 127 + 14 - ex;
+          // (2^up may lie outside fp32's range: two factors)
+          u0 = __int_as_float((127 + up / 2) << 23), u1 = __int_as_float((127 + up - up / 2) << 23);
+          back = __int_as_float((127 - up / 2) << 23) * __int_as_float((127 - up + up / 2) << 23);
         }
-        float s4[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int i = 0; i < TILE / 32; ++i) {
-          uint32_t v[32];
-          tmem_ld32(tS + i * 32, v);
-          tmem_ld_wait();
-          if (masked) mask(v, i);
-          uint32_t hi[16], lo[16];
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const float p0 = pa_exp2(fmaf(__uint_as_float(v[2 * e]), sc, -ref));
-            const float p1 = pa_exp2(fmaf(__uint_as_float(v[2 * e + 1]), sc, -ref));
-            s4[e & 3] += p0 + p1;
-            pa_terms(kType, p0, p1, hi[e], lo[e]);
+#pragma unroll 4
+        for (int k = 0; k < D / 16; ++k) {
+          const int i = half * (D / 16) + k;
+          uint4 x = in ? *reinterpret_cast<const uint4*>(from + i * 16) : make_uint4(0u, 0u, 0u, 0u);
+          if (KIND >= kPaE4m3 && c.type == LTRI_TYPE_BF16) {
+            auto as_half = [&](uint32_t y) {
+              const float2 f = paged_unpack(LTRI_TYPE_BF16, y);
+              return paged_pack(LTRI_TYPE_FP16, f.x * u0 * u1, f.y * u0 * u1);
+            };
+            x = make_uint4(as_half(x.x), as_half(x.y), as_half(x.z), as_half(x.w));
           }
-          tmem_st16(tS + i * 32, hi);
-          tmem_st16(tS + i * 32 + 16, lo);
+          pa_store(to + (i >> 3) * 16384 + (((i & 7) ^ (r & 7)) << 4), pa_order<KIND>(x));
         }
-        sum += (s4[0] + s4[1]) + (s4[2] + s4[3]);
-        tmem_st_wait();
-        fence_before_sync();
-        arrive(B_PREADY + q * SB + b);
-      }
-      if (!ok) break;
-      // the next part's queries while this one's last products run
-      more = pa_next(w, wk, c.Hkv);
+        fence_async_smem();
+        arrive(B_QFULL + q);
+      };
+      // (a tile of queries without a row in the unit takes no part in it)
+      auto skip = [&]() {
+        while (more && w.rows - w.rho <= q * 128) {
+          jt += w.end - w.tile;
+          more = next_part(w);
+        }
+      };
       skip();
       if (more) load_queries();
-      ok = wait(B_ODONE + q, unit);
-      if (!__all_sync(0xffffffffu, ok)) break;
-      fence_after_sync();
-      const bool whole = now.begin == 0 && now.end == now.e.tiles;
-      const float by = !whole ? 1.f : sum == 0.f ? 0.f : 1.f / sum, vs = whole ? pa_v_scale<KIND>(c, now.head) : 1.f;
-      const int tok = now.e.start + rho / c.G, h = now.head * c.G + rho % c.G;
-      float* part = wk.part + (size_t)(2 * blockIdx.x + (now.begin == 0 ? 1 : 0)) * pa_part_floats<KIND, D>();
+      while (more) {
+        const int rho = w.rho + q * 128 + r, head = w.head, begin = w.tile, end = w.end;
+        const bool row_ok = rho < w.rows, whole = begin == 0 && end == w.tiles;
+        const int own = (row_ok ? w.base + rho / c.G + 1 : 0) - half * (TILE / 2);  // slots that the row sees
+        const size_t to_row = (size_t)(w.start + rho / c.G) * c.Hq + head * c.G + rho % c.G;
+        float sc = c.scale;
+        if (KIND == kPaInt4) sc = (float)((double)c.scale * back * kI4Back);
+        if (KIND == kPaE4m3) sc = (float)((double)c.scale * c.ks[head] * back);
+        if (KIND >= kPaE4m3 && sc < 0x1p-126f) sc = 0x1p-126f;  // (as for single tokens)
+        float ref = kPaNone, sum = 0.f;
+        for (int t = begin; t < end; ++t, ++n, ++jt) {
+          const int b = n % SB;
+          const uint32_t tS = tmem + lanes + (SB == 2 ? b * TILE : q * 128) + half * (TILE / 2);
+          ok = wait(B_SREADY + q * SB + b, n / SB);
+          fence_after_sync();
+          // columns that the row sees, as a number of the first ones, and where pages are missing, a bit each
+          const int lim = own - t * TILE;
+          const uint32_t* there = s_there[jt & 7] + half * CH;
+          bool some = lim < TILE / 2;
+#pragma unroll
+          for (int i = 0; i < CH; ++i) some |= there[i] != 0xffffffffu;
+          some = __any_sync(0xffffffffu, some);
+          auto seen = [&](int i) {  // of 32 columns
+            const int l = lim - i * 32;
+            return (l >= 32 ? 0xffffffffu : l <= 0 ? 0u : (1u << l) - 1u) & there[i];
+          };
+          float top = -INFINITY;
 #pragma unroll 1
-      for (int i = 0; i < D / 32; ++i) {
-        uint32_t v[32];
-        tmem_ld32(tO + i * 32, v);
-        tmem_ld_wait();
-        float z[32];
+          for (int i = 0; i < CH; ++i) {
+            uint32_t v[32];
+            tmem_ld32(tS + i * 32, v);
+            tmem_ld_wait();
+            if (some) {
+              const uint32_t m = seen(i);
 #pragma unroll
-        for (int e = 0; e < 32; ++e) z[e] = __uint_as_float(v[e]) * by * vs;
-        if (!row_ok) continue;
-        if (whole) {
-          pa_put32<KIND>(c.type, a.out + ((size_t)tok * c.Hq + h) * (D * 2) + i * 64, z);
-        } else {
+              for (int e = 0; e < 32; ++e)
+                if (!(m >> e & 1u)) v[e] = 0xff800000u;
+            }
+            float m4[4] = {-INFINITY, -INFINITY, -INFINITY, top};
 #pragma unroll
-          for (int e = 0; e < 8; ++e)
-            *reinterpret_cast<float4*>(part + ((size_t)(q * (D / 4) + i * 8 + e) * 128 + r) * 4) =
-                make_float4(z[4 * e], z[4 * e + 1], z[4 * e + 2], z[4 * e + 3]);
+            for (int e = 0; e < 32; e += 2)
+              m4[e / 2 & 3] = fmaxf(m4[e / 2 & 3], fmaxf(__uint_as_float(v[e]), __uint_as_float(v[e + 1])));
+            top = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
+          }
+          top *= sc;
+          if (pa_any(1 + q, !ok || top > ref + (kOff + kGrow))) {
+            s_top[q][half][r] = top;
+            if (!ok) s_bad[q] = 1;
+            if (pa_any(1 + q, false) || s_bad[q]) {
+              ok = false;
+              break;
+            }
+            top = fmaxf(top, s_top[q][half ^ 1][r]);
+            const float to = top > ref + (kOff + kGrow) ? fmaxf(ref, top - kOff) : ref, by = pa_exp2(ref - to);
+            ref = to;
+            sum *= by;
+            if (t > begin && __any_sync(0xffffffffu, by != 1.f)) {
+              // (two S: the products with V of the tile before are seen to end; if they are not, so is the CTA's end)
+              if (SB == 2) wait(B_PVDONE, n - 1);
+              fence_after_sync();
+#pragma unroll 1
+              for (int i = 0; i < D / 32; ++i) {
+                uint32_t o[16];
+                tmem_ld16(tO + i * 16, o);
+                tmem_ld_wait();
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * by);
+                tmem_st16(tO + i * 16, o);
+              }
+              tmem_st_wait();
+            }
+          }
+          const unsigned long long sc2 = pa_pair(sc, sc), ref2 = pa_pair(-ref, -ref);
+          unsigned long long s2[2] = {0ull, 0ull};
+#pragma unroll 1
+          for (int k = 0; k < 2 * CH; ++k) {
+            uint32_t v[16], hi[8], lo[8];
+            tmem_ld16(tS + k * 16, v);
+            tmem_ld_wait();
+            if (some) {
+              const uint32_t m = seen(k >> 1) >> (k & 1) * 16;
+#pragma unroll
+              for (int e = 0; e < 16; ++e)
+                if (!(m >> e & 1u)) v[e] = 0xff800000u;
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const float2 x = pa_split(pa_fma2(pa_pair(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1])), sc2, ref2));
+              const unsigned long long p = pa_pair(pa_exp2(x.x), pa_exp2(x.y));
+              s2[e & 1] = pa_add2(s2[e & 1], p);
+              pa_terms(kType, p, hi[e], lo[e]);
+            }
+            tmem_st8(tS + k * 16, hi);
+            tmem_st8(tS + k * 16 + 8, lo);
+            if (k & 1) {
+              tmem_st_wait();
+              fence_before_sync();
+              arrive(B_PREADY + 2 * (q * SB + b) + (k >> 1));
+            }
+          }
+          const float2 s = pa_split(pa_add2(s2[0], s2[1]));
+          sum += s.x + s.y;
         }
+        if (!ok) break;
+        // the next part's queries while this one's last products run
+        more = next_part(w);
+        skip();
+        if (more) load_queries();
+        s_sum[q][half][r] = sum;
+        ok = wait(B_ODONE + q, unit);
+        if (pa_any(1 + q, !ok)) break;
+        sum = s_sum[q][0][r] + s_sum[q][1][r];
+        fence_after_sync();
+        const float by = !whole ? 1.f : sum == 0.f ? 0.f : 1.f / sum, vs = whole ? pa_v_scale<KIND>(c, head) : 1.f;
+        float* part = wk.part + (size_t)(2 * blockIdx.x + (begin == 0 ? 1 : 0)) * pa_part_floats<KIND, D>();
+#pragma unroll 1
+        for (int k = 0; k < D / 64; ++k) {
+          const int i = half * (D / 64) + k;
+          uint32_t v[32];
+          tmem_ld32(tO + k * 32, v);
+          tmem_ld_wait();
+          float z[32];
+#pragma unroll
+          for (int e = 0; e < 32; ++e) z[e] = __uint_as_float(v[e]) * by * vs;
+          if (!row_ok) continue;
+          if (whole) {
+            pa_put32<KIND>(c.type, a.out + to_row * (D * 2) + i * 64, z);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              *reinterpret_cast<float4*>(part + ((size_t)(q * (D / 4) + i * 8 + e) * 128 + r) * 4) =
+                  make_float4(z[4 * e], z[4 * e + 1], z[4 * e + 2], z[4 * e + 3]);
+          }
+        }
+        fence_before_sync();
+        arrive(B_OFREE + q);
+        if (row_ok && half == 0) {
+          if (whole && a.lse)
+            a.lse[to_row] = sum == 0.f ? -INFINITY : (ref + log2f(sum)) * 0.69314718055994531f;
+          if (!whole) *reinterpret_cast<float2*>(part + (size_t)ROWS * D + (q * 128 + r) * 2) = make_float2(ref, sum);
+        }
+        ++unit;
       }
-      fence_before_sync();
-      arrive(B_OFREE + q);
-      if (row_ok) {
-        if (whole && a.lse)
-          a.lse[(size_t)tok * c.Hq + h] = sum == 0.f ? -INFINITY : (ref + log2f(sum)) * 0.69314718055994531f;
-        if (!whole) *reinterpret_cast<float2*>(part + (size_t)ROWS * D + (q * 128 + r) * 2) = make_float2(ref, sum);
-      }
-      ++unit;
     }
   }
   __syncthreads();
   if (tid == 0 && s_abort && atomicCAS(&c.status[0], 0, (int)LTRI_ETIMEOUT) == 0) c.status[1] = blockIdx.x;
-  if (warp == 16) tmem_dealloc(tmem, 512);
+  if (warp == kPaIssuer) tmem_dealloc(tmem, 512);
 }
 
 // Joins the parts of a unit that begins in CTA x's run and does not end there: 128 query rows of it, 32 elements a thread.
