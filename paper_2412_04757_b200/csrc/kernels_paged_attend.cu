@@ -48,7 +48,11 @@ constexpr int kPaThreads = 32 * (kPaIssuer + 4);
 constexpr long long kPaWaitLimit = 10 * kWaitLimitCycles;
 constexpr float kPaNone = -3.0e38f;  // reference of sums that nothing has entered yet: below every logit, and finite
 
-// A block of a row's query rows, and the first of its KV heads' tiles in the line (they follow each other).
+// What a unit costs besides its tiles (queries to be loaded, outputs to be written, while the products wait), as tiles: it takes so
+// many more places in the line.  (Without them the CTAs with the shortest units were through 1.3 times as late as the others.)
+constexpr int kPaUnit = 2;
+
+// A block of a row's query rows, and the first of its KV heads' places in the line (they follow each other).
 struct __align__(32) PaEntry {
   int row, block;
   int start, m;      // the row's first token in q, its tokens
@@ -57,7 +61,7 @@ struct __align__(32) PaEntry {
   long long before;
 };
 struct PaPlan {
-  long long total;   // tiles
+  long long total;   // places
   int entries;
   int pad;
 };
@@ -172,7 +176,7 @@ __global__ void __launch_bounds__(kPlThreads)
       e.base = paged_len(c, r, lo) - e.m;
       if (e.base < 0 && e.block == 0) paged_status(c, lo);
       e.tiles = max(1, (pa_limit(e, c.G, rows) + tile - 1) / tile);
-      n = (long long)e.tiles * c.Hkv;
+      n = (long long)(e.tiles + kPaUnit) * c.Hkv;
     }
     long long all;
     e.before = total + scan(n, all);
@@ -192,7 +196,7 @@ struct PaPlace {
   int rows, rho;          // query rows of the row, and the unit's first
   int base, limit;        // slots in front of the row's tokens, and those that the unit's last token sees
   int tiles, tile, end;   // of the unit; the place; behind the part
-  long long left;         // tiles of the run behind the part
+  long long left;         // places of the run behind the part
 };
 __device__ __forceinline__ void pa_entry(PaPlace& w, const PaEntry& e, int G, int rows) {
   w.row = e.row;
@@ -203,17 +207,23 @@ __device__ __forceinline__ void pa_entry(PaPlace& w, const PaEntry& e, int G, in
   w.limit = pa_limit(e, G, rows);
   w.tiles = e.tiles;
 }
+// The unit's part in the run, whose next place is the unit's number `at`; false if it has none (the run ends in front of the first
+// tile).
+__device__ __forceinline__ bool pa_part(PaPlace& w, int at) {
+  const int n = (int)min((long long)(w.tiles + kPaUnit - at), w.left);
+  w.left -= n;
+  w.tile = max(0, at - kPaUnit);
+  w.end = max(0, at + n - kPaUnit);
+  return w.tile < w.end;
+}
 // The next part; false at the run's end.
 __device__ __forceinline__ bool pa_next(PaPlace& w, const PaWork& wk, int heads, int G, int rows) {
   if (w.left <= 0) return false;
-  w.tile = 0;
   if (++w.head == heads) {
     w.head = 0;
     pa_entry(w, wk.entry[++w.at], G, rows);
   }
-  w.end = (int)min((long long)w.tiles, w.left);
-  w.left -= w.end;
-  return true;
+  return pa_part(w, 0);
 }
 // The next tile; false at the run's end.
 __device__ __forceinline__ bool pa_step(PaPlace& w, const PaWork& wk, int heads, int G, int rows) {
@@ -348,6 +358,7 @@ __global__ void __launch_bounds__(kPaThreads, 1)
   __shared__ __align__(16) uint32_t s_there[8][4];
   // of a tile of queries: rows' largest logits of each half of the columns, and their sums
   __shared__ float s_top[QT][2][128], s_sum[QT][2][128];
+  __shared__ uint32_t s_most[QT][2][128];  // and their queries' largest elements
   __shared__ int s_bad[QT];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t sbase = (smem_addr(smem_raw) + 1023u) & ~1023u, sQ = sbase, sKV = sbase + QT * Sh::kQBytes;
@@ -387,19 +398,18 @@ __global__ void __launch_bounds__(kPaThreads, 1)
   // the CTA's run
   const long long total = wk.plan->total;
   const long long per = (total + gridDim.x - 1) / gridDim.x, c0 = blockIdx.x * per;
-  const bool works = c0 < total;
-  if (warp == 0 && works) {
+  __shared__ bool s_works;
+  if (tid == 0 && c0 >= total) s_works = false;
+  if (warp == 0 && c0 < total) {
     const int at = pa_find(wk, wk.plan->entries, c0);
     if (lane == 0) {
       const PaEntry e = wk.entry[at];
       PaPlace w;
       pa_entry(w, e, c.G, ROWS);
       w.at = at;
-      w.head = (int)((c0 - e.before) / e.tiles);
-      w.tile = (int)((c0 - e.before) % e.tiles);
+      w.head = (int)((c0 - e.before) / (e.tiles + kPaUnit));
       w.left = min(per, total - c0);
-      w.end = (int)min((long long)w.tiles, w.tile + w.left);
-      w.left -= w.end - w.tile;
+      s_works = pa_part(w, (int)((c0 - e.before) % (e.tiles + kPaUnit)));
       s_place = w;
     }
   }
@@ -407,6 +417,7 @@ __global__ void __launch_bounds__(kPaThreads, 1)
   __syncthreads();
   fence_after_sync();
   const uint32_t tmem = s_tmem;
+  const bool works = s_works;
   auto next_part = [&](PaPlace& w) { return pa_next(w, wk, c.Hkv, c.G, ROWS); };
 
   if (warp >= kPaSoftmax && warp < kPaIssuer) {
@@ -678,38 +689,53 @@ __global__ void __launch_bounds__(kPaThreads, 1)
         const int tok = w.start + rho / c.G, h = w.head * c.G + rho % c.G;
         const unsigned char* from = a.q + (in ? tok * a.q_stride + (size_t)h * (D * 2) : 0);
         const uint32_t to = sQ + q * Sh::kQBytes + r * 128;
+        // (eight chunks of 16 bytes at a time on their way)
+        constexpr int GROUP = D / 16 < 8 ? D / 16 : 8, GROUPS = D / 16 / GROUP;
+        uint4 x[GROUP];
+        auto load = [&](int g) {
+#pragma unroll
+          for (int k = 0; k < GROUP; ++k)
+            x[k] = in ? *reinterpret_cast<const uint4*>(from + (half * (D / 16) + g * GROUP + k) * 16) : make_uint4(0u, 0u, 0u, 0u);
+        };
+        load(0);
         back = 1.f;
         float u0 = 1.f, u1 = 1.f;
-        if (KIND >= kPaE4m3 && c.type == LTRI_TYPE_BF16) {
+        constexpr bool kHalves = KIND >= kPaE4m3;
+        if (kHalves && c.type == LTRI_TYPE_BF16) {
           // bf16 queries as halves: a power of two brings the row's largest element to [2^14, 2^15)
           uint32_t most = 0;
-          if (in) {
-#pragma unroll 8
-            for (int i = 0; i < D / 8; ++i) {
-              const uint4 x = *reinterpret_cast<const uint4*>(from + i * 16);
-              most = __vmaxu2(most, __vmaxu2(__vmaxu2(x.x & 0x7fff7fffu, x.y & 0x7fff7fffu),
-                                             __vmaxu2(x.z & 0x7fff7fffu, x.w & 0x7fff7fffu)));
-            }
+#pragma unroll 1
+          for (int g = 0; g < GROUPS; ++g) {
+            if (g) load(g);
+#pragma unroll
+            for (int k = 0; k < GROUP; ++k)
+              most = __vmaxu2(most, __vmaxu2(__vmaxu2(x[k].x & 0x7fff7fffu, x[k].y & 0x7fff7fffu),
+                                             __vmaxu2(x[k].z & 0x7fff7fffu, x[k].w & 0x7fff7fffu)));
           }
-          most = max(most & 0xffffu, most >> 16);
-          const int ex = (int)(most >> 7);  // biased exponent
+          if (GROUPS > 1) load(0);
+          s_most[q][half][r] = max(most & 0xffffu, most >> 16);
+          pa_any(1 + q, false);
+          const int ex = (int)(max(s_most[q][0][r], s_most[q][1][r]) >> 7);  // biased exponent
           const int up = ex == 0 || ex == 255 ? 0 : 127 + 14 - ex;
           // (2^up may lie outside fp32's range: two factors)
           u0 = __int_as_float((127 + up / 2) << 23), u1 = __int_as_float((127 + up - up / 2) << 23);
           back = __int_as_float((127 - up / 2) << 23) * __int_as_float((127 - up + up / 2) << 23);
         }
-#pragma unroll 4
-        for (int k = 0; k < D / 16; ++k) {
-          const int i = half * (D / 16) + k;
-          uint4 x = in ? *reinterpret_cast<const uint4*>(from + i * 16) : make_uint4(0u, 0u, 0u, 0u);
-          if (KIND >= kPaE4m3 && c.type == LTRI_TYPE_BF16) {
-            auto as_half = [&](uint32_t y) {
-              const float2 f = paged_unpack(LTRI_TYPE_BF16, y);
-              return paged_pack(LTRI_TYPE_FP16, f.x * u0 * u1, f.y * u0 * u1);
-            };
-            x = make_uint4(as_half(x.x), as_half(x.y), as_half(x.z), as_half(x.w));
+#pragma unroll 1
+        for (int g = 0; g < GROUPS; ++g) {
+          if (g) load(g);
+#pragma unroll
+          for (int k = 0; k < GROUP; ++k) {
+            const int i = half * (D / 16) + g * GROUP + k;
+            if (kHalves && c.type == LTRI_TYPE_BF16) {
+              auto as_half = [&](uint32_t y) {
+                const float2 f = paged_unpack(LTRI_TYPE_BF16, y);
+                return paged_pack(LTRI_TYPE_FP16, f.x * u0 * u1, f.y * u0 * u1);
+              };
+              x[k] = make_uint4(as_half(x[k].x), as_half(x[k].y), as_half(x[k].z), as_half(x[k].w));
+            }
+            pa_store(to + (i >> 3) * 16384 + (((i & 7) ^ (r & 7)) << 4), pa_order<KIND>(x[k]));
           }
-          pa_store(to + (i >> 3) * 16384 + (((i & 7) ^ (r & 7)) << 4), pa_order<KIND>(x));
         }
         fence_async_smem();
         arrive(B_QFULL + q);
@@ -873,7 +899,7 @@ __global__ void __launch_bounds__(kPaThreads, 1)
   if (warp == kPaIssuer) tmem_dealloc(tmem, 512);
 }
 
-// Joins the parts of a unit that begins in CTA x's run and does not end there: 128 query rows of it, 32 elements a thread.
+// Joins the parts of a unit whose first tile is in CTA x's run and whose last is not: 128 query rows of it, 32 elements a thread.
 template <int KIND, int D>
 __global__ void __launch_bounds__(128) k_paged_attend_join(PagedCache c, PagedQueries a, PaWork wk, int ctas) {
   using Sh = PaShape<KIND, D>;
@@ -888,9 +914,9 @@ __global__ void __launch_bounds__(128) k_paged_attend_join(PagedCache c, PagedQu
   }
   __syncthreads();
   const PaEntry e = wk.entry[s_at];
-  const int head = (int)((c1 - 1 - e.before) / e.tiles);
-  const long long begin = e.before + (long long)head * e.tiles, end = begin + e.tiles;
-  if (begin < c0 || end == c1) return;
+  const int places = e.tiles + kPaUnit, head = (int)((c1 - 1 - e.before) / places);
+  const long long begin = e.before + (long long)head * places + kPaUnit, end = begin + e.tiles;
+  if (begin < c0 || begin >= c1 || end == c1) return;
   const int parts = (int)((end - 1) / per - blockIdx.x) + 1;
   const int q = blockIdx.y, r = threadIdx.x, i = blockIdx.z;
   const int rho = e.block * Sh::kRows + q * 128 + r;
