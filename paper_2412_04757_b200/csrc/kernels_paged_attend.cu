@@ -16,9 +16,8 @@
 // of units that CTAs share are joined by a third kernel, in the order of the line.
 //
 // Roles of a CTA's 28 warps: 0-7 and 8-15 softmax of the two tiles of 128 query rows (two threads a row; they also load the row's
-// queries and write its outputs), 16-23 bring K and V tiles into shared memory, 24 issues the products.  TMEM: S0, S1, O0, O1 of
-// 128 columns each; P replaces S in its columns.  head_dim 256: one tile of query rows, whose O takes 256 columns, and two S of 64
-// columns in turn.
+// queries and write its outputs), 16-23 bring K and V tiles into shared memory, 24 and 25 issue the products.  TMEM: two S of 64
+// columns in turn for each tile of query rows, in whose columns P replaces S, then the two O.  head_dim 256: one tile of query rows.
 #include "paged_int4.cuh"
 #include "tc_util.cuh"
 
@@ -32,7 +31,7 @@ template <int KIND, int D>
 struct PaShape {
   static constexpr int kRow = KIND == kPaInt4 ? D / 2 : KIND == kPaE4m3 ? D : 2 * D;  // bytes of a cached row
   static constexpr int kQt = D == 256 ? 1 : 2;          // tiles of 128 query rows
-  static constexpr int kSb = D == 256 ? 2 : 1;          // S of each
+  static constexpr int kSb = 2;                         // S of each, of 64 slots
   static constexpr int kRows = 128 * kQt;               // query rows of a unit
   static constexpr int kTile = D == 256 ? 64 : 128;     // slots
   static constexpr int kStages = D == 64 ? 4 : 2;
@@ -338,23 +337,23 @@ template <int KIND, int D>
 __global__ void __launch_bounds__(kPaThreads, 1)
     k_paged_attend(PagedCache c, int layer, const int* table, long long table_stride, PagedQueries a, PaWork wk) {
   using Sh = PaShape<KIND, D>;
-  constexpr int QT = Sh::kQt, SB = Sh::kSb, TILE = Sh::kTile, S = Sh::kStages, ROWS = Sh::kRows;
+  constexpr int QT = Sh::kQt, SB = Sh::kSb, TILE = Sh::kTile, S = Sh::kStages, ROWS = Sh::kRows, SUBS = TILE / 64;
   constexpr int kType = KIND == kPaBf16 ? LTRI_TYPE_BF16 : LTRI_TYPE_FP16;  // of the products
   // as for single tokens: halves have their largest probability at 2^kOff, and a reference moves only when a logit exceeds it
   // by kGrow
   constexpr float kOff = KIND == kPaBf16 ? 0.f : 10.f, kGrow = 4.f;
   extern __shared__ unsigned char smem_raw[];
-  enum {  // (P is handed over in up to two parts)
+  enum {
     B_KFULL = 0, B_VFULL = S, B_KEMPTY = 2 * S, B_VEMPTY = 3 * S, B_QFULL = 4 * S, B_SREADY = B_QFULL + QT,
-    B_PREADY = B_SREADY + QT * SB, B_OFREE = B_PREADY + 2 * QT * SB, B_ODONE = B_OFREE + QT, B_PVDONE = B_ODONE + QT,
-    B_DRAIN = B_PVDONE + 1, B_COUNT = B_DRAIN + 1
+    B_PREADY = B_SREADY + QT * SB, B_OFREE = B_PREADY + QT * SB, B_ODONE = B_OFREE + QT, B_PVDONE = B_ODONE + QT,
+    B_DRAIN = B_PVDONE + QT, B_COUNT = B_DRAIN + 1
   };
   __shared__ __align__(8) unsigned long long bars[B_COUNT];
   __shared__ uint32_t s_tmem;
   __shared__ int s_abort;
   __shared__ PaPlace s_place;
   // by tile: slots that have a page, a bit each.  (Eight tiles: when the K of tile j is written, that of j - S has met its
-  // queries, and so the softmax of j - S - 1 and those in front of it have ended.)
+  // queries, which takes that the softmax of j - S - 1 and those in front of it have ended.)
   __shared__ __align__(16) uint32_t s_there[8][4];
   // of a tile of queries: rows' largest logits of each half of the columns, and their sums
   __shared__ float s_top[QT][2][128], s_sum[QT][2][128];
@@ -383,13 +382,12 @@ __global__ void __launch_bounds__(kPaThreads, 1)
       mbar_init(bar(B_QFULL + q), 8);
       mbar_init(bar(B_OFREE + q), 8);
       mbar_init(bar(B_ODONE + q), 1);
+      mbar_init(bar(B_PVDONE + q), 1);
       for (int b = 0; b < SB; ++b) {
         mbar_init(bar(B_SREADY + q * SB + b), 1);
-        mbar_init(bar(B_PREADY + 2 * (q * SB + b)), 8);
-        mbar_init(bar(B_PREADY + 2 * (q * SB + b) + 1), 8);
+        mbar_init(bar(B_PREADY + q * SB + b), 8);
       }
     }
-    mbar_init(bar(B_PVDONE), 1);
     mbar_init(bar(B_DRAIN), QT);
     fence_mbar_init();
   }
@@ -569,15 +567,16 @@ __global__ void __launch_bounds__(kPaThreads, 1)
     if (works && warp < kPaIssuer + QT && lane == 0) {
       constexpr uint32_t kFmt = kType == LTRI_TYPE_BF16 ? 1u : 0u;
       constexpr uint32_t kF = (1u << 4) | (kFmt << 7) | (kFmt << 10) | (8u << 24);  // fp32 sums, both operands' type, M = 128
-      constexpr uint32_t idesc_qk = kF | (uint32_t)(TILE >> 3) << 17, idesc_pv = kF | 1u << 16 | (uint32_t)(D >> 3) << 17;
+      constexpr uint32_t idesc_qk = kF | (uint32_t)(64 >> 3) << 17, idesc_pv = kF | 1u << 16 | (uint32_t)(D >> 3) << 17;
       const int q = warp - kPaIssuer;
       const uint64_t dQ = make_desc(sQ + q * Sh::kQBytes, 16, 1024), dK = make_desc(sKV, 16, 1024);
       const uint64_t dV = make_desc(sKV + Sh::kMat, TILE * 128, 1024);
       const uint32_t tS = tmem + q * 128, tO = tmem + 256 + q * D;
-      const uint32_t bars0 = bar(0), q_bars = bars0 + 8 * q, s_bars = bars0 + 8 * (q * SB), p_bars = bars0 + 16 * (q * SB);
-      auto issue_qk = [&](int b, int st) {
-        const uint64_t db = dK + (uint32_t)(st * (2 * Sh::kMat >> 4));
-        const uint32_t d = tS + b * TILE;
+      const uint32_t bars0 = bar(0), q_bars = bars0 + 8 * q, s_bars = bars0 + 8 * (q * SB);
+      // 64 slots of the tile in stage st
+      auto issue_qk = [&](int b, int st, int sub) {
+        const uint64_t db = dK + (uint32_t)(st * (2 * Sh::kMat >> 4) + sub * (64 * 128 >> 4));
+        const uint32_t d = tS + b * 64;
 #pragma unroll
         for (int ks = 0; ks < D / 16; ++ks) {
           const uint32_t half = ks >> 2, in = (ks & 3) * 32;
@@ -585,15 +584,14 @@ __global__ void __launch_bounds__(kPaThreads, 1)
         }
         mma_commit(s_bars + 8 * B_SREADY + 8 * b);
       };
-      // P of 16 slots: 8 columns of first terms, 8 of second ones.  A part is 32 slots of either half of the tile.
-      auto issue_pv = [&](int b, int st, int part, bool acc) {
-        const uint32_t pa = tS + b * TILE + part * 32;
-        const uint64_t db = dV + (uint32_t)(st * (2 * Sh::kMat >> 4) + part * (32 * 128 >> 4));
+      // P of 16 slots: 8 columns of first terms, 8 of second ones
+      auto issue_pv = [&](int b, int st, int sub, bool acc) {
+        const uint32_t pa = tS + b * 64;
+        const uint64_t db = dV + (uint32_t)(st * (2 * Sh::kMat >> 4) + sub * (64 * 128 >> 4));
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const int slot = (i >> 1) * (TILE / 2) + (i & 1) * 16;
-          mma_ts(tO, pa + slot + 8, db + (slot * 128 >> 4), idesc_pv, acc || i > 0);
-          mma_ts(tO, pa + slot, db + (slot * 128 >> 4), idesc_pv, true);
+          mma_ts(tO, pa + i * 16 + 8, db + (i * 16 * 128 >> 4), idesc_pv, acc || i > 0);
+          mma_ts(tO, pa + i * 16, db + (i * 16 * 128 >> 4), idesc_pv, true);
         }
       };
       auto wait_at = [&](uint32_t at, uint32_t parity) { return pa_wait(at, parity, abortp); };
@@ -618,46 +616,41 @@ __global__ void __launch_bounds__(kPaThreads, 1)
         ok = wait_at(q_bars + 8 * B_QFULL, unit_turn) && wait_at(bars0 + 8 * B_KFULL + 8 * st, turn);
         if (!ok) break;
         fence_after_sync();
-        issue_qk(b, st);
-        mma_commit(bars0 + 8 * B_KEMPTY + 8 * st);
+        issue_qk(b, st, 0);
+        if (SUBS == 1) mma_commit(bars0 + 8 * B_KEMPTY + 8 * st);
         bool first = true;
+        int sub = 0;
+        left *= SUBS;
 #pragma unroll 1
         for (; left > 0; --left) {
-          const bool next = left > 1;
-          const uint32_t nst = st + 1 == S ? 0 : st + 1, nturn = turn ^ (nst == 0);
-          if (SB == 2 && next) {
-            ok = wait_at(bars0 + 8 * B_KFULL + 8 * nst, nturn);
-            if (!ok) break;
-            fence_after_sync();
-            issue_qk(b ^ 1, nst);
-            mma_commit(bars0 + 8 * B_KEMPTY + 8 * nst);
+          // S of the next 64 slots, while this one's softmax runs
+          const bool last = sub + 1 == SUBS;  // of the tile
+          const uint32_t nst = !last ? st : st + 1 == S ? 0 : st + 1, nturn = turn ^ (last && nst == 0);
+          const int nsub = last ? 0 : sub + 1;
+          if (left > 1) {
+            if (last) {
+              ok = wait_at(bars0 + 8 * B_KFULL + 8 * nst, nturn);
+              if (!ok) break;
+              fence_after_sync();
+            }
+            issue_qk(b ^ 1, nst, nsub);
+            if (nsub + 1 == SUBS) mma_commit(bars0 + 8 * B_KEMPTY + 8 * nst);
           }
-          ok = wait_at(bars0 + 8 * B_VFULL + 8 * st, turn);
-#pragma unroll 1
-          for (int part = 0; part < TILE / 64; ++part) {
-            ok = ok && wait_at(p_bars + 8 * B_PREADY + 16 * b + 8 * part, s_turn >> b & 1);
-            // the first product of a part of a unit overwrites O: the one before it must have been read
-            if (part == 0 && first && had) ok = ok && wait_at(q_bars + 8 * B_OFREE, unit_turn ^ 1);
-            if (!ok) break;
-            fence_after_sync();
-            issue_pv(b, st, part, !first || part > 0);
-          }
+          ok = (sub > 0 || wait_at(bars0 + 8 * B_VFULL + 8 * st, turn)) && wait_at(s_bars + 8 * B_PREADY + 8 * b, s_turn >> b & 1);
+          // the first product of a part of a unit overwrites O: the one before it must have been read
+          if (first && had) ok = ok && wait_at(q_bars + 8 * B_OFREE, unit_turn ^ 1);
           if (!ok) break;
-          mma_commit(bars0 + 8 * B_VEMPTY + 8 * st);
-          if (SB == 2) mma_commit(bars0 + 8 * B_PVDONE);
-          if (SB == 1 && next) {
-            ok = wait_at(bars0 + 8 * B_KFULL + 8 * nst, nturn);
-            if (!ok) break;
-            fence_after_sync();
-            issue_qk(0, nst);
-            mma_commit(bars0 + 8 * B_KEMPTY + 8 * nst);
-          }
-          if (!next) mma_commit(q_bars + 8 * B_ODONE);
+          fence_after_sync();
+          issue_pv(b, st, sub, !first);
+          if (last) mma_commit(bars0 + 8 * B_VEMPTY + 8 * st);
+          mma_commit(q_bars + 8 * B_PVDONE);
+          if (left == 1) mma_commit(q_bars + 8 * B_ODONE);
           s_turn ^= 1u << b;
           first = false;
           st = nst;
           turn = nturn;
-          if (SB == 2) b ^= 1;
+          sub = nsub;
+          b ^= 1;
         }
         unit_turn ^= 1;
         had = true;
@@ -674,7 +667,6 @@ __global__ void __launch_bounds__(kPaThreads, 1)
     // Two threads a row, each with half of S's columns and of O's.  Every decision is one of all 256 threads of a tile of queries,
     // so that they meet at the same barriers.
     if (works && warp < 8 * QT) {
-      constexpr int CH = TILE / 64;  // times 32 columns a thread
       const int q = warp >> 3, half = warp >> 2 & 1, r = (warp & 3) * 32 + lane;
       const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
       const uint32_t tO = tmem + lanes + 256 + q * D + half * (D / 2);
@@ -752,48 +744,35 @@ __global__ void __launch_bounds__(kPaThreads, 1)
       while (more) {
         const int rho = w.rho + q * 128 + r, head = w.head, begin = w.tile, end = w.end;
         const bool row_ok = rho < w.rows, whole = begin == 0 && end == w.tiles;
-        const int own = (row_ok ? w.base + rho / c.G + 1 : 0) - half * (TILE / 2);  // slots that the row sees
+        const int own = (row_ok ? w.base + rho / c.G + 1 : 0) - half * 32;  // slots that the row sees
         const size_t to_row = (size_t)(w.start + rho / c.G) * c.Hq + head * c.G + rho % c.G;
         float sc = c.scale;
         if (KIND == kPaInt4) sc = (float)((double)c.scale * back * kI4Back);
         if (KIND == kPaE4m3) sc = (float)((double)c.scale * c.ks[head] * back);
         if (KIND >= kPaE4m3 && sc < 0x1p-126f) sc = 0x1p-126f;  // (as for single tokens)
         float ref = kPaNone, sum = 0.f;
-        for (int t = begin; t < end; ++t, ++n, ++jt) {
-          const int b = n % SB;
-          const uint32_t tS = tmem + lanes + (SB == 2 ? b * TILE : q * 128) + half * (TILE / 2);
-          ok = wait(B_SREADY + q * SB + b, n / SB);
-          fence_after_sync();
-          // columns that the row sees, as a number of the first ones, and where pages are missing, a bit each
-          const int lim = own - t * TILE;
-          const uint32_t* there = s_there[jt & 7] + half * CH;
-          bool some = lim < TILE / 2;
-#pragma unroll
-          for (int i = 0; i < CH; ++i) some |= there[i] != 0xffffffffu;
-          some = __any_sync(0xffffffffu, some);
-          auto seen = [&](int i) {  // of 32 columns
-            const int l = lim - i * 32;
-            return (l >= 32 ? 0xffffffffu : l <= 0 ? 0u : (1u << l) - 1u) & there[i];
-          };
-          float top = -INFINITY;
 #pragma unroll 1
-          for (int i = 0; i < CH; ++i) {
-            uint32_t v[32];
-            tmem_ld32(tS + i * 32, v);
-            tmem_ld_wait();
-            if (some) {
-              const uint32_t m = seen(i);
+        for (int s = begin * SUBS; s < end * SUBS; ++s, ++n) {  // 64 slots, of which this thread has 32
+          const int b = n & 1, tile = s / SUBS;
+          const uint32_t tS = tmem + lanes + q * 128 + b * 64 + half * 32;
+          ok = wait(B_SREADY + q * SB + b, n >> 1);
+          fence_after_sync();
+          uint32_t v[32];
+          tmem_ld32(tS, v);
+          // columns that the row sees, and that have a page, a bit each
+          const int l = own - s * 64;
+          const uint32_t seen = (l >= 32 ? 0xffffffffu : l <= 0 ? 0u : (1u << l) - 1u) & s_there[(jt + tile - begin) & 7][s % SUBS * 2 + half];
+          tmem_ld_wait();
+          if (__any_sync(0xffffffffu, seen != 0xffffffffu)) {
 #pragma unroll
-              for (int e = 0; e < 32; ++e)
-                if (!(m >> e & 1u)) v[e] = 0xff800000u;
-            }
-            float m4[4] = {-INFINITY, -INFINITY, -INFINITY, top};
-#pragma unroll
-            for (int e = 0; e < 32; e += 2)
-              m4[e / 2 & 3] = fmaxf(m4[e / 2 & 3], fmaxf(__uint_as_float(v[e]), __uint_as_float(v[e + 1])));
-            top = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
+            for (int e = 0; e < 32; ++e)
+              if (!(seen >> e & 1u)) v[e] = 0xff800000u;
           }
-          top *= sc;
+          float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+          for (int e = 0; e < 32; e += 2)
+            m4[e / 2 & 3] = fmaxf(m4[e / 2 & 3], fmaxf(__uint_as_float(v[e]), __uint_as_float(v[e + 1])));
+          float top = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * sc;
           if (pa_any(1 + q, !ok || top > ref + (kOff + kGrow))) {
             s_top[q][half][r] = top;
             if (!ok) s_bad[q] = 1;
@@ -805,9 +784,9 @@ __global__ void __launch_bounds__(kPaThreads, 1)
             const float to = top > ref + (kOff + kGrow) ? fmaxf(ref, top - kOff) : ref, by = pa_exp2(ref - to);
             ref = to;
             sum *= by;
-            if (t > begin && __any_sync(0xffffffffu, by != 1.f)) {
-              // (two S: the products with V of the tile before are seen to end; if they are not, so is the CTA's end)
-              if (SB == 2) wait(B_PVDONE, n - 1);
+            if (s > begin * SUBS && __any_sync(0xffffffffu, by != 1.f)) {
+              // (the products with V of the slots before are seen to end; if they are not, so is the CTA's end)
+              wait(B_PVDONE + q, n - 1);
               fence_after_sync();
 #pragma unroll 1
               for (int i = 0; i < D / 32; ++i) {
@@ -823,36 +802,27 @@ __global__ void __launch_bounds__(kPaThreads, 1)
           }
           const unsigned long long sc2 = pa_pair(sc, sc), ref2 = pa_pair(-ref, -ref);
           unsigned long long s2[2] = {0ull, 0ull};
-#pragma unroll 1
-          for (int k = 0; k < 2 * CH; ++k) {
-            uint32_t v[16], hi[8], lo[8];
-            tmem_ld16(tS + k * 16, v);
-            tmem_ld_wait();
-            if (some) {
-              const uint32_t m = seen(k >> 1) >> (k & 1) * 16;
 #pragma unroll
-              for (int e = 0; e < 16; ++e)
-                if (!(m >> e & 1u)) v[e] = 0xff800000u;
-            }
+          for (int k = 0; k < 2; ++k) {
+            uint32_t hi[8], lo[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-              const float2 x = pa_split(pa_fma2(pa_pair(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1])), sc2, ref2));
+              const float2 x = pa_split(pa_fma2(pa_pair(__uint_as_float(v[k * 16 + 2 * e]), __uint_as_float(v[k * 16 + 2 * e + 1])), sc2, ref2));
               const unsigned long long p = pa_pair(pa_exp2(x.x), pa_exp2(x.y));
               s2[e & 1] = pa_add2(s2[e & 1], p);
               pa_terms(kType, p, hi[e], lo[e]);
             }
             tmem_st8(tS + k * 16, hi);
             tmem_st8(tS + k * 16 + 8, lo);
-            if (k & 1) {
-              tmem_st_wait();
-              fence_before_sync();
-              arrive(B_PREADY + 2 * (q * SB + b) + (k >> 1));
-            }
           }
-          const float2 s = pa_split(pa_add2(s2[0], s2[1]));
-          sum += s.x + s.y;
+          tmem_st_wait();
+          fence_before_sync();
+          arrive(B_PREADY + q * SB + b);
+          const float2 both = pa_split(pa_add2(s2[0], s2[1]));
+          sum += both.x + both.y;
         }
         if (!ok) break;
+        jt += end - begin;
         // the next part's queries while this one's last products run
         more = next_part(w);
         skip();
