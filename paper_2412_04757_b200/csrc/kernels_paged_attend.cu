@@ -224,10 +224,6 @@ __device__ __forceinline__ bool pa_next(PaPlace& w, const PaWork& wk, int heads,
   }
   return pa_part(w, 0);
 }
-// The next tile; false at the run's end.
-__device__ __forceinline__ bool pa_step(PaPlace& w, const PaWork& wk, int heads, int G, int rows) {
-  return ++w.tile < w.end || pa_next(w, wk, heads, G, rows);
-}
 // One warp: the entry of a tile (below the line's total).
 __device__ __forceinline__ int pa_find(const PaWork& wk, int entries, long long tile) {
   const int lane = threadIdx.x & 31;
@@ -434,22 +430,28 @@ __global__ void __launch_bounds__(kPaThreads, 1)
     // A lane finds out about one of the warp's slots, and the others ask it.  (Every lane about those whose rows it loads: 3000 of
     // 9300 cycles a tile.)
     int page, page_next;
+    const int mine = lw * MINE + lane % MINE;
+    const int* pages_row = table + wp.row * table_stride;
     auto ask_page = [&]() {
-      const int slot = wp.tile * TILE + lw * MINE + lane % MINE;
-      const int x = more_p && slot < wp.limit ? table[wp.row * table_stride + paged_nth(c, slot)] : -1;
-      if (more_p) more_p = pa_step(wp, wk, c.Hkv, c.G, ROWS);
+      const int slot = wp.tile * TILE + mine;
+      const int x = more_p && slot < wp.limit ? pages_row[paged_nth(c, slot)] : -1;
+      if (++wp.tile == wp.end && more_p) {
+        more_p = next_part(wp);
+        pages_row = table + wp.row * table_stride;
+      }
       return x;
     };
+    const unsigned char* head_row = pages + wd.head * c.hs;
     long long off = -1;
     uint32_t there = 0;  // slots with a page, of the tile whose rows are asked for
     constexpr int SW = D <= 128 ? 1 : 2;
-    uint32_t scales[SW];  // of a 4-bit row (64 elements: K's and V's in one word)
+    uint32_t scales[SW];  // of a 4-bit row (64 elements: K's and V's in one word); 0 where there is no slot
     auto locate = [&]() {
-      const int slot = wd.tile * TILE + lw * MINE + lane % MINE;
+      const int slot = wd.tile * TILE + mine;
       const bool in = more_d && slot < wd.limit, has = in && (unsigned)page < (unsigned)c.n_pages;
       if (in && !has) paged_status(c, wd.row);
       const int place = slot - paged_nth(c, slot) * c.P;
-      off = has ? (long long)paged_row(c, 0, page, wd.head, place) : -1;
+      off = has ? (unsigned)page * c.ps + (unsigned)place * c.ts : -1;
       if constexpr (KIND == kPaInt4) {
         const size_t word = has ? paged_word(c, layer, page, wd.head, place) : 0;
         const uint32_t* sc = reinterpret_cast<const uint32_t*>(c.sc) + (D == 64 ? word : (word * 2 + of_v) * SW);
@@ -461,30 +463,33 @@ __global__ void __launch_bounds__(kPaThreads, 1)
     uint4 raw[kCopy ? 1 : PASSES][kCopy ? 1 : KC];
     auto ask_rows = [&]() {
       if constexpr (!kCopy) {
+        // (numbers of 4 bits without a slot: a scale of 0 makes zeros of whatever they are, so that those of page 0 will do)
+        const unsigned char* from0 = head_row + ch0 * 16;
 #pragma unroll
         for (int p = 0; p < PASSES; ++p) {
-          const long long o = shfl_ll(off, p * SL + sub);
-          const unsigned char* from = pages + o + ch0 * 16;
+          const long long o = shfl_ll(KIND == kPaInt4 ? max(off, 0ll) : off, p * SL + sub);
+          const uint4* from = reinterpret_cast<const uint4*>(from0 + o);
 #pragma unroll
           for (int k = 0; k < KC; ++k)
-            raw[p][k] = o < 0 ? make_uint4(0u, 0u, 0u, 0u) : *reinterpret_cast<const uint4*>(from + k * CL * 16);
+            raw[p][k] = KIND != kPaInt4 && o < 0 ? make_uint4(0u, 0u, 0u, 0u) : from[k * CL];
         }
       }
     };
-    // where a lane's 16-byte chunk of a tile's row goes; chunks further on and rows of other passes lie at distances that all lanes
-    // share, but for the swizzle's bits
+    // Where chunk i of those behind a lane's first one goes in a row of the tile: the swizzle's bits of the two do not meet (a lane's
+    // first chunk is a multiple of OUT, and those of other lanes lie a multiple of CL * OUT, 4 at least, further on).
     constexpr int OUT = PaChunk<KIND>::kOut;
-    const int row0 = lw * MINE + sub;
-    auto place_of = [&](uint32_t mat, int p, int oc) {
-      return mat + (oc >> 3) * (TILE * 128) + (row0 + p * SL) * 128 + (((oc & 7) ^ (row0 & 7)) << 4);  // (SL is a multiple of 8)
+    const int row0 = lw * MINE + sub, oc0 = ch0 * OUT;
+    const uint32_t lane_at = (oc0 >> 3) * (TILE * 128) + row0 * 128 + (((oc0 & 7) ^ (row0 & 7)) << 4);
+    auto place_of = [&](uint32_t mat, int p, int i) {  // (SL is a multiple of 8)
+      return ((mat + lane_at) ^ ((i & 7) << 4)) + (i >> 3) * (TILE * 128) + p * (SL * 128);
     };
     auto copy_rows = [&](uint32_t mat) {
 #pragma unroll
       for (int p = 0; p < PASSES; ++p) {
         const long long o = shfl_ll(off, p * SL + sub);
-        const unsigned char* from = pages + (o < 0 ? 0 : o + ch0 * 16);
+        const unsigned char* from = head_row + max(o, 0ll) + ch0 * 16;
 #pragma unroll
-        for (int k = 0; k < KC; ++k) pa_request(place_of(mat, p, ch0 + k * CL), from + (o < 0 ? 0 : k * CL * 16), o >= 0);
+        for (int k = 0; k < KC; ++k) pa_request(place_of(mat, p, k * CL), from + k * CL * 16, o >= 0);
       }
       asm volatile("cp.async.commit_group;" ::: "memory");
     };
@@ -514,7 +519,7 @@ __global__ void __launch_bounds__(kPaThreads, 1)
                   v[i] = (uint32_t)h.x | (uint32_t)h.y << 16;
                 }
               }
-              pa_store(place_of(mat, p, (ch0 + k * CL) * OUT + o), make_uint4(v[0], v[1], v[2], v[3]));
+              pa_store(place_of(mat, p, k * CL * OUT + o), make_uint4(v[0], v[1], v[2], v[3]));
             }
           }
         fence_async_smem();
@@ -548,7 +553,10 @@ __global__ void __launch_bounds__(kPaThreads, 1)
         write_rows(mat);
         arrive(full + st);
       }
-      more_d = pa_step(wd, wk, c.Hkv, c.G, ROWS);  // now of the next tile
+      if (++wd.tile == wd.end) {  // now of the next tile
+        more_d = next_part(wd);
+        head_row = pages + wd.head * c.hs;
+      }
       page = page_next;
       page_next = ask_page();
       locate();
