@@ -36,19 +36,23 @@ template <int KIND, int D, int NT>
 struct PdShape {
   static constexpr int kRow = KIND == kPdInt4 ? D / 2 : KIND == kPdE4m3 ? D : 2 * D;  // bytes of a cached row
   static constexpr int kScales = KIND == kPdInt4 ? D / 16 : 0;  // bytes of a slot's scales, K's and V's
+  // 4-bit rows take the instructions of the other kinds for a quarter of 16-bit rows' bytes: twelve warps where their registers
+  // allow it.
+  static constexpr bool kWide = KIND == kPdInt4 && (NT == 2 || D == 256);
   // Blocks of 16 slots in a tile: 8 KB of rows or more, since what a tile costs besides its rows (cursors, page numbers, the
   // reference) took 8-bit rows in tiles of 16 slots to 1.4 times the instructions.
-  static constexpr int kMt = kRow >= 256 ? 1 : kRow == 32 ? 4 : 256 / kRow;
+  static constexpr int kMt = KIND == kPdInt4 ? (D == 256 ? 2 : 4) : kRow >= 256 ? 1 : 256 / kRow;
   static constexpr int kTile = 16 * kMt;                        // slots
   static constexpr int kStage = kTile * (2 * kRow + kScales);   // K rows, V rows, scales
-  static constexpr int kWarps = kRow == 512 ? 4 : 8;            // of a CTA, one CTA an SM
-  static constexpr int kFit = (232448 - 2048) / (kWarps * (kStage + 8 * kTile));
+  static constexpr int kTable = KIND == kPdInt4 ? 5 * D : 0;    // a block's scales, of a warp: 32 + 128 bytes for 32 elements
+  static constexpr int kWarps = kRow == 512 ? 4 : KIND == kPdInt4 && !kWide ? 12 : 8;  // of a CTA, one CTA an SM
+  static constexpr int kFit = ((232448 - (KIND == kPdInt4 ? 1024 : 2048)) / kWarps - kTable) / (kStage + 8 * kTile);
   static constexpr int kStages = kFit > 8 ? 8 : kFit;
   static constexpr int kAhead = kStages - 1;                    // tiles that rows are on their way of
   static constexpr int kPages = 2 * kStages;                    // tiles whose page numbers are known or on their way
   static constexpr int kRing = kStages * kStage;                // of a warp
-  static constexpr int kSmem = kWarps * (kRing + kPages * kTile * 4);
-  static_assert(kStages >= 3, "two tiles on their way and one in use");
+  static constexpr int kSmem = kWarps * (kRing + kPages * kTile * 4 + kTable);
+  static_assert(kStages >= (KIND == kPdInt4 ? 2 : 3), "tiles on their way and one in use");
 };
 
 // Parts of a unit, up to which the warp that hands in the last of them joins them; more of them take a whole CTA, behind a
@@ -90,6 +94,19 @@ template <int KIND>
 __device__ __forceinline__ void pd_mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
   if (KIND == kPdBf16) mma_bf16(c, a, b0, b1);
   else mma_fp16(c, a, b0, b1);
+}
+// d = a b + c, where c is not d's registers: zeros and what a sum begins with need no moves
+__device__ __forceinline__ void pd_mma_from(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, float c0, float c1,
+                                            float c2, float c3) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};\n"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(c0), "f"(c1), "f"(c2), "f"(c3));
+}
+__device__ __forceinline__ void pd_add2(float& a, float& b, float c, float d) {
+  asm("{\n.reg .b64 x, y;\nmov.b64 x, {%0, %1};\nmov.b64 y, {%2, %3};\nadd.rn.f32x2 x, x, y;\nmov.b64 {%0, %1}, x;\n}\n"
+      : "+f"(a), "+f"(b)
+      : "f"(c), "f"(d));
 }
 // Two e4m3 values, the lower or the upper ones of x, as two halves.
 __device__ __forceinline__ uint32_t pd_halves_lo(uint32_t x) {
@@ -182,6 +199,34 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
   const uint32_t lane_s = ring_s + lane_row * Sh::kRow + ((in ^ pd_swizzle<RC>(lane_row)) << 4);
   const long long vk = c.v - c.k;
   auto issue = [&](const PdCursor& u, const int* s_page, int st) {
+    if constexpr (KIND == kPdInt4) {
+      // A lane finds out about the slots `lane`, lane + 32 ..., and asks for their scales; the lanes that ask for their rows ask it.
+      // Slots that are not there have scales of zero, which make zeros of whatever their numbers are: those of page 0 will do, as
+      // will for the new token's slot, which is written over, what its page holds.
+      long long off[(TILE + 31) / 32];
+#pragma unroll
+      for (int j = 0; j < (TILE + 31) / 32; ++j) {
+        if (j * 32 + lane >= TILE) break;
+        const int slot = u.tile * TILE + j * 32 + lane, page = s_page[j * 32 + lane];
+        const bool has = (unsigned)page < (unsigned)c.n_pages;
+        if (!has && slot < u.n) paged_status(c, u.row);
+        const unsigned place = has ? slot - paged_nth(c, slot) * c.P : 0u, at_page = has ? page : 0;
+        off[j] = at_page * c.ps + place * c.ts;
+        const size_t word = (size_t)at_page * (unsigned)(c.Hkv * c.P) + place + paged_word(c, layer, 0, u.head, 0);
+        pd_request<Sh::kScales>(ring_s + st * Sh::kStage + 2 * TILE * Sh::kRow + (j * 32 + lane) * Sh::kScales,
+                                c.sc + word * Sh::kScales, has);
+      }
+      const unsigned char* head = c.k + paged_row(c, layer, 0, u.head, 0) + in * 16;
+      const uint32_t sk = lane_s + st * Sh::kStage;
+#pragma unroll
+      for (int i = 0; i < TILE / kStep; ++i) {
+        const unsigned char* from = head + shfl_ll(off[i * kStep / 32], (i * kStep + lane_row) & 31);
+        const uint32_t to = (sk ^ (pd_swizzle<RC>(i * kStep % 16) << 4)) + i * (kStep * Sh::kRow);
+        cp_async16(to, from, 16);
+        cp_async16(to + TILE * Sh::kRow, from + vk, 16);
+      }
+      return;
+    }
     // the new token's row comes from the caller (in 8 bits: later, when the tile is used), rows without a slot are zeros:
     // their probability of zero meets their values
     const int fresh = a.k && u.n - 1 - u.tile * TILE < TILE ? u.n - 1 - u.tile * TILE : -1;
@@ -214,16 +259,7 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
         }
       }
     }
-    if constexpr (KIND == kPdInt4) {
-#pragma unroll
-      for (int j = lane; j < TILE; j += 32) {
-        const int slot = u.tile * TILE + j, page = s_page[j];
-        const bool there = (unsigned)page < (unsigned)c.n_pages && j != fresh;
-        const size_t word = there ? paged_word(c, layer, page, u.head, slot - paged_nth(c, slot) * c.P) : 0;
-        pd_request<Sh::kScales>(ring_s + st * Sh::kStage + 2 * TILE * Sh::kRow + j * Sh::kScales, c.sc + word * Sh::kScales, there);
-      }
-    }
-    if (KIND != kPdE4m3 && KIND != kPdInt4 && fresh >= 0 && lane < RC) {
+    if (KIND != kPdE4m3 && fresh >= 0 && lane < RC) {
       const int bytes = (unsigned)s_page[fresh] < (unsigned)c.n_pages ? 16 : 0;
       const size_t at = u.row * a.kv_stride + (size_t)u.head * (2 * D) + lane * 16;
       const uint32_t to = ring_s + st * Sh::kStage + fresh * Sh::kRow + ((lane ^ pd_swizzle<RC>(fresh)) << 4);
@@ -234,7 +270,7 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
   // The queries of a unit as the products' columns (head g of each block), and the scales of its KV head.  Behind the requests
   // of rows that fill the memory's queues a load takes 3000 cycles, so where there are registers the next unit's are asked for
   // when the first of its rows are.
-  constexpr bool kEarly = NT * D <= 128;
+  constexpr bool kEarly = NT * D <= 128 && KIND != kPdInt4;
   struct Queries {
     uint32_t b[NT][DT][2];
     float ks, vs;
@@ -440,6 +476,161 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
       }
     }
   };
+  // A tile of 4-bit rows, a block of 16 slots after the other: all of a block's work is little code, which the warps' turns keep in
+  // the instruction caches, and few registers, which lets more warps hide its latencies.
+  unsigned char* table4 = dsm + W * (Sh::kRing + Sh::kPages * TILE * 4) + warp * Sh::kTable;
+  auto int4_tile = [&](int stage_at, int page_at, int slot0) {
+    constexpr int B = D / kI4Block;
+    const unsigned char* s_sc = ring + stage_at * Sh::kStage + 2 * TILE * Sh::kRow;
+    const uint32_t sk = ring_s + stage_at * Sh::kStage, sv = sk + TILE * Sh::kRow;
+    const int row = lane & 15;  // K's and V's matrices: 8 slots, 8 more; 32 elements, 32 more
+    const uint32_t at = row * Sh::kRow + ((lane >> 4 ^ pd_swizzle<RC>(row)) << 4);
+#pragma unroll 1
+    for (int m = 0; m < MT; ++m) {
+      const int left = cu.n - slot0 - m * 16;
+      if (left <= 0) break;
+      // The block's scales: K's as halves [16 slots][B], V's as the factors of i4_values for pairs of slots [8][B]
+      __syncwarp();
+      {
+        const unsigned char* from = s_sc + (m * 16 + (lane >> 1)) * Sh::kScales + (lane & 1) * (B / 2);
+        unsigned short* to = reinterpret_cast<unsigned short*>(table4) + (lane >> 1) * B + (lane & 1) * (B / 2);
+#pragma unroll
+        for (int i = 0; i < B / 2; ++i) to[i] = (unsigned short)(from[i] << 7);
+        I4Scale* tv = reinterpret_cast<I4Scale*>(table4 + 32 * B);
+#pragma unroll
+        for (int i = lane; i < 8 * B; i += 32) {
+          const unsigned char* v = s_sc + (m * 16 + i / B * 2) * Sh::kScales + Sh::kScales / 2 + i % B;
+          tv[i] = i4_factors(v[0] << 7 | v[Sh::kScales] << 23);
+        }
+      }
+      __syncwarp();
+      // S^T = sum over the blocks of 32 elements of scale * (numbers Q^T): a product's accumulator begins with what makes up for the
+      // numbers' offset
+      float x[NT][4];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) x[nt][0] = x[nt][1] = x[nt][2] = x[nt][3] = 0.f;
+#pragma unroll
+      for (int b2 = 0; b2 < B; b2 += 2) {
+        uint32_t w[4];
+        ldsm_x4(w, ((sk + at) ^ (b2 << 4)) + m * 16 * Sh::kRow);
+        const float2 lo = __half22float2(reinterpret_cast<const __half2*>(table4)[(g * B + b2) / 2]);
+        const float2 hi = __half22float2(reinterpret_cast<const __half2*>(table4)[((g + 8) * B + b2) / 2]);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const int b = b2 + j;
+          const uint32_t w0 = w[2 * j], w1 = w[2 * j + 1], u0 = w0 >> 8, u1 = w1 >> 8;
+          const uint32_t f0[4] = {w0 & 0x000f000fu, w1 & 0x000f000fu, w0 & 0x00f000f0u, w1 & 0x00f000f0u};
+          const uint32_t f1[4] = {u0 & 0x000f000fu, u1 & 0x000f000fu, u0 & 0x00f000f0u, u1 & 0x00f000f0u};
+          const float s0 = j ? lo.y : lo.x, s1 = j ? hi.y : hi.x;
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            float z[4];
+            pd_mma_from(z, f0, q.b[nt][2 * b][0], q.b[nt][2 * b][1], bias[nt][b][0], bias[nt][b][1], bias[nt][b][0], bias[nt][b][1]);
+            pd_mma<KIND>(z, f1, q.b[nt][2 * b + 1][0], q.b[nt][2 * b + 1][1]);
+            x[nt][0] = fmaf(s0, z[0], x[nt][0]);
+            x[nt][1] = fmaf(s0, z[1], x[nt][1]);
+            x[nt][2] = fmaf(s1, z[2], x[nt][2]);
+            x[nt][3] = fmaf(s1, z[3], x[nt][3]);
+          }
+        }
+      }
+      // lane: slots g and g + 8 (x[..][0..1], x[..][2..3]), heads 2 q4 and 2 q4 + 1
+      const int* s_page = s_pages + page_at * TILE + m * 16;
+      if (!__all_sync(0xffffffffu, (unsigned)s_page[row] < (unsigned)c.n_pages)) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const bool there = (unsigned)s_page[g + 8 * e] < (unsigned)c.n_pages;
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+            if (!there) x[nt][2 * e] = x[nt][2 * e + 1] = -INFINITY;
+        }
+      }
+      if (c.w) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int page = s_page[g + 8 * e];
+          if ((unsigned)page >= (unsigned)c.n_pages) continue;
+          const int slot = slot0 + m * 16 + g + 8 * e, place = slot - paged_nth(c, slot) * c.P;
+          const size_t word = ((size_t)page * c.Hkv + cu.head) * c.P + place;
+          float* to = wk.logits + word * paged_even(c.G);
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            const int in_group = cu.block * H + nt * 8 + 2 * q4;
+            const float2 y = make_float2(x[nt][2 * e] * sc[nt][0], x[nt][2 * e + 1] * sc[nt][1]);
+            if (in_group < c.G) *reinterpret_cast<float2*>(to + in_group) = y;
+          }
+        }
+      }
+      bool grow = false;
+      float top[NT][2];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          top[nt][e] = fmaxf(x[nt][e], x[nt][e + 2]) * sc[nt][e];
+          grow |= top[nt][e] > ref[nt][e] + (kOff + kGrow);
+        }
+      if (__any_sync(0xffffffffu, grow)) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+#pragma unroll
+            for (int d = 4; d < 32; d <<= 1) top[nt][e] = fmaxf(top[nt][e], __shfl_xor_sync(0xffffffffu, top[nt][e], d));
+            const float to = fmaxf(ref[nt][e], top[nt][e] - kOff), by = pd_exp2(ref[nt][e] - to);
+            ref[nt][e] = to;
+            sum[nt][e] *= by;
+#pragma unroll
+            for (int i = 0; i < DT; ++i) {
+              O[nt][i][e] *= by;
+              O[nt][i][e + 2] *= by;
+            }
+          }
+      }
+      uint32_t term[2][NT][2];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        float p[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          p[e] = pd_exp2(fmaf(x[nt][e], sc[nt][e & 1], -ref[nt][e & 1]));
+          sum[nt][e & 1] += p[e];
+        }
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const uint32_t h = paged_pack(LTRI_TYPE_FP16, p[2 * e], p[2 * e + 1]);
+          const float2 back = paged_unpack(LTRI_TYPE_FP16, h);
+          term[0][nt][e] = pd_transpose(h);
+          term[1][nt][e] = pd_transpose(paged_pack(LTRI_TYPE_FP16, p[2 * e] - back.x, p[2 * e + 1] - back.y));
+        }
+      }
+      // O^T += V^T P^T.  A 16-byte chunk's 8 groups of four neighbours are the 8 rows of a transposed matrix: row g has elements 4g
+      // to 4g + 3 of slots 2 q4 and 2 q4 + 1 (b[0], b[2]: of 32 elements and the next 32) or of slots 8 further (b[1], b[3]).
+      // A block's products are added up by themselves (see below).
+      const I4Scale* tv = reinterpret_cast<const I4Scale*>(table4 + 32 * B);
+#pragma unroll
+      for (int i = 0; i < DT; i += 4) {
+        uint32_t b[4], v4[4][4];
+        ldsm_x4_t(b, ((sv + at) ^ (i << 3)) + m * 16 * Sh::kRow);
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) i4_values(v4[2 * j + e], b[2 * j + e], tv[(q4 + 4 * e) * B + i / 2 + j]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t f[4] = {v4[0][j], v4[2][j], v4[1][j], v4[3][j]};
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            float z[4];
+            pd_mma_from(z, f, term[1][nt][0], term[1][nt][1], 0.f, 0.f, 0.f, 0.f);
+            pd_mma<KIND>(z, f, term[0][nt][0], term[0][nt][1]);
+            pd_add2(O[nt][i + j][0], O[nt][i + j][1], z[0], z[1]);
+            pd_add2(O[nt][i + j][2], O[nt][i + j][3], z[2], z[3]);
+          }
+        }
+      }
+    }
+  };
   // This CTA's part of a unit that other CTAs share is complete in this warp's sums: into the workspace with it.  Of a unit of
   // few parts the last to hand in its own adds up all of them (in their order, so that it does not matter who it is) and
   // returns true; units of many are left to the whole CTA.
@@ -483,6 +674,23 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
   int stage_at = 0, page_at = 0;            // of tile `at`
   int stage_in = 0, page_in = 0, page_rq = 0;  // of the tiles that are requested
   auto next = [](int x, int n) { return x + 1 == n ? 0 : x + 1; };
+  auto ahead = [&](int at) {
+    if (at >= -Sh::kAhead && at + Sh::kAhead < mine) {
+      if (kEarly && ci.tile == 0 && at > -Sh::kAhead && next_at <= at) {
+        next_at = at + Sh::kAhead;
+        load_queries(q_next, ci);
+      }
+      issue(ci, s_pages + page_in * TILE, stage_in);
+      stage_in = next(stage_in, S);
+      page_in = next(page_in, Sh::kPages);
+      pd_advance<TILE>(ci, c, r, wk.blocks);
+    }
+    if (at + 2 * Sh::kAhead < mine) {
+      request_pages(cp, page_rq);
+      page_rq = next(page_rq, Sh::kPages);
+      pd_advance<TILE>(cp, c, r, wk.blocks);
+    }
+  };
 #pragma unroll 1
   for (int at = mine > 0 ? -2 * Sh::kAhead : 0; at < mine; ++at) {
     if (at == -Sh::kAhead) {
@@ -512,6 +720,8 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
       }
       cp_async_wait<S - 2>();
       __syncwarp();
+      // (4-bit rows have few stages: the next tile's are on their way while this one is used)
+      if (KIND == kPdInt4) ahead(at);
       unsigned char* stage = ring + stage_at * Sh::kStage;
       const uint32_t sk = ring_s + stage_at * Sh::kStage, sv = sk + TILE * Sh::kRow;
       const int* s_page = s_pages + page_at * TILE;
@@ -568,6 +778,9 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
           c.pos[paged_word(c, layer, page, cu.head, place)] = a.row_pos ? a.row_pos[cu.row] : cu.n - 1;
         __syncwarp();
       }
+      if constexpr (KIND == kPdInt4) {
+        int4_tile(stage_at, page_at, slot0);
+      } else {
       float x[MT][NT][4];
       // (a tile lies on a multiple of its rows' length: the chunk's bits of an address can be set by xor)
       const uint32_t k_at = sk + (lane & 15) * Sh::kRow + ((lane >> 4 ^ pd_swizzle<RC>(lane & 15)) << 4);
@@ -575,46 +788,7 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
       for (int m = 0; m < MT; ++m) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) x[m][nt][0] = x[m][nt][1] = x[m][nt][2] = x[m][nt][3] = 0.f;
-        if constexpr (KIND == kPdInt4) {
-          // S^T = sum over the blocks of 32 elements of scale * (numbers Q^T): a product's accumulator begins with what makes up
-          // for the numbers' offset
-          const unsigned char* sc_k = stage + 2 * TILE * Sh::kRow + (m * 16 + g) * Sh::kScales;
-          float s_lo[D / kI4Block], s_hi[D / kI4Block];
-#pragma unroll
-          for (int b = 0; b < D / kI4Block; b += 2) {
-            const int at_b = b / 4 * 4, in_b = b % 4;  // (64 elements a row: two scales beside V's, in one word)
-            const float2 lo = i4_scales_f32(*reinterpret_cast<const uint32_t*>(sc_k + at_b), in_b,
-                                            *reinterpret_cast<const uint32_t*>(sc_k + at_b), in_b + 1);
-            const float2 hi = i4_scales_f32(*reinterpret_cast<const uint32_t*>(sc_k + 8 * Sh::kScales + at_b), in_b,
-                                            *reinterpret_cast<const uint32_t*>(sc_k + 8 * Sh::kScales + at_b), in_b + 1);
-            s_lo[b] = lo.x;
-            s_lo[b + 1] = lo.y;
-            s_hi[b] = hi.x;
-            s_hi[b + 1] = hi.y;
-          }
-#pragma unroll
-          for (int b2 = 0; b2 < D / kI4Block; b2 += 2) {
-            uint32_t w[4];
-            ldsm_x4(w, (k_at ^ (b2 << 4)) + m * 16 * Sh::kRow);
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-              const int b = b2 + j;
-              const uint32_t w0 = w[2 * j], w1 = w[2 * j + 1], u0 = w0 >> 8, u1 = w1 >> 8;
-              const uint32_t f0[4] = {w0 & 0x000f000fu, w1 & 0x000f000fu, w0 & 0x00f000f0u, w1 & 0x00f000f0u};
-              const uint32_t f1[4] = {u0 & 0x000f000fu, u1 & 0x000f000fu, u0 & 0x00f000f0u, u1 & 0x00f000f0u};
-#pragma unroll
-              for (int nt = 0; nt < NT; ++nt) {
-                float z[4] = {bias[nt][b][0], bias[nt][b][1], bias[nt][b][0], bias[nt][b][1]};
-                pd_mma<KIND>(z, f0, q.b[nt][2 * b][0], q.b[nt][2 * b][1]);
-                pd_mma<KIND>(z, f1, q.b[nt][2 * b + 1][0], q.b[nt][2 * b + 1][1]);
-                x[m][nt][0] = fmaf(s_lo[b], z[0], x[m][nt][0]);
-                x[m][nt][1] = fmaf(s_lo[b], z[1], x[m][nt][1]);
-                x[m][nt][2] = fmaf(s_hi[b], z[2], x[m][nt][2]);
-                x[m][nt][3] = fmaf(s_hi[b], z[3], x[m][nt][3]);
-              }
-            }
-          }
-        } else if (KIND == kPdE4m3) {
+        if (KIND == kPdE4m3) {
 #pragma unroll
           for (int i = 0; i < DT; i += 2) {
             uint32_t b[4];
@@ -730,11 +904,10 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
       // tensor cores cut off what an accumulator has no bits for, always towards zero: with O as the accumulator small values
       // beside large ones were lost, and outputs over bf16 pages differed twice as much from fp32 arithmetic's.  64 ragged rows in
       // 8 bits 61.5 us, with O 59.8; rows of 256 in 16 bits 35.8 and 34.7; the others no slower.)
-      constexpr bool kPacked = KIND == kPdE4m3 || KIND == kPdInt4;
-      const int v_row = kPacked ? lane & 15 : (lane & 7) + (lane >> 4) * 8;
-      const int v_ch = kPacked ? lane >> 4 : (lane >> 3) & 1;
+      const int v_row = KIND == kPdE4m3 ? lane & 15 : (lane & 7) + (lane >> 4) * 8;
+      const int v_ch = KIND == kPdE4m3 ? lane >> 4 : (lane >> 3) & 1;
       const uint32_t v_at = sv + v_row * Sh::kRow + ((v_ch ^ pd_swizzle<RC>(v_row)) << 4);
-      constexpr int kAtOnce = KIND == kPdInt4 ? 4 : KIND == kPdE4m3 ? 2 : 1;  // slices of 16 elements
+      constexpr int kAtOnce = KIND == kPdE4m3 ? 2 : 1;  // slices of 16 elements
 #pragma unroll
       for (int i = 0; i < DT; i += kAtOnce) {
         float z[kAtOnce][NT][4];
@@ -745,33 +918,10 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
           uint32_t b[4];
-          ldsm_x4_t(b, (v_at ^ (KIND == kPdInt4 ? i << 3 : i << (KIND == kPdE4m3 ? 4 : 5))) + m * 16 * Sh::kRow);
-          uint32_t v4[4][4];
-          if constexpr (KIND == kPdInt4) {
-            // a 16-byte chunk's 8 groups of four neighbours are the 8 rows of a transposed matrix: row g has elements 4g to
-            // 4g + 3 of slots 2 q4 and 2 q4 + 1 (b[0], b[2]: of 32 elements and the next 32) or of slots 8 further (b[1], b[3])
-            const unsigned char* sc_v = stage + 2 * TILE * Sh::kRow + (m * 16 + 2 * q4) * Sh::kScales + Sh::kScales / 2;
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const unsigned char* at_s = sc_v + e * 8 * Sh::kScales;
-              // (64 elements a row: V's two scales are the upper half of their word)
-              const int at_b = D == 64 ? -2 : i / 8 * 4, in_b = D == 64 ? 2 : i / 4 * 2 % 4;
-              const uint32_t s0 = *reinterpret_cast<const uint32_t*>(at_s + at_b);
-              const uint32_t s1 = *reinterpret_cast<const uint32_t*>(at_s + Sh::kScales + at_b);
-#pragma unroll
-              for (int j = 0; j < 2; ++j)
-                i4_values(v4[2 * j + e], b[2 * j + e], i4_factors(i4_scales(s0, in_b + j, s1, in_b + j)));
-            }
-          }
+          ldsm_x4_t(b, (v_at ^ (i << (KIND == kPdE4m3 ? 4 : 5))) + m * 16 * Sh::kRow);
 #pragma unroll
           for (int j = 0; j < kAtOnce; ++j) {
             uint32_t f[4] = {b[0], b[1], b[2], b[3]};
-            if constexpr (KIND == kPdInt4) {  // rows g: an element of b[0] and b[1], rows g + 8: the same of the next 32
-              f[0] = v4[0][j];
-              f[1] = v4[2][j];
-              f[2] = v4[1][j];
-              f[3] = v4[3][j];
-            }
             if (KIND == kPdE4m3) {
               // a 16-byte chunk's 8 pairs of neighbours are the 8 rows of a transposed matrix: row g has elements 2g and 2g + 1
               // of slots 2 q4 and 2 q4 + 1
@@ -794,6 +944,7 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int e = 0; e < 4; ++e) O[nt][i + j][e] += z[j][nt][e];
+      }
       }
       __syncwarp();
       stage_at = next(stage_at, S);
@@ -823,21 +974,7 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
       }
       pd_advance<TILE>(cu, c, r, wk.blocks);
     }
-    if (at >= -Sh::kAhead && at + Sh::kAhead < mine) {
-      if (kEarly && ci.tile == 0 && at > -Sh::kAhead && next_at <= at) {
-        next_at = at + Sh::kAhead;
-        load_queries(q_next, ci);
-      }
-      issue(ci, s_pages + page_in * TILE, stage_in);
-      stage_in = next(stage_in, S);
-      page_in = next(page_in, Sh::kPages);
-      pd_advance<TILE>(ci, c, r, wk.blocks);
-    }
-    if (at + 2 * Sh::kAhead < mine) {
-      request_pages(cp, page_rq);
-      page_rq = next(page_rq, Sh::kPages);
-      pd_advance<TILE>(cp, c, r, wk.blocks);
-    }
+    if (KIND != kPdInt4 || at < 0) ahead(at);
     cp_async_commit();
     const bool begins = at >= 0 && at + 1 < mine && cu.tile == 0;
     if (at == -Sh::kAhead - 1 || (begins && !(kEarly && next_at == at + 1))) load_queries(q, cu);

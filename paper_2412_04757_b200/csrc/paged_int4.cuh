@@ -38,7 +38,7 @@ __device__ __forceinline__ float2 i4_scales_f32(uint32_t a, int lo, uint32_t b, 
 // Numbers to values.  Four bits below an exponent of 2^10 are 1024 + number + 8, or 1024 + 16 (number + 8) where they stand four
 // places higher: a multiply-add takes the offset away and the scale in, exactly (1032 and 1152 times a scale's four significant
 // bits have no more than eleven).
-struct I4Scale {
+struct __align__(16) I4Scale {
   uint32_t s0, c0, s1, c1;
 };
 __device__ __forceinline__ I4Scale i4_factors(uint32_t halves) {
@@ -49,13 +49,20 @@ __device__ __forceinline__ I4Scale i4_factors(uint32_t halves) {
   f.c1 = i4_mul(halves, 0xC880C880u);  // -1152 * 2^-7 = -9
   return f;
 }
+// (x & MASK) | 0x64006400, one instruction
+template <uint32_t MASK>
+__device__ __forceinline__ uint32_t i4_raised(uint32_t x) {
+  uint32_t d;
+  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(d) : "r"(x), "n"(MASK), "r"(0x64006400u));
+  return d;
+}
 // Elements i and i + 4 of the eight in w (of two rows' four each, the same element of both), for i = 0 to 3.
 __device__ __forceinline__ void i4_values(uint32_t (&v)[4], uint32_t w, const I4Scale& f) {
   const uint32_t u = w >> 8;
-  v[0] = i4_fma((w & 0x000f000fu) | 0x64006400u, f.s0, f.c0);
-  v[1] = i4_fma((w & 0x00f000f0u) | 0x64006400u, f.s1, f.c1);
-  v[2] = i4_fma((u & 0x000f000fu) | 0x64006400u, f.s0, f.c0);
-  v[3] = i4_fma((u & 0x00f000f0u) | 0x64006400u, f.s1, f.c1);
+  v[0] = i4_fma(i4_raised<0x000f000fu>(w), f.s0, f.c0);
+  v[1] = i4_fma(i4_raised<0x00f000f0u>(w), f.s1, f.c1);
+  v[2] = i4_fma(i4_raised<0x000f000fu>(u), f.s0, f.c0);
+  v[3] = i4_fma(i4_raised<0x00f000f0u>(u), f.s1, f.c1);
 }
 
 // The scale nearest to x >= 0, ties to even, as its byte (not for NaN).
