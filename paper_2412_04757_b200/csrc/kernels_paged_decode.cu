@@ -44,12 +44,12 @@ struct PdShape {
   static constexpr int kMt = KIND == kPdInt4 ? (D == 256 ? 2 : 4) : kRow >= 256 ? 1 : 256 / kRow;
   static constexpr int kTile = 16 * kMt;                        // slots
   static constexpr int kStage = kTile * (2 * kRow + kScales);   // K rows, V rows, scales
-  static constexpr int kTable = KIND == kPdInt4 ? 5 * D : 0;    // a block's scales, of a warp: 32 + 128 bytes for 32 elements
+  static constexpr int kTable = KIND == kPdInt4 ? 8 * D : 0;    // factors of V's values of 32 slots, of a warp: 256 bytes for 32 elements
   static constexpr int kWarps = kRow == 512 ? 4 : KIND == kPdInt4 && !kWide ? 12 : 8;  // of a CTA, one CTA an SM
-  static constexpr int kFit = ((232448 - (KIND == kPdInt4 ? 1024 : 2048)) / kWarps - kTable) / (kStage + 8 * kTile);
+  static constexpr int kFit = ((232448 - (KIND == kPdInt4 ? 1024 : 2048)) / kWarps - kTable + (KIND == kPdInt4 ? 4 * kTile : 0)) / (kStage + 8 * kTile);
   static constexpr int kStages = kFit > 8 ? 8 : kFit;
   static constexpr int kAhead = kStages - 1;                    // tiles that rows are on their way of
-  static constexpr int kPages = 2 * kStages;                    // tiles whose page numbers are known or on their way
+  static constexpr int kPages = 2 * kStages - (KIND == kPdInt4 ? 1 : 0);  // tiles whose page numbers are known or on their way
   static constexpr int kRing = kStages * kStage;                // of a warp
   static constexpr int kSmem = kWarps * (kRing + kPages * kTile * 4 + kTable);
   static_assert(kStages >= (KIND == kPdInt4 ? 2 : 3), "tiles on their way and one in use");
@@ -476,8 +476,8 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
       }
     }
   };
-  // A tile of 4-bit rows, a block of 16 slots after the other: all of a block's work is little code, which the warps' turns keep in
-  // the instruction caches, and few registers, which lets more warps hide its latencies.
+  // A tile of 4-bit rows, 32 slots after the other: all of their work is little code, which the warps' turns keep in the instruction
+  // caches, and few registers, which lets more warps hide its latencies.  (16 slots at a time: 16 rows of 24576 slots of 128 145 us.)
   unsigned char* table4 = dsm + W * (Sh::kRing + Sh::kPages * TILE * 4) + warp * Sh::kTable;
   auto int4_tile = [&](int stage_at, int page_at, int slot0) {
     constexpr int B = D / kI4Block;
@@ -485,81 +485,82 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
     const uint32_t sk = ring_s + stage_at * Sh::kStage, sv = sk + TILE * Sh::kRow;
     const int row = lane & 15;  // K's and V's matrices: 8 slots, 8 more; 32 elements, 32 more
     const uint32_t at = row * Sh::kRow + ((lane >> 4 ^ pd_swizzle<RC>(row)) << 4);
+    I4Scale* tv = reinterpret_cast<I4Scale*>(table4);  // [B][16 pairs of slots]
 #pragma unroll 1
-    for (int m = 0; m < MT; ++m) {
-      const int left = cu.n - slot0 - m * 16;
-      if (left <= 0) break;
-      // The block's scales: K's as halves [16 slots][B], V's as the factors of i4_values for pairs of slots [8][B]
+    for (int m0 = 0; m0 < MT; m0 += 2) {
+      if (slot0 + m0 * 16 >= cu.n) break;
       __syncwarp();
-      {
-        const unsigned char* from = s_sc + (m * 16 + (lane >> 1)) * Sh::kScales + (lane & 1) * (B / 2);
-        unsigned short* to = reinterpret_cast<unsigned short*>(table4) + (lane >> 1) * B + (lane & 1) * (B / 2);
 #pragma unroll
-        for (int i = 0; i < B / 2; ++i) to[i] = (unsigned short)(from[i] << 7);
-        I4Scale* tv = reinterpret_cast<I4Scale*>(table4 + 32 * B);
-#pragma unroll
-        for (int i = lane; i < 8 * B; i += 32) {
-          const unsigned char* v = s_sc + (m * 16 + i / B * 2) * Sh::kScales + Sh::kScales / 2 + i % B;
-          tv[i] = i4_factors(v[0] << 7 | v[Sh::kScales] << 23);
-        }
+      for (int i = lane; i < 16 * B; i += 32) {
+        const unsigned char* v = s_sc + (m0 * 16 + i % 16 * 2) * Sh::kScales + Sh::kScales / 2 + i / 16;
+        tv[i] = i4_factors(v[0] << 7 | v[Sh::kScales] << 23);
       }
-      __syncwarp();
       // S^T = sum over the blocks of 32 elements of scale * (numbers Q^T): a product's accumulator begins with what makes up for the
       // numbers' offset
-      float x[NT][4];
+      float x[2][NT][4];
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) x[nt][0] = x[nt][1] = x[nt][2] = x[nt][3] = 0.f;
+      for (int m = 0; m < 2; ++m) {
 #pragma unroll
-      for (int b2 = 0; b2 < B; b2 += 2) {
-        uint32_t w[4];
-        ldsm_x4(w, ((sk + at) ^ (b2 << 4)) + m * 16 * Sh::kRow);
-        const float2 lo = __half22float2(reinterpret_cast<const __half2*>(table4)[(g * B + b2) / 2]);
-        const float2 hi = __half22float2(reinterpret_cast<const __half2*>(table4)[((g + 8) * B + b2) / 2]);
+        for (int nt = 0; nt < NT; ++nt) x[m][nt][0] = x[m][nt][1] = x[m][nt][2] = x[m][nt][3] = 0.f;
+        const unsigned char* sc_k = s_sc + ((m0 + m) * 16 + g) * Sh::kScales;
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const int b = b2 + j;
-          const uint32_t w0 = w[2 * j], w1 = w[2 * j + 1], u0 = w0 >> 8, u1 = w1 >> 8;
-          const uint32_t f0[4] = {w0 & 0x000f000fu, w1 & 0x000f000fu, w0 & 0x00f000f0u, w1 & 0x00f000f0u};
-          const uint32_t f1[4] = {u0 & 0x000f000fu, u1 & 0x000f000fu, u0 & 0x00f000f0u, u1 & 0x00f000f0u};
-          const float s0 = j ? lo.y : lo.x, s1 = j ? hi.y : hi.x;
+        for (int b2 = 0; b2 < B; b2 += 2) {
+          uint32_t w[4];
+          ldsm_x4(w, ((sk + at) ^ (b2 << 4)) + (m0 + m) * 16 * Sh::kRow);
+          // (64 elements a row: two scales beside V's, in one word)
+          const uint32_t s_lo = *reinterpret_cast<const uint32_t*>(sc_k + b2 / 4 * 4);
+          const uint32_t s_hi = *reinterpret_cast<const uint32_t*>(sc_k + 8 * Sh::kScales + b2 / 4 * 4);
+          const float2 lo = i4_scales_f32(s_lo, b2 % 4, s_lo, b2 % 4 + 1), hi = i4_scales_f32(s_hi, b2 % 4, s_hi, b2 % 4 + 1);
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            float z[4];
-            pd_mma_from(z, f0, q.b[nt][2 * b][0], q.b[nt][2 * b][1], bias[nt][b][0], bias[nt][b][1], bias[nt][b][0], bias[nt][b][1]);
-            pd_mma<KIND>(z, f1, q.b[nt][2 * b + 1][0], q.b[nt][2 * b + 1][1]);
-            x[nt][0] = fmaf(s0, z[0], x[nt][0]);
-            x[nt][1] = fmaf(s0, z[1], x[nt][1]);
-            x[nt][2] = fmaf(s1, z[2], x[nt][2]);
-            x[nt][3] = fmaf(s1, z[3], x[nt][3]);
+          for (int j = 0; j < 2; ++j) {
+            const int b = b2 + j;
+            const uint32_t w0 = w[2 * j], w1 = w[2 * j + 1], u0 = w0 >> 8, u1 = w1 >> 8;
+            const uint32_t f0[4] = {w0 & 0x000f000fu, w1 & 0x000f000fu, w0 & 0x00f000f0u, w1 & 0x00f000f0u};
+            const uint32_t f1[4] = {u0 & 0x000f000fu, u1 & 0x000f000fu, u0 & 0x00f000f0u, u1 & 0x00f000f0u};
+            const float s0 = j ? lo.y : lo.x, s1 = j ? hi.y : hi.x;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+              float z[4];
+              pd_mma_from(z, f0, q.b[nt][2 * b][0], q.b[nt][2 * b][1], bias[nt][b][0], bias[nt][b][1], bias[nt][b][0], bias[nt][b][1]);
+              pd_mma<KIND>(z, f1, q.b[nt][2 * b + 1][0], q.b[nt][2 * b + 1][1]);
+              x[m][nt][0] = fmaf(s0, z[0], x[m][nt][0]);
+              x[m][nt][1] = fmaf(s0, z[1], x[m][nt][1]);
+              x[m][nt][2] = fmaf(s1, z[2], x[m][nt][2]);
+              x[m][nt][3] = fmaf(s1, z[3], x[m][nt][3]);
+            }
           }
         }
       }
-      // lane: slots g and g + 8 (x[..][0..1], x[..][2..3]), heads 2 q4 and 2 q4 + 1
-      const int* s_page = s_pages + page_at * TILE + m * 16;
-      if (!__all_sync(0xffffffffu, (unsigned)s_page[row] < (unsigned)c.n_pages)) {
+      // lane: slots g and g + 8 of a block (x[..][..][0..1], x[..][..][2..3]), heads 2 q4 and 2 q4 + 1
+      const int* s_page = s_pages + page_at * TILE + m0 * 16;
+      if (!__all_sync(0xffffffffu, (unsigned)s_page[lane] < (unsigned)c.n_pages)) {
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const bool there = (unsigned)s_page[g + 8 * e] < (unsigned)c.n_pages;
+        for (int m = 0; m < 2; ++m)
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-            if (!there) x[nt][2 * e] = x[nt][2 * e + 1] = -INFINITY;
-        }
+          for (int e = 0; e < 2; ++e) {
+            const bool there = (unsigned)s_page[m * 16 + g + 8 * e] < (unsigned)c.n_pages;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+              if (!there) x[m][nt][2 * e] = x[m][nt][2 * e + 1] = -INFINITY;
+          }
       }
       if (c.w) {
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const int page = s_page[g + 8 * e];
-          if ((unsigned)page >= (unsigned)c.n_pages) continue;
-          const int slot = slot0 + m * 16 + g + 8 * e, place = slot - paged_nth(c, slot) * c.P;
-          const size_t word = ((size_t)page * c.Hkv + cu.head) * c.P + place;
-          float* to = wk.logits + word * paged_even(c.G);
+        for (int m = 0; m < 2; ++m)
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            const int in_group = cu.block * H + nt * 8 + 2 * q4;
-            const float2 y = make_float2(x[nt][2 * e] * sc[nt][0], x[nt][2 * e + 1] * sc[nt][1]);
-            if (in_group < c.G) *reinterpret_cast<float2*>(to + in_group) = y;
+          for (int e = 0; e < 2; ++e) {
+            const int page = s_page[m * 16 + g + 8 * e];
+            if ((unsigned)page >= (unsigned)c.n_pages) continue;
+            const int slot = slot0 + (m0 + m) * 16 + g + 8 * e, place = slot - paged_nth(c, slot) * c.P;
+            const size_t word = ((size_t)page * c.Hkv + cu.head) * c.P + place;
+            float* to = wk.logits + word * paged_even(c.G);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+              const int in_group = cu.block * H + nt * 8 + 2 * q4;
+              const float2 y = make_float2(x[m][nt][2 * e] * sc[nt][0], x[m][nt][2 * e + 1] * sc[nt][1]);
+              if (in_group < c.G) *reinterpret_cast<float2*>(to + in_group) = y;
+            }
           }
-        }
       }
       bool grow = false;
       float top[NT][2];
@@ -567,7 +568,7 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          top[nt][e] = fmaxf(x[nt][e], x[nt][e + 2]) * sc[nt][e];
+          top[nt][e] = fmaxf(fmaxf(x[0][nt][e], x[0][nt][e + 2]), fmaxf(x[1][nt][e], x[1][nt][e + 2])) * sc[nt][e];
           grow |= top[nt][e] > ref[nt][e] + (kOff + kGrow);
         }
       if (__any_sync(0xffffffffu, grow)) {
@@ -587,47 +588,58 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
             }
           }
       }
-      uint32_t term[2][NT][2];
+      uint32_t term[2][2][NT][2];
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        float p[4];
+      for (int m = 0; m < 2; ++m)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          p[e] = pd_exp2(fmaf(x[nt][e], sc[nt][e & 1], -ref[nt][e & 1]));
-          sum[nt][e & 1] += p[e];
-        }
+        for (int nt = 0; nt < NT; ++nt) {
+          float p[4];
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const uint32_t h = paged_pack(LTRI_TYPE_FP16, p[2 * e], p[2 * e + 1]);
-          const float2 back = paged_unpack(LTRI_TYPE_FP16, h);
-          term[0][nt][e] = pd_transpose(h);
-          term[1][nt][e] = pd_transpose(paged_pack(LTRI_TYPE_FP16, p[2 * e] - back.x, p[2 * e + 1] - back.y));
-        }
-      }
-      // O^T += V^T P^T.  A 16-byte chunk's 8 groups of four neighbours are the 8 rows of a transposed matrix: row g has elements 4g
-      // to 4g + 3 of slots 2 q4 and 2 q4 + 1 (b[0], b[2]: of 32 elements and the next 32) or of slots 8 further (b[1], b[3]).
-      // A block's products are added up by themselves (see below).
-      const I4Scale* tv = reinterpret_cast<const I4Scale*>(table4 + 32 * B);
+          for (int e = 0; e < 4; ++e) {
+            p[e] = pd_exp2(fmaf(x[m][nt][e], sc[nt][e & 1], -ref[nt][e & 1]));
+            sum[nt][e & 1] += p[e];
+          }
 #pragma unroll
-      for (int i = 0; i < DT; i += 4) {
-        uint32_t b[4], v4[4][4];
-        ldsm_x4_t(b, ((sv + at) ^ (i << 3)) + m * 16 * Sh::kRow);
-#pragma unroll
-        for (int e = 0; e < 2; ++e)
-#pragma unroll
-          for (int j = 0; j < 2; ++j) i4_values(v4[2 * j + e], b[2 * j + e], tv[(q4 + 4 * e) * B + i / 2 + j]);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const uint32_t f[4] = {v4[0][j], v4[2][j], v4[1][j], v4[3][j]};
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            float z[4];
-            pd_mma_from(z, f, term[1][nt][0], term[1][nt][1], 0.f, 0.f, 0.f, 0.f);
-            pd_mma<KIND>(z, f, term[0][nt][0], term[0][nt][1]);
-            pd_add2(O[nt][i + j][0], O[nt][i + j][1], z[0], z[1]);
-            pd_add2(O[nt][i + j][2], O[nt][i + j][3], z[2], z[3]);
+          for (int e = 0; e < 2; ++e) {
+            const uint32_t h = paged_pack(LTRI_TYPE_FP16, p[2 * e], p[2 * e + 1]);
+            const float2 back = paged_unpack(LTRI_TYPE_FP16, h);
+            term[0][m][nt][e] = pd_transpose(h);
+            term[1][m][nt][e] = pd_transpose(paged_pack(LTRI_TYPE_FP16, p[2 * e] - back.x, p[2 * e + 1] - back.y));
           }
         }
+      __syncwarp();
+      // O^T += V^T P^T.  A 16-byte chunk's 8 groups of four neighbours are the 8 rows of a transposed matrix: row g has elements 4g
+      // to 4g + 3 of slots 2 q4 and 2 q4 + 1 (b[0], b[2]: of 32 elements and the next 32) or of slots 8 further (b[1], b[3]).
+      // The products of the 32 slots are added up by themselves (see below).
+#pragma unroll
+      for (int i = 0; i < DT; i += 4) {
+        float z[4][NT][4];
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+          uint32_t b[4], v4[4][4];
+          ldsm_x4_t(b, ((sv + at) ^ (i << 3)) + (m0 + m) * 16 * Sh::kRow);
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) i4_values(v4[2 * j + e], b[2 * j + e], tv[(i / 2 + j) * 16 + m * 8 + e * 4 + q4]);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const uint32_t f[4] = {v4[0][j], v4[2][j], v4[1][j], v4[3][j]};
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+              if (m == 0) pd_mma_from(z[j][nt], f, term[1][m][nt][0], term[1][m][nt][1], 0.f, 0.f, 0.f, 0.f);
+              else pd_mma<KIND>(z[j][nt], f, term[1][m][nt][0], term[1][m][nt][1]);
+              pd_mma<KIND>(z[j][nt], f, term[0][m][nt][0], term[0][m][nt][1]);
+            }
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            pd_add2(O[nt][i + j][0], O[nt][i + j][1], z[j][nt][0], z[j][nt][1]);
+            pd_add2(O[nt][i + j][2], O[nt][i + j][3], z[j][nt][2], z[j][nt][3]);
+          }
       }
     }
   };
