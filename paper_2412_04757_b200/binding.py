@@ -499,7 +499,7 @@ class LtriPaged:
             self.params.workspace_bytes = nbytes
             self._keep = (k_pages, v_pages, k_scale, v_scale, weights, positions, block_scales)
             self.dtype, self._q_shape, self._kv_shape = dtype, (n_q_heads, D), (hkv, D)
-            self._sizes, self._i32 = {}, torch.int32
+            self._sizes, self._token_sizes, self._i32, self._f32 = {}, {}, torch.int32, torch.float32
             self._raw_stream = torch._C._cuda_getCurrentRawStream
             self._index = self.device.index
             if int4:
@@ -543,6 +543,33 @@ class LtriPaged:
             self._sizes[n] = s
         return s
 
+    def _sizes_of_tokens(self, n):
+        """The shapes that go with n tokens of ragged rows: [n][Hkv][head_dim], [n][Hq][head_dim], [n][Hkv], [n][Hq]."""
+        s = self._token_sizes.get(n)
+        if s is None:
+            if len(self._token_sizes) > 4096:
+                self._token_sizes.clear()
+            size = self.torch.Size
+            s = (size((n, *self._kv_shape)), size((n, *self._q_shape)), size((n, self._kv_shape[0])), size((n, self._q_shape[0])))
+            self._token_sizes[n] = s
+        return s
+
+    def _starts(self, t, n):
+        if t.dtype is self._i32 and t.get_device() == self._index and t.dim() == 1 and t.numel() == n + 1 and t.is_contiguous():
+            return t.data_ptr()
+        raise ValueError(f"starts is int32 ({n + 1},), contiguous, on the cache's device")
+
+    def _both(self, k, v, size):
+        """Token stride of k and v, of the same strides (0: dense)."""
+        dtype, index = self.dtype, self._index
+        if (k.dtype is dtype and v.dtype is dtype and k.shape == size and v.shape == size and k.is_contiguous()
+                and v.is_contiguous() and k.get_device() == index and v.get_device() == index):
+            return 0
+        stride = self._heads(k, size, "k")
+        if self._heads(v, size, "v") != stride:
+            raise ValueError("k and v have the same strides")
+        return stride
+
     def _rows(self, table, lens):
         """(rows, table columns, table row stride) of a call, checked."""
         if table.dtype is not self._i32 or table.dim() != 2 or table.get_device() != self._index or (
@@ -577,14 +604,12 @@ class LtriPaged:
         """k, v [tokens][Hkv][head_dim] into the last slots of their rows; starts int32 [rows + 1] on the device, row_pos int32
         [rows], weights float32 [tokens][Hkv].  lens counts the tokens already."""
         n, cols, ts = self._rows(table, lens)
-        tokens, i32 = k.shape[0], self._i32
-        size = (tokens, *self._kv_shape)
-        sp = self._dense(starts, i32, (n + 1,), "starts")
-        stride = self._heads(k, size, "k")
-        if self._heads(v, size, "v") != stride:
-            raise ValueError("k and v have the same strides")
-        rp = None if row_pos is None else self._dense(row_pos, i32, self._sizes_of(n)[0], "row_pos")
-        wp = None if weights is None else self._dense(weights, self.torch.float32, size[:2], "weights")
+        tokens = k.shape[0]
+        sizes = self._sizes_of_tokens(tokens)
+        sp = self._starts(starts, n)
+        stride = self._both(k, v, sizes[0])
+        rp = None if row_pos is None else self._dense(row_pos, self._i32, self._sizes_of(n)[0], "row_pos")
+        wp = None if weights is None else self._dense(weights, self._f32, sizes[2], "weights")
         if tokens == 0:
             return
         s = self._raw_stream(self._index) if stream is None else stream.cuda_stream
@@ -600,17 +625,21 @@ class LtriPaged:
         if k is None and v is None:
             raise ValueError("k, v or both")
         tokens = (v if k is None else k).shape[0]
-        size = (tokens, *self._kv_shape)
-        sp = self._dense(starts, self._i32, (n + 1,), "starts")
-        strides = {self._heads(t, size, name) for t, name in ((k, "k"), (v, "v")) if t is not None}
-        if len(strides) != 1:
-            raise ValueError("k and v have the same strides")
+        size = self._sizes_of_tokens(tokens)[0]
+        sp = self._starts(starts, n)
+        kp = vp = None
+        if k is None:
+            stride, vp = self._heads(v, size, "v"), v.data_ptr()
+        elif v is None:
+            stride, kp = self._heads(k, size, "k"), k.data_ptr()
+        else:
+            stride, kp, vp = self._both(k, v, size), k.data_ptr(), v.data_ptr()
         fp = None if first is None else self._dense(first, self._i32, self._sizes_of(n)[0], "first")
         if tokens == 0:
             return
         s = self._raw_stream(self._index) if stream is None else stream.cuda_stream
-        rc = self.lib.ltri_paged_read(self._h, layer, table.data_ptr(), cols, ts, lens.data_ptr(), n, sp, fp, tokens,
-                                      None if k is None else k.data_ptr(), None if v is None else v.data_ptr(), strides.pop(), s)
+        rc = self.lib.ltri_paged_read(self._h, layer, table.data_ptr(), cols, ts, lens.data_ptr(), n, sp, fp, tokens, kp, vp,
+                                      stride, s)
         if rc:
             self._done(rc, "ltri_paged_read")
 
@@ -649,14 +678,15 @@ class LtriPaged:
         pages, over the rows' slots up to their own.  lse: float32 [tokens][Hq], filled if given.  Returns out."""
         n, cols, ts = self._rows(table, lens)
         tokens = q.shape[0]
-        size = (tokens, *self._q_shape)
-        sp = self._dense(starts, self._i32, (n + 1,), "starts")
+        sizes = self._sizes_of_tokens(tokens)
+        size = sizes[1]
+        sp = self._starts(starts, n)
         qs = self._heads(q, size, "q")
         if out is None:
             with self.torch.cuda.stream(stream):
                 out = self.torch.empty(size, dtype=self.dtype, device=self.device)
         op = self._dense(out, self.dtype, size, "out")
-        lp = None if lse is None else self._dense(lse, self.torch.float32, size[:2], "lse")
+        lp = None if lse is None else self._dense(lse, self._f32, sizes[3], "lse")
         if tokens == 0:
             return out
         s = self._raw_stream(self._index) if stream is None else stream.cuda_stream

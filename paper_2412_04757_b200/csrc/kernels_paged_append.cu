@@ -48,11 +48,12 @@ __global__ void __launch_bounds__(kAppThreads)
     }
     const int in_row = paged_nth(c, (int)slot), page = paged_page(c, r, row, in_row), place = (int)slot - in_row * c.P;
     if (page < 0) continue;
+    const size_t at0 = paged_row(c, layer, page, 0, place), word0 = paged_word(c, layer, page, 0, place);
 #pragma unroll
     for (int u = 0; u < CHUNKS; ++u) {
       const int in = in0 + u * lanes, head = in >> shift, ch = in & (chunks - 1);
       if (in >= per_token) continue;
-      const size_t at = paged_row(c, layer, page, head, place);
+      const size_t at = at0 + head * c.hs;
       if (c.cache_type == LTRI_TYPE_E4M3) {
         *reinterpret_cast<uint2*>(c.k + at + ch * 8) = paged_quantise(c.type, kx[u], c.ks[head]);
         *reinterpret_cast<uint2*>(c.v + at + ch * 8) = paged_quantise(c.type, vx[u], c.vs[head]);
@@ -63,7 +64,7 @@ __global__ void __launch_bounds__(kAppThreads)
         *reinterpret_cast<uint32_t*>(c.k + at + ch * 4) = kn;
         *reinterpret_cast<uint32_t*>(c.v + at + ch * 4) = vn;
         if ((ch & 3) == 0) {
-          unsigned char* to = c.sc + paged_word(c, layer, page, head, place) * (c.D / 16) + ch / 4;
+          unsigned char* to = c.sc + (word0 + (unsigned)head * (unsigned)c.P) * (c.D / 16) + ch / 4;
           to[0] = (unsigned char)ks;
           to[c.D / 32] = (unsigned char)vs;
         }
@@ -72,7 +73,7 @@ __global__ void __launch_bounds__(kAppThreads)
         *reinterpret_cast<uint4*>(c.v + at + ch * 16) = vx[u];
       }
       if (c.w && ch == 0) {
-        const size_t word = paged_word(c, layer, page, head, place);
+        const size_t word = word0 + (unsigned)head * (unsigned)c.P;
         c.w[word] = a.weights ? a.weights[tok * c.Hkv + head] : 0.f;
         c.pos[word] = a.row_pos ? a.row_pos[row] + (int)nth : (int)slot;
       }

@@ -23,7 +23,9 @@ __device__ __forceinline__ uint4 i4_elements(int type, uint32_t w, unsigned scal
     const uint32_t s2 = paged_pack(LTRI_TYPE_BF16, f, f), c2 = paged_pack(LTRI_TYPE_BF16, -136.f * f, -136.f * f);
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(v[i]) : "r"((w >> (4 * i) & 0x000f000fu) | 0x43004300u), "r"(s2), "r"(c2));
+      asm("{\n.reg .b32 t;\nlop3.b32 t, %1, 0x000f000f, %2, 0xEA;\nfma.rn.bf16x2 %0, t, %3, %4;\n}\n"
+          : "=r"(v[i])
+          : "r"(w >> (4 * i)), "r"(0x43004300u), "r"(s2), "r"(c2));
   }
   // v[i]: elements i and i + 4
   return make_uint4(__byte_perm(v[0], v[1], 0x5410), __byte_perm(v[2], v[3], 0x5410), __byte_perm(v[0], v[1], 0x7632),
@@ -74,42 +76,47 @@ __global__ void __launch_bounds__(kRdThreads)
     } else {
       paged_status(c, row);
     }
+    const size_t at0 = page < 0 ? 0 : paged_row(c, layer, page, 0, place);
+    const size_t word0 = page < 0 ? 0 : paged_word(c, layer, page, 0, place);
+    uint4 x[2][CHUNKS];
+    unsigned sc[2][CHUNKS];
+    float f[2][CHUNKS];
 #pragma unroll
-    for (int of_v = 0; of_v < 2; ++of_v) {
-      unsigned char* out = of_v ? a.v : a.k;
-      if (!out) continue;
-      const unsigned char* pages = of_v ? c.v : c.k;
-      const float* scales = of_v ? c.vs : c.ks;
-      uint4 x[CHUNKS];
-      unsigned sc[CHUNKS];
-      float f[CHUNKS];
+    for (int u = 0; u < CHUNKS; ++u) {
+      const int in = in0 + u * lanes, head = in >> shift, ch = in & (chunks - 1);
+      const size_t at = at0 + head * c.hs + ch * BYTES;
+      const unsigned char* scales = c.sc + (word0 + (unsigned)head * (unsigned)c.P) * (c.D / 16) + ch / 4;
 #pragma unroll
-      for (int u = 0; u < CHUNKS; ++u) {
-        const int in = in0 + u * lanes, head = in >> shift, ch = in & (chunks - 1);
-        x[u] = make_uint4(0u, 0u, 0u, 0u);
-        sc[u] = 0u;
-        f[u] = 0.f;
-        if (in >= per_token || page < 0) continue;
-        const unsigned char* from = pages + paged_row(c, layer, page, head, place) + ch * BYTES;
-        if (BYTES == 16) x[u] = __ldcs(reinterpret_cast<const uint4*>(from));
+      for (int of_v = 0; of_v < 2; ++of_v) {
+        x[of_v][u] = make_uint4(0u, 0u, 0u, 0u);
+        sc[of_v][u] = 0u;
+        f[of_v][u] = 0.f;
+        if (in >= per_token || page < 0 || !(of_v ? a.v : a.k)) continue;
+        const unsigned char* from = (of_v ? c.v : c.k) + at;
+        if (BYTES == 16) x[of_v][u] = __ldcs(reinterpret_cast<const uint4*>(from));
         if (BYTES == 8) {
           const uint2 y = __ldcs(reinterpret_cast<const uint2*>(from));
-          x[u].x = y.x;
-          x[u].y = y.y;
-          f[u] = scales[head];
+          x[of_v][u].x = y.x;
+          x[of_v][u].y = y.y;
+          f[of_v][u] = (of_v ? c.vs : c.ks)[head];
         }
         if (BYTES == 4) {
-          x[u].x = __ldcs(reinterpret_cast<const uint32_t*>(from));
-          sc[u] = c.sc[(paged_word(c, layer, page, head, place) * 2 + of_v) * (c.D / kI4Block) + ch / 4];
+          x[of_v][u].x = __ldcs(reinterpret_cast<const uint32_t*>(from));
+          sc[of_v][u] = scales[of_v ? c.D / kI4Block : 0];
         }
       }
+    }
 #pragma unroll
-      for (int u = 0; u < CHUNKS; ++u) {
-        const int in = in0 + u * lanes;
-        if (in >= per_token) continue;
-        uint4 y = x[u];
-        if (BYTES == 8) y = e4m3_elements(c.type, make_uint2(x[u].x, x[u].y), f[u]);
-        if (BYTES == 4) y = i4_elements(c.type, x[u].x, sc[u]);
+    for (int u = 0; u < CHUNKS; ++u) {
+      const int in = in0 + u * lanes;
+      if (in >= per_token) continue;
+#pragma unroll
+      for (int of_v = 0; of_v < 2; ++of_v) {
+        unsigned char* out = of_v ? a.v : a.k;
+        if (!out) continue;
+        uint4 y = x[of_v][u];
+        if (BYTES == 8) y = e4m3_elements(c.type, make_uint2(y.x, y.y), f[of_v][u]);
+        if (BYTES == 4) y = i4_elements(c.type, y.x, sc[of_v][u]);
         __stcs(reinterpret_cast<uint4*>(out + tok * a.stride + in * 16), y);
       }
     }

@@ -65,22 +65,40 @@ __device__ __forceinline__ void i4_values(uint32_t (&v)[4], uint32_t w, const I4
   v[3] = i4_fma(i4_raised<0x00f000f0u>(u), f.s1, f.c1);
 }
 
-// The scale nearest to x >= 0, ties to even, as its byte (not for NaN).
+// The scale nearest to x >= 0, ties to even, as its byte.  (An infinity may have become NaN in products: both are the largest one.)
 __device__ __forceinline__ unsigned i4_scale_byte(float x) {
+  x = fminf(x, 480.f);
   const unsigned u = __float_as_uint(x);
   // below 2^-14 the scales lie 2^-17 apart, as fp32's numbers from 64 to 128 do
   const float s = x < 0x1p-14f ? __fadd_rn(__fadd_rn(x, 96.f), -96.f)
                                : __uint_as_float((u + 0x7ffffu + (u >> 20 & 1u)) & 0xfff00000u);
-  return __half_as_ushort(__float2half_rn(fminf(s, 480.f))) >> 7;
+  return __half_as_ushort(__float2half_rn(s)) >> 7;
+}
+
+__device__ __forceinline__ unsigned long long i4_pair(float a, float b) {
+  unsigned long long x;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(x) : "f"(a), "f"(b));
+  return x;
+}
+// (number + 8 of a value's quotient in the last bits, over 1.5 * 2^23) of a pair
+__device__ __forceinline__ void i4_numbers(uint32_t& a, uint32_t& b, float2 x, float r, float rest) {
+  unsigned long long y;
+  asm("{\n.reg .b64 t;\nmul.rn.f32x2 t, %1, %3;\nfma.rn.f32x2 t, %1, %2, t;\nadd.rn.f32x2 %0, t, %4;\n}\n"
+      : "=l"(y)
+      : "l"(i4_pair(x.x, x.y)), "l"(i4_pair(r, r)), "l"(i4_pair(rest, rest)), "l"(i4_pair(12582920.f, 12582920.f)));
+  asm("mov.b64 {%0, %1}, %2;" : "=r"(a), "=r"(b) : "l"(y));
 }
 
 // Eight elements of `type` by the four lanes of a block (neighbours, all of them here): their numbers, element i in bits 4i,
 // and the block's scale.
+// Quotients are products with a reciprocal in two terms, whose rounding is the quotient's where that is a midpoint: of two numbers,
+// or of two scales (a quotient of up to eleven bits by 7 or by a scale is one, or further from it than fp32's rounding).
+// (With divisions, clamps of every element and masks: 22700 tokens of eight KV heads of 128 40 us.)
 __device__ __forceinline__ uint32_t i4_quantise(int type, const uint4& x, unsigned& scale) {
   const unsigned lanes = 0xfu << (threadIdx.x & 28);
-  const uint32_t in[4] = {x.x, x.y, x.z, x.w};
+  uint4 in = x;
   // magnitudes are ordered as their bits are, NaN above all
-  uint32_t most = __vmaxu2(__vmaxu2(in[0] & 0x7fff7fffu, in[1] & 0x7fff7fffu), __vmaxu2(in[2] & 0x7fff7fffu, in[3] & 0x7fff7fffu));
+  uint32_t most = __vmaxu2(__vmaxu2(in.x & 0x7fff7fffu, in.y & 0x7fff7fffu), __vmaxu2(in.z & 0x7fff7fffu, in.w & 0x7fff7fffu));
   most = __vmaxu2(most, __shfl_xor_sync(lanes, most, 1));
   most = __vmaxu2(most, __shfl_xor_sync(lanes, most, 2));
   most = max(most & 0xffffu, most >> 16);
@@ -88,23 +106,33 @@ __device__ __forceinline__ uint32_t i4_quantise(int type, const uint4& x, unsign
     scale = kI4Nan;
     return 0x88888888u;
   }
-  // (a quotient of up to eleven bits by 7 is a midpoint of two scales, or further from it than fp32's rounding)
-  scale = i4_scale_byte(__fdiv_rn(paged_unpack(type, most).x, 7.f));
+  constexpr float kR7 = 1.f / 7.f, kRest7 = (float)(1.0 / 7.0 - (double)kR7);
+  const float m = paged_unpack(type, most).x;
+  scale = i4_scale_byte(__fmaf_rn(m, kR7, m * kRest7));
   const float s = __half2float(__ushort_as_half((unsigned short)(scale << 7)));
   if (s == 0.f) return 0x88888888u;
-  // 1 / s in two terms, so that the product with an element is its quotient rounded once: exact where that is a midpoint
-  const float r = __frcp_rn(s), rest = __fmaf_rn(-s, r, 1.f) * r, most_s = 7.f * s;
-  uint32_t got = 0u;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    float2 f = paged_unpack(type, in[i]);
-    f.x = fminf(fmaxf(f.x, -most_s), most_s);
-    f.y = fminf(fmaxf(f.y, -most_s), most_s);
-    const float a = __fmaf_rn(f.x, r, f.x * rest), b = __fmaf_rn(f.y, r, f.y * rest);
-    // the last bits of 1.5 * 2^23 + 8 + y are the whole number nearest to y, and 8
-    got |= (__float_as_uint(a + 12582920.f) & 15u) << (8 * i) | (__float_as_uint(b + 12582920.f) & 15u) << (8 * i + 4);
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(s));
+  const float rest = __fmaf_rn(-s, r, 1.f) * r;
+  if (m >= 7.5f * s) {
+    // beyond the largest scale, or between the smallest ones: elements are clamped (elsewhere m / s is 7.4375 at most)
+    const float lim = 7.f * s;
+    auto clamped = [&](uint32_t y) {
+      const float2 f = paged_unpack(type, y);
+      return paged_pack(type, fminf(fmaxf(f.x, -lim), lim), fminf(fmaxf(f.y, -lim), lim));
+    };
+    in = make_uint4(clamped(in.x), clamped(in.y), clamped(in.z), clamped(in.w));
   }
-  return got;
+  uint32_t n[8];
+  i4_numbers(n[0], n[1], paged_unpack(type, in.x), r, rest);
+  i4_numbers(n[2], n[3], paged_unpack(type, in.y), r, rest);
+  i4_numbers(n[4], n[5], paged_unpack(type, in.z), r, rest);
+  i4_numbers(n[6], n[7], paged_unpack(type, in.w), r, rest);
+  // their sum at distances of four bits, less what stands in front of the numbers
+  uint32_t got = n[7];
+#pragma unroll
+  for (int i = 6; i >= 0; --i) got = got * 16u + n[i];
+  return got - 0x4b400000u * 0x11111111u;
 }
 #endif
 
