@@ -10,7 +10,9 @@ namespace ltri {
 
 constexpr int kAppThreads = 256;
 
-template <int CHUNKS>
+// INT4: the rows' type where the pages hold 4 bits, else -1.  (With the type looked at as the kernel runs, as over other pages whose
+// rows take few instructions: 40 us for those tokens over 4-bit pages, 37 so.)
+template <int CHUNKS, int INT4>
 __global__ void __launch_bounds__(kAppThreads)
     k_paged_append(PagedCache c, PagedRows r, int layer, PagedAppend a, int lanes, int parts) {
   chain_wait();
@@ -54,13 +56,13 @@ __global__ void __launch_bounds__(kAppThreads)
       const int in = in0 + u * lanes, head = in >> shift, ch = in & (chunks - 1);
       if (in >= per_token) continue;
       const size_t at = at0 + head * c.hs;
-      if (c.cache_type == LTRI_TYPE_E4M3) {
+      if (INT4 < 0 && c.cache_type == LTRI_TYPE_E4M3) {
         *reinterpret_cast<uint2*>(c.k + at + ch * 8) = paged_quantise(c.type, kx[u], c.ks[head]);
         *reinterpret_cast<uint2*>(c.v + at + ch * 8) = paged_quantise(c.type, vx[u], c.vs[head]);
-      } else if (c.cache_type == LTRI_TYPE_INT4) {
+      } else if (INT4 >= 0) {
         // (the four lanes of a block have the same token and head, and are all here: rows are multiples of four chunks)
         unsigned ks, vs;
-        const uint32_t kn = i4_quantise(c.type, kx[u], ks), vn = i4_quantise(c.type, vx[u], vs);
+        const uint32_t kn = i4_quantise(INT4, kx[u], ks), vn = i4_quantise(INT4, vx[u], vs);
         *reinterpret_cast<uint32_t*>(c.k + at + ch * 4) = kn;
         *reinterpret_cast<uint32_t*>(c.v + at + ch * 4) = vn;
         if ((ch & 3) == 0) {
@@ -89,7 +91,9 @@ cudaError_t launch_paged_append(const PagedCache& c, const PagedRows& r, int lay
   const int chunks = few ? 1 : 4, parts = (per_token + chunks * lanes - 1) / (chunks * lanes);
   const long long per_block = (kAppThreads / 32) * (32 / lanes), blocks = (a.n_tokens * parts + per_block - 1) / per_block;
   const int grid = (int)(blocks < c.sms * 16ll ? blocks : c.sms * 16ll);
-  const auto kernel = few ? k_paged_append<1> : k_paged_append<4>;
+  const auto kernel = c.cache_type != LTRI_TYPE_INT4 ? (few ? k_paged_append<1, -1> : k_paged_append<4, -1>)
+                      : c.type == LTRI_TYPE_BF16 ? (few ? k_paged_append<1, LTRI_TYPE_BF16> : k_paged_append<4, LTRI_TYPE_BF16>)
+                                                 : (few ? k_paged_append<1, LTRI_TYPE_FP16> : k_paged_append<4, LTRI_TYPE_FP16>);
   return launch_chained(kernel, dim3(grid), dim3(kAppThreads), 0, s, c, r, layer, a, lanes, parts);
 }
 

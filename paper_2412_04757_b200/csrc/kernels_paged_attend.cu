@@ -7,8 +7,9 @@
 //
 // Bound: the tensor cores where there are many tokens (two products of 2 D flops a pair of token and slot), so both run on
 // tcgen05.mma: S = Q K^T from shared memory, O += P V with P in TMEM.  P enters as two 16-bit terms, the second what the first has
-// left over: the outputs then carry the rounding of their type once, and the tensor pipe has three products to do instead of
-// two.  Rows of 8 and 4 bits become halves on their way into shared memory, exactly; queries over them become halves too, each row
+// left over, so that the outputs carry the rounding of their type once; for bf16 outputs of products in halves as one, whose
+// 2^-11 is an eighth of the outputs' own half step.  (With two of them there too the tensor pipe has three products to do instead
+// of two: 512 tokens over 24576 slots 307 us, 263 so.)  Rows of 8 and 4 bits become halves on their way into shared memory, exactly; queries over them become halves too, each row
 // scaled by a power of two.  With few tokens it is the cache's bytes and the CTAs' latency.
 //
 // Work: units are (row, KV head, block of query rows), as long as the tiles of slots that their last token sees.  A small kernel
@@ -259,6 +260,11 @@ __device__ __forceinline__ unsigned long long pa_add2(unsigned long long a, unsi
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
   return d;
 }
+// A pair of fp32 values as `type`.
+__device__ __forceinline__ uint32_t pa_term(int type, unsigned long long p) {
+  const float2 f = pa_split(p);
+  return paged_pack(type, f.x, f.y);
+}
 // Two terms of `type` that add up to a pair of fp32 values.
 __device__ __forceinline__ void pa_terms(int type, unsigned long long p, uint32_t& hi, uint32_t& lo) {
   const float2 f = pa_split(p);
@@ -329,7 +335,7 @@ __device__ __forceinline__ float pa_v_scale(const PagedCache& c, int head) {
   return KIND == kPaInt4 ? kI4Back : KIND == kPaE4m3 ? c.vs[head] : 1.f;
 }
 
-template <int KIND, int D>
+template <int KIND, int D, int TERMS>
 __global__ void __launch_bounds__(kPaThreads, 1)
     k_paged_attend(PagedCache c, int layer, const int* table, long long table_stride, PagedQueries a, PaWork wk) {
   using Sh = PaShape<KIND, D>;
@@ -592,14 +598,14 @@ __global__ void __launch_bounds__(kPaThreads, 1)
         }
         mma_commit(s_bars + 8 * B_SREADY + 8 * b);
       };
-      // P of 16 slots: 8 columns of first terms, 8 of second ones
+      // P of 16 slots: 8 columns of first terms, 8 of second ones, if there are any
       auto issue_pv = [&](int b, int st, int sub, bool acc) {
         const uint32_t pa = tS + b * 64;
         const uint64_t db = dV + (uint32_t)(st * (2 * Sh::kMat >> 4) + sub * (64 * 128 >> 4));
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          mma_ts(tO, pa + i * 16 + 8, db + (i * 16 * 128 >> 4), idesc_pv, acc || i > 0);
-          mma_ts(tO, pa + i * 16, db + (i * 16 * 128 >> 4), idesc_pv, true);
+          if (TERMS == 2) mma_ts(tO, pa + i * 16 + 8, db + (i * 16 * 128 >> 4), idesc_pv, acc || i > 0);
+          mma_ts(tO, pa + i * 16, db + (i * 16 * 128 >> 4), idesc_pv, TERMS == 2 || acc || i > 0);
         }
       };
       auto wait_at = [&](uint32_t at, uint32_t parity) { return pa_wait(at, parity, abortp); };
@@ -818,10 +824,11 @@ __global__ void __launch_bounds__(kPaThreads, 1)
               const float2 x = pa_split(pa_fma2(pa_pair(__uint_as_float(v[k * 16 + 2 * e]), __uint_as_float(v[k * 16 + 2 * e + 1])), sc2, ref2));
               const unsigned long long p = pa_pair(pa_exp2(x.x), pa_exp2(x.y));
               s2[e & 1] = pa_add2(s2[e & 1], p);
-              pa_terms(kType, p, hi[e], lo[e]);
+              if (TERMS == 2) pa_terms(kType, p, hi[e], lo[e]);
+              else hi[e] = pa_term(kType, p);
             }
             tmem_st8(tS + k * 16, hi);
-            tmem_st8(tS + k * 16 + 8, lo);
+            if (TERMS == 2) tmem_st8(tS + k * 16 + 8, lo);
           }
           tmem_st_wait();
           fence_before_sync();
@@ -929,9 +936,14 @@ __global__ void __launch_bounds__(128) k_paged_attend_join(PagedCache c, PagedQu
 
 namespace {
 
+// Terms of the probabilities: one where the outputs have fewer bits than it, by three.
+template <int KIND>
+constexpr int one_term() { return KIND >= kPaE4m3 ? 1 : 2; }
+
 template <int KIND, int D>
 cudaError_t prepare_one() {
-  return allow_smem(k_paged_attend<KIND, D>, PaShape<KIND, D>::kSmem);
+  return first_error(allow_smem(k_paged_attend<KIND, D, 2>, PaShape<KIND, D>::kSmem),
+                     allow_smem(k_paged_attend<KIND, D, one_term<KIND>()>, PaShape<KIND, D>::kSmem));
 }
 template <int KIND>
 cudaError_t prepare_kind() {
@@ -944,7 +956,8 @@ cudaError_t launch_one(const PagedCache& c, const PagedRows& r, int layer, const
   cudaError_t e = launch_chained(k_paged_attend_plan, dim3(1), dim3(kPlThreads), 0, s, c, r, a.starts, a.n_tokens, wk, Sh::kRows,
                                  Sh::kTile);
   if (e != cudaSuccess) return e;
-  e = launch_chained(k_paged_attend<KIND, D>, dim3(c.sms), dim3(kPaThreads), Sh::kSmem, s, c, layer, r.table, r.table_stride, a, wk);
+  const auto kernel = c.type == LTRI_TYPE_BF16 ? k_paged_attend<KIND, D, one_term<KIND>()> : k_paged_attend<KIND, D, 2>;
+  e = launch_chained(kernel, dim3(c.sms), dim3(kPaThreads), Sh::kSmem, s, c, layer, r.table, r.table_stride, a, wk);
   if (e != cudaSuccess) return e;
   return launch_chained(k_paged_attend_join<KIND, D>, dim3(c.sms, Sh::kQt, D / 32), dim3(128), 0, s, c, a, wk, c.sms);
 }
