@@ -283,6 +283,41 @@ __device__ __forceinline__ bool pa_any(int id, bool so) {
       : "memory");
   return any != 0;
 }
+// TMEM in the layout of mma.sync's accumulators: a warp has 16 rows, its lane t rows t / 4 and t / 4 + 8; of every eight columns
+// t % 4 * 2 and the next one (r[4 i], r[4 i + 1]; r[4 i + 2], r[4 i + 3]), of every four columns of pairs t % 4 (r[2 i]; r[2 i + 1]).
+__device__ __forceinline__ void pa_ld64(uint32_t taddr, uint32_t (&r)[32]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.16x256b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]),
+        "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]),
+        "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void pa_ld32(uint32_t taddr, uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void pa_st32(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile("tcgen05.st.sync.aligned.16x256b.x4.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, "
+      "%14, %15, %16};" ::"r"(taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
+      "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
+__device__ __forceinline__ void pa_st_pairs(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile("tcgen05.st.sync.aligned.16x128b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, "
+      "%14, %15, %16};" ::"r"(taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
+      "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
 // A bulk of 16 bytes on its way into shared memory, or zeros.
 __device__ __forceinline__ void pa_request(uint32_t to, const void* from, bool there) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(there ? 16 : 0) : "memory");
@@ -357,10 +392,9 @@ __global__ void __launch_bounds__(kPaThreads, 1)
   // by tile: slots that have a page, a bit each.  (Eight tiles: when the K of tile j is written, that of j - S has met its
   // queries, which takes that the softmax of j - S - 1 and those in front of it have ended.)
   __shared__ __align__(16) uint32_t s_there[8][4];
-  // of a tile of queries: rows' largest logits of each half of the columns, and their sums
-  __shared__ float s_top[QT][2][128], s_sum[QT][2][128];
-  __shared__ uint32_t s_most[QT][2][128];  // and their queries' largest elements
-  __shared__ int s_bad[QT];
+  // of a tile of queries' rows: references and sums, what their queries were divided by, and the largest elements of those' halves
+  __shared__ float s_ref[QT][128], s_sum[QT][128], s_back[QT][128];
+  __shared__ uint32_t s_most[QT][2][128];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t sbase = (smem_addr(smem_raw) + 1023u) & ~1023u, sQ = sbase, sKV = sbase + QT * Sh::kQBytes;
   auto bar = [&](int i) { return smem_addr(&bars[i]); };
@@ -380,7 +414,6 @@ __global__ void __launch_bounds__(kPaThreads, 1)
       mbar_init(bar(B_VEMPTY + i), QT);
     }
     for (int q = 0; q < QT; ++q) {
-      s_bad[q] = 0;
       mbar_init(bar(B_QFULL + q), 8);
       mbar_init(bar(B_OFREE + q), 8);
       mbar_init(bar(B_ODONE + q), 1);
@@ -598,14 +631,14 @@ __global__ void __launch_bounds__(kPaThreads, 1)
         }
         mma_commit(s_bars + 8 * B_SREADY + 8 * b);
       };
-      // P of 16 slots: 8 columns of first terms, 8 of second ones, if there are any
+      // P: 32 columns of first terms, 32 of second ones, if there are any
       auto issue_pv = [&](int b, int st, int sub, bool acc) {
         const uint32_t pa = tS + b * 64;
         const uint64_t db = dV + (uint32_t)(st * (2 * Sh::kMat >> 4) + sub * (64 * 128 >> 4));
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          if (TERMS == 2) mma_ts(tO, pa + i * 16 + 8, db + (i * 16 * 128 >> 4), idesc_pv, acc || i > 0);
-          mma_ts(tO, pa + i * 16, db + (i * 16 * 128 >> 4), idesc_pv, TERMS == 2 || acc || i > 0);
+          if (TERMS == 2) mma_ts(tO, pa + 32 + i * 8, db + (i * 16 * 128 >> 4), idesc_pv, acc || i > 0);
+          mma_ts(tO, pa + i * 8, db + (i * 16 * 128 >> 4), idesc_pv, TERMS == 2 || acc || i > 0);
         }
       };
       auto wait_at = [&](uint32_t at, uint32_t parity) { return pa_wait(at, parity, abortp); };
@@ -678,16 +711,16 @@ __global__ void __launch_bounds__(kPaThreads, 1)
     __syncwarp();
   } else {
     // ------------------------------------------------------------------ softmax, queries and outputs
-    // Two threads a row, each with half of S's columns and of O's.  Every decision is one of all 256 threads of a tile of queries,
-    // so that they meet at the same barriers.
+    // A warp has 16 rows of S, four lanes each, so that a softmax needs no other warp.  Queries and outputs go by rows of a lane, two
+    // threads each, with half of the elements.  Whatever goes wrong, all 256 threads of a tile of queries meet at the same barriers.
     if (works && warp < 8 * QT) {
       const int q = warp >> 3, half = warp >> 2 & 1, r = (warp & 3) * 32 + lane;
-      const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+      const int row16 = (warp & 3) * 32 + half * 16 + (lane >> 2);
+      const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, lanes16 = lanes + ((uint32_t)(half * 16) << 16);
       const uint32_t tO = tmem + lanes + 256 + q * D + half * (D / 2);
       PaPlace w = s_place;
       int n = 0, unit = 0, jt = 0;  // tiles and parts of this tile of queries; the CTA's tiles
       bool ok = true, more = true;
-      float back = 1.f;
       // the row's queries of part w into shared memory (free: all products with the last ones have been seen to end)
       auto load_queries = [&]() {
         const int rho = w.rho + q * 128 + r;
@@ -704,7 +737,6 @@ __global__ void __launch_bounds__(kPaThreads, 1)
             x[k] = in ? *reinterpret_cast<const uint4*>(from + (half * (D / 16) + g * GROUP + k) * 16) : make_uint4(0u, 0u, 0u, 0u);
         };
         load(0);
-        back = 1.f;
         float u0 = 1.f, u1 = 1.f;
         constexpr bool kHalves = KIND >= kPaE4m3;
         if (kHalves && c.type == LTRI_TYPE_BF16) {
@@ -725,7 +757,7 @@ __global__ void __launch_bounds__(kPaThreads, 1)
           const int up = ex == 0 || ex == 255 ? 0 : 127 + 14 - ex;
           // (2^up may lie outside fp32's range: two factors)
           u0 = __int_as_float((127 + up / 2) << 23), u1 = __int_as_float((127 + up - up / 2) << 23);
-          back = __int_as_float((127 - up / 2) << 23) * __int_as_float((127 - up + up / 2) << 23);
+          if (half == 0) s_back[q][r] = __int_as_float((127 - up / 2) << 23) * __int_as_float((127 - up + up / 2) << 23);
         }
 #pragma unroll 1
         for (int g = 0; g < GROUPS; ++g) {
@@ -758,94 +790,128 @@ __global__ void __launch_bounds__(kPaThreads, 1)
       while (more) {
         const int rho = w.rho + q * 128 + r, head = w.head, begin = w.tile, end = w.end;
         const bool row_ok = rho < w.rows, whole = begin == 0 && end == w.tiles;
-        const int own = (row_ok ? w.base + rho / c.G + 1 : 0) - half * 32;  // slots that the row sees
         const size_t to_row = (size_t)(w.start + rho / c.G) * c.Hq + head * c.G + rho % c.G;
-        float sc = c.scale;
-        if (KIND == kPaInt4) sc = (float)((double)c.scale * back * kI4Back);
-        if (KIND == kPaE4m3) sc = (float)((double)c.scale * c.ks[head] * back);
-        if (KIND >= kPaE4m3 && sc < 0x1p-126f) sc = 0x1p-126f;  // (as for single tokens)
-        float ref = kPaNone, sum = 0.f;
+        pa_any(1 + q, false);  // (s_back is there, and s_sum and s_ref of the part before have been read)
+        // this lane's two rows: slots that they see, logits' factors, references and sums
+        int own[2];
+        unsigned long long sc2[2], ref2[2], sum2[2];
+        float sc[2], ref[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int at = w.rho + q * 128 + row16 + 8 * i;
+          own[i] = at < w.rows ? w.base + at / c.G + 1 : 0;
+          sc[i] = c.scale;
+          if (KIND >= kPaE4m3) {
+            const float back = c.type == LTRI_TYPE_BF16 ? s_back[q][row16 + 8 * i] : 1.f;
+            const float f = (float)((double)c.scale * (KIND == kPaE4m3 ? c.ks[head] : kI4Back) * back);
+            sc[i] = f < 0x1p-126f ? 0x1p-126f : f;  // (as for single tokens)
+          }
+          ref[i] = kPaNone;
+          sc2[i] = pa_pair(sc[i], sc[i]);
+          ref2[i] = pa_pair(-ref[i], -ref[i]);
+          sum2[i] = 0ull;
+        }
 #pragma unroll 1
-        for (int s = begin * SUBS; s < end * SUBS; ++s, ++n) {  // 64 slots, of which this thread has 32
-          const int b = n & 1, tile = s / SUBS;
-          const uint32_t tS = tmem + lanes + q * 128 + b * 64 + half * 32;
-          ok = wait(B_SREADY + q * SB + b, n >> 1);
+        for (int s = begin * SUBS; s < end * SUBS; ++s, ++n) {  // 64 slots
+          const int b = n & 1;
+          const uint32_t tS = tmem + lanes16 + q * 128 + b * 64;
+          ok = ok && __all_sync(0xffffffffu, wait(B_SREADY + q * SB + b, n >> 1));
+          if (!ok) continue;
           fence_after_sync();
           uint32_t v[32];
-          tmem_ld32(tS, v);
-          // columns that the row sees, and that have a page, a bit each
-          const int l = own - s * 64;
-          const uint32_t seen = (l >= 32 ? 0xffffffffu : l <= 0 ? 0u : (1u << l) - 1u) & s_there[(jt + tile - begin) & 7][s % SUBS * 2 + half];
+          pa_ld64(tS, v);
+          // columns that a row sees, and those that have a page, a bit each
+          const uint32_t* there = s_there[(jt + s / SUBS - begin) & 7] + s % SUBS * 2;
+          const uint32_t t0 = there[0], t1 = there[1];
+          const int l0 = own[0] - s * 64, l1 = own[1] - s * 64;
           tmem_ld_wait();
-          if (__any_sync(0xffffffffu, seen != 0xffffffffu)) {
+          if (__any_sync(0xffffffffu, min(l0, l1) < 64 || (t0 & t1) != 0xffffffffu)) {
 #pragma unroll
-            for (int e = 0; e < 32; ++e)
-              if (!(seen >> e & 1u)) v[e] = 0xff800000u;
-          }
-          float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+            for (int i = 0; i < 2; ++i) {
+              const int l = i ? l1 : l0;
 #pragma unroll
-          for (int e = 0; e < 32; e += 2)
-            m4[e / 2 & 3] = fmaxf(m4[e / 2 & 3], fmaxf(__uint_as_float(v[e]), __uint_as_float(v[e + 1])));
-          float top = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * sc;
-          if (pa_any(1 + q, !ok || top > ref + (kOff + kGrow))) {
-            s_top[q][half][r] = top;
-            if (!ok) s_bad[q] = 1;
-            if (pa_any(1 + q, false) || s_bad[q]) {
-              ok = false;
-              break;
+              for (int k = 0; k < 2; ++k) {
+                const int lk = l - k * 32;
+                const uint32_t m = ((lk >= 32 ? 0xffffffffu : lk <= 0 ? 0u : (1u << lk) - 1u) & (k ? t1 : t0)) >> (lane & 3) * 2;
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                  if (!(m >> (e / 2 * 8 + (e & 1)) & 1u)) v[16 * k + e / 2 * 4 + 2 * i + (e & 1)] = 0xff800000u;
+              }
             }
-            top = fmaxf(top, s_top[q][half ^ 1][r]);
-            const float to = top > ref + (kOff + kGrow) ? fmaxf(ref, top - kOff) : ref, by = pa_exp2(ref - to);
-            ref = to;
-            sum *= by;
-            if (s > begin * SUBS && __any_sync(0xffffffffu, by != 1.f)) {
+          }
+          float top[2];
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            float m2[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              m2[e & 1] = fmaxf(m2[e & 1], fmaxf(__uint_as_float(v[4 * e + 2 * i]), __uint_as_float(v[4 * e + 2 * i + 1])));
+            top[i] = fmaxf(m2[0], m2[1]) * sc[i];
+          }
+          if (__any_sync(0xffffffffu, top[0] > ref[0] + (kOff + kGrow) || top[1] > ref[1] + (kOff + kGrow))) {
+            float by[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 1));
+              top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 2));
+              const float to = top[i] > ref[i] + (kOff + kGrow) ? fmaxf(ref[i], top[i] - kOff) : ref[i];
+              by[i] = pa_exp2(ref[i] - to);
+              ref[i] = to;
+              ref2[i] = pa_pair(-to, -to);
+              const float2 x = pa_split(sum2[i]);
+              sum2[i] = pa_pair(x.x * by[i], x.y * by[i]);
+            }
+            if (s > begin * SUBS) {
               // (the products with V of the slots before are seen to end; if they are not, so is the CTA's end)
-              wait(B_PVDONE + q, n - 1);
+              ok = __all_sync(0xffffffffu, wait(B_PVDONE + q, n - 1));
               fence_after_sync();
 #pragma unroll 1
               for (int i = 0; i < D / 32; ++i) {
                 uint32_t o[16];
-                tmem_ld16(tO + i * 16, o);
+                pa_ld32(tmem + lanes16 + 256 + q * D + i * 32, o);
                 tmem_ld_wait();
 #pragma unroll
-                for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * by);
-                tmem_st16(tO + i * 16, o);
+                for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * by[e >> 1 & 1]);
+                pa_st32(tmem + lanes16 + 256 + q * D + i * 32, o);
               }
               tmem_st_wait();
             }
           }
-          const unsigned long long sc2 = pa_pair(sc, sc), ref2 = pa_pair(-ref, -ref);
-          unsigned long long s2[2] = {0ull, 0ull};
+          uint32_t hi[16], lo[16];
 #pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            uint32_t hi[8], lo[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const float2 x = pa_split(pa_fma2(pa_pair(__uint_as_float(v[k * 16 + 2 * e]), __uint_as_float(v[k * 16 + 2 * e + 1])), sc2, ref2));
-              const unsigned long long p = pa_pair(pa_exp2(x.x), pa_exp2(x.y));
-              s2[e & 1] = pa_add2(s2[e & 1], p);
-              if (TERMS == 2) pa_terms(kType, p, hi[e], lo[e]);
-              else hi[e] = pa_term(kType, p);
-            }
-            tmem_st8(tS + k * 16, hi);
-            if (TERMS == 2) tmem_st8(tS + k * 16 + 8, lo);
+          for (int e = 0; e < 16; ++e) {  // columns e / 2 * 8 + ..., of row e & 1
+            const int i = e & 1;
+            const float2 x = pa_split(pa_fma2(pa_pair(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1])), sc2[i], ref2[i]));
+            const unsigned long long p = pa_pair(pa_exp2(x.x), pa_exp2(x.y));
+            sum2[i] = pa_add2(sum2[i], p);
+            if (TERMS == 2) pa_terms(kType, p, hi[e], lo[e]);
+            else hi[e] = pa_term(kType, p);
           }
+          pa_st_pairs(tS, hi);
+          if (TERMS == 2) pa_st_pairs(tS + 32, lo);
           tmem_st_wait();
           fence_before_sync();
           arrive(B_PREADY + q * SB + b);
-          const float2 both = pa_split(pa_add2(s2[0], s2[1]));
-          sum += both.x + both.y;
         }
-        if (!ok) break;
         jt += end - begin;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const float2 x = pa_split(sum2[i]);
+          float all = x.x + x.y;
+          all += __shfl_xor_sync(0xffffffffu, all, 1);
+          all += __shfl_xor_sync(0xffffffffu, all, 2);
+          if ((lane & 3) == 0) {
+            s_sum[q][row16 + 8 * i] = all;
+            s_ref[q][row16 + 8 * i] = ref[i];
+          }
+        }
         // the next part's queries while this one's last products run
         more = next_part(w);
         skip();
         if (more) load_queries();
-        s_sum[q][half][r] = sum;
-        ok = wait(B_ODONE + q, unit);
+        ok = ok && wait(B_ODONE + q, unit);
         if (pa_any(1 + q, !ok)) break;
-        sum = s_sum[q][0][r] + s_sum[q][1][r];
+        const float sum = s_sum[q][r], top = s_ref[q][r];
         fence_after_sync();
         const float by = !whole ? 1.f : sum == 0.f ? 0.f : 1.f / sum, vs = whole ? pa_v_scale<KIND>(c, head) : 1.f;
         float* part = wk.part + (size_t)(2 * blockIdx.x + (begin == 0 ? 1 : 0)) * pa_part_floats<KIND, D>();
@@ -872,8 +938,8 @@ __global__ void __launch_bounds__(kPaThreads, 1)
         arrive(B_OFREE + q);
         if (row_ok && half == 0) {
           if (whole && a.lse)
-            a.lse[to_row] = sum == 0.f ? -INFINITY : (ref + log2f(sum)) * 0.69314718055994531f;
-          if (!whole) *reinterpret_cast<float2*>(part + (size_t)ROWS * D + (q * 128 + r) * 2) = make_float2(ref, sum);
+            a.lse[to_row] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.69314718055994531f;
+          if (!whole) *reinterpret_cast<float2*>(part + (size_t)ROWS * D + (q * 128 + r) * 2) = make_float2(top, sum);
         }
         ++unit;
       }
