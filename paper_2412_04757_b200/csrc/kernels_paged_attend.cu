@@ -283,6 +283,26 @@ __device__ __forceinline__ bool pa_any(int id, bool so) {
       : "memory");
   return any != 0;
 }
+// The products' instructions, for a warp that runs together: one of its lanes issues, and the operands are the warp's.  (A single
+// lane in a branch of its own: MEASURE.)
+__device__ __forceinline__ void pa_mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate) {
+  asm volatile(
+      "{\n.reg .pred p, e;\nsetp.ne.b32 p, %4, 0;\nelect.sync _|e, 0xffffffff;\n"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void pa_mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool accumulate) {
+  asm volatile(
+      "{\n.reg .pred p, e;\nsetp.ne.b32 p, %4, 0;\nelect.sync _|e, 0xffffffff;\n"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void pa_commit(uint32_t bar) {
+  asm volatile(
+      "{\n.reg .pred e;\nelect.sync _|e, 0xffffffff;\n"
+      "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}\n" ::"r"(bar)
+      : "memory");
+}
 // TMEM in the layout of mma.sync's accumulators: a warp has 16 rows, its lane t rows t / 4 and t / 4 + 8; of every eight columns
 // t % 4 * 2 and the next one (r[4 i], r[4 i + 1]; r[4 i + 2], r[4 i + 3]), of every four columns of pairs t % 4 (r[2 i]; r[2 i + 1]).
 __device__ __forceinline__ void pa_ld64(uint32_t taddr, uint32_t (&r)[32]) {
@@ -609,13 +629,13 @@ __global__ void __launch_bounds__(kPaThreads, 1)
     }
   } else if (warp >= kPaIssuer) {
     // ------------------------------------------------------------------ products
-    // A thread for each tile of query rows: S(q) of the next tile of slots follows O(q) += P(q) V of this one, and the other
+    // A warp for each tile of query rows: S(q) of the next tile of slots follows O(q) += P(q) V of this one, and the other
     // tile's products run while this one's softmax does.
-    if (works && warp < kPaIssuer + QT && lane == 0) {
+    if (works && warp < kPaIssuer + QT) {
       constexpr uint32_t kFmt = kType == LTRI_TYPE_BF16 ? 1u : 0u;
       constexpr uint32_t kF = (1u << 4) | (kFmt << 7) | (kFmt << 10) | (8u << 24);  // fp32 sums, both operands' type, M = 128
       constexpr uint32_t idesc_qk = kF | (uint32_t)(64 >> 3) << 17, idesc_pv = kF | 1u << 16 | (uint32_t)(D >> 3) << 17;
-      const int q = warp - kPaIssuer;
+      const int q = __shfl_sync(0xffffffffu, warp, 0) - kPaIssuer;
       const uint64_t dQ = make_desc(sQ + q * Sh::kQBytes, 16, 1024), dK = make_desc(sKV, 16, 1024);
       const uint64_t dV = make_desc(sKV + Sh::kMat, TILE * 128, 1024);
       const uint32_t tS = tmem + q * 128, tO = tmem + 256 + q * D;
@@ -627,9 +647,9 @@ __global__ void __launch_bounds__(kPaThreads, 1)
 #pragma unroll
         for (int ks = 0; ks < D / 16; ++ks) {
           const uint32_t half = ks >> 2, in = (ks & 3) * 32;
-          mma_ss(d, dQ + ((half * 16384 + in) >> 4), db + ((half * (TILE * 128) + in) >> 4), idesc_qk, ks > 0);
+          pa_mma_ss(d, dQ + ((half * 16384 + in) >> 4), db + ((half * (TILE * 128) + in) >> 4), idesc_qk, ks > 0);
         }
-        mma_commit(s_bars + 8 * B_SREADY + 8 * b);
+        pa_commit(s_bars + 8 * B_SREADY + 8 * b);
       };
       // P: 32 columns of first terms, 32 of second ones, if there are any
       auto issue_pv = [&](int b, int st, int sub, bool acc) {
@@ -637,11 +657,11 @@ __global__ void __launch_bounds__(kPaThreads, 1)
         const uint64_t db = dV + (uint32_t)(st * (2 * Sh::kMat >> 4) + sub * (64 * 128 >> 4));
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          if (TERMS == 2) mma_ts(tO, pa + 32 + i * 8, db + (i * 16 * 128 >> 4), idesc_pv, acc || i > 0);
-          mma_ts(tO, pa + i * 8, db + (i * 16 * 128 >> 4), idesc_pv, TERMS == 2 || acc || i > 0);
+          if (TERMS == 2) pa_mma_ts(tO, pa + 32 + i * 8, db + (i * 16 * 128 >> 4), idesc_pv, acc || i > 0);
+          pa_mma_ts(tO, pa + i * 8, db + (i * 16 * 128 >> 4), idesc_pv, TERMS == 2 || acc || i > 0);
         }
       };
-      auto wait_at = [&](uint32_t at, uint32_t parity) { return pa_wait(at, parity, abortp); };
+      auto wait_at = [&](uint32_t at, uint32_t parity) { return __all_sync(0xffffffffu, pa_wait(at, parity, abortp)) != 0; };
       PaPlace w = s_place;
       uint32_t st = 0, turn = 0;           // the stage and its parity
       uint32_t s_turn = 0, unit_turn = 0;  // a bit for each S: the parity of S and P; that of the parts of units
@@ -653,9 +673,9 @@ __global__ void __launch_bounds__(kPaThreads, 1)
           // none of this tile's rows: its leave to the stages alone
           for (; ok && left > 0; --left) {
             ok = wait_at(bars0 + 8 * B_KFULL + 8 * st, turn);
-            mbar_arrive(bars0 + 8 * B_KEMPTY + 8 * st);
+            if (lane == 0) mbar_arrive(bars0 + 8 * B_KEMPTY + 8 * st);
             ok = ok && wait_at(bars0 + 8 * B_VFULL + 8 * st, turn);
-            mbar_arrive(bars0 + 8 * B_VEMPTY + 8 * st);
+            if (lane == 0) mbar_arrive(bars0 + 8 * B_VEMPTY + 8 * st);
             if (++st == S) st = 0, turn ^= 1;
           }
           continue;
@@ -664,7 +684,7 @@ __global__ void __launch_bounds__(kPaThreads, 1)
         if (!ok) break;
         fence_after_sync();
         issue_qk(b, st, 0);
-        if (SUBS == 1) mma_commit(bars0 + 8 * B_KEMPTY + 8 * st);
+        if (SUBS == 1) pa_commit(bars0 + 8 * B_KEMPTY + 8 * st);
         bool first = true;
         int sub = 0;
         left *= SUBS;
@@ -681,7 +701,7 @@ __global__ void __launch_bounds__(kPaThreads, 1)
               fence_after_sync();
             }
             issue_qk(b ^ 1, nst, nsub);
-            if (nsub + 1 == SUBS) mma_commit(bars0 + 8 * B_KEMPTY + 8 * nst);
+            if (nsub + 1 == SUBS) pa_commit(bars0 + 8 * B_KEMPTY + 8 * nst);
           }
           ok = (sub > 0 || wait_at(bars0 + 8 * B_VFULL + 8 * st, turn)) && wait_at(s_bars + 8 * B_PREADY + 8 * b, s_turn >> b & 1);
           // the first product of a part of a unit overwrites O: the one before it must have been read
@@ -689,9 +709,9 @@ __global__ void __launch_bounds__(kPaThreads, 1)
           if (!ok) break;
           fence_after_sync();
           issue_pv(b, st, sub, !first);
-          if (last) mma_commit(bars0 + 8 * B_VEMPTY + 8 * st);
-          mma_commit(q_bars + 8 * B_PVDONE);
-          if (left == 1) mma_commit(q_bars + 8 * B_ODONE);
+          if (last) pa_commit(bars0 + 8 * B_VEMPTY + 8 * st);
+          pa_commit(q_bars + 8 * B_PVDONE);
+          if (left == 1) pa_commit(q_bars + 8 * B_ODONE);
           s_turn ^= 1u << b;
           first = false;
           st = nst;
@@ -703,12 +723,11 @@ __global__ void __launch_bounds__(kPaThreads, 1)
         had = true;
       } while (ok && next_part(w));
       // nothing of this CTA's is under way when it gives its TMEM back
-      mma_commit(bar(B_DRAIN));
+      pa_commit(bar(B_DRAIN));
       const long long t0 = clock64();
       while (!mbar_try_suspend(bar(B_DRAIN), 0, 2000u) && clock64() - t0 < kPaWaitLimit) {
       }
     }
-    __syncwarp();
   } else {
     // ------------------------------------------------------------------ softmax, queries and outputs
     // A warp has 16 rows of S, four lanes each, so that a softmax needs no other warp.  Queries and outputs go by rows of a lane, two
