@@ -9,16 +9,18 @@
 // tcgen05.mma: S = Q K^T from shared memory, O += P V with P in TMEM.  P enters as two 16-bit terms, the second what the first has
 // left over, so that the outputs carry the rounding of their type once; for bf16 outputs of products in halves as one, whose
 // 2^-11 is an eighth of the outputs' own half step.  (With two of them there too the tensor pipe has three products to do instead
-// of two: 512 tokens over 24576 slots 307 us, 263 so.)  Rows of 8 and 4 bits become halves on their way into shared memory, exactly; queries over them become halves too, each row
-// scaled by a power of two.  With few tokens it is the cache's bytes and the CTAs' latency.
+// of two: 512 tokens over 24576 slots 307 us, 263 so, both before the softmax was within a warp.)  Rows of 8 and 4 bits become halves
+// on their way into shared memory, exactly; queries over them become halves too, each row scaled by a power of two.  With few tokens
+// it is the cache's bytes and the CTAs' latency.
 //
 // Work: units are (row, KV head, block of query rows), as long as the tiles of slots that their last token sees.  A small kernel
 // puts all units' tiles into one line, of which every CTA (one per SM) takes an equal run, across units if need be; the partial sums
 // of units that CTAs share are joined by a third kernel, in the order of the line.
 //
-// Roles of a CTA's 28 warps: 0-7 and 8-15 softmax of the two tiles of 128 query rows (two threads a row; they also load the row's
-// queries and write its outputs), 16-23 bring K and V tiles into shared memory, 24 and 25 issue the products.  TMEM: two S of 64
-// columns in turn for each tile of query rows, in whose columns P replaces S, then the two O.  head_dim 256: one tile of query rows.
+// Roles of a CTA's 28 warps: 0-7 and 8-15 softmax of the two tiles of 128 query rows (16 rows a warp, four lanes a row; they also load
+// the queries and write the outputs, two threads a row), 16-19 bring K tiles into shared memory, 20-23 V tiles, 24 and 25 issue the
+// products.  TMEM: two S of 64 columns in turn for each tile of query rows, in whose columns P replaces S, then the two O.  head_dim
+// 256: one tile of query rows.
 #include "paged_int4.cuh"
 #include "tc_util.cuh"
 
@@ -284,7 +286,7 @@ __device__ __forceinline__ bool pa_any(int id, bool so) {
   return any != 0;
 }
 // The products' instructions, for a warp that runs together: one of its lanes issues, and the operands are the warp's.  (A single
-// lane in a branch of its own: MEASURE.)
+// lane in a branch of its own: 512 tokens over 24576 slots take 248 us, 241 so.)
 __device__ __forceinline__ void pa_mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate) {
   asm volatile(
       "{\n.reg .pred p, e;\nsetp.ne.b32 p, %4, 0;\nelect.sync _|e, 0xffffffff;\n"
@@ -343,19 +345,13 @@ __device__ __forceinline__ void pa_request(uint32_t to, const void* from, bool t
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(there ? 16 : 0) : "memory");
 }
 
-// Sixteen bytes of a cached row as 16-bit elements, in the order that the products take them (see pa_element).
+// Sixteen bytes of a cached row as 16-bit elements, in the order that the products take them (see pa_order).
 template <int KIND>
 struct PaChunk {
   static constexpr int kOut = KIND == kPaInt4 ? 4 : KIND == kPaE4m3 ? 2 : 1;  // chunks of 16 bytes
 };
 
-// Which element of each eight stands at place i of a 16-byte chunk: numbers of 4 bits come out of a word in pairs of i and i + 4.
-template <int KIND>
-__device__ __forceinline__ constexpr int pa_element(int i) {
-  return KIND == kPaInt4 ? (i & 1) * 4 + i / 2 : i;
-}
-
-// Eight elements of a dense row in that order.
+// Eight elements of a dense row in that order: numbers of 4 bits come out of a word in pairs of element i and i + 4.
 template <int KIND>
 __device__ __forceinline__ uint4 pa_order(const uint4& x) {
   if (KIND != kPaInt4) return x;

@@ -129,6 +129,21 @@ def test_attend_split_over_ctas(kind, rows, n, m, hq, hkv, dim):
         assert all(torch.equal(x, y) for x, y in zip(first, again))
 
 
+@pytest.mark.parametrize("kind,dim", [("int4-bf16", 64), ("int4-bf16", 128), ("bf16", 128), ("e4m3-fp16", 64), ("int4-fp16", 256)])
+@pytest.mark.parametrize("hq,hkv", [(8, 2), (12, 12), (32, 2)])
+def test_attend_of_few_and_many_tokens_together(kind, dim, hq, hkv):
+    # units of one tile of query rows and of two in turn, whole and in parts, of every number of tiles up to a dozen
+    news = [1, 70, 5, 8, 300, 2, 9, 130, 3, 16, 1, 40, 7]
+    lens = [511, 700, 512, 513, 1200, 640, 641, 1300, 1500, 90, 1409, 600, 769]
+    c = make(kind, lens, hq, hkv, dim, 32, seed=dim + hq)
+    c.fill()
+    lp = c.handle(max_tokens=sum(news))
+    q = c.randn(sum(news), hq, dim)
+    first = [x.clone() for x in attend(c, news, lp, q)]
+    again = attend(c, news, lp, q)
+    assert all(torch.equal(x, y) for x, y in zip(first, again))
+
+
 @pytest.mark.parametrize("kind", KINDS)
 @pytest.mark.parametrize("q_scale,scale", [(30.0, 0.05), (2.0 ** -9, 40.0)])
 def test_attend_of_large_and_small_queries(kind, q_scale, scale):
@@ -218,6 +233,82 @@ def test_a_row_without_any_page_and_more_tokens_than_slots():
         assert (out[rows] == 0).all() and (lse[rows] == -math.inf).all()
     assert (out[90:] == 2.0).all() and (lse[90:] == 3.0).all()
     check(c, 0, q[10:], out[10:], lse[10:], [40, 0, 0], [0, 40, 40, 40])
+
+
+@pytest.mark.parametrize("kind,dim", [("bf16", 256), ("int4-bf16", 64)])
+def test_attend_of_thousands_of_rows(kind, dim):
+    # (more rows, and at head_dim 256 more blocks of queries, than the threads that lay them out)
+    rows = 2300
+    lens = [(i * 7) % 12 for i in range(rows)]
+    news = [min(n, i % 5) for i, n in enumerate(lens)]
+    c = make(kind, lens, 2, 1, dim, 4, seed=22)
+    c.fill()
+    lp, total = c.handle(max_tokens=sum(news)), sum(news)
+    q, lse = c.randn(total, 2, dim), torch.empty(total, 2, device="cuda")
+    starts = starts_of(news)
+    out = lp.ltri_paged_attend(0, c.table, c.lens(), ints(starts), q, lse=lse)
+    assert lp.ltri_paged_sync_status() == binding.LTRI_OK
+    some = [*range(0, 40), *range(1000, 1060), *range(2040, 2060), *range(2260, 2300)]
+    check(c, 0, q, out, lse, [m if r in set(some) else 0 for r, m in enumerate(news)], starts)
+    assert out.isfinite().all() and lse.isfinite().all()
+
+
+def test_attend_of_rows_without_a_token():
+    c = make("int4-bf16", [40, 0, 20], 4, 2, 128, 16, seed=23)
+    c.fill()
+    lp, q = c.handle(max_tokens=9), c.randn(9, 4, 128)
+    out, lse = torch.full_like(q, 2.0), torch.full((9, 4), 3.0, device="cuda")
+    lp.ltri_paged_attend(0, c.table, c.lens(), ints([4, 4, 4, 4]), q, out=out, lse=lse)
+    assert lp.ltri_paged_sync_status() == binding.LTRI_OK
+    assert (out == 2.0).all() and (lse == 3.0).all()
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_infinities_and_nan_in_keys_that_are_not_seen(kind):
+    # token i sees the slots up to its own: those of the later ones hold what their logits make NaN and infinite
+    c = make(kind, [300], 4, 2, 128, 16, seed=24)
+    c.fill()
+    lp, q = c.handle(max_tokens=200), c.randn(200, 4, 128)
+    lse = torch.empty(200, 4, device="cuda")
+    want = lp.ltri_paged_attend(0, c.table, c.lens(), ints([0, 200]), q, lse=lse).clone()
+    pg, off = c.places(0, 300)
+    for slot, bad in ((230, math.inf), (231, -math.inf), (260, math.nan)):
+        row = torch.zeros(1, 2, 128)
+        row[:, :, 7] = bad
+        if kind.startswith("int4"):
+            row = torch.where(row == 0, row, math.nan)  # (infinities are clamped in 4 bits)
+            c.store(0, pg[slot:slot + 1], off[slot:slot + 1], 0, row)
+        else:
+            ref.put(c.k[0], pg[slot:slot + 1], off[slot:slot + 1], row.to(c.k.dtype))
+    got = lp.ltri_paged_attend(0, c.table, c.lens(), ints([0, 200]), q)
+    assert torch.equal(got[:130], want[:130]) and not got[160:].isfinite().any()
+
+
+def test_attend_beyond_32_bits():
+    # pages 2 MiB apart (a view of one page in 1024 of a larger tensor): the last ones lie 5 GiB behind the first
+    for kind in ("bf16", "int4"):
+        pages, P, hkv = 2600, 128, 2
+        row = 64 if kind == "bf16" else 32  # elements of the tensor
+        dtype = BF16 if kind == "bf16" else torch.uint8
+        step = (1 << 21) // (2 if kind == "bf16" else 1)
+        bases = [torch.zeros(pages, step, dtype=dtype, device="cuda") for _ in range(2)]
+        k, v = (b.as_strided((1, pages, hkv, P, row), (0, step, row, row * hkv, 1), 0) for b in bases)
+        sc = {} if kind == "bf16" else dict(block_scales=torch.zeros(1, pages, hkv, P, 2, 2, dtype=torch.uint8, device="cuda"))
+        lp = binding.LtriPaged(k, v, 4, dtype=BF16, max_rows=1, max_tokens=70, **sc)
+        table, lens, starts = ints([[0, pages - 1]]), ints([2 * P]), ints([0, 70])
+        g = torch.Generator().manual_seed(3)
+        x, y = (torch.randn(70, hkv, 64, generator=g).to(BF16) for _ in range(2))
+        q = torch.randn(70, 4, 64, generator=g).to(BF16)
+        lp.ltri_paged_append(0, table, lens, starts, x.cuda(), y.cuda())
+        out = lp.ltri_paged_attend(0, table, lens, starts, q.cuda())
+        assert lp.ltri_paged_sync_status() == binding.LTRI_OK
+        K, V = ((r.double() if kind == "bf16" else i4.quantise(r)[2]).repeat_interleave(2, 1) for r in (x, y))
+        # (all other slots hold zeros: logits of 0, values of 0)
+        logits = torch.einsum("ihd,jhd->hij", q.double(), K) / 8
+        p = torch.where(torch.ones(70, 70).tril().bool(), logits.exp(), 0.0)
+        want = torch.einsum("hij,jhd->ihd", p, V) / (p.sum(-1) + 2 * P - 70).T[:, :, None]
+        size = torch.einsum("hij,jhd->ihd", p, V.abs()) / (p.sum(-1) + 2 * P - 70).T[:, :, None]
+        assert ((out.cpu().double() - want).abs() <= want.abs() * 2.0 ** -8 + size * 2.0 ** -10 + 1e-6).all()
 
 
 @pytest.mark.parametrize("starts", [[0, 30, 20, 60], [5, 5, 90, 90], [-4, 10, 20, 30], [0, 2 ** 31 - 1, 20, 30], [60, 60, 0, 60]])

@@ -80,6 +80,18 @@ def test_append_and_read_back(dtype, layout, page, dim, hkv, weighted):
                 assert (got[:2] == 3.0).all() and (got[-3:] == 3.0).all()
 
 
+def test_append_of_strided_rows():
+    c = i4.Cache([50, 9], 3, 3, 128, 16, BF16, seed=5)
+    lp = c.handle()
+    both = c.randn(59, 2, 3, 128)  # (K and V side by side)
+    lp.ltri_paged_append(0, c.table, c.lens(), ints([0, 50, 59]), both[:, 0], both[:, 1])
+    assert lp.ltri_paged_sync_status() == binding.LTRI_OK
+    back = torch.empty_like(both)
+    lp.ltri_paged_read(0, c.table, c.lens(), ints([0, 50, 59]), back[:, 0], back[:, 1])
+    for which in (0, 1):
+        assert torch.equal(back[:, which].cpu().double(), i4.quantise(both[:, which].contiguous().cpu())[2])
+
+
 def test_append_of_infinities_and_nan():
     c = i4.Cache([6], 1, 1, 64, 4, BF16, seed=3)
     lp = c.handle()
