@@ -1017,14 +1017,14 @@ __global__ void __launch_bounds__(128) k_paged_attend_join(PagedCache c, PagedQu
 
 namespace {
 
-// Terms of the probabilities: one where the outputs have fewer bits than it, by three.
+// Terms of the probabilities for bf16 outputs: one where it has three bits more than they have.
 template <int KIND>
-constexpr int one_term() { return KIND >= kPaE4m3 ? 1 : 2; }
+constexpr int kPaTerms = KIND >= kPaE4m3 ? 1 : 2;
 
 template <int KIND, int D>
 cudaError_t prepare_one() {
   return first_error(allow_smem(k_paged_attend<KIND, D, 2>, PaShape<KIND, D>::kSmem),
-                     allow_smem(k_paged_attend<KIND, D, one_term<KIND>()>, PaShape<KIND, D>::kSmem));
+                     allow_smem(k_paged_attend<KIND, D, kPaTerms<KIND>>, PaShape<KIND, D>::kSmem));
 }
 template <int KIND>
 cudaError_t prepare_kind() {
@@ -1037,7 +1037,7 @@ cudaError_t launch_one(const PagedCache& c, const PagedRows& r, int layer, const
   cudaError_t e = launch_chained(k_paged_attend_plan, dim3(1), dim3(kPlThreads), 0, s, c, r, a.starts, a.n_tokens, wk, Sh::kRows,
                                  Sh::kTile);
   if (e != cudaSuccess) return e;
-  const auto kernel = c.type == LTRI_TYPE_BF16 ? k_paged_attend<KIND, D, one_term<KIND>()> : k_paged_attend<KIND, D, 2>;
+  const auto kernel = c.type == LTRI_TYPE_BF16 ? k_paged_attend<KIND, D, kPaTerms<KIND>> : k_paged_attend<KIND, D, 2>;
   e = launch_chained(kernel, dim3(c.sms), dim3(kPaThreads), Sh::kSmem, s, c, layer, r.table, r.table_stride, a, wk);
   if (e != cudaSuccess) return e;
   return launch_chained(k_paged_attend_join<KIND, D>, dim3(c.sms, Sh::kQt, D / 32), dim3(128), 0, s, c, a, wk, c.sms);
