@@ -30,13 +30,22 @@ __device__ __forceinline__ void pd_advance(PdCursor& u, const PagedCache& c, con
   u.n = max(u.n, 0);
 }
 
+// A CTA's run of n tiles dealt evenly to its warps, the first n % warps of which have one more: where warp w's begin, and whose tile
+// `at` is.
+__device__ __forceinline__ int pd_share(int n, int w, int warps) { return w * (n / warps) + min(w, n % warps); }
+__device__ __forceinline__ int pd_sharer(int n, int at, int warps) {
+  const int each = n / warps, more = n % warps;
+  return at < more * (each + 1) ? at / (each + 1) : more + (at - more * (each + 1)) / max(each, 1);
+}
+
 // All lanes of a warp: the tiles of the whole call, and the cursor of tile `runs_before` * per, where per is every run's length
-// (returned) when `runs` of them cover the line.
+// (returned) when `runs` of them cover the line.  EVEN: per is a CTA's run, and its `warps` warps have their shares of it, so that
+// SMs differ by a tile where they would differ by one a warp.
 // Where every unit can have a CTA of its own and a warp no more than one of its tiles, it begins with one, as if all were as
 // long as the CTAs' runs (`lone`; the cursor may then lie behind the unit's end): no two CTAs share a unit, and the join at
 // the end, two trips through L2, is spared.  (8 query heads, 2 KV heads, 100 slots: 7.1 us, 9.5 dealt evenly; with up to three
 // tiles a warp, 300 slots: 9.0 and 8.6.)
-template <int TILE>
+template <int TILE, bool EVEN = false>
 __device__ __forceinline__ int pd_deal(PdCursor& u, int& total, bool& lone, int runs, int runs_before, int warps,
                                        const PagedCache& c, const PagedRows& r, int blocks) {
   const int lane = threadIdx.x & 31, per_row = c.Hkv * blocks;
@@ -58,7 +67,8 @@ __device__ __forceinline__ int pd_deal(PdCursor& u, int& total, bool& lone, int 
       const int unit = (unsigned)runs_before / (unsigned)warps;
       total = units * warps;
       lone = true;
-      if (unit >= units) return 1;
+      const int one = EVEN ? warps : 1;
+      if (unit >= units) return one;
       const int nth = unit / per_row, in_row = unit - nth * per_row;
       u.row = __fns(rows, 0, nth + 1);
       u.n = __shfl_sync(0xffffffffu, n0, u.row);
@@ -66,7 +76,7 @@ __device__ __forceinline__ int pd_deal(PdCursor& u, int& total, bool& lone, int 
       u.tile = runs_before - unit * warps;
       u.head = in_row / blocks;
       u.block = in_row - u.head * blocks;
-      return 1;
+      return one;
     }
   }
   const int inc0 = scan((n0 + TILE - 1) / TILE * per_row);
@@ -76,8 +86,9 @@ __device__ __forceinline__ int pd_deal(PdCursor& u, int& total, bool& lone, int 
     const int row = base + lane;
     total += __reduce_add_sync(0xffffffffu, row < r.n ? (paged_len(c, r, row) + TILE - 1) / TILE * per_row : 0);
   }
+  if (EVEN) runs /= warps;
   const int per = (int)((unsigned)(total + runs - 1) / (unsigned)runs);
-  int left = runs_before * per;
+  int left = EVEN ? runs_before / warps * per + pd_share(per, runs_before % warps, warps) : runs_before * per;
   if (left >= total) return per;
   for (int base = 0; base < r.n; base += 32) {
     const int row = base + lane;

@@ -1,6 +1,8 @@
 """Host-only checks of 4-bit pages: the C entry points' refusals, and the format's definition."""
 import ctypes
 import math
+import os
+import subprocess
 
 import pytest
 import torch
@@ -79,3 +81,10 @@ def test_null_handles_of_attend_are_refused(lib):
     bad = binding.LTRI_EINVAL
     assert lib.ltri_paged_attend(None, 0, None, 1, 1, None, 1, None, 1, None, 0, None, None, None, 0, None) == bad
     assert lib.ltri_paged_attend_workspace_bytes(None, 8) == 0
+
+
+def test_every_tile_of_4_bit_rows_is_dealt_once_and_in_order(tmp_path):
+    here, out = os.path.dirname(os.path.abspath(__file__)), str(tmp_path / "deal")
+    subprocess.check_call(["g++", "-O1", "-std=c++20", "-pthread", os.path.join(here, "paged_deal_even_host.cpp"), "-o", out])
+    r = subprocess.run([out], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stdout
