@@ -174,8 +174,8 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
   PdCursor cu;
   int total;
   bool lone;  // the CTA has one unit, and all of it
-  // 4-bit rows, where an SM's instructions are the bound: its warps' runs may differ by a tile.  (Equal ones: 16 rows of 24576 slots of 128 in
-  // bf16 141 us, 134 so; one row of 131072 62.6 and 58.5; 64 ragged rows of 64 41.6 and 39.5; 300 slots 0.2 us less.)
+  // 4-bit rows, where an SM's instructions are the bound: its warps' runs may differ by a tile.  (Equal ones: 16 rows of 24576 slots
+  // of 128 141 us, 134 so; one row of 131072 62.6 and 58.5; 64 ragged rows of 64 41.6 and 39.5; 300 slots 0.2 us less.)
   constexpr bool kEven = KIND == kPdInt4;
   const int per = pd_deal<TILE, kEven>(cu, total, lone, gridDim.x * W, blockIdx.x * W + warp, W, c, r, wk.blocks);
   const int run = kEven ? per : W * per;
@@ -482,7 +482,8 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
     }
   };
   // A tile of 4-bit rows, 32 slots after the other: all of their work is little code, which the warps' turns keep in the instruction
-  // caches, and few registers, which lets more warps hide its latencies.  (16 slots at a time: 16 rows of 24576 slots of 128 145 us.)
+  // caches, and few registers, which lets more warps hide its latencies.  (16 slots at a time: 16 rows of 24576 slots of 128
+  // 145 us, 141 so.)
   unsigned char* table4 = dsm + W * (Sh::kRing + Sh::kPages * TILE * 4) + warp * Sh::kTable;
   auto int4_tile = [&](int stage_at, int page_at, int slot0) {
     constexpr int B = D / kI4Block;
