@@ -46,6 +46,12 @@ struct PaShape {
 constexpr int kPaSoftmax = 16, kPaLoaders = 8;  // warps
 constexpr int kPaIssuer = kPaSoftmax + kPaLoaders;  // this warp
 constexpr int kPaThreads = 32 * (kPaIssuer + 4);
+// Registers a thread: of the launch (prepare_kernel sees that it has them), and of the roles, which add up to them.  (All
+// 72, which the softmax's loop has not enough of: attend of 512 tokens over 24576 slots 234 us, with these 225; five drafted tokens
+// of 16 rows 62 and 58; 96, 40 and 40, or 88, 64 and 24: no faster.)
+constexpr int kPaRegs = 72, kPaSoftmaxRegs = 88, kPaLoadRegs = 56, kPaIssueRegs = 40;
+static_assert(kPaSoftmax * kPaSoftmaxRegs + kPaLoaders * kPaLoadRegs + 4 * kPaIssueRegs <= kPaThreads / 32 * kPaRegs,
+              "more would wait for ever");
 // Upper bound of any single wait, in SM cycles (about ten seconds: a CTA's longest run of tiles lies far below)
 constexpr long long kPaWaitLimit = 10 * kWaitLimitCycles;
 constexpr float kPaNone = -3.0e38f;  // reference of sums that nothing has entered yet: below every logit, and finite
@@ -411,6 +417,8 @@ __global__ void __launch_bounds__(kPaThreads, 1)
   // of a tile of queries' rows: references and sums, what their queries were divided by, and the largest elements of those' halves
   __shared__ float s_ref[QT][128], s_sum[QT][128], s_back[QT][128];
   __shared__ uint32_t s_most[QT][2][128];
+  // where the softmax's warps are, while their loops run, which want the registers
+  __shared__ PaPlace s_where[kPaSoftmax];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t sbase = (smem_addr(smem_raw) + 1023u) & ~1023u, sQ = sbase, sKV = sbase + QT * Sh::kQBytes;
   auto bar = [&](int i) { return smem_addr(&bars[i]); };
@@ -471,6 +479,7 @@ __global__ void __launch_bounds__(kPaThreads, 1)
 
   if (warp >= kPaSoftmax && warp < kPaIssuer) {
     // ------------------------------------------------------------------ K and V tiles
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kPaLoadRegs));
     // Four warps bring K and four V, so that what a tile costs them (page numbers, addresses, the wait for its stage) passes twice
     // at a time.
     constexpr int RC = Sh::kRow / 16, CL = RC < 4 ? RC : 4, SL = 32 / CL;  // lanes: SL slots, CL chunks of 16 bytes of each
@@ -625,6 +634,7 @@ __global__ void __launch_bounds__(kPaThreads, 1)
     }
   } else if (warp >= kPaIssuer) {
     // ------------------------------------------------------------------ products
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kPaIssueRegs));
     // A warp for each tile of query rows: S(q) of the next tile of slots follows O(q) += P(q) V of this one, and the other
     // tile's products run while this one's softmax does.
     if (works && warp < kPaIssuer + QT) {
@@ -726,6 +736,7 @@ __global__ void __launch_bounds__(kPaThreads, 1)
     }
   } else {
     // ------------------------------------------------------------------ softmax, queries and outputs
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kPaSoftmaxRegs));
     // A warp has 16 rows of S, four lanes each, so that a softmax needs no other warp.  Queries and outputs go by rows of a lane, two
     // threads each, with half of the elements.  Whatever goes wrong, all 256 threads of a tile of queries meet at the same barriers.
     if (works && warp < 8 * QT) {
@@ -803,9 +814,8 @@ __global__ void __launch_bounds__(kPaThreads, 1)
       skip();
       if (more) load_queries();
       while (more) {
-        const int rho = w.rho + q * 128 + r, head = w.head, begin = w.tile, end = w.end;
-        const bool row_ok = rho < w.rows, whole = begin == 0 && end == w.tiles;
-        const size_t to_row = (size_t)(w.start + rho / c.G) * c.Hq + head * c.G + rho % c.G;
+        const int begin = w.tile, end = w.end;
+        if (lane == 0) s_where[warp] = w;
         pa_any(1 + q, false);  // (s_back is there, and s_sum and s_ref of the part before have been read)
         // this lane's two rows: slots that they see, logits' factors, references and sums
         int own[2];
@@ -818,7 +828,7 @@ __global__ void __launch_bounds__(kPaThreads, 1)
           sc[i] = c.scale;
           if (KIND >= kPaE4m3) {
             const float back = c.type == LTRI_TYPE_BF16 ? s_back[q][row16 + 8 * i] : 1.f;
-            const float f = (float)((double)c.scale * (KIND == kPaE4m3 ? c.ks[head] : kI4Back) * back);
+            const float f = (float)((double)c.scale * (KIND == kPaE4m3 ? c.ks[w.head] : kI4Back) * back);
             sc[i] = f < 0x1p-126f ? 0x1p-126f : f;  // (as for single tokens)
           }
           ref[i] = kPaNone;
@@ -920,6 +930,11 @@ __global__ void __launch_bounds__(kPaThreads, 1)
             s_ref[q][row16 + 8 * i] = ref[i];
           }
         }
+        __syncwarp();
+        w = s_where[warp];
+        const int rho = w.rho + q * 128 + r, head = w.head;
+        const bool row_ok = rho < w.rows, whole = begin == 0 && end == w.tiles;
+        const size_t to_row = (size_t)(w.start + rho / c.G) * c.Hq + head * c.G + rho % c.G;
         // the next part's queries while this one's last products run
         more = next_part(w);
         skip();
@@ -1021,10 +1036,18 @@ namespace {
 template <int KIND>
 constexpr int kPaTerms = KIND >= kPaE4m3 ? 1 : 2;
 
+template <typename F>
+cudaError_t prepare_kernel(F* fn, int smem) {
+  cudaFuncAttributes a;
+  cudaError_t e = cudaFuncGetAttributes(&a, fn);
+  // the roles' registers come out of the launch's
+  if (e == cudaSuccess && a.numRegs < kPaRegs) e = cudaErrorInvalidConfiguration;
+  return first_error(e, allow_smem(fn, smem));
+}
 template <int KIND, int D>
 cudaError_t prepare_one() {
-  return first_error(allow_smem(k_paged_attend<KIND, D, 2>, PaShape<KIND, D>::kSmem),
-                     allow_smem(k_paged_attend<KIND, D, kPaTerms<KIND>>, PaShape<KIND, D>::kSmem));
+  return first_error(prepare_kernel(k_paged_attend<KIND, D, 2>, PaShape<KIND, D>::kSmem),
+                     prepare_kernel(k_paged_attend<KIND, D, kPaTerms<KIND>>, PaShape<KIND, D>::kSmem));
 }
 template <int KIND>
 cudaError_t prepare_kind() {
