@@ -197,13 +197,14 @@ __global__ void __launch_bounds__(kPlThreads)
   }
 }
 
-// A place in a CTA's run of the line: a part of a unit after the other, and their tiles.
+// A place in a CTA's run of the line: a part of a unit after the other, in stretches of up to `most` tiles, and their tiles.
 struct PaPlace {
   int at, head;           // entry, KV head
   int row, start;         // of the batch; the row's first token in q
   int rows, rho;          // query rows of the row, and the unit's first
   int base, limit;        // slots in front of the row's tokens, and those that the unit's last token sees
-  int tiles, tile, end;   // of the unit; the place; behind the part
+  int tiles, first, stop; // of the unit; the part's first, and behind the part
+  int tile, end;          // the place; behind the stretch
   long long left;         // places of the run behind the part
 };
 __device__ __forceinline__ void pa_entry(PaPlace& w, const PaEntry& e, int G, int rows) {
@@ -217,21 +218,27 @@ __device__ __forceinline__ void pa_entry(PaPlace& w, const PaEntry& e, int G, in
 }
 // The unit's part in the run, whose next place is the unit's number `at`; false if it has none (the run ends in front of the first
 // tile).
-__device__ __forceinline__ bool pa_part(PaPlace& w, int at) {
+__device__ __forceinline__ bool pa_part(PaPlace& w, int at, int most) {
   const int n = (int)min((long long)(w.tiles + kPaUnit - at), w.left);
   w.left -= n;
-  w.tile = max(0, at - kPaUnit);
-  w.end = max(0, at + n - kPaUnit);
+  w.first = w.tile = max(0, at - kPaUnit);
+  w.stop = max(0, at + n - kPaUnit);
+  w.end = min(w.stop, w.tile + most);
   return w.tile < w.end;
 }
-// The next part; false at the run's end.
-__device__ __forceinline__ bool pa_next(PaPlace& w, const PaWork& wk, int heads, int G, int rows) {
+// The next stretch; false at the run's end.
+__device__ __forceinline__ bool pa_next(PaPlace& w, const PaWork& wk, int heads, int G, int rows, int most) {
+  if (w.end < w.stop) {
+    w.tile = w.end;
+    w.end = min(w.stop, w.tile + most);
+    return true;
+  }
   if (w.left <= 0) return false;
   if (++w.head == heads) {
     w.head = 0;
     pa_entry(w, wk.entry[++w.at], G, rows);
   }
-  return pa_part(w, 0);
+  return pa_part(w, 0, most);
 }
 // One warp: the entry of a tile (below the line's total).
 __device__ __forceinline__ int pa_find(const PaWork& wk, int entries, long long tile) {
@@ -401,6 +408,12 @@ __global__ void __launch_bounds__(kPaThreads, 1)
   // as for single tokens: halves have their largest probability at 2^kOff, and a reference moves only when a logit exceeds it
   // by kGrow
   constexpr float kOff = KIND == kPaBf16 ? 0.f : 10.f, kGrow = 4.f;
+  // Tiles that O adds up before its sums go elsewhere.  (The tensor cores cut off what an accumulator has no bits for, towards zero.
+  // Measured over values of one sign: 2^13 slots with two terms take 2^-14 of the sum, an eighth of fp16 outputs' half step, 2^16
+  // 2^-11, an eighth of bf16 ones'.  For as long as a CTA's part is, fp16 outputs over 108152 slots of 12 heads were off by 1.2
+  // times what their rounding is.)
+  constexpr bool kToBf16 = KIND == kPaBf16 || (KIND != kPaFp16 && TERMS == 1);
+  constexpr int kMost = (kToBf16 ? 1 << 16 : 1 << 13) / TILE;
   extern __shared__ unsigned char smem_raw[];
   enum {
     B_KFULL = 0, B_VFULL = S, B_KEMPTY = 2 * S, B_VEMPTY = 3 * S, B_QFULL = 4 * S, B_SREADY = B_QFULL + QT,
@@ -466,7 +479,7 @@ __global__ void __launch_bounds__(kPaThreads, 1)
       w.at = at;
       w.head = (int)((c0 - e.before) / (e.tiles + kPaUnit));
       w.left = min(per, total - c0);
-      s_works = pa_part(w, (int)((c0 - e.before) % (e.tiles + kPaUnit)));
+      s_works = pa_part(w, (int)((c0 - e.before) % (e.tiles + kPaUnit)), kMost);
       s_place = w;
     }
   }
@@ -475,7 +488,7 @@ __global__ void __launch_bounds__(kPaThreads, 1)
   fence_after_sync();
   const uint32_t tmem = s_tmem;
   const bool works = s_works;
-  auto next_part = [&](PaPlace& w) { return pa_next(w, wk, c.Hkv, c.G, ROWS); };
+  auto next_part = [&](PaPlace& w) { return pa_next(w, wk, c.Hkv, c.G, ROWS, kMost); };
 
   if (warp >= kPaSoftmax && warp < kPaIssuer) {
     // ------------------------------------------------------------------ K and V tiles
@@ -813,6 +826,7 @@ __global__ void __launch_bounds__(kPaThreads, 1)
       };
       skip();
       if (more) load_queries();
+      float old_top = kPaNone, old_sum = 0.f;  // of the part's stretches so far
       while (more) {
         const int begin = w.tile, end = w.end;
         if (lane == 0) s_where[warp] = w;
@@ -932,19 +946,27 @@ __global__ void __launch_bounds__(kPaThreads, 1)
         }
         __syncwarp();
         w = s_where[warp];
-        const int rho = w.rho + q * 128 + r, head = w.head;
-        const bool row_ok = rho < w.rows, whole = begin == 0 && end == w.tiles;
+        const int rho = w.rho + q * 128 + r, head = w.head, first = w.first;
+        const bool row_ok = rho < w.rows, final = end == w.stop, whole = final && first == 0 && end == w.tiles;
         const size_t to_row = (size_t)(w.start + rho / c.G) * c.Hq + head * c.G + rho % c.G;
         // the next part's queries while this one's last products run
         more = next_part(w);
         skip();
-        if (more) load_queries();
+        if (!final) arrive(B_QFULL + q);
+        else if (more) load_queries();
         ok = ok && wait(B_ODONE + q, unit);
         if (pa_any(1 + q, !ok)) break;
-        const float sum = s_sum[q][r], top = s_ref[q][r];
+        float sum = s_sum[q][r], top = s_ref[q][r], now = 1.f, old = 0.f;
+        if (begin > first) {
+          const float to = fmaxf(top, old_top);
+          now = pa_exp2(top - to), old = pa_exp2(old_top - to);
+          sum = sum * now + old_sum * old;
+          top = to;
+        }
+        old_top = top, old_sum = sum;
         fence_after_sync();
         const float by = !whole ? 1.f : sum == 0.f ? 0.f : 1.f / sum, vs = whole ? pa_v_scale<KIND>(c, head) : 1.f;
-        float* part = wk.part + (size_t)(2 * blockIdx.x + (begin == 0 ? 1 : 0)) * pa_part_floats<KIND, D>();
+        float* part = wk.part + (size_t)(2 * blockIdx.x + (first == 0 ? 1 : 0)) * pa_part_floats<KIND, D>();
 #pragma unroll 1
         for (int k = 0; k < D / 64; ++k) {
           const int i = half * (D / 64) + k;
@@ -953,8 +975,20 @@ __global__ void __launch_bounds__(kPaThreads, 1)
           tmem_ld_wait();
           float z[32];
 #pragma unroll
-          for (int e = 0; e < 32; ++e) z[e] = __uint_as_float(v[e]) * by * vs;
+          for (int e = 0; e < 32; ++e) z[e] = __uint_as_float(v[e]);
           if (!row_ok) continue;
+          if (begin > first) {  // (a thread's own stores)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const float4 y = *reinterpret_cast<const float4*>(part + ((size_t)(q * (D / 4) + i * 8 + e) * 128 + r) * 4);
+              z[4 * e] = z[4 * e] * now + y.x * old;
+              z[4 * e + 1] = z[4 * e + 1] * now + y.y * old;
+              z[4 * e + 2] = z[4 * e + 2] * now + y.z * old;
+              z[4 * e + 3] = z[4 * e + 3] * now + y.w * old;
+            }
+          }
+#pragma unroll
+          for (int e = 0; e < 32; ++e) z[e] = z[e] * by * vs;
           if (whole) {
             pa_put32<KIND>(c.type, a.out + to_row * (D * 2) + i * 64, z);
           } else {
@@ -969,7 +1003,7 @@ __global__ void __launch_bounds__(kPaThreads, 1)
         if (row_ok && half == 0) {
           if (whole && a.lse)
             a.lse[to_row] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.69314718055994531f;
-          if (!whole) *reinterpret_cast<float2*>(part + (size_t)ROWS * D + (q * 128 + r) * 2) = make_float2(top, sum);
+          if (final && !whole) *reinterpret_cast<float2*>(part + (size_t)ROWS * D + (q * 128 + r) * 2) = make_float2(top, sum);
         }
         ++unit;
       }

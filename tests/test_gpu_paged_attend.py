@@ -144,6 +144,43 @@ def test_attend_of_few_and_many_tokens_together(kind, dim, hq, hkv):
     assert all(torch.equal(x, y) for x, y in zip(first, again))
 
 
+@pytest.mark.parametrize("kind,dim", [("fp16", 64), ("int4-fp16", 128), ("e4m3-fp16", 256)])
+def test_sums_of_many_slots_do_not_fall_behind(kind, dim):
+    # The tensor cores' sums are cut off towards zero: k additions take k / 2 times 2^-24 of a sum that grows evenly (half of the
+    # last place, which is 2^-23 of it at the most), and as much again where products lose their own last places beside the sum.
+    # Two for each 16 slots of up to 2^13: 2^-14 on the average, which values of one sign show.  The outputs' roundings do not
+    # average out, since all outputs lie within a few of their steps of 1: they are known from the exact values, and taken out.
+    n, m, hq, hkv = 100000, 600, 16, 4
+    c = make(kind, [n], hq, hkv, dim, 128, seed=dim)
+    pg, off = c.places(0, n)
+    K, V = torch.randn(n, hkv, dim, generator=c.g), torch.rand(n, hkv, dim, generator=c.g) + 0.5
+    if kind.startswith("int4"):
+        c.store(0, pg, off, 0, K)
+        c.store(0, pg, off, 1, V)
+    else:
+        ref.put(c.k[0], pg, off, K.to(c.k.dtype))
+        ref.put(c.v[0], pg, off, V.to(c.v.dtype))
+    lp, q = c.handle(max_tokens=m), c.randn(m, hq, dim, scale=0.5)
+    lse = torch.empty(m, hq, device="cuda")
+    out = lp.ltri_paged_attend(0, c.table, c.lens(), ints([0, m]), q, lse=lse)
+    assert lp.ltri_paged_sync_status() == binding.LTRI_OK
+    K, V = (x.cuda() for x in c.row(0, 0, n))
+    seen = torch.arange(n, device="cuda") <= (n - m + torch.arange(m, device="cuda"))[:, None]
+    for h in (0, 7, 13):
+        logits = torch.where(seen, q[:, h].double() @ K[:, h // 4].T * dim ** -0.5, -math.inf)
+        want = torch.softmax(logits, -1) @ V[:, h // 4]
+        assert abs(float(((out[:, h].double() - want.to(c.dtype).double()) / want).mean())) <= 2.0 ** -14
+        assert (lse[:, h].double() - torch.logsumexp(logits, -1)).abs().max() <= 1e-4
+
+
+@pytest.mark.parametrize("q_scale", [1.0, 4.0])
+def test_long_units_within_one_cta(q_scale):
+    # (more units than CTAs, each longer than what O adds up at a time)
+    c = make("fp16", [10100] * 10, 16, 16, 64, 128, seed=31)
+    c.fill()
+    attend(c, [2, 1, 0, 2, 3, 1, 1, 2, 1, 5], q_scale=q_scale)
+
+
 @pytest.mark.parametrize("kind", KINDS)
 @pytest.mark.parametrize("q_scale,scale", [(30.0, 0.05), (2.0 ** -9, 40.0)])
 def test_attend_of_large_and_small_queries(kind, q_scale, scale):
