@@ -441,9 +441,9 @@ class LtriPaged:
     k_pages, v_pages: [layers][pages][Hkv][page tokens][head_dim] CUDA tensors with the same strides (a permuted view of
     token-major pages, or the halves of one tensor, will do), of ``dtype`` or float8_e4m3fn with k_scale, v_scale (float32
     [Hkv]), or of 4 bits: uint8 [layers][pages][Hkv][page tokens][head_dim / 2] with block_scales (uint8
-    [layers][pages][Hkv][page tokens][2][head_dim / 32], contiguous).  weights (float32) and positions (int32), both or neither: [layers][pages][Hkv][page tokens], contiguous.  The
-    tensors stay the caller's; the handle keeps references to them.  It allocates its workspace on ``stream`` (None: the one
-    that is current when it is made): let it go only when its calls on other streams are through.  max_tokens: tokens of the
+    [layers][pages][Hkv][page tokens][2][head_dim / 32], contiguous).  weights (float32) and positions (int32), both or neither:
+    [layers][pages][Hkv][page tokens], contiguous.  The tensors stay the caller's; the handle keeps references to them.  It
+    allocates its workspace on ``stream`` (None: the one that is current when it is made): let it go only when its calls on other streams are through.  max_tokens: tokens of the
     largest ltri_paged_attend call, whose workspace it allocates too (0: none).
     """
 

@@ -3,7 +3,9 @@
 // Bound: HBM, every row is read once and written once.  A warp's lanes ask for up to CHUNKS 16-byte chunks each of a token's K
 // rows and as many of its V rows before they look up the token's row, slot and page, which the loads do not depend on.
 // Consecutive lanes take consecutive chunks, so both sides move whole rows whatever the order of the axes.  (A chunk a thread,
-// behind the lookups: 38 us for 22700 tokens of eight KV heads, 33 so.)
+// behind the lookups: 38 us for 22700 tokens of eight KV heads, 33 so.)  Over 4-bit pages, which those tokens are in 33 to 37 us in,
+// the quantisation's instructions bound it: 64% of the issue slots are taken.  (Four CTAs an SM at 64 registers instead of three
+// at 80: no faster; five at 48: 4 us more.)
 #include "paged_int4.cuh"
 
 namespace ltri {

@@ -24,6 +24,11 @@
 // all but one (270), 6.2 to 6.7 TB/s; one row of 131072, 88 to 94 us, 5.7 to 6.1 TB/s.  What a call costs beyond its bytes is 10
 // to 15 us: two dependent lookups before the first row (lengths, pages), and after the last one the joins; 300 slots of one row
 // take 8.6 to 9.5 us.  32 query heads of one KV head, 16 rows of 24576 slots: 76 to 83 us, 64 of them 138 to 167, at a floor of 31.
+//
+// 4-bit rows: a quarter of the bytes for the same products, and numbers to be unpacked, so that instructions are the bound (some 410 of
+// a warp for 16 slots of 128; half of the issue slots are taken).  K's numbers enter the products as they stand, as the smallest
+// halves, and their scales are applied to the sums of 32 elements; V's become values by one multiply-add for two.  The same 16
+// rows 132 to 134 us (66 at the copy rate), the row of 131072 57 to 58.5 (22), 300 slots 9.5 to 9.8.
 #include "mma_util.cuh"
 #include "paged_deal.cuh"
 #include "paged_int4.cuh"
@@ -46,7 +51,8 @@ struct PdShape {
   static constexpr int kStage = kTile * (2 * kRow + kScales);   // K rows, V rows, scales
   static constexpr int kTable = KIND == kPdInt4 ? 8 * D : 0;    // factors of V's values of 32 slots, of a warp: 256 bytes for 32 elements
   static constexpr int kWarps = kRow == 512 ? 4 : KIND == kPdInt4 && !kWide ? 12 : 8;  // of a CTA, one CTA an SM
-  static constexpr int kFit = ((232448 - (KIND == kPdInt4 ? 1024 : 2048)) / kWarps - kTable + (KIND == kPdInt4 ? 4 * kTile : 0)) / (kStage + 8 * kTile);
+  static constexpr int kRoom = (232448 - (KIND == kPdInt4 ? 1024 : 2048)) / kWarps - kTable;  // of a warp
+  static constexpr int kFit = (kRoom + (KIND == kPdInt4 ? 4 * kTile : 0)) / (kStage + 8 * kTile);
   static constexpr int kStages = kFit > 8 ? 8 : kFit;
   static constexpr int kAhead = kStages - 1;                    // tiles that rows are on their way of
   static constexpr int kPages = 2 * kStages - (KIND == kPdInt4 ? 1 : 0);  // tiles whose page numbers are known or on their way
