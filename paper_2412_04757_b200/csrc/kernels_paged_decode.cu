@@ -305,15 +305,15 @@ __global__ void __launch_bounds__(PdShape<KIND, D, NT>::kWarps * 32, 1)
           x.b[nt][i + 1][0] = __byte_perm(e.y, e.w, 0x5410);
           x.b[nt][i + 1][1] = __byte_perm(e.y, e.w, 0x7632);
         }
-        continue;
-      }
+      } else {
 #pragma unroll
-      for (int i = 0; i < DT; ++i) {
-        // (8-bit rows: a 16-byte chunk is one step of 16, of which a lane holds four neighbours)
+        for (int i = 0; i < DT; ++i) {
+          // (8-bit rows: a 16-byte chunk is one step of 16, of which a lane holds four neighbours)
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const int el = KIND == kPdE4m3 ? i * 16 + q4 * 4 + 2 * j : i * 16 + q4 * 2 + 8 * j;
-          x.b[nt][i][j] = in_group < c.G ? *reinterpret_cast<const uint32_t*>(qr + el * 2) : 0u;
+          for (int j = 0; j < 2; ++j) {
+            const int el = KIND == kPdE4m3 ? i * 16 + q4 * 4 + 2 * j : i * 16 + q4 * 2 + 8 * j;
+            x.b[nt][i][j] = in_group < c.G ? *reinterpret_cast<const uint32_t*>(qr + el * 2) : 0u;
+          }
         }
       }
     }

@@ -173,6 +173,33 @@ def test_sums_of_many_slots_do_not_fall_behind(kind, dim):
         assert (lse[:, h].double() - torch.logsumexp(logits, -1)).abs().max() <= 1e-4
 
 
+def test_parts_of_more_slots_than_a_bf16_sum_takes():
+    # 40 units of 300000 slots: the CTAs' parts have some 80000, which O adds up in stretches of 2^16 at most
+    n, m = 300000, 600
+    c = make("bf16", [n], 16, 4, 64, 128, seed=33)
+    pg, off = c.places(0, n)
+    g = torch.Generator(device="cuda").manual_seed(34)
+    for pages in (c.k, c.v):
+        ref.put(pages[0], pg, off, torch.randn(n, 4, 64, generator=g, device="cuda").to(BF16).cpu())
+    lp, q = c.handle(max_tokens=m), c.randn(m, 16, 64, scale=3.0)
+    lse = torch.empty(m, 16, device="cuda")
+    out = lp.ltri_paged_attend(0, c.table, c.lens(), ints([0, m]), q, lse=lse)
+    assert lp.ltri_paged_sync_status() == binding.LTRI_OK
+    K, V = (x.cuda() for x in c.row(0, 0, n))
+    which = torch.arange(0, m, 12, device="cuda")
+    seen = torch.arange(n, device="cuda") <= (n - m + which)[:, None]
+    for h in (0, 6, 13):
+        k, v, qh = K[:, h // 4], V[:, h // 4], q[which, h].double()
+        logits = torch.where(seen, qh @ k.T / 8, -math.inf)
+        p = torch.softmax(logits, -1)
+        want = p @ v
+        # (as above; the sums of a stretch lose 2^-11 of what they add up)
+        d = (qh.abs() @ k.abs().T).amax(-1) / 8 * (64 + 8) * 2.0 ** -23
+        tol = (torch.expm1(2 * d) + 2.0 ** -21 + 2.0 ** -17 + 2.0 ** -10)[:, None] * (p @ v.abs())
+        assert ((out[which, h].double() - want).abs() <= want.abs() * 2.0 ** -8 + tol).all()
+        assert ((lse[which, h].double() - torch.logsumexp(logits, -1)).abs() <= d + 1e-4).all()
+
+
 @pytest.mark.parametrize("q_scale", [1.0, 4.0])
 def test_long_units_within_one_cta(q_scale):
     # (more units than CTAs, each longer than what O adds up at a time)
