@@ -60,10 +60,6 @@ static_assert(kPaSoftmax * kPaSoftmaxRegs + kPaLoaders * kPaLoadRegs + 4 * kPaIs
 constexpr long long kPaWaitLimit = 10 * kWaitLimitCycles;
 constexpr float kPaNone = -3.0e38f;  // reference of sums that nothing has entered yet: below every logit, and finite
 
-// What a unit costs besides its tiles (queries to be loaded, outputs to be written, while the products wait), as tiles: it takes so
-// many more places in the line.  (Without them the CTAs with the shortest units were through 1.3 times as late as the others.)
-constexpr int kPaUnit = 2;
-
 // A block of a row's query rows, and the first of its KV heads' places in the line (they follow each other).
 struct __align__(32) PaEntry {
   int row, block;
@@ -109,6 +105,12 @@ __device__ __forceinline__ int pa_limit(const PaEntry& e, int G, int rows) {
   const int last = min(e.m * G, (e.block + 1) * rows) - 1;
   return max(0, e.base + min(last / G + 1, e.m));
 }
+
+// What a unit costs besides its tiles (queries to be loaded, outputs to be written, while the products wait), as tiles: it takes so
+// many more places in the line.  (None: the CTAs with the shortest units were through 1.3 times as late as the others.  With one tile
+// of query rows 2, 16 ragged rows of five tokens 58 us; 1 or 3 60, 4 62.  With both 4, three prompts of up to 16384 tokens 4.0 to 4.2
+// ms; 1 4.9, 2 4.4, 3 4.1 to 4.2.)
+__device__ __forceinline__ int pa_extra(const PaEntry& e, int G, int rows) { return e.m * G - e.block * rows > 128 ? 4 : 2; }
 
 // ---- the line of tiles ----
 constexpr int kPlThreads = 1024;
@@ -188,7 +190,7 @@ __global__ void __launch_bounds__(kPlThreads)
       e.base = paged_len(c, r, lo) - e.m;
       if (e.base < 0 && e.block == 0) paged_status(c, lo);
       e.tiles = max(1, (pa_limit(e, c.G, rows) + tile - 1) / tile);
-      n = (long long)(e.tiles + kPaUnit) * c.Hkv;
+      n = (long long)(e.tiles + pa_extra(e, c.G, rows)) * c.Hkv;
     }
     long long all;
     e.before = total + scan(n, all);
@@ -207,7 +209,8 @@ struct PaPlace {
   int row, start;         // of the batch; the row's first token in q
   int rows, rho;          // query rows of the row, and the unit's first
   int base, limit;        // slots in front of the row's tokens, and those that the unit's last token sees
-  int tiles, first, stop; // of the unit; the part's first, and behind the part
+  int tiles, extra;       // of the unit; its places in front of them
+  int first, stop;        // the part's first tile, and behind it
   int tile, end;          // the place; behind the stretch
   long long left;         // places of the run behind the part
 };
@@ -219,14 +222,15 @@ __device__ __forceinline__ void pa_entry(PaPlace& w, const PaEntry& e, int G, in
   w.base = e.base;
   w.limit = pa_limit(e, G, rows);
   w.tiles = e.tiles;
+  w.extra = pa_extra(e, G, rows);
 }
 // The unit's part in the run, whose next place is the unit's number `at`; false if it has none (the run ends in front of the first
 // tile).
 __device__ __forceinline__ bool pa_part(PaPlace& w, int at, int most) {
-  const int n = (int)min((long long)(w.tiles + kPaUnit - at), w.left);
+  const int n = (int)min((long long)(w.tiles + w.extra - at), w.left);
   w.left -= n;
-  w.first = w.tile = max(0, at - kPaUnit);
-  w.stop = max(0, at + n - kPaUnit);
+  w.first = w.tile = max(0, at - w.extra);
+  w.stop = max(0, at + n - w.extra);
   w.end = min(w.stop, w.tile + most);
   return w.tile < w.end;
 }
@@ -481,9 +485,9 @@ __global__ void __launch_bounds__(kPaThreads, 1)
       PaPlace w;
       pa_entry(w, e, c.G, ROWS);
       w.at = at;
-      w.head = (int)((c0 - e.before) / (e.tiles + kPaUnit));
+      w.head = (int)((c0 - e.before) / (e.tiles + w.extra));
       w.left = min(per, total - c0);
-      s_works = pa_part(w, (int)((c0 - e.before) % (e.tiles + kPaUnit)), kMost);
+      s_works = pa_part(w, (int)((c0 - e.before) % (e.tiles + w.extra)), kMost);
       s_place = w;
     }
   }
@@ -1033,8 +1037,8 @@ __global__ void __launch_bounds__(128) k_paged_attend_join(PagedCache c, PagedQu
   }
   __syncthreads();
   const PaEntry e = wk.entry[s_at];
-  const int places = e.tiles + kPaUnit, head = (int)((c1 - 1 - e.before) / places);
-  const long long begin = e.before + (long long)head * places + kPaUnit, end = begin + e.tiles;
+  const int extra = pa_extra(e, c.G, Sh::kRows), places = e.tiles + extra, head = (int)((c1 - 1 - e.before) / places);
+  const long long begin = e.before + (long long)head * places + extra, end = begin + e.tiles;
   if (begin < c0 || begin >= c1 || end == c1) return;
   const int parts = (int)((end - 1) / per - blockIdx.x) + 1;
   const int q = blockIdx.y, r = threadIdx.x, i = blockIdx.z;
