@@ -22,9 +22,9 @@
 // products.  TMEM: two S of 64 columns in turn for each tile of query rows, in whose columns P replaces S, then the two O.  head_dim
 // 256: one tile of query rows.
 //
-// Measured over 4-bit pages, 32 query and 8 KV heads of 128: 512 tokens over 24576 slots 222 to 228 us in a stream of calls (some 900
-// TFLOP/s; 122 at the rate of large matrix products), three prompts of up to 16384 tokens in fp16 4.6 ms, 16 ragged rows of up to 8000
-// slots with five tokens each 58 us.
+// Measured over 4-bit pages, 32 query and 8 KV heads of 128: 512 tokens over 24576 slots 218 to 220 us in a stream of calls (some
+// 930 TFLOP/s; 122 at the rate of large matrix products), three prompts of up to 16384 tokens in fp16 4.1 to 4.2 ms, 16 ragged rows of
+// up to 8000 slots with five tokens each 58 to 59 us.
 #include "paged_int4.cuh"
 #include "tc_util.cuh"
 
