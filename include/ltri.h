@@ -509,9 +509,8 @@ int ltri_paged_decode(ltri_paged* cache, int layer, const int32_t* table, int ta
  * Queries without a slot (more than lens[r] of them) have outputs of 0 and an lse of -infinity, as have those of rows of bad
  * lengths, and are recorded as LTRI_EDEVICE.  Weights are not accumulated.  V rows of the call's own tokens have to be finite:
  * the products multiply those that a token does not see by 0.
- * Logits and sums are fp32.  The probabilities enter the product with V as 16-bit terms: two of them, 22 bits as in
- * ltri_paged_decode, where `type` is fp16; one of 11 bits where it is bf16 over 8-bit and 4-bit pages, an eighth of the outputs' own
- * half step; two, 16 bits, over bf16 pages.  The tensor cores' sums, which are cut off towards zero, are taken over by fp32
+ * Logits and sums are fp32.  The probabilities enter the product with V as two 16-bit terms: 22 bits as in ltri_paged_decode over
+ * fp16, 8-bit and 4-bit pages, 16 bits over bf16 ones.  The tensor cores' sums, which are cut off towards zero, are taken over by fp32
  * arithmetic every 2^13 slots where `type` is fp16, every 2^16 where it is bf16: up to there they lose about an eighth of the outputs'
  * half step.  Outputs are the same bits for the same inputs and the same device. */
 int ltri_paged_attend(ltri_paged* cache, int layer, const int32_t* table, int table_pages, int64_t table_stride,

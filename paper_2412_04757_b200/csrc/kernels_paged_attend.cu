@@ -7,11 +7,11 @@
 //
 // Bound: the tensor cores where there are many tokens (two products of 2 D flops a pair of token and slot), so both run on
 // tcgen05.mma: S = Q K^T from shared memory, O += P V with P in TMEM.  P enters as two 16-bit terms, the second what the first has
-// left over, so that the outputs carry the rounding of their type once; for bf16 outputs of products in halves as one, whose
-// 2^-11 is an eighth of the outputs' own half step.  (With two of them there too the tensor pipe has three products to do instead
-// of two: 512 tokens over 24576 slots 307 us, 263 so, both before the softmax was within a warp.)  Rows of 8 and 4 bits become halves
-// on their way into shared memory, exactly; queries over them become halves too, each row scaled by a power of two.  With few tokens
-// it is the cache's bytes and the CTAs' latency.
+// left over, so that the outputs carry the rounding of their type once, also where values cancel, and drafted tokens have what single
+// ones have.  (One half's 11 bits would spare bf16 outputs a third of the tensor work, 226 us instead of 258 for 512 tokens over
+// 24576 slots; of two probabilities 2^-14 apart whose V are 1 and -1 it leaves nothing.)  Rows of 8 and 4 bits become halves on their
+// way into shared memory, exactly; queries over them become halves too, each row scaled by a power of two.  With few tokens it is
+// the cache's bytes and the CTAs' latency.
 //
 // Work: units are (row, KV head, block of query rows), as long as the tiles of slots that their last token sees.  A small kernel
 // puts all units' tiles into one line, of which every CTA (one per SM) takes an equal run, across units if need be; the partial sums
@@ -283,11 +283,6 @@ __device__ __forceinline__ unsigned long long pa_add2(unsigned long long a, unsi
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
   return d;
 }
-// A pair of fp32 values as `type`.
-__device__ __forceinline__ uint32_t pa_term(int type, unsigned long long p) {
-  const float2 f = pa_split(p);
-  return paged_pack(type, f.x, f.y);
-}
 // Two terms of `type` that add up to a pair of fp32 values.
 __device__ __forceinline__ void pa_terms(int type, unsigned long long p, uint32_t& hi, uint32_t& lo) {
   const float2 f = pa_split(p);
@@ -407,7 +402,7 @@ __device__ __forceinline__ float pa_v_scale(const PagedCache& c, int head) {
   return KIND == kPaInt4 ? kI4Back : KIND == kPaE4m3 ? c.vs[head] : 1.f;
 }
 
-template <int KIND, int D, int TERMS>
+template <int KIND, int D>
 __global__ void __launch_bounds__(kPaThreads, 1)
     k_paged_attend(PagedCache c, int layer, const int* table, long long table_stride, PagedQueries a, PaWork wk) {
   using Sh = PaShape<KIND, D>;
@@ -420,8 +415,7 @@ __global__ void __launch_bounds__(kPaThreads, 1)
   // Measured over values of one sign: 2^13 slots with two terms take 2^-14 of the sum, an eighth of fp16 outputs' half step, 2^16
   // 2^-11, an eighth of bf16 ones'.  For as long as a CTA's part is, fp16 outputs over 108152 slots of 12 heads were off by 1.2
   // times what their rounding is.)
-  constexpr bool kToBf16 = KIND == kPaBf16 || (KIND != kPaFp16 && TERMS == 1);
-  constexpr int kMost = (kToBf16 ? 1 << 16 : 1 << 13) / TILE;
+  const int most = (c.type == LTRI_TYPE_BF16 ? 1 << 16 : 1 << 13) / TILE;
   extern __shared__ unsigned char smem_raw[];
   enum {
     B_KFULL = 0, B_VFULL = S, B_KEMPTY = 2 * S, B_VEMPTY = 3 * S, B_QFULL = 4 * S, B_SREADY = B_QFULL + QT,
@@ -487,7 +481,7 @@ __global__ void __launch_bounds__(kPaThreads, 1)
       w.at = at;
       w.head = (int)((c0 - e.before) / (e.tiles + w.extra));
       w.left = min(per, total - c0);
-      s_works = pa_part(w, (int)((c0 - e.before) % (e.tiles + w.extra)), kMost);
+      s_works = pa_part(w, (int)((c0 - e.before) % (e.tiles + w.extra)), most);
       s_place = w;
     }
   }
@@ -496,7 +490,7 @@ __global__ void __launch_bounds__(kPaThreads, 1)
   fence_after_sync();
   const uint32_t tmem = s_tmem;
   const bool works = s_works;
-  auto next_part = [&](PaPlace& w) { return pa_next(w, wk, c.Hkv, c.G, ROWS, kMost); };
+  auto next_part = [&](PaPlace& w) { return pa_next(w, wk, c.Hkv, c.G, ROWS, most); };
 
   if (warp >= kPaSoftmax && warp < kPaIssuer) {
     // ------------------------------------------------------------------ K and V tiles
@@ -678,14 +672,14 @@ __global__ void __launch_bounds__(kPaThreads, 1)
         }
         pa_commit(s_bars + 8 * B_SREADY + 8 * b);
       };
-      // P: 32 columns of first terms, 32 of second ones, if there are any
+      // P: 32 columns of first terms, 32 of second ones
       auto issue_pv = [&](int b, int st, int sub, bool acc) {
         const uint32_t pa = tS + b * 64;
         const uint64_t db = dV + (uint32_t)(st * (2 * Sh::kMat >> 4) + sub * (64 * 128 >> 4));
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          if (TERMS == 2) pa_mma_ts(tO, pa + 32 + i * 8, db + (i * 16 * 128 >> 4), idesc_pv, acc || i > 0);
-          pa_mma_ts(tO, pa + i * 8, db + (i * 16 * 128 >> 4), idesc_pv, TERMS == 2 || acc || i > 0);
+          pa_mma_ts(tO, pa + 32 + i * 8, db + (i * 16 * 128 >> 4), idesc_pv, acc || i > 0);
+          pa_mma_ts(tO, pa + i * 8, db + (i * 16 * 128 >> 4), idesc_pv, true);
         }
       };
       auto wait_at = [&](uint32_t at, uint32_t parity) { return __all_sync(0xffffffffu, pa_wait(at, parity, abortp)) != 0; };
@@ -931,11 +925,10 @@ __global__ void __launch_bounds__(kPaThreads, 1)
             const float2 x = pa_split(pa_fma2(pa_pair(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1])), sc2[i], ref2[i]));
             const unsigned long long p = pa_pair(pa_exp2(x.x), pa_exp2(x.y));
             sum2[i] = pa_add2(sum2[i], p);
-            if (TERMS == 2) pa_terms(kType, p, hi[e], lo[e]);
-            else hi[e] = pa_term(kType, p);
+            pa_terms(kType, p, hi[e], lo[e]);
           }
           pa_st_pairs(tS, hi);
-          if (TERMS == 2) pa_st_pairs(tS + 32, lo);
+          pa_st_pairs(tS + 32, lo);
           tmem_st_wait();
           fence_before_sync();
           arrive(B_PREADY + q * SB + b);
@@ -1074,10 +1067,6 @@ __global__ void __launch_bounds__(128) k_paged_attend_join(PagedCache c, PagedQu
 
 namespace {
 
-// Terms of the probabilities for bf16 outputs: one where it has three bits more than they have.
-template <int KIND>
-constexpr int kPaTerms = KIND >= kPaE4m3 ? 1 : 2;
-
 template <typename F>
 cudaError_t prepare_kernel(F* fn, int smem) {
   cudaFuncAttributes a;
@@ -1088,8 +1077,7 @@ cudaError_t prepare_kernel(F* fn, int smem) {
 }
 template <int KIND, int D>
 cudaError_t prepare_one() {
-  return first_error(prepare_kernel(k_paged_attend<KIND, D, 2>, PaShape<KIND, D>::kSmem),
-                     prepare_kernel(k_paged_attend<KIND, D, kPaTerms<KIND>>, PaShape<KIND, D>::kSmem));
+  return prepare_kernel(k_paged_attend<KIND, D>, PaShape<KIND, D>::kSmem);
 }
 template <int KIND>
 cudaError_t prepare_kind() {
@@ -1102,8 +1090,7 @@ cudaError_t launch_one(const PagedCache& c, const PagedRows& r, int layer, const
   cudaError_t e = launch_chained(k_paged_attend_plan, dim3(1), dim3(kPlThreads), 0, s, c, r, a.starts, a.n_tokens, wk, Sh::kRows,
                                  Sh::kTile);
   if (e != cudaSuccess) return e;
-  const auto kernel = c.type == LTRI_TYPE_BF16 ? k_paged_attend<KIND, D, kPaTerms<KIND>> : k_paged_attend<KIND, D, 2>;
-  e = launch_chained(kernel, dim3(c.sms), dim3(kPaThreads), Sh::kSmem, s, c, layer, r.table, r.table_stride, a, wk);
+  e = launch_chained(k_paged_attend<KIND, D>, dim3(c.sms), dim3(kPaThreads), Sh::kSmem, s, c, layer, r.table, r.table_stride, a, wk);
   if (e != cudaSuccess) return e;
   return launch_chained(k_paged_attend_join<KIND, D>, dim3(c.sms, Sh::kQt, D / 32), dim3(128), 0, s, c, a, wk, c.sms);
 }
