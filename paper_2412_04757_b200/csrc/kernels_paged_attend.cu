@@ -9,9 +9,11 @@
 // tcgen05.mma: S = Q K^T from shared memory, O += P V with P in TMEM.  P enters as two 16-bit terms, the second what the first has
 // left over, so that the outputs carry the rounding of their type once, also where values cancel, and drafted tokens have what single
 // ones have.  (One half's 11 bits would spare bf16 outputs a third of the tensor work, 226 us instead of 258 for 512 tokens over
-// 24576 slots; of two probabilities 2^-14 apart whose V are 1 and -1 it leaves nothing.)  Rows of 8 and 4 bits become halves on their
-// way into shared memory, exactly; queries over them become halves too, each row scaled by a power of two.  With few tokens it is
-// the cache's bytes and the CTAs' latency.
+// 24576 slots; of two probabilities 2^-14 apart whose V are 1 and -1 it leaves nothing.  Over bf16 pages two terms are 16 bits, and
+// three would be fp32's: their 96 columns leave TMEM no room for a second S, without which the same call takes 469 us instead of
+// 264, and at head_dim 256, where there is room, 647 instead of 545.)  Rows of 8 and 4 bits become halves on their way into
+// shared memory, exactly; queries over them become halves too, each row scaled by a power of two.  With few tokens it is the
+// cache's bytes and the CTAs' latency.
 //
 // Work: units are (row, KV head, block of query rows), as long as the tiles of slots that their last token sees.  A small kernel
 // puts all units' tiles into one line, of which every CTA (one per SM) takes an equal run, across units if need be; the partial sums
@@ -412,10 +414,10 @@ __global__ void __launch_bounds__(kPaThreads, 1)
   // by kGrow
   constexpr float kOff = KIND == kPaBf16 ? 0.f : 10.f, kGrow = 4.f;
   // Tiles that O adds up before its sums go elsewhere.  (The tensor cores cut off what an accumulator has no bits for, towards zero.
-  // Measured over values of one sign: 2^13 slots with two terms take 2^-14 of the sum, an eighth of fp16 outputs' half step, 2^16
-  // 2^-11, an eighth of bf16 ones'.  For as long as a CTA's part is, fp16 outputs over 108152 slots of 12 heads were off by 1.2
-  // times what their rounding is.)
-  const int most = (c.type == LTRI_TYPE_BF16 ? 1 << 16 : 1 << 13) / TILE;
+  // Measured over values of one sign: 2^13 slots take 2^-14 of the sum, an eighth of fp16 outputs' half step, 2^16 2^-11.  For as
+  // long as a CTA's part is, fp16 outputs over 108152 slots of 12 heads were off by 1.2 times what their rounding is, and bf16 ones
+  // that values of both signs leave small by more than theirs.)
+  constexpr int kMost = (1 << 13) / TILE;
   extern __shared__ unsigned char smem_raw[];
   enum {
     B_KFULL = 0, B_VFULL = S, B_KEMPTY = 2 * S, B_VEMPTY = 3 * S, B_QFULL = 4 * S, B_SREADY = B_QFULL + QT,
@@ -481,7 +483,7 @@ __global__ void __launch_bounds__(kPaThreads, 1)
       w.at = at;
       w.head = (int)((c0 - e.before) / (e.tiles + w.extra));
       w.left = min(per, total - c0);
-      s_works = pa_part(w, (int)((c0 - e.before) % (e.tiles + w.extra)), most);
+      s_works = pa_part(w, (int)((c0 - e.before) % (e.tiles + w.extra)), kMost);
       s_place = w;
     }
   }
@@ -490,7 +492,7 @@ __global__ void __launch_bounds__(kPaThreads, 1)
   fence_after_sync();
   const uint32_t tmem = s_tmem;
   const bool works = s_works;
-  auto next_part = [&](PaPlace& w) { return pa_next(w, wk, c.Hkv, c.G, ROWS, most); };
+  auto next_part = [&](PaPlace& w) { return pa_next(w, wk, c.Hkv, c.G, ROWS, kMost); };
 
   if (warp >= kPaSoftmax && warp < kPaIssuer) {
     // ------------------------------------------------------------------ K and V tiles
