@@ -974,6 +974,7 @@ __global__ void __launch_bounds__(kPaThreads, 1)
         for (int k = 0; k < D / 64; ++k) {
           const int i = half * (D / 64) + k;
           uint32_t v[32];
+          __syncwarp();  // (lanes without a row have gone ahead)
           tmem_ld32(tO + k * 32, v);
           tmem_ld_wait();
           float z[32];
