@@ -507,8 +507,8 @@ int ltri_paged_decode(ltri_paged* cache, int layer, const int32_t* table, int ta
  *   workspace DEVICE, 256-byte aligned, at least ltri_paged_attend_workspace_bytes(cache, n_tokens): scratch of this call alone
  *             until it is through.  Nothing has to be in it.
  * Queries without a slot (more than lens[r] of them) have outputs of 0 and an lse of -infinity, as have those of rows of bad
- * lengths, and are recorded as LTRI_EDEVICE.  Weights are not accumulated.  V rows of the call's own tokens have to be finite:
- * the products multiply those that a token does not see by 0.
+ * lengths, and are recorded as LTRI_EDEVICE.  Weights are not accumulated.  Elements of V rows that are not finite make that element
+ * of the outputs NaN, or infinite, of the tokens that see their slot, and of no others.
  * Logits and sums are fp32.  The probabilities enter the product with V as two 16-bit terms: 22 bits as in ltri_paged_decode over
  * fp16, 8-bit and 4-bit pages, 16 bits over bf16 ones.  The tensor cores' sums, which are cut off towards zero, are taken over by fp32
  * arithmetic every 2^13 slots: up to there they lose about 2^-14 of a sum of values of one sign, an eighth of fp16 outputs' half step.

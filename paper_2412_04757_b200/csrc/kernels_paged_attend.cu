@@ -15,6 +15,11 @@
 // shared memory, exactly; queries over them become halves too, each row scaled by a power of two.  With few tokens it is the
 // cache's bytes and the CTAs' latency.
 //
+// A probability of 0 times a value that is not finite is NaN, which a later token's V row must not make of an earlier one's outputs.
+// So the V rows of the call's own tokens are looked through beforehand, beside the dealing of the work (a few MB; looking at them
+// as they come into shared memory, in every call: prompts 8% longer).  Where any is not finite, such elements enter the products
+// as 0 in slots that some of a unit's tokens do not see, and the outputs of the tokens that do see them become NaN as they are written.
+//
 // Work: units are (row, KV head, block of query rows), as long as the tiles of slots that their last token sees.  A small kernel
 // puts all units' tiles into one line, of which every CTA (one per SM) takes an equal run, across units if need be; the partial sums
 // of units that CTAs share are joined by a third kernel, in the order of the line.
@@ -81,6 +86,8 @@ struct PaWork {
   PaEntry* entry;
   int max_entries;
   int* row_first;    // [n_rows + 1]: entries in front of a row's
+  int* spoilt;       // [scans]: whether a CTA has found tokens' V rows that are not finite
+  int scans;
   float* part;       // [CTAs][2]: partial sums, O as [tile][D / 4][128][4], then references and sums of the rows
 };
 
@@ -114,14 +121,66 @@ __device__ __forceinline__ int pa_limit(const PaEntry& e, int G, int rows) {
 // ms; 1 4.9, 2 4.4, 3 4.1 to 4.2.)
 __device__ __forceinline__ int pa_extra(const PaEntry& e, int G, int rows) { return e.m * G - e.block * rows > 128 ? 4 : 2; }
 
+// Elements of `type` that are not finite, their exponents all ones: the upper bits of those halves of x, after one more in the last
+// place of the exponent.
+__device__ __forceinline__ uint32_t pa_not_finite(int type, uint32_t x) {
+  return (type == LTRI_TYPE_BF16 ? (x & 0x7f807f80u) + 0x00800080u : (x & 0x7c007c00u) + 0x04000400u) & 0x80008000u;
+}
+// They become 0.
+__device__ __forceinline__ uint32_t pa_finite(int type, uint32_t x) { return x & ~((pa_not_finite(type, x) >> 15) * 0xffffu); }
+
+// ---- V rows of the call's own tokens that are not finite: a token a warp ----
+__device__ __forceinline__ bool pa_scan(const PagedCache& c, const PagedRows& r, int layer, const int* starts, long long n_tokens,
+                                        long long first, long long step) {
+  // (a lane has 16 bytes of a row, of 4-bit rows the scale of a block)
+  const int lane = threadIdx.x & 31, of_row = c.cache_type == LTRI_TYPE_INT4 ? c.D / 32 : c.row_bytes / 16;
+  bool bad = false;
+  for (long long tok = first; tok < n_tokens; tok += step) {
+    int lo = 0, hi = r.n;  // the last row that starts at or in front of the token
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (starts[mid] <= tok) lo = mid;
+      else hi = mid - 1;
+    }
+    if (lo >= r.n || starts[lo] > tok || starts[lo] < 0) continue;
+    const int n = r.lens[lo], end = starts[lo + 1];
+    const long long slot = (long long)n - end + tok;
+    if (tok >= end || end > n_tokens || (unsigned)n > (unsigned)r.cap || slot < 0) continue;
+    const int nth = paged_nth(c, (int)slot), page = r.table[lo * r.table_stride + nth], place = (int)slot - nth * c.P;
+    if ((unsigned)page >= (unsigned)c.n_pages) continue;
+    for (int i = lane; i < c.Hkv * of_row; i += 32) {
+      const int head = i / of_row, in = i % of_row;
+      if (c.cache_type == LTRI_TYPE_INT4) {
+        bad |= (c.sc[paged_word(c, layer, page, head, place) * (c.D / 16) + c.D / 32 + in] & 0xf8) == 0xf8;
+      } else {
+        const uint4 x = *reinterpret_cast<const uint4*>(c.v + paged_row(c, layer, page, head, place) + in * 16);
+        if (c.cache_type == LTRI_TYPE_E4M3) {
+          auto nan = [](uint32_t y) { return ((y & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; };
+          bad |= (nan(x.x) | nan(x.y) | nan(x.z) | nan(x.w)) != 0u;
+        } else {
+          bad |= (pa_not_finite(c.type, x.x) | pa_not_finite(c.type, x.y) | pa_not_finite(c.type, x.z) | pa_not_finite(c.type, x.w)) != 0u;
+        }
+      }
+    }
+  }
+  return bad;
+}
+
 // ---- the line of tiles ----
 constexpr int kPlThreads = 1024;
 __global__ void __launch_bounds__(kPlThreads)
-    k_paged_attend_plan(PagedCache c, PagedRows r, const int* starts, long long n_tokens, PaWork wk, int rows, int tile) {
+    k_paged_attend_plan(PagedCache c, PagedRows r, int layer, const int* starts, long long n_tokens, PaWork wk, int rows, int tile) {
   __shared__ long long s_sum[32];
   __shared__ long long s_total;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   chain_wait();
+  if (blockIdx.x > 0) {
+    const long long warps = kPlThreads / 32, mine = blockIdx.x - 1;
+    const bool bad = pa_scan(c, r, layer, starts, n_tokens, mine * warps + warp, wk.scans * warps);
+    const int any = __syncthreads_or(bad);
+    if (tid == 0) wk.spoilt[mine] = any;
+    return;
+  }
   // Sum of all threads in front of this one, and of all of them.
   auto scan = [&](long long x, long long& all) {
     long long inc = x;
@@ -399,6 +458,31 @@ __device__ __forceinline__ void pa_put32(int type, unsigned char* to, const floa
   }
 }
 
+// Of 32 elements those that are not finite in any of a row's slots [slot, end), a bit each.  (Out of line, and seldom called.)  `at`:
+// the elements of page 0's first place, or, of 4-bit rows, the byte of their scale; `ps` and `ts` its strides.
+template <int KIND>
+static __device__ __noinline__ uint32_t pa_spoilt(const unsigned char* at, long long ps, long long ts, const int* pages, int n_pages,
+                                                  int P, unsigned p_mul, int p_shift, int slot, int end) {
+  uint32_t bits = 0u;
+#pragma unroll 1
+  for (; slot < end; ++slot) {
+    const int nth = (int)(((unsigned long long)(unsigned)slot * p_mul) >> p_shift), page = pages[nth];
+    if ((unsigned)page >= (unsigned)n_pages) continue;
+    const unsigned char* x = at + (unsigned)page * ps + (unsigned)(slot - nth * P) * ts;
+    if (KIND == kPaInt4) {
+      if ((*x & 0xf8) == 0xf8) return 0xffffffffu;
+    } else if (KIND == kPaE4m3) {
+#pragma unroll 1
+      for (int i = 0; i < 32; ++i) bits |= (uint32_t)((x[i] & 0x7f) == 0x7f) << i;
+    } else {
+      constexpr unsigned kMost = KIND == kPaBf16 ? 0x7f80u : 0x7c00u;
+#pragma unroll 1
+      for (int i = 0; i < 32; ++i) bits |= (uint32_t)((reinterpret_cast<const unsigned short*>(x)[i] & kMost) == kMost) << i;
+    }
+  }
+  return bits;
+}
+
 template <int KIND>
 __device__ __forceinline__ float pa_v_scale(const PagedCache& c, int head) {
   return KIND == kPaInt4 ? kI4Back : KIND == kPaE4m3 ? c.vs[head] : 1.f;
@@ -472,7 +556,13 @@ __global__ void __launch_bounds__(kPaThreads, 1)
   // the CTA's run
   const long long total = wk.plan->total;
   const long long per = (total + gridDim.x - 1) / gridDim.x, c0 = blockIdx.x * per;
-  __shared__ bool s_works;
+  __shared__ bool s_works, s_spoilt;
+  if (warp == 1) {
+    int bad = 0;
+    for (int i = lane; i < wk.scans; i += 32) bad |= wk.spoilt[i];
+    bad = __any_sync(0xffffffffu, bad);
+    if (lane == 0) s_spoilt = bad != 0;
+  }
   if (tid == 0 && c0 >= total) s_works = false;
   if (warp == 0 && c0 < total) {
     const int at = pa_find(wk, wk.plan->entries, c0);
@@ -574,6 +664,20 @@ __global__ void __launch_bounds__(kPaThreads, 1)
       }
       asm volatile("cp.async.commit_group;" ::: "memory");
     };
+    // Elements of this lane's that are not finite, in slots that not all of the unit's tokens see, become 0.  (Slow: seldom called.)
+    auto clean = [&](uint32_t mat, int from) {
+#pragma unroll 1
+      for (int i = 0; i < PASSES * KC * OUT; ++i) {
+        const int p = i / (KC * OUT), k = i % (KC * OUT);
+        if (row0 + p * SL < from) continue;
+        const uint32_t at = place_of(mat, p, k / OUT * (CL * OUT) + k % OUT);
+        uint4 x;
+        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "r"(at) : "memory");
+        pa_store(at, make_uint4(pa_finite(kType, x.x), pa_finite(kType, x.y), pa_finite(kType, x.z), pa_finite(kType, x.w)));
+      }
+    };
+    auto seen_by_all = [&](const PaPlace& w) { return w.base + w.rho / c.G + 1 - w.tile * TILE; };
+    const bool cleans = of_v && s_spoilt;
     auto write_rows = [&](uint32_t mat) {
       if constexpr (!kCopy) {
 #pragma unroll
@@ -603,7 +707,6 @@ __global__ void __launch_bounds__(kPaThreads, 1)
               pa_store(place_of(mat, p, k * CL * OUT + o), make_uint4(v[0], v[1], v[2], v[3]));
             }
           }
-        fence_async_smem();
       }
     };
     if (works) {
@@ -625,6 +728,10 @@ __global__ void __launch_bounds__(kPaThreads, 1)
       }
       if (kCopy) {
         copy_rows(mat);
+        if (cleans) {
+          asm volatile("cp.async.wait_group 0;" ::: "memory");
+          clean(mat, seen_by_all(wd));
+        }
         if (jt > 0) {  // the tile before has arrived
           asm volatile("cp.async.wait_group 1;" ::: "memory");
           fence_async_smem();
@@ -632,6 +739,8 @@ __global__ void __launch_bounds__(kPaThreads, 1)
         }
       } else {
         write_rows(mat);
+        if (cleans) clean(mat, seen_by_all(wd));
+        fence_async_smem();
         arrive(full + st);
       }
       if (++wd.tile == wd.end) {  // now of the next tile
@@ -1004,6 +1113,25 @@ __global__ void __launch_bounds__(kPaThreads, 1)
         }
         fence_before_sync();
         arrive(B_OFREE + q);
+        if (s_spoilt && row_ok) {  // (by the slots that this row sees; s_where still has the stretch's place)
+          const PaPlace& u = s_where[warp];
+          const int from = max(u.base + u.rho / c.G + 1, u.tile * TILE), end = min(u.base + (u.rho + q * 128 + r) / c.G + 1, u.end * TILE);
+#pragma unroll 1
+          for (int i = half * (D / 64); i < (half + 1) * (D / 64); ++i) {
+            const unsigned char* at = KIND == kPaInt4 ? c.sc + paged_word(c, layer, 0, u.head, 0) * (D / 16) + D / 32 + i
+                                                      : c.v + layer * c.ls + u.head * c.hs + i * (Sh::kRow * 32 / D);
+            const long long ps = KIND == kPaInt4 ? (long long)c.Hkv * c.P * (D / 16) : c.ps;
+            const uint32_t bad = pa_spoilt<KIND>(at, ps, KIND == kPaInt4 ? D / 16 : c.ts, table + u.row * table_stride, c.n_pages, c.P,
+                                                 c.p_mul, c.p_shift, from, end);
+#pragma unroll 1
+            for (int e = 0; e < 32; ++e) {
+              if (!(bad >> e & 1u)) continue;
+              if (whole) reinterpret_cast<unsigned short*>(a.out)[to_row * D + i * 32 + e] = 0x7fffu;  // (NaN of both types)
+              else part[((size_t)(q * (D / 4) + i * 8 + e / 4) * 128 + r) * 4 + e % 4] = __int_as_float(0x7fffffff);
+            }
+          }
+        }
+        __syncwarp();  // (s_where)
         if (row_ok && half == 0) {
           if (whole && a.lse)
             a.lse[to_row] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.69314718055994531f;
@@ -1090,8 +1218,8 @@ cudaError_t prepare_kind() {
 template <int KIND, int D>
 cudaError_t launch_one(const PagedCache& c, const PagedRows& r, int layer, const PagedQueries& a, const PaWork& wk, cudaStream_t s) {
   using Sh = PaShape<KIND, D>;
-  cudaError_t e = launch_chained(k_paged_attend_plan, dim3(1), dim3(kPlThreads), 0, s, c, r, a.starts, a.n_tokens, wk, Sh::kRows,
-                                 Sh::kTile);
+  cudaError_t e = launch_chained(k_paged_attend_plan, dim3(1 + wk.scans), dim3(kPlThreads), 0, s, c, r, layer, a.starts, a.n_tokens,
+                                 wk, Sh::kRows, Sh::kTile);
   if (e != cudaSuccess) return e;
   e = launch_chained(k_paged_attend<KIND, D>, dim3(c.sms), dim3(kPaThreads), Sh::kSmem, s, c, layer, r.table, r.table_stride, a, wk);
   if (e != cudaSuccess) return e;
@@ -1109,6 +1237,12 @@ long long entries_of(const PagedCache& c, long long n_tokens, long long n_rows) 
   return n_tokens * c.G / rows_of_unit(c.D) + n_rows;
 }
 
+// CTAs that look through the tokens' V rows: a token a warp, as long as there are SMs.
+int scans_of(const PagedCache& c, long long n_tokens) {
+  const long long warps = kPlThreads / 32, most = c.sms > 1 ? c.sms - 1 : 1;
+  return (int)((n_tokens + warps - 1) / warps < most ? (n_tokens + warps - 1) / warps : most);
+}
+
 // Carves the workspace; returns its size.
 size_t layout(const PagedCache& c, long long n_tokens, long long n_rows, PaWork* wk, unsigned char* base) {
   size_t off = 0;
@@ -1119,9 +1253,11 @@ size_t layout(const PagedCache& c, long long n_tokens, long long n_rows, PaWork*
   };
   const long long entries = entries_of(c, n_tokens, n_rows);
   unsigned char *plan = take(sizeof(PaPlan)), *entry = take(entries * sizeof(PaEntry)), *rows = take((n_rows + 1) * sizeof(int));
+  const int scans = scans_of(c, n_tokens);
+  unsigned char* spoilt = take(scans * sizeof(int));
   unsigned char* part = take((size_t)c.sms * 2 * rows_of_unit(c.D) * (c.D + 2) * sizeof(float));
   if (wk) *wk = PaWork{reinterpret_cast<PaPlan*>(plan), reinterpret_cast<PaEntry*>(entry), (int)entries,
-                       reinterpret_cast<int*>(rows), reinterpret_cast<float*>(part)};
+                       reinterpret_cast<int*>(rows), reinterpret_cast<int*>(spoilt), scans, reinterpret_cast<float*>(part)};
   return off;
 }
 
