@@ -472,7 +472,7 @@ int ltri_paged_append(ltri_paged* cache, int layer, const int32_t* table, int ta
  *            with the same starts writes).  Slots that the row does not have, or whose page is none, read as 0 and are recorded
  *            as LTRI_EDEVICE.
  *   k, v     [n_tokens][n_kv_heads][head_dim], token stride kv_stride elements (0: dense); one of them may be NULL
- * Values over 8-bit pages are rounded once to `type`; the others are exact. */
+ * Values over 8-bit pages are the exact products rounded once to `type`; the others are exact. */
 int ltri_paged_read(ltri_paged* cache, int layer, const int32_t* table, int table_pages, int64_t table_stride,
                     const int32_t* lens, int n_rows, const int32_t* starts, const int32_t* first, int64_t n_tokens, void* k,
                     void* v, int64_t kv_stride, void* cuda_stream);
