@@ -1206,13 +1206,11 @@ cudaError_t prepare_kernel(F* fn, int smem) {
   if (e == cudaSuccess && a.numRegs < kPaRegs) e = cudaErrorInvalidConfiguration;
   return first_error(e, allow_smem(fn, smem));
 }
-template <int KIND, int D>
-cudaError_t prepare_one() {
-  return prepare_kernel(k_paged_attend<KIND, D>, PaShape<KIND, D>::kSmem);
-}
 template <int KIND>
-cudaError_t prepare_kind() {
-  return first_error(prepare_one<KIND, 64>(), first_error(prepare_one<KIND, 128>(), prepare_one<KIND, 256>()));
+cudaError_t prepare_kind(int D) {
+  if (D == 64) return prepare_kernel(k_paged_attend<KIND, 64>, PaShape<KIND, 64>::kSmem);
+  if (D == 128) return prepare_kernel(k_paged_attend<KIND, 128>, PaShape<KIND, 128>::kSmem);
+  return prepare_kernel(k_paged_attend<KIND, 256>, PaShape<KIND, 256>::kSmem);
 }
 
 template <int KIND, int D>
@@ -1263,9 +1261,10 @@ size_t layout(const PagedCache& c, long long n_tokens, long long n_rows, PaWork*
 
 }  // namespace
 
-cudaError_t prepare_paged_attend() {
-  return first_error(first_error(prepare_kind<kPaBf16>(), prepare_kind<kPaFp16>()),
-                     first_error(prepare_kind<kPaE4m3>(), prepare_kind<kPaInt4>()));
+cudaError_t prepare_paged_attend(const PagedCache& c) {
+  if (c.cache_type == LTRI_TYPE_INT4) return prepare_kind<kPaInt4>(c.D);
+  if (c.cache_type == LTRI_TYPE_E4M3) return prepare_kind<kPaE4m3>(c.D);
+  return c.type == LTRI_TYPE_BF16 ? prepare_kind<kPaBf16>(c.D) : prepare_kind<kPaFp16>(c.D);
 }
 
 size_t paged_attend_workspace(const PagedCache& c, long long n_tokens, long long n_rows) {

@@ -1193,8 +1193,8 @@ cudaError_t prepare_dim() {
   return first_error(prepare_one<KIND, D, 1>(), prepare_one<KIND, D, 2>());
 }
 template <int KIND>
-cudaError_t prepare_kind() {
-  return first_error(prepare_dim<KIND, 64>(), first_error(prepare_dim<KIND, 128>(), prepare_dim<KIND, 256>()));
+cudaError_t prepare_kind(int D) {
+  return D == 64 ? prepare_dim<KIND, 64>() : D == 128 ? prepare_dim<KIND, 128>() : prepare_dim<KIND, 256>();
 }
 
 template <int KIND, int D, int NT>
@@ -1219,9 +1219,10 @@ cudaError_t launch_kind(const PagedCache& c, const PagedRows& r, int layer, cons
 
 }  // namespace
 
-cudaError_t prepare_paged() {
-  return first_error(first_error(prepare_kind<kPdBf16>(), prepare_kind<kPdFp16>()),
-                     first_error(prepare_kind<kPdE4m3>(), prepare_kind<kPdInt4>()));
+cudaError_t prepare_paged(const PagedCache& c) {
+  if (c.cache_type == LTRI_TYPE_INT4) return prepare_kind<kPdInt4>(c.D);
+  if (c.cache_type == LTRI_TYPE_E4M3) return prepare_kind<kPdE4m3>(c.D);
+  return c.type == LTRI_TYPE_BF16 ? prepare_kind<kPdBf16>(c.D) : prepare_kind<kPdFp16>(c.D);
 }
 
 PagedBlocks paged_blocks(int group) {

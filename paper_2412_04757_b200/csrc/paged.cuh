@@ -91,9 +91,10 @@ size_t paged_part_floats(int group, int head_dim);  // partial sums of one block
 constexpr int kPagedWarps = 16;                     // of an attention CTA, at most
 int paged_decode_kernels(const PagedCache& c);  // launches of a decode call
 
-cudaError_t prepare_paged();
+// (for the handle's own type and head_dim)
+cudaError_t prepare_paged(const PagedCache& c);
 cudaError_t prepare_paged_evict();
-cudaError_t prepare_paged_attend();
+cudaError_t prepare_paged_attend(const PagedCache& c);
 size_t paged_attend_workspace(const PagedCache& c, long long n_tokens, long long n_rows);
 cudaError_t launch_paged_attend(const PagedCache& c, const PagedRows& r, int layer, const PagedQueries& a, unsigned char* workspace,
                                 cudaStream_t s);

@@ -12,6 +12,7 @@ struct ltri_paged {
   int device = 0;
   int blocks = 1;  // of a KV head's query heads
   int last_cuda = 0;
+  cudaError_t attend = cudaSuccess;  // of its kernels' preparation: what its calls end with
   int64_t launches = 0;
 };
 
@@ -187,7 +188,9 @@ int create(const ltri_paged_params* p, uint8_t* block_scales, cudaStream_t s, lt
   cudaError_t e = cudaGetDevice(&c->device);
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&d.sms, cudaDevAttrMultiProcessorCount, c->device);
   if (d.sms > kPagedMaxSms) d.sms = kPagedMaxSms;
-  if (e == cudaSuccess) e = first_error(first_error(prepare_paged(), prepare_paged_evict()), prepare_paged_attend());
+  if (e == cudaSuccess) e = first_error(prepare_paged(d), prepare_paged_evict());
+  if (e == cudaSuccess) c->attend = prepare_paged_attend(d);
+  if (c->attend != cudaSuccess) cudaGetLastError();
   if (e == cudaSuccess) d.evict_cluster = paged_evict_cluster();
   if (e == cudaSuccess) e = cudaMemsetAsync(p->workspace, 0, zeroed, s);
   if (e == cudaSuccess) e = cudaStreamSynchronize(s);
@@ -305,6 +308,7 @@ int ltri_paged_attend(ltri_paged* cache, int layer, const int32_t* table, int ta
   if (!(out == q && (qs == row || n_tokens == 1)) && meets(out, n_tokens * row, q, n_tokens, row, qs)) return LTRI_EINVAL;
   OnDevice on(cache->device);
   if (!on.ok) return done(cache, cudaErrorInvalidDevice, 0);
+  if (cache->attend != cudaSuccess) return done(cache, cache->attend, 0);
   const PagedQueries a{starts, n_tokens, static_cast<const unsigned char*>(q), qs, static_cast<unsigned char*>(out), lse};
   return done(cache, launch_paged_attend(cache->c, r, layer, a, static_cast<unsigned char*>(workspace),
                                          static_cast<cudaStream_t>(cuda_stream)), 3);
