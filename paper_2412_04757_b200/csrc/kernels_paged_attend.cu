@@ -116,9 +116,11 @@ __device__ __forceinline__ int pa_limit(const PaEntry& e, int G, int rows) {
 }
 
 // What a unit costs besides its tiles (queries to be loaded, outputs to be written, while the products wait), as tiles: it takes so
-// many more places in the line.  (None: the CTAs with the shortest units were through 1.3 times as late as the others.  With one tile
-// of query rows 2, 16 ragged rows of five tokens 58 us; 1 or 3 60, 4 62.  With both 4, three prompts of up to 16384 tokens 4.0 to 4.2
-// ms; 1 4.9, 2 4.4, 3 4.1 to 4.2.)
+// many more places in the line.  Four where more than 128 query rows are left of the row's, so that both tiles of query rows have some,
+// or the unit is full at head_dim 256, where a tile has half the slots; else two.  (None: the CTAs with the shortest units were
+// through 1.3 times as late as the others.  Of 16 ragged rows of five tokens, with 2 58 us; 1 or 3 60, 4 62; of three prompts of up to
+// 16384 tokens, with 4 4.0 to 4.2 ms in a stream of calls; 1 4.9, 2 4.4, 3 4.1 to 4.2: both measured with one term of the
+// probabilities.  Head_dim 256, prompts of 8192 and 3001 tokens: 2.07 ms, with 2 for all units 2.49.)
 __device__ __forceinline__ int pa_extra(const PaEntry& e, int G, int rows) { return e.m * G - e.block * rows > 128 ? 4 : 2; }
 
 // Elements of `type` that are not finite, their exponents all ones: the upper bits of those halves of x, after one more in the last
