@@ -536,6 +536,11 @@ int ltri_paged_evict(ltri_paged* cache, int layer_begin, int layer_count, const 
 /* First device-side error recorded since the last call of this function (then cleared): LTRI_EDEVICE, or LTRI_ETIMEOUT if a
  * bounded wait inside ltri_paged_attend expired.  Synchronises. */
 int ltri_paged_sync_status(ltri_paged* cache, void* cuda_stream);
+/* Test hook for the bounded waits of ltri_paged_attend (failure detection).  Calls of the handle wait for at most limit_cycles SM
+ * cycles (1 to 10^8; 0: the usual limit of about ten seconds) wherever they wait, and with `held` their K rows (1), their V rows (2) or
+ * both (3) never arrive in shared memory (0: they do; else limit_cycles is not 0): a wait runs out, the kernel returns with outputs
+ * that are undefined, and ltri_paged_sync_status gives LTRI_ETIMEOUT.  Nothing faults or hangs, and the handle stays usable. */
+int ltri_paged_debug_wait(ltri_paged* cache, int64_t limit_cycles, int held);
 /* cudaError_t of the last failed runtime call (0 if none). */
 int ltri_paged_last_cuda_error(const ltri_paged* cache);
 /* Kernels launched through this handle since it was created (host counter). */

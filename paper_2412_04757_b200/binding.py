@@ -33,7 +33,7 @@ EXPORTS = [
     "ltri_debug_load_index", "ltri_debug_wait_timeout",
     "ltri_paged_workspace_bytes", "ltri_paged_create", "ltri_paged_destroy", "ltri_paged_append", "ltri_paged_decode",
     "ltri_paged_create_int4", "ltri_paged_read", "ltri_paged_attend", "ltri_paged_attend_workspace_bytes",
-    "ltri_paged_evict", "ltri_paged_sync_status", "ltri_paged_last_cuda_error", "ltri_paged_launch_count",
+    "ltri_paged_evict", "ltri_paged_sync_status", "ltri_paged_debug_wait", "ltri_paged_last_cuda_error", "ltri_paged_launch_count",
 ]
 KERNEL_CLASSES = ["append", "evict_index", "attn_local", "map_pass", "segment", "score_topk", "attn_retrieved",
                   "decode_retrieve", "decode_attn", "pager_pull"]
@@ -140,6 +140,7 @@ def load():
         L.ltri_paged_attend_workspace_bytes.argtypes = [vp, i64]
         L.ltri_paged_evict.argtypes = [vp, ip, ip, vp, ip, i64, vp, vp, ip, ip, ip, ip, vp]
         L.ltri_paged_sync_status.argtypes = [vp, vp]
+        L.ltri_paged_debug_wait.argtypes = [vp, i64, ip]
         L.ltri_paged_last_cuda_error.argtypes = [vp]
         L.ltri_paged_launch_count.restype = i64
         L.ltri_paged_launch_count.argtypes = [vp]
@@ -708,6 +709,10 @@ class LtriPaged:
 
     def ltri_paged_sync_status(self, stream=None) -> int:
         return int(self.lib.ltri_paged_sync_status(self._h, self._stream(stream)))
+
+    def ltri_paged_debug_wait(self, limit_cycles: int = 0, held: int = 0):
+        """Limits the waits of ltri_paged_attend and keeps K rows (1) or V rows (2) back from it; without arguments: as usual."""
+        _check(self.lib.ltri_paged_debug_wait(self._h, limit_cycles, held), "ltri_paged_debug_wait")
 
     def ltri_paged_launch_count(self) -> int:
         return int(self.lib.ltri_paged_launch_count(self._h))

@@ -63,8 +63,8 @@ constexpr int kPaThreads = 32 * (kPaIssuer + 4);
 constexpr int kPaRegs = 72, kPaSoftmaxRegs = 88, kPaLoadRegs = 56, kPaIssueRegs = 40;
 static_assert(kPaSoftmax * kPaSoftmaxRegs + kPaLoaders * kPaLoadRegs + 4 * kPaIssueRegs <= kPaThreads / 32 * kPaRegs,
               "more would wait for ever");
-// Upper bound of any single wait, in SM cycles (about ten seconds: a CTA's longest run of tiles lies far below)
-constexpr long long kPaWaitLimit = 10 * kWaitLimitCycles;
+// Upper bound of the wait for a CTA's last products, in SM cycles, whatever the handle's limit: TMEM is theirs until they end.
+constexpr long long kPaDrainLimit = 10 * kWaitLimitCycles;
 constexpr float kPaNone = -3.0e38f;  // reference of sums that nothing has entered yet: below every logit, and finite
 
 // A block of a row's query rows, and the first of its KV heads' places in the line (they follow each other).
@@ -97,11 +97,11 @@ __host__ __device__ constexpr size_t pa_part_floats() {
 }
 
 // mbar_wait with all but the first try out of line
-static __device__ __noinline__ bool pa_wait_long(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
-  return mbar_wait(bar, parity, abort_flag, kPaWaitLimit);
+static __device__ __noinline__ bool pa_wait_long(uint32_t bar, uint32_t parity, volatile int* abort_flag, long long limit) {
+  return mbar_wait(bar, parity, abort_flag, limit);
 }
-__device__ __forceinline__ bool pa_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
-  return mbar_try(bar, parity) || pa_wait_long(bar, parity, abort_flag);
+__device__ __forceinline__ bool pa_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, long long limit) {
+  return mbar_try(bar, parity) || pa_wait_long(bar, parity, abort_flag, limit);
 }
 __device__ __forceinline__ float pa_exp2(float x) {
   float y;
@@ -526,7 +526,7 @@ __global__ void __launch_bounds__(kPaThreads, 1)
   const uint32_t sbase = (smem_addr(smem_raw) + 1023u) & ~1023u, sQ = sbase, sKV = sbase + QT * Sh::kQBytes;
   auto bar = [&](int i) { return smem_addr(&bars[i]); };
   volatile int* abortp = &s_abort;
-  auto wait = [&](int i, int parity) { return mbar_wait(bar(i), parity & 1, abortp, kPaWaitLimit); };
+  auto wait = [&](int i, int parity) { return mbar_wait(bar(i), parity & 1, abortp, c.wait_limit); };
   auto arrive = [&](int i) {
     __syncwarp();
     if (lane == 0) mbar_arrive(bar(i));
@@ -598,7 +598,7 @@ __global__ void __launch_bounds__(kPaThreads, 1)
     const bool of_v = warp - kPaSoftmax >= 4;
     const int lw = warp & 3, sub = lane % SL, ch0 = lane / SL, full = of_v ? B_VFULL : B_KFULL;
     const unsigned char* pages = (of_v ? c.v : c.k) + layer * c.ls;
-    bool more_p = works, more_d = works;
+    bool more_p = works, more_d = works && !(c.held >> of_v & 1);
     PaPlace wd = s_place, wp = s_place;  // of the rows that are asked for, of the page numbers
     // A lane finds out about one of the warp's slots, and the others ask it.  (Every lane about those whose rows it loads: 3000 of
     // 9300 cycles a tile.)
@@ -795,7 +795,7 @@ __global__ void __launch_bounds__(kPaThreads, 1)
           pa_mma_ts(tO, pa + i * 8, db + (i * 16 * 128 >> 4), idesc_pv, true);
         }
       };
-      auto wait_at = [&](uint32_t at, uint32_t parity) { return __all_sync(0xffffffffu, pa_wait(at, parity, abortp)) != 0; };
+      auto wait_at = [&](uint32_t at, uint32_t parity) { return __all_sync(0xffffffffu, pa_wait(at, parity, abortp, c.wait_limit)) != 0; };
       PaPlace w = s_place;
       uint32_t st = 0, turn = 0;           // the stage and its parity
       uint32_t s_turn = 0, unit_turn = 0;  // a bit for each S: the parity of S and P; that of the parts of units
@@ -859,7 +859,7 @@ __global__ void __launch_bounds__(kPaThreads, 1)
       // nothing of this CTA's is under way when it gives its TMEM back
       pa_commit(bar(B_DRAIN));
       const long long t0 = clock64();
-      while (!mbar_try_suspend(bar(B_DRAIN), 0, 2000u) && clock64() - t0 < kPaWaitLimit) {
+      while (!mbar_try_suspend(bar(B_DRAIN), 0, 2000u) && clock64() - t0 < kPaDrainLimit) {
       }
     }
   } else {

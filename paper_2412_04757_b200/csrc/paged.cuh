@@ -37,6 +37,8 @@ struct PagedCache {
   float* lse2;                  // [max_rows][Hq], with weights: their sums, log2
   int* seen;                    // [max_rows]: CTAs of an eviction that have read the row's length; zero between calls
   int sms, evict_cluster;
+  long long wait_limit;         // of an attend call's waits, SM cycles
+  int held;                     // tests: bit 0: K rows, bit 1: V rows never arrive there
 };
 
 // One call's rows.

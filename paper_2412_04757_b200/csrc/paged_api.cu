@@ -19,6 +19,8 @@ struct ltri_paged {
 namespace {
 
 constexpr int64_t kPagedMaxTokens = 1 << 24;  // of an attend call: query rows of a KV head are counted in 32 bits
+// Upper bound of any wait of an attend call, in SM cycles (about ten seconds: a CTA's longest run of tiles lies far below)
+constexpr long long kPagedWaitLimit = 20000000000ll;
 constexpr int kPagedMaxSms = 256;  // CTAs that a decode call can have partial sums of
 
 int element_bits(int type) { return type == LTRI_TYPE_INT4 ? 4 : type == LTRI_TYPE_E4M3 ? 8 : 16; }
@@ -178,6 +180,7 @@ int create(const ltri_paged_params* p, uint8_t* block_scales, cudaStream_t s, lt
   d.ts = p->page_tokens > 1 ? bytes(p->token_stride) : 0;
   d.scale = (p->softmax_scale > 0.f ? p->softmax_scale : 1.f / std::sqrt((float)d.D)) * 1.4426950408889634f;
   d.decay = p->weight_decay;
+  d.wait_limit = kPagedWaitLimit;
   d.k = static_cast<unsigned char*>(p->k_pages);
   d.v = static_cast<unsigned char*>(p->v_pages);
   d.ks = p->k_scale;
@@ -347,6 +350,13 @@ int ltri_paged_sync_status(ltri_paged* cache, void* cuda_stream) {
   }
   if (e != cudaSuccess) return done(cache, e, 0);
   return w[0];
+}
+
+int ltri_paged_debug_wait(ltri_paged* cache, int64_t limit_cycles, int held) {
+  if (!cache || limit_cycles < 0 || limit_cycles > 100000000 || held < 0 || held > 3 || (held && !limit_cycles)) return LTRI_EINVAL;
+  cache->c.wait_limit = limit_cycles ? limit_cycles : kPagedWaitLimit;
+  cache->c.held = held;
+  return LTRI_OK;
 }
 
 int ltri_paged_last_cuda_error(const ltri_paged* cache) { return cache ? cache->last_cuda : 0; }
