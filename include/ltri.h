@@ -512,6 +512,7 @@ int ltri_paged_decode(ltri_paged* cache, int layer, const int32_t* table, int ta
  * Logits and sums are fp32.  The probabilities enter the product with V as two 16-bit terms: 22 bits as in ltri_paged_decode over
  * fp16, 8-bit and 4-bit pages, 16 bits over bf16 ones.  The tensor cores' sums, which are cut off towards zero, are taken over by fp32
  * arithmetic every 2^13 slots: up to there they lose about 2^-14 of a sum of values of one sign, an eighth of fp16 outputs' half step.
+ * Logits and products q.K of any magnitude below 10^38; over bf16 pages 16 times the sum of a row's |V| has to stay below it, too.
  * Outputs are the same bits for the same inputs and the same device.  LTRI_ECUDA where the device cannot run its kernel (found out
  * when the handle is created, which it does not prevent). */
 int ltri_paged_attend(ltri_paged* cache, int layer, const int32_t* table, int table_pages, int64_t table_stride,

@@ -444,8 +444,9 @@ class LtriPaged:
     [Hkv]), or of 4 bits: uint8 [layers][pages][Hkv][page tokens][head_dim / 2] with block_scales (uint8
     [layers][pages][Hkv][page tokens][2][head_dim / 32], contiguous).  weights (float32) and positions (int32), both or neither:
     [layers][pages][Hkv][page tokens], contiguous.  The tensors stay the caller's; the handle keeps references to them.  It
-    allocates its workspace on ``stream`` (None: the one that is current when it is made): let it go only when its calls on other streams are through.  max_tokens: tokens of the
-    largest ltri_paged_attend call, whose workspace it allocates too (0: none).
+    allocates its workspace on ``stream`` (None: the one that is current when it is made): let it go only when its calls on
+    other streams are through.  max_tokens: tokens of the largest ltri_paged_attend call, whose workspace it allocates too
+    (0: none).
     """
 
     def __init__(self, k_pages, v_pages, n_q_heads, dtype=None, max_rows=1, k_scale=None, v_scale=None, weights=None,

@@ -4,7 +4,7 @@ import torch
 
 from paper_2412_04757_b200 import binding
 from tests import paged_reference as ref
-from tests.test_gpu_paged_attend import BF16, FP16, ints, make
+from tests.test_gpu_paged_attend import attend, ints, make
 
 pytestmark = pytest.mark.gpu
 
@@ -59,6 +59,15 @@ def test_probabilities_meet_v_with_all_their_bits(dim, kind, hq):
             bound = 2 * most * (off + 2.0 ** -23)
             bound = bound + (want.abs() * ref.HALF_STEP[c.dtype]).clamp(min=2.0 ** -25)
             assert ((out[r, h] - want).abs() <= bound).all(), (r, h)
+
+
+@pytest.mark.parametrize("power", [110, -110])
+def test_values_of_the_stated_range(power):
+    # 300 slots of |V| up to 6 times 2^110: 16 times their sum is 2^125, 4 * 10^37
+    c = make("bf16", [300, 40], 8, 2, 128, 16, seed=9)
+    c.fill()
+    c.v.mul_(2.0 ** power)
+    attend(c, [130, 40])
 
 
 @pytest.mark.parametrize("kind,dim", [("bf16", 64), ("e4m3-bf16", 128), ("int4-bf16", 64), ("fp16", 64)])

@@ -11,7 +11,8 @@ LIMIT = 200_000  # SM cycles: a tenth of a millisecond
 
 
 @pytest.mark.parametrize("held", [1, 2, 3])
-@pytest.mark.parametrize("kind,dim,hq,hkv", [("bf16", 128, 8, 2), ("e4m3-bf16", 64, 4, 4), ("int4-fp16", 256, 4, 1), ("int4-bf16", 128, 32, 2)])
+@pytest.mark.parametrize("kind,dim,hq,hkv", [("bf16", 128, 8, 2), ("e4m3-bf16", 64, 4, 4), ("int4-fp16", 256, 4, 1),
+                                             ("int4-bf16", 128, 32, 2)])
 def test_a_wait_that_runs_out_ends_the_call(kind, dim, hq, hkv, held):
     # whole units and parts of them, rows of few tokens and of many
     lens, news = [700, 3, 0, 2600, 130], [300, 3, 0, 5, 130]
