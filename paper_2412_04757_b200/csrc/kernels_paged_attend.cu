@@ -29,9 +29,9 @@
 // products.  TMEM: two S of 64 columns in turn for each tile of query rows, in whose columns P replaces S, then the two O.  head_dim
 // 256: one tile of query rows.
 //
-// Measured over 4-bit pages, 32 query and 8 KV heads of 128: 512 tokens over 24576 slots 218 to 220 us in a stream of calls (some
-// 930 TFLOP/s; 122 at the rate of large matrix products), three prompts of up to 16384 tokens in fp16 4.1 to 4.2 ms, 16 ragged rows of
-// up to 8000 slots with five tokens each 58 to 59 us.
+// Measured over 4-bit pages, 32 query and 8 KV heads of 128: 512 tokens over 24576 slots 249 to 261 us in a short series of calls,
+// 279 to 285 in a long one, which the power limit slows (715 TFLOP/s; 122 us at the rate of large matrix products), three prompts of up
+// to 16384 tokens in fp16 4.2 ms, and 4.7 in a long series, 16 ragged rows of up to 8000 slots with five tokens each 57 to 59 us.
 #include "paged_int4.cuh"
 #include "tc_util.cuh"
 
@@ -58,8 +58,8 @@ constexpr int kPaSoftmax = 16, kPaLoaders = 8;  // warps
 constexpr int kPaIssuer = kPaSoftmax + kPaLoaders;  // this warp
 constexpr int kPaThreads = 32 * (kPaIssuer + 4);
 // Registers a thread: of the launch (prepare_kernel sees that it has them), and of the roles, which add up to them.  (All
-// 72, which the softmax's loop has not enough of: attend of 512 tokens over 24576 slots 234 us, with these 225; five drafted tokens
-// of 16 rows 62 and 58; 96, 40 and 40, or 88, 64 and 24: no faster.)
+// 72, which the softmax's loop has not enough of: with one term of the probabilities 512 tokens over 24576 slots 234 us, with these
+// 225; five drafted tokens of 16 rows 62 and 58; 96, 40 and 40, or 88, 64 and 24: no faster.)
 constexpr int kPaRegs = 72, kPaSoftmaxRegs = 88, kPaLoadRegs = 56, kPaIssueRegs = 40;
 static_assert(kPaSoftmax * kPaSoftmaxRegs + kPaLoaders * kPaLoadRegs + 4 * kPaIssueRegs <= kPaThreads / 32 * kPaRegs,
               "more would wait for ever");
