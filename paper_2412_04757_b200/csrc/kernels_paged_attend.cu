@@ -16,9 +16,9 @@
 // cache's bytes and the CTAs' latency.
 //
 // A probability of 0 times a value that is not finite is NaN, which a later token's V row must not make of an earlier one's outputs.
-// So the V rows of the call's own tokens are looked through beforehand, beside the dealing of the work (a few MB; looking at them
-// as they come into shared memory, in every call: prompts 8% longer).  Where any is not finite, such elements enter the products
-// as 0 in slots that some of a unit's tokens do not see, and the outputs of the tokens that do see them become NaN as they are written.
+// So the V rows of the call's own tokens are looked through beforehand, beside the dealing of the work (their bytes once more: calls are
+// 0 to 2% longer; looking at every row as it comes into shared memory: prompts 8%).  Where any is not finite, such elements enter the
+// products as 0 in slots that some of a unit's tokens do not see, and outputs of tokens that do see them become NaN as they are written.
 //
 // Work: units are (row, KV head, block of query rows), as long as the tiles of slots that their last token sees.  A small kernel
 // puts all units' tiles into one line, of which every CTA (one per SM) takes an equal run, across units if need be; the partial sums
